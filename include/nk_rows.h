@@ -1,0 +1,77 @@
+/*
+ * nk_rows — layers whose weight is chosen row by row, for NVIDIA B200 (sm_100a), beside the dense GEMM of
+ * nk_gemm.h and in the same library:
+ *
+ *   nk_grouped   products grouped by expert over ragged groups of rows, and their gradients
+ *
+ * Conventions are those of nk_gemm.h: DEVICE pointers on the plan's device, nothing is allocated on the
+ * device, nothing synchronises inside a run call, failures are status codes, and a plan (with its workspace)
+ * serves one stream at a time: two runs of a plan whose work can overlap on the device race.
+ * Matrices are row-major; "ld" fields are row strides in elements (0: dense).
+ */
+#ifndef NK_ROWS_H
+#define NK_ROWS_H
+
+#include "nk_gemm.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ------------------------------------------------------------------ products grouped by expert
+ *
+ * `offsets` is a device array of groups + 1 non-decreasing INT32 row numbers, 0 <= offsets[0],
+ * offsets[groups] <= rows: group g owns the rows offsets[g] .. offsets[g+1]-1 of the row arrays (empty groups
+ * are fine).  It is read by the kernel, never by the host, so a plan serves every way of spreading the rows.
+ *
+ *   NK_GROUPED_ROWS      C[t][0..N) = A[t][0..K) . B_g            for the rows t of every group g
+ *                        B_g is [K][N] (layout_b NK_ROW_MAJOR) or kept as its transpose, [N][K]
+ *                        (NK_TRANSPOSED, the [out][in] of a linear layer).  Rows of C outside all groups are
+ *                        not touched.  The gradient of the rows, dA[t] = dC[t] . B_g^T, is the same product with
+ *                        N and K exchanged and the other layout_b: no copy of the weights is made.
+ *   NK_GROUPED_WEIGHTS   C_g[K][N] = sum over the rows t of group g of A[t][0..K)^T . B[t][0..N)
+ *                        the gradient of the weights (A: the rows, B: the gradient of the result; exchange the
+ *                        two for weights kept as [N][K]).  A group without rows gives zeros.
+ *
+ * 16-bit operands of one type, FP32 accumulation, C in FP32 or rounded once to the operands' type.  beta = 1
+ * adds C's old values in FP32 before the rounding (accumulated gradients); with beta = 0 they are never read.
+ * With NK_GROUPED_ROWS a row of C depends on its own row of A and its group's weight only: infinities and NaN in
+ * other rows, groups or beyond offsets[groups] stay there.
+ * Offsets that are negative, beyond `rows` or decreasing are clamped to the running maximum within [0, rows] (no
+ * access leaves the arrays) and reported by nk_grouped_check.
+ */
+typedef struct nk_grouped_s* nk_grouped_t;
+typedef enum { NK_GROUPED_ROWS = 0, NK_GROUPED_WEIGHTS = 1 } nk_grouped_kind_t;
+#define NK_GROUPED_MAX_GROUPS 1024
+
+typedef struct {
+    int64_t groups;    /* 1 .. NK_GROUPED_MAX_GROUPS */
+    int64_t rows;      /* extent of the row arrays; 0 is allowed */
+    int64_t N, K;      /* multiples of 8 */
+    int32_t kind;      /* nk_grouped_kind_t */
+    int32_t in_dtype;  /* NK_BF16 or NK_F16: A and B */
+    int32_t out_dtype; /* NK_F32, or the operands' type */
+    int32_t layout_b;  /* NK_GROUPED_ROWS: NK_ROW_MAJOR or NK_TRANSPOSED; NK_GROUPED_WEIGHTS: NK_ROW_MAJOR */
+    int32_t beta;      /* 0 or 1 */
+    int32_t device;
+    int64_t lda, ldb, ldc; /* row strides of A, of B (of one B_g) and of C (of one C_g); multiples of 8; 0: dense */
+    int64_t stride_g;      /* elements from B_g to B_g+1 (ROWS) or from C_g to C_g+1 (WEIGHTS); multiple of 8; 0: dense */
+} nk_grouped_desc_t;
+
+nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out);
+/* Device scratch a run needs (FP32 partial sums where few tiles are cut along K); contents need no initialisation. */
+size_t nk_grouped_workspace_bytes(nk_grouped_t plan);
+/* A, B, C and workspace 16-byte aligned; A, B and C may be NULL where they have no element (rows = 0). */
+nk_status_t nk_grouped_run(nk_grouped_t plan, const void* A, const void* B, void* C, const int32_t* offsets,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* Synchronise the device and report, once: NK_ERR_INVALID_ARG if a run met offsets that break the rule above,
+ * NK_ERR_TIMEOUT if a bounded wait ran out (results undefined), else NK_OK. */
+nk_status_t nk_grouped_check(nk_grouped_t plan);
+const char* nk_grouped_kernel_name(nk_grouped_t plan);
+const char* nk_grouped_last_cuda_error(nk_grouped_t plan);
+nk_status_t nk_grouped_destroy(nk_grouped_t plan);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* NK_ROWS_H */

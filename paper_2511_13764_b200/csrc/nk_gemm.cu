@@ -14,6 +14,7 @@
 #include <new>
 
 #include "aux_kernels.cuh"
+#include "host_util.cuh"
 #include "simt_f32.cuh"
 #include "umma_bf16.cuh"
 #include "umma_bf16_pair.cuh"
@@ -32,11 +33,6 @@ __device__ unsigned int g_status_word[NK_STATUS_SLOTS];
 static std::atomic<unsigned> g_next_status_slot{0};
 
 enum Variant { V_NAIVE = 0, V_SIMT = 1, V_UMMA = 2, V_SKINNY = 3, V_SPLIT3 = 4, V_SMALL = 5, V_SWAP = 6 };
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 }  // namespace nk
 
@@ -101,21 +97,14 @@ static void set_err(nk_gemm_s* p, const char* what, cudaError_t e) {
     snprintf(p->cuda_err, sizeof(p->cuda_err), "%s: %s", what, cudaGetErrorString(e));
 }
 
-struct DeviceGuard {
-    int prev = -1;
-    bool changed = false;
-    cudaError_t err = cudaSuccess;
-    explicit DeviceGuard(int dev) {
-        err = cudaGetDevice(&prev);
-        if (err == cudaSuccess && prev != dev) {
-            err = cudaSetDevice(dev);
-            changed = (err == cudaSuccess);
-        }
-    }
-    ~DeviceGuard() {
-        if (changed) cudaSetDevice(prev);
-    }
-};
+nk_status_t take_status_slot(unsigned int** slot) {
+    void* sym = nullptr;
+    if (cudaGetSymbolAddress(&sym, g_status_word) != cudaSuccess) return NK_ERR_CUDA;
+    *slot = static_cast<unsigned int*>(sym) + (g_next_status_slot.fetch_add(1) % NK_STATUS_SLOTS);
+    // the slot may carry the word of a plan that was destroyed without a check
+    const unsigned int z = 0;
+    return cudaMemcpy(*slot, &z, sizeof(z), cudaMemcpyHostToDevice) == cudaSuccess ? NK_OK : NK_ERR_CUDA;
+}
 
 static inline bool is16(int dt) { return dt == NK_BF16 || dt == NK_F16; }   // a 16-bit element type
 static inline bool is_s8(const nk_gemm_desc_t& d) { return d.in_dtype == NK_S8; }
@@ -867,14 +856,8 @@ nk_status_t nk_gemm_create(const nk_gemm_desc_t* desc, nk_gemm_t* out) {
 
     DeviceGuard guard(d.device);
     if (guard.err != cudaSuccess) { delete p; return NK_ERR_DEVICE; }
-    void* sym = nullptr;
-    if (cudaGetSymbolAddress(&sym, g_status_word) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
-    p->status_dev = static_cast<unsigned int*>(sym) + (g_next_status_slot.fetch_add(1) % NK_STATUS_SLOTS);
-    {
-        // the slot may carry the word of a plan that was destroyed without a check
-        const unsigned int z = 0;
-        if (cudaMemcpy(p->status_dev, &z, sizeof(z), cudaMemcpyHostToDevice) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
-    }
+    const nk_status_t slot = take_status_slot(&p->status_dev);
+    if (slot != NK_OK) { delete p; return slot; }
 
     if (d.in_dtype == NK_F32 && (d.flags & NK_FLAG_F32_TENSOR) && force != NK_FLAG_KERNEL_NAIVE) {
         // x = hi + mid + lo in BF16 (to 2^-27 of x); A.B = sum of the nine cross terms, of which the six

@@ -1,0 +1,206 @@
+// Host side of nk_grouped: descriptor validation, TMA maps, the launch.
+#include "rows_host.cuh"
+#include "grouped.cuh"
+
+namespace nk {
+
+// Arrival counters of the K splits, zero between launches (the last arriver of a tile clears its own).  A plan
+// holds a slot of this table from create to destroy; where none is free it runs without K splits.
+constexpr int SPLIT_SLOTS = 1024, SPLIT_COUNTERS = 128;
+__device__ unsigned int g_split_counter[SPLIT_SLOTS][SPLIT_COUNTERS];
+static std::mutex g_split_mutex;
+static bool g_split_taken[SPLIT_SLOTS];
+
+static int take_split_slot() {
+    std::lock_guard<std::mutex> lock(g_split_mutex);
+    for (int i = 0; i < SPLIT_SLOTS; ++i)
+        if (!g_split_taken[i]) {
+            g_split_taken[i] = true;
+            return i;
+        }
+    return -1;
+}
+static void give_split_slot(int slot) {
+    if (slot < 0) return;
+    std::lock_guard<std::mutex> lock(g_split_mutex);
+    g_split_taken[slot] = false;
+}
+
+}  // namespace nk
+
+struct nk_grouped_s : nk::PlanBase {
+    nk_grouped_desc_t d;          // strides filled in
+    int pairs;                    // CTA pairs that fit the device
+    int split_slot;
+    unsigned int* counters;
+    CUtensorMap map_a, map_b, map_b16;
+    const void *cached_a, *cached_b, *cached_c;
+    char name[64];
+};
+
+using namespace nk;
+
+namespace nk {
+
+// tcgen05 instruction descriptor without N: kind::f16, FP32 accumulator, M = 256 over the pair
+static uint32_t grouped_idesc(bool a_mn, bool b_mn, bool f16) {
+    uint32_t d = 1u << 4;
+    d |= (f16 ? 0u : 1u) << 7 | (f16 ? 0u : 1u) << 10;
+    d |= (a_mn ? 1u : 0u) << 15 | (b_mn ? 1u : 0u) << 16;
+    return d | (256u >> 4) << 24;
+}
+
+typedef void (*GroupedKernel)(CUtensorMap, CUtensorMap, CUtensorMap, GroupedParams);
+static GroupedKernel grouped_kernel_for(const nk_grouped_desc_t& d) {
+    if (d.kind == NK_GROUPED_WEIGHTS) return grouped_kernel<true, true>;
+    return d.layout_b == NK_TRANSPOSED ? grouped_kernel<false, false> : grouped_kernel<false, true>;
+}
+
+}  // namespace nk
+
+extern "C" {
+
+nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) {
+    if (out) *out = nullptr;
+    if (!desc || !out) return NK_ERR_INVALID_ARG;
+    nk_grouped_desc_t d = *desc;
+    if (d.groups <= 0 || d.rows < 0 || d.N <= 0 || d.K <= 0) return NK_ERR_INVALID_ARG;
+    if (d.kind != NK_GROUPED_ROWS && d.kind != NK_GROUPED_WEIGHTS) return NK_ERR_INVALID_ARG;
+    if (d.in_dtype < NK_F32 || d.in_dtype > NK_E5M2) return NK_ERR_INVALID_ARG;
+    if (!is_half_type(d.in_dtype)) return NK_ERR_UNSUPPORTED;
+    if (d.out_dtype != NK_F32 && d.out_dtype != d.in_dtype) return NK_ERR_INVALID_ARG;
+    if (d.layout_b != NK_ROW_MAJOR && d.layout_b != NK_TRANSPOSED && d.layout_b != NK_BLOCKED32) return NK_ERR_INVALID_ARG;
+    if (d.layout_b == NK_BLOCKED32 || (d.kind == NK_GROUPED_WEIGHTS && d.layout_b != NK_ROW_MAJOR)) return NK_ERR_UNSUPPORTED;
+    if (d.beta != 0 && d.beta != 1) return NK_ERR_INVALID_ARG;
+    if (d.groups > NK_GROUPED_MAX_GROUPS || d.N > (1 << 24) || d.K > (1 << 24) || d.rows >= (1ll << 31) - 4096) return NK_ERR_UNSUPPORTED;
+    if (d.N % 8 || d.K % 8 || d.lda % 8 || d.ldb % 8 || d.ldc % 8 || d.stride_g % 8) return NK_ERR_MISALIGNED;
+    const bool weights = d.kind == NK_GROUPED_WEIGHTS;
+    const int64_t b_cols = weights || d.layout_b == NK_ROW_MAJOR ? d.N : d.K;       // width of B's rows
+    const int64_t b_rows = d.layout_b == NK_ROW_MAJOR ? d.K : d.N;                  // rows of one B_g
+    if (d.lda == 0) d.lda = d.K;
+    if (d.ldb == 0) d.ldb = b_cols;
+    if (d.ldc == 0) d.ldc = d.N;
+    if (d.lda < d.K || d.ldb < b_cols || d.ldc < d.N) return NK_ERR_INVALID_ARG;
+    const int64_t item = weights ? d.K * d.ldc : b_rows * d.ldb;
+    if (d.stride_g == 0) d.stride_g = item;
+    if (d.stride_g < item) return NK_ERR_INVALID_ARG;                               // items overlap
+    // TMA strides are below 2^40 bytes; unit numbers stay below 2^24
+    if (d.lda >= (1ll << 38) || d.ldb >= (1ll << 38) || d.stride_g >= (1ll << 38)) return NK_ERR_UNSUPPORTED;
+    const int64_t tiles = weights ? d.groups * div_up(d.N, 256) * div_up(d.K, 256) : (d.rows / 256 + d.groups) * div_up(d.N, 256);
+    if (tiles >= (1 << 24)) return NK_ERR_UNSUPPORTED;
+
+    int sms = 0;
+    nk_status_t s = usable_device(d.device, &sms);
+    if (s != NK_OK) return s;
+    nk_grouped_s* p = new (std::nothrow) nk_grouped_s();
+    if (!p) return NK_ERR_INVALID_ARG;
+    p->d = d;
+    p->split_slot = -1;
+    if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
+    DeviceGuard guard(d.device);
+    if (!encode_tiled()) { delete p; return NK_ERR_CUDA; }
+    const void* kernel = reinterpret_cast<const void*>(grouped_kernel_for(d));
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
+    p->pairs = sms / 2;
+    if (!weights) {
+        void* sym = nullptr;
+        p->split_slot = take_split_slot();
+        if (p->split_slot >= 0) {
+            if (cudaGetSymbolAddress(&sym, g_split_counter) != cudaSuccess) { give_split_slot(p->split_slot); delete p; return NK_ERR_CUDA; }
+            p->counters = static_cast<unsigned int*>(sym) + p->split_slot * SPLIT_COUNTERS;
+        }
+    }
+    snprintf(p->name, sizeof(p->name), "grouped_%s_256x256x64_s%d_pair", weights ? "weights" : d.layout_b == NK_TRANSPOSED ? "rows_t" : "rows", GRP_STAGES);
+    *out = p;
+    return NK_OK;
+}
+
+// partial sums: one slab of 256 x 256 FP32 per (tile, split); there are at most as many as pairs
+size_t nk_grouped_workspace_bytes(nk_grouped_t p) {
+    if (!p || p->split_slot < 0) return 0;
+    return static_cast<size_t>(p->pairs) * GRP_TILE * GRP_TILE * sizeof(float);
+}
+
+nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C, const int32_t* offsets, void* workspace,
+                           size_t workspace_bytes, void* cuda_stream) {
+    if (!p || !offsets) return NK_ERR_INVALID_ARG;
+    const nk_grouped_desc_t& d = p->d;
+    const bool weights = d.kind == NK_GROUPED_WEIGHTS;
+    if (!weights && d.rows == 0) return NK_OK;
+    if (!C || (d.rows > 0 && (!A || !B))) return NK_ERR_INVALID_ARG;
+    if (misaligned16(A) || misaligned16(B) || misaligned16(C) || misaligned16(workspace) || (reinterpret_cast<uintptr_t>(offsets) & 3u))
+        return NK_ERR_MISALIGNED;
+    const size_t need = nk_grouped_workspace_bytes(p);
+    if (need && (!workspace || workspace_bytes < need)) return NK_ERR_WORKSPACE;
+    DeviceGuard guard(d.device);
+    if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
+    if (d.rows == 0) A = B = C;        // no row is loaded; the maps only need an address
+    const int64_t rows = d.rows ? d.rows : 1;
+    if (!p->cached_c || p->cached_a != A || p->cached_b != B) {
+        const bool f16 = d.in_dtype == NK_F16;
+        bool ok;
+        if (weights) {
+            ok = encode_map(&p->map_a, B, f16, d.N, rows, 1, d.ldb, 0, 64) && encode_map(&p->map_b, A, f16, d.K, rows, 1, d.lda, 0, 64);
+            p->map_b16 = p->map_b;
+        } else {
+            ok = (d.layout_b == NK_ROW_MAJOR ? encode_map(&p->map_a, B, f16, d.N, d.K, d.groups, d.ldb, d.stride_g, 64)
+                                             : encode_map(&p->map_a, B, f16, d.K, d.N, d.groups, d.ldb, d.stride_g, 128)) &&
+                 encode_map(&p->map_b, A, f16, d.K, rows, 1, d.lda, 0, 128) && encode_map(&p->map_b16, A, f16, d.K, rows, 1, d.lda, 0, 16);
+        }
+        if (!ok) {
+            p->cached_c = nullptr;
+            snprintf(p->cuda_err, sizeof(p->cuda_err), "cuTensorMapEncodeTiled failed");
+            return NK_ERR_CUDA;
+        }
+        p->cached_a = A;
+        p->cached_b = B;
+        p->cached_c = C;               // (set: the maps are valid)
+    }
+    GroupedParams g = {};
+    g.groups = static_cast<int>(d.groups);
+    g.rows = static_cast<int>(d.rows);
+    g.I = static_cast<int>(d.N);
+    g.J = static_cast<int>(d.K);
+    g.kb_total = static_cast<int>(div_up(d.K, GRP_BK));
+    g.tiles_i = static_cast<int>(div_up(d.N, GRP_TILE));
+    g.tiles_j = static_cast<int>(div_up(d.K, GRP_TILE));
+    g.beta = d.beta;
+    g.out16 = d.out_dtype != NK_F32;
+    g.f16 = d.in_dtype == NK_F16;
+    g.idesc = grouped_idesc(weights || d.layout_b == NK_ROW_MAJOR, weights, g.f16);
+    g.offsets = offsets;
+    g.C = C;
+    g.ldc = d.ldc;
+    g.stride_c = d.stride_g;
+    g.partial = need ? static_cast<float*>(workspace) : nullptr;
+    g.counter = p->counters;
+    g.status = p->status_dev;
+    // no more pairs than units can exist (a few rows of many groups: one tile column per row) times K splits
+    int64_t most = weights ? d.groups * g.tiles_i * g.tiles_j : (d.rows / 256 + (d.rows < d.groups ? d.rows : d.groups)) * g.tiles_i;
+    if (!weights) most *= GRP_MAX_SPLITS;
+    const int pairs = static_cast<int>(most < p->pairs ? most : p->pairs);
+    grouped_kernel_for(d)<<<2 * pairs, GRP_THREADS, GRP_SMEM, static_cast<cudaStream_t>(cuda_stream)>>>(p->map_a, p->map_b, p->map_b16, g);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? NK_OK : p->cuda("grouped launch", e);
+}
+
+nk_status_t nk_grouped_check(nk_grouped_t p) {
+    if (!p) return NK_ERR_INVALID_ARG;
+    const nk_status_t s = base_check(p);
+    if (s == NK_ERR_TIMEOUT && p->counters) {
+        DeviceGuard guard(p->device);
+        cudaMemset(p->counters, 0, SPLIT_COUNTERS * sizeof(unsigned int));   // an abandoned tile may have left a count
+    }
+    return s;
+}
+
+const char* nk_grouped_kernel_name(nk_grouped_t p) { return p ? p->name : ""; }
+const char* nk_grouped_last_cuda_error(nk_grouped_t p) { return p ? p->cuda_err : ""; }
+
+nk_status_t nk_grouped_destroy(nk_grouped_t p) {
+    if (p) give_split_slot(p->split_slot);
+    delete p;
+    return NK_OK;
+}
+
+}  // extern "C"

@@ -539,6 +539,17 @@ __device__ __forceinline__ void umma_commit_pair_if(uint32_t bar, uint16_t cta_m
                  : "memory");
 }
 
+// a / b for 0 <= a < 2^24, 0 < b < 2^24 without the integer-division routine (some forty dependent
+// instructions; the producer decodes its first unit before it can issue the first load, and on a
+// short problem that wait is visible): a single-precision estimate, then one exact correction step.
+__device__ __forceinline__ int div_small(int a, int b) {
+    int q = __float2int_rz(__fdividef(__int2float_rz(a), __int2float_rz(b)));
+    int r = a - q * b;             // the estimate is off by one at most (the loops run once or not at all)
+    while (r < 0) { --q; r += b; }
+    while (r >= b) { ++q; r -= b; }
+    return q;
+}
+
 // Shared-memory matrix descriptor (tcgen05): start address, leading/stride byte
 // offsets in 16-byte units, descriptor version 1, swizzle mode in bits 61..63
 // (0 none, 2 = 128-byte, 4 = 64-byte, 6 = 32-byte).

@@ -107,17 +107,6 @@ __host__ __device__ constexpr int umma_smem_bytes(int BN, int stages) {
 // a CTA's 128 x BN accumulator are shared out over the splits, so a CTA's slots never exceed one
 // accumulator (BN * 512 bytes), which fits the stage ring of every variant
 
-// a / b for 0 <= a < 2^24, 0 < b < 2^24 without the integer-division routine (some forty dependent
-// instructions; the producer decodes its first unit before it can issue the first load, and on a
-// short problem that wait is visible): a single-precision estimate, then one exact correction step.
-__device__ __forceinline__ int div_small(int a, int b) {
-    int q = __float2int_rz(__fdividef(__int2float_rz(a), __int2float_rz(b)));
-    int r = a - q * b;             // the estimate is off by one at most (the loops run once or not at all)
-    while (r < 0) { --q; r += b; }
-    while (r >= b) { ++q; r -= b; }
-    return q;
-}
-
 // tile id -> (m block, n block): groups of `group_m` M tiles sweep across N so
 // that CTAs running at the same time share A rows and B columns in L2.
 __device__ __forceinline__ void umma_tile_coords(const UmmaParams& p, int tile, int& mb, int& nb) {

@@ -1,0 +1,375 @@
+"""Products grouped by expert (nk_grouped) against the formula in 64 bits: ragged and empty groups, every
+operand layout and type, strides, accumulation, the gradients, and what the call refuses.
+
+Tolerances are those of the dense GEMM's parity tests, for the same reasons: FP32 accumulation of exact
+products, so |c - y| <= 1e-5 * max sum |a b|, plus half a unit in the last place of a 16-bit result."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_13764_b200 as nk
+from nk_testlib import TOL_BF16_REL, TOL_F16_ABS, TOL_F16_REL, TOL_REL_SMAX
+
+TYPES = {"bf16": (nk.BF16, torch.bfloat16), "f16": (nk.F16, torch.float16), "f32": (nk.F32, torch.float32)}
+SENTINEL = 7.0
+
+
+def offsets_of(sizes, first=0):
+    return torch.tensor(np.concatenate([[first], first + np.cumsum(sizes)]), dtype=torch.int32)
+
+
+def rand(shape, kind, gen, scale=1.0):
+    return (torch.randn(shape, generator=gen, dtype=torch.float32) * scale).to(TYPES[kind][1])
+
+
+def padded(x, ld, fill=float("nan")):
+    """x as a strided view of rows of ld elements; what lies between is `fill`."""
+    if ld == x.shape[-1]:
+        return x.cuda().contiguous()
+    buf = torch.full((*x.shape[:-1], ld), fill, dtype=x.dtype)
+    buf[..., :x.shape[-1]] = x
+    return buf.cuda()
+
+
+def close(got, want, size, kind):
+    """size: the largest sum of |products| of any element."""
+    want, got = want.cpu(), got.double().cpu()
+    tol = TOL_REL_SMAX * size + {"bf16": TOL_BF16_REL, "f16": TOL_F16_REL, "f32": 0.0}[kind] * want.abs() + (TOL_F16_ABS if kind == "f16" else 0)
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, first at {bad.nonzero()[0].tolist()}: got {got[bad][0]} want {want[bad][0]}"
+
+
+def scratch(plan):
+    return torch.full((max(16, plan.workspace_bytes),), 255, dtype=torch.uint8, device="cuda")
+
+
+def run_rows(sizes, N, K, kind="bf16", out="bf16", layout="row", first=0, spare=0, lda=0, ldb=0, ldc=0, gap=0, beta=0, seed=0, spoil=True):
+    """One forward product; returns (C rows of the groups as float64, formula, sum of |products|)."""
+    gen = torch.Generator().manual_seed(seed)
+    G, rows = len(sizes), first + sum(sizes) + spare
+    off = offsets_of(sizes, first)
+    A = rand((rows, K), kind, gen)
+    if spoil:                                    # rows of no group must not matter
+        A[:first] = float("nan")
+        A[first + sum(sizes):] = float("inf")
+    W = rand((G, K, N), kind, gen, K ** -0.5)
+    stored = W if layout == "row" else W.transpose(1, 2).contiguous()
+    lda, ldb, ldc = lda or K, ldb or stored.shape[2], ldc or N
+    stride = stored.shape[1] * ldb + gap
+    wbuf = torch.full((G * stride,), float("nan"), dtype=W.dtype)
+    for g in range(G):
+        view = wbuf[g * stride: g * stride + stored.shape[1] * ldb].view(stored.shape[1], ldb)
+        view[:, : stored.shape[2]] = stored[g]
+    C = torch.full((rows, ldc), SENTINEL, dtype=TYPES[out][1])
+    if beta:
+        C[:, :N] = rand((rows, N), out, gen)
+    before = C.clone()
+    plan = nk.GroupedPlan(G, rows, N, K, in_dtype=TYPES[kind][0], out_dtype=TYPES[out][0], beta=beta,
+                          layout_b=nk.ROW_MAJOR if layout == "row" else nk.TRANSPOSED, lda=lda, ldb=ldb, ldc=ldc, stride_g=stride)
+    dC = C.cuda()
+    dA, dW, dO = padded(A, lda), wbuf.cuda(), off.cuda()
+    plan.run(dA, dW, dC, dO, workspace=scratch(plan), stream=torch.cuda.current_stream().cuda_stream)
+    plan.check()
+    got = dC.cpu()
+    want = torch.zeros(rows, N, dtype=torch.float64)
+    size = 1e-30
+    for g in range(G):
+        lo, hi = int(off[g]), int(off[g + 1])
+        a, w = A[lo:hi].double().cuda(), W[g].double().cuda()
+        want[lo:hi] = (a @ w).cpu()
+        if hi > lo:
+            size = max(size, float((a.abs() @ w.abs()).max()))
+    lo, hi = first, first + sum(sizes)
+    if beta:
+        want[lo:hi] += before[lo:hi, :N].double()
+        size += float(before[lo:hi, :N].double().abs().max()) if hi > lo else 0
+    # nothing but the groups' rows and columns was written
+    assert torch.equal(got[:lo].nan_to_num(3), before[:lo].nan_to_num(3)) and torch.equal(got[hi:], before[hi:])
+    assert torch.equal(got[:, N:], before[:, N:])
+    close(got[lo:hi, :N], want[lo:hi], size, out)
+    return plan
+
+
+def run_weights(sizes, N, K, kind="bf16", out="f32", first=0, spare=0, lda=0, ldb=0, ldc=0, gap=0, beta=0, seed=0, poison=None):
+    gen = torch.Generator().manual_seed(seed)
+    G, rows = len(sizes), first + sum(sizes) + spare
+    off = offsets_of(sizes, first)
+    A, B = rand((rows, K), kind, gen), rand((rows, N), kind, gen)
+    for x in (A, B):
+        x[:first] = float("nan")
+        x[first + sum(sizes):] = float("inf")
+    if poison is not None:                       # a whole group of NaN must stay in its own gradient
+        A[off[poison]:off[poison + 1]] = float("nan")
+        B[off[poison]:off[poison + 1]] = float("inf")
+    lda, ldb, ldc = lda or K, ldb or N, ldc or N
+    stride = K * ldc + gap
+    C = torch.full((G * stride,), SENTINEL, dtype=TYPES[out][1])
+    view = lambda t, g: t[g * stride: g * stride + K * ldc].view(K, ldc)   # noqa: E731
+    if beta:
+        for g in range(G):
+            view(C, g)[:, :N] = rand((K, N), out, gen)
+    before = C.clone()
+    plan = nk.GroupedPlan(G, rows, N, K, kind=nk.GROUPED_WEIGHTS, in_dtype=TYPES[kind][0], out_dtype=TYPES[out][0], beta=beta,
+                          lda=lda, ldb=ldb, ldc=ldc, stride_g=stride)
+    dC = C.cuda()
+    dA, dB, dO = padded(A, lda), padded(B, ldb), off.cuda()
+    plan.run(dA, dB, dC, dO, workspace=scratch(plan), stream=torch.cuda.current_stream().cuda_stream)
+    plan.check()
+    got = dC.cpu()
+    for g in range(G):
+        lo, hi = int(off[g]), int(off[g + 1])
+        c, old = view(got, g), view(before, g)
+        assert torch.equal(c[:, N:], old[:, N:])
+        assert torch.equal(got[g * stride + K * ldc:(g + 1) * stride], before[g * stride + K * ldc:(g + 1) * stride])
+        if g == poison:
+            assert c[:, :N].isnan().all() or hi == lo
+            continue
+        a, b = A[lo:hi].double().cuda(), B[lo:hi].double().cuda()
+        want = (a.t() @ b).cpu()
+        size = float((a.abs().t() @ b.abs()).max()) if hi > lo else 1e-30
+        if beta:
+            want = want + old[:, :N].double()
+            size += float(old[:, :N].double().abs().max())
+        close(c[:, :N], want, size, out)
+    return plan
+
+
+GROUPS = {
+    "one_row": [1],
+    "single_group": [300],
+    "tile_edges": [255, 256, 257, 1, 0, 33],
+    "empty_first_last": [0, 40, 0, 0, 17, 0],
+    "all_empty": [0, 0, 0],
+    "many_small": [(i * 7) % 5 for i in range(97)],
+    "one_takes_all": [0] * 9 + [700] + [0] * 6,
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(GROUPS))
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+def test_rows_of_ragged_groups(name, layout):
+    run_rows(GROUPS[name], 264, 200, layout=layout, seed=1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("out", ["same", "f32"])
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("beta", [0, 1])
+def test_rows_types_layouts_strides(kind, out, layout, beta):
+    run_rows([5, 130, 0, 64], 328, 136, kind=kind, out=kind if out == "same" else out, layout=layout, first=11, spare=9,
+             lda=152, ldb=344, ldc=336, gap=40, beta=beta, seed=2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,K", [(8, 8), (8, 4096), (1000, 8), (256, 64), (520, 1032), (1024, 2048)])
+def test_rows_sizes(N, K):
+    for layout in ("row", "transposed"):
+        run_rows([3, 1, 0, 70, 2], N, K, out="f32", layout=layout, seed=3)
+
+
+@pytest.mark.gpu
+def test_rows_many_tiles():
+    # more tiles than CTA pairs, more than eight row tiles in a group
+    run_rows([2600, 513, 1, 900], 1288, 512, seed=4)
+    run_rows([2600, 513, 1, 900], 1288, 512, layout="transposed", kind="f16", out="f16", seed=4)
+
+
+@pytest.mark.gpu
+def test_rows_most_groups():
+    gen = np.random.default_rng(5)
+    run_rows(gen.integers(0, 4, 1024).tolist(), 136, 72, seed=5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 2, 40])
+def test_rows_cut_along_k(rows):
+    """Few tiles and a long contraction: K splits, their partial sums added in the same order on every run."""
+    gen = torch.Generator().manual_seed(6)
+    A, W = rand((rows, 8192), "bf16", gen).cuda(), rand((1, 8192, 512), "bf16", gen, 0.01).cuda()
+    off = torch.tensor([0, rows], dtype=torch.int32).cuda()
+    plan = nk.GroupedPlan(1, rows, 512, 8192, out_dtype=nk.F32)
+    outs = []
+    ws = scratch(plan)
+    for _ in range(20):
+        C = torch.full((rows, 512), float("nan"), device="cuda")
+        plan.run(A, W, C, off, workspace=ws, stream=torch.cuda.current_stream().cuda_stream)
+        outs.append(C)
+    plan.check()
+    assert all(torch.equal(outs[0], c) for c in outs)
+    close(outs[0], A.double() @ W[0].double(), float((A.double().abs() @ W[0].double().abs()).max()), "f32")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(GROUPS))
+def test_weights_of_ragged_groups(name):
+    run_weights(GROUPS[name], 264, 200, seed=11)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("out", ["same", "f32"])
+@pytest.mark.parametrize("beta", [0, 1])
+def test_weights_types_strides(kind, out, beta):
+    run_weights([5, 130, 0, 64, 65, 79, 80], 328, 136, kind=kind, out=kind if out == "same" else out, first=11, spare=9,
+                lda=152, ldb=344, ldc=336, gap=40, beta=beta, seed=12)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,K", [(8, 8), (8, 1000), (1000, 8), (256, 256), (520, 296), (1024, 2048)])
+def test_weights_sizes(N, K):
+    run_weights([3, 1, 0, 70, 2], N, K, seed=13)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes,poison", [([37, 5, 50], 1), ([64, 7, 9], 1), ([1, 1, 1], 1), ([15, 16, 17], 2), ([100, 0, 31], 0)])
+def test_weights_neighbours_of_nan(sizes, poison):
+    run_weights(sizes, 136, 264, poison=poison, seed=14)
+
+
+@pytest.mark.gpu
+def test_weights_many_tiles():
+    run_weights([2049, 0, 700, 33, 1], 1288, 1032, out="bf16", seed=15)
+
+
+@pytest.mark.gpu
+def test_rows_neighbours_of_nan():
+    """Infinities and NaN of a row or a weight stay in the rows they belong to."""
+    gen = torch.Generator().manual_seed(16)
+    A, W = rand((90, 64), "bf16", gen), rand((3, 64, 72), "bf16", gen)
+    A[40] = float("nan")
+    W[2] = float("inf")
+    off = torch.tensor([0, 30, 60, 90], dtype=torch.int32)
+    plan = nk.GroupedPlan(3, 90, 72, 64, out_dtype=nk.F32)
+    C = torch.zeros(90, 72, device="cuda")
+    plan.run(A.cuda(), W.cuda(), C, off.cuda(), workspace=scratch(plan), stream=torch.cuda.current_stream().cuda_stream)
+    plan.check()
+    C = C.cpu()
+    keep = [i for i in range(60) if i != 40]
+    assert C[keep].isfinite().all() and C[40].isnan().all() and not C[60:].isfinite().any()
+
+
+@pytest.mark.gpu
+def test_gradients_against_differences():
+    """d/ds of sum(G * (X + s E) W) and of sum(G * X (W + s E)): the loss is linear in s, so the difference
+    quotient of the 64-bit formula is exact up to its rounding."""
+    gen = torch.Generator().manual_seed(17)
+    sizes, N, K = [3, 0, 61], 40, 72
+    rows, off = 64, offsets_of(sizes)
+    X, W, dY = rand((rows, K), "bf16", gen), rand((3, K, N), "bf16", gen), rand((rows, N), "bf16", gen)
+    st = torch.cuda.current_stream().cuda_stream
+    dX, dW = torch.empty(rows, K, device="cuda"), torch.empty(3, K, N, device="cuda")
+    back = nk.GroupedPlan(3, rows, K, N, layout_b=nk.TRANSPOSED, out_dtype=nk.F32)
+    back.run(dY.cuda(), W.cuda(), dX, off.cuda(), workspace=scratch(back), stream=st)
+    grad = nk.GroupedPlan(3, rows, N, K, kind=nk.GROUPED_WEIGHTS, out_dtype=nk.F32)
+    grad.run(X.cuda(), dY.cuda(), dW, off.cuda(), workspace=scratch(grad), stream=st)
+    back.check(), grad.check()
+
+    def loss(x, w):
+        y = torch.cat([x[off[g]:off[g + 1]] @ w[g] for g in range(3)])
+        return float((y * dY.double()).sum())
+
+    x, w = X.double(), W.double()
+    h = 2.0 ** -6
+    for _ in range(5):
+        ex, ew = torch.randn(x.shape, generator=gen).double(), torch.randn(w.shape, generator=gen).double()
+        for grad_of, num in ((float((dX.cpu().double() * ex).sum()), (loss(x + h * ex, w) - loss(x - h * ex, w)) / (2 * h)),
+                             (float((dW.cpu().double() * ew).sum()), (loss(x, w + h * ew) - loss(x, w - h * ew)) / (2 * h))):
+            # n terms of size about sqrt(contraction) each carry a relative FP32 accumulation error below 1e-5
+            n = dX.numel() + dW.numel()
+            assert abs(grad_of - num) <= 1e-5 * np.sqrt(n) * 10 * np.sqrt(max(sizes)), (grad_of, num)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("off", [[0, 50, 20, 90], [-5, 30, 60, 90], [0, 30, 60, 95], [0, -1, 200, 3], [90, 60, 30, 0]])
+def test_offsets_that_break_the_rule_are_reported(off):
+    """The kernel clamps them: nothing outside the arrays is touched, and the check says so once."""
+    gen = torch.Generator().manual_seed(18)
+    A, W, B = rand((90, 64), "bf16", gen).cuda(), rand((3, 64, 72), "bf16", gen).cuda(), rand((90, 72), "bf16", gen).cuda()
+    o = torch.tensor(off, dtype=torch.int32).cuda()
+    st = torch.cuda.current_stream().cuda_stream
+    for plan, args, shape in ((nk.GroupedPlan(3, 90, 72, 64, out_dtype=nk.F32), (A, W), (90, 72)),
+                              (nk.GroupedPlan(3, 90, 72, 64, kind=nk.GROUPED_WEIGHTS, out_dtype=nk.F32), (A, B), (3, 64, 72))):
+        C = torch.full((int(np.prod(shape)) + 512,), SENTINEL, device="cuda")
+        plan.run(*args, C[256:], o, workspace=scratch(plan), stream=st)
+        with pytest.raises(nk.NkError) as e:
+            plan.check()
+        assert e.value.status == 1 and "offsets" in str(e.value)
+        plan.check()
+        assert (C[:256] == SENTINEL).all() and (C[-256:] == SENTINEL).all()
+
+
+@pytest.mark.gpu
+def test_no_rows():
+    plan = nk.GroupedPlan(4, 0, 64, 32)
+    off = torch.zeros(5, dtype=torch.int32, device="cuda")
+    plan.run(None, None, None, off, workspace=scratch(plan))
+    plan.check()
+    grad = nk.GroupedPlan(4, 0, 64, 32, kind=nk.GROUPED_WEIGHTS)
+    C = torch.full((4, 32, 64), SENTINEL, device="cuda")
+    grad.run(None, None, C, off, workspace=scratch(grad))
+    grad.check()
+    assert (C == 0).all()
+
+
+@pytest.mark.gpu
+def test_other_stream_and_new_pointers():
+    """A plan follows the pointers and the stream of each call."""
+    gen = torch.Generator().manual_seed(19)
+    plan = nk.GroupedPlan(2, 50, 40, 64, out_dtype=nk.F32)
+    ws = scratch(plan)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        A, W = rand((50, 64), "bf16", gen).cuda(), rand((2, 64, 40), "bf16", gen).cuda()
+        off = torch.tensor([0, 20, 50], dtype=torch.int32).cuda()
+        C = torch.zeros(50, 40, device="cuda")
+        side.wait_stream(torch.cuda.current_stream())
+        plan.run(A, W, C, off, workspace=ws, stream=side.cuda_stream)
+        side.synchronize()
+        want = torch.cat([A[:20].double() @ W[0].double(), A[20:].double() @ W[1].double()])
+        close(C, want, float((A.double().abs() @ W.double().abs().sum(0)).max()), "f32")
+
+
+@pytest.mark.gpu
+def test_run_refusals():
+    plan = nk.GroupedPlan(2, 50, 40, 64)
+    x = torch.zeros(1 << 16, dtype=torch.bfloat16, device="cuda")
+    c = torch.zeros(1 << 16, device="cuda")
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    ws = scratch(plan)
+    for args, kw, status in (((None, x, c, off), dict(workspace=ws), 1), ((x, x, None, off), dict(workspace=ws), 1),
+                             ((x, x, c, None), dict(workspace=ws), 1), ((x[1:], x, c, off), dict(workspace=ws), 3),
+                             ((x, x[4:], c, off), dict(workspace=ws), 3), ((x, x, c[1:], off), dict(workspace=ws), 3),
+                             ((x, x, c, off), dict(), 4), ((x, x, c, off), dict(workspace=ws, workspace_bytes=plan.workspace_bytes - 1), 4)):
+        with pytest.raises(nk.NkError) as e:
+            plan.run(*args, **kw)
+        assert e.value.status == status
+
+
+REFUSED = [
+    (dict(groups=0), 1), (dict(rows=-1), 1), (dict(N=0), 1), (dict(K=-8), 1), (dict(kind=2), 1), (dict(in_dtype=9), 1),
+    (dict(in_dtype=nk.F32), 2), (dict(in_dtype=nk.S8), 2), (dict(in_dtype=nk.E4M3), 2), (dict(out_dtype=nk.F16), 1),
+    (dict(layout_b=7), 1), (dict(layout_b=nk.BLOCKED32), 2), (dict(kind=nk.GROUPED_WEIGHTS, layout_b=nk.TRANSPOSED), 2),
+    (dict(beta=2), 1), (dict(groups=1025), 2), (dict(N=12), 3), (dict(K=20), 3), (dict(lda=36), 3), (dict(lda=24), 1),
+    (dict(ldb=8), 1), (dict(ldc=8), 1), (dict(stride_g=64), 1), (dict(stride_g=4100), 3), (dict(rows=1 << 31), 2),
+    (dict(rows=(1 << 31) - 8192, N=1 << 20), 2),
+]
+
+
+@pytest.mark.parametrize("kw,status", REFUSED)
+def test_descriptor_refusals_need_no_device(kw, status):
+    args = dict(groups=2, rows=50, N=64, K=32)
+    args.update(kw)
+    with pytest.raises(nk.NkError) as e:
+        nk.GroupedPlan(**args)
+    assert e.value.status == status
+
+
+def test_null_handles():
+    from paper_2511_13764_b200 import rows
+    L = rows.lib()
+    assert L.nk_grouped_create(None, None) == 1
+    assert L.nk_grouped_workspace_bytes(None) == 0 and L.nk_grouped_check(None) == 1 and L.nk_grouped_destroy(None) == 0
+    assert L.nk_grouped_run(None, None, None, None, None, None, 0, None) == 1
+    assert L.nk_grouped_kernel_name(None) == b"" and L.nk_grouped_last_cuda_error(None) == b""
