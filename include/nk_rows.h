@@ -2,6 +2,8 @@
  * nk_rows — layers whose weight is chosen row by row, for NVIDIA B200 (sm_100a), beside the dense GEMM of
  * nk_gemm.h and in the same library:
  *
+ *   nk_route     which experts a row goes to and with what weight, the rows' way to their experts' order and
+ *                back, and the gradients of both
  *   nk_grouped   products grouped by expert over ragged groups of rows, and their gradients
  *
  * Conventions are those of nk_gemm.h: DEVICE pointers on the plan's device, nothing is allocated on the
@@ -70,6 +72,62 @@ nk_status_t nk_grouped_check(nk_grouped_t plan);
 const char* nk_grouped_kernel_name(nk_grouped_t plan);
 const char* nk_grouped_last_cuda_error(nk_grouped_t plan);
 nk_status_t nk_grouped_destroy(nk_grouped_t plan);
+
+/* ------------------------------------------------------------------ routing of rows to experts
+ *
+ * nk_route_run: for every token t, from its row of logits z[t][0..experts):
+ *   experts[t][j]  the indices of its topk largest logits, the largest first, ties by the lower index
+ *   gates[t][j]    softmax(z[t]) at experts[t][j] (over all experts; renormalise = 0), or the softmax over the
+ *                  chosen ones only (renormalise = 1), in FP32
+ *   offsets[e]     (experts + 1 of them) how many (token, j) pairs go to experts below e: the row offsets that
+ *                  nk_grouped takes
+ *   slots[t][j]    the pair's place in the experts' order: offsets[e] + the number of tokens before t that chose e
+ * Logits of minus infinity are experts that may not be chosen: they are chosen only where fewer than topk others
+ * are left, with gate 0; a row with nothing else has all gates 0.  A NaN is smaller than every number in the
+ * choice, and the gates of its row are NaN.
+ *
+ * nk_route_backward: dlogits[t][e] (FP32) from dgates[t][j] = dL / dgates[t][j], logits and experts of the run:
+ *   dz_e = p_e (d_e - sum_j d_j gates_j), d_e = dgates[t][j] where e = experts[t][j], else 0; p the softmax above.
+ *   A row whose logits are all minus infinity gets zeros.
+ * nk_route_dispatch: Xs[slots[t][j]] = X[t].
+ * nk_route_combine:  Y[t] = sum_j gates[t][j] * Ys[slots[t][j]], summed in j's order in FP32, rounded once; gates NULL:
+ *   all ones, which is the gradient of nk_route_dispatch.
+ * nk_route_combine_backward: dYs[slots[t][j]] = gates[t][j] * dY[t] and dgates[t][j] = <dY[t], Ys[slots[t][j]]> (FP32).
+ * A slot outside [0, tokens * topk) is a dropped pair: nothing is written for it, it adds nothing to Y, its dgates
+ * is 0.  X, Y, dY have `tokens` rows; Xs, Ys, dYs have tokens * topk rows; all of `width` 16-bit elements of one type.
+ */
+typedef struct nk_route_s* nk_route_t;
+#define NK_ROUTE_MAX_EXPERTS 1024
+#define NK_ROUTE_MAX_TOPK 32
+
+typedef struct {
+    int64_t tokens;       /* 0 .. 2^24 */
+    int64_t experts;      /* 1 .. NK_ROUTE_MAX_EXPERTS */
+    int64_t topk;         /* 1 .. min(experts, NK_ROUTE_MAX_TOPK) */
+    int64_t width;        /* a multiple of 8; 0: only run and backward are used */
+    int64_t ld_logits;    /* row stride of logits in elements; 0: experts */
+    int64_t ld_tokens;    /* row stride of X, Y, dY; a multiple of 8; 0: width */
+    int64_t ld_slots;     /* row stride of Xs, Ys, dYs; a multiple of 8; 0: width */
+    int32_t logits_dtype; /* NK_F32, NK_BF16 or NK_F16 */
+    int32_t dtype;        /* NK_BF16 or NK_F16: the rows */
+    int32_t renormalise;  /* 0 or 1 */
+    int32_t device;
+} nk_route_desc_t;
+
+nk_status_t nk_route_create(const nk_route_desc_t* desc, nk_route_t* out);
+size_t nk_route_workspace_bytes(nk_route_t plan); /* of nk_route_run; contents need no initialisation */
+nk_status_t nk_route_run(nk_route_t plan, const void* logits, float* gates, int32_t* experts, int32_t* offsets, int32_t* slots,
+                         void* workspace, size_t workspace_bytes, void* cuda_stream);
+nk_status_t nk_route_backward(nk_route_t plan, const void* logits, const int32_t* experts, const float* dgates, float* dlogits,
+                              void* cuda_stream);
+nk_status_t nk_route_dispatch(nk_route_t plan, const void* X, const int32_t* slots, void* Xs, void* cuda_stream);
+nk_status_t nk_route_combine(nk_route_t plan, const void* Ys, const int32_t* slots, const float* gates, void* Y, void* cuda_stream);
+nk_status_t nk_route_combine_backward(nk_route_t plan, const void* dY, const void* Ys, const int32_t* slots, const float* gates,
+                                      void* dYs, float* dgates, void* cuda_stream);
+nk_status_t nk_route_check(nk_route_t plan); /* synchronises the device */
+const char* nk_route_kernel_name(nk_route_t plan);
+const char* nk_route_last_cuda_error(nk_route_t plan);
+nk_status_t nk_route_destroy(nk_route_t plan);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,374 @@
+// Routing: the choice of experts and their weights, the experts' order, the rows' way there and back.
+// Everything here is bound by memory or, for a decoding step, by launches: one pass over each array, no
+// floating-point atomics, and every sum in an order that does not depend on timing.
+#pragma once
+#include "half.cuh"
+
+namespace nk {
+
+struct RouteParams {
+    int tokens, experts, topk, renormalise;
+    int logits_type;            // 0 FP32, 1 BF16, 2 FP16
+    long long ld_logits;
+    const void* logits;
+    float* gates;
+    int* chosen;                // [tokens][topk]
+    int* offsets;               // [experts + 1]
+    int* slots;                 // [tokens][topk]
+    int* counts;                // [blocks][experts]: pairs of a block of tokens, by expert
+    int per_block;              // tokens of a block
+};
+
+__device__ __forceinline__ float route_load(const RouteParams& p, int t, int e) {
+    const size_t o = static_cast<size_t>(t) * p.ld_logits + e;
+    if (p.logits_type == 0) return static_cast<const float*>(p.logits)[o];
+    return half_bits_to_f32(static_cast<const uint16_t*>(p.logits)[o], p.logits_type == 2);
+}
+
+// Unsigned key in the order of the numbers: both zeros alike, NaN below every number (1), 0 left for "taken".
+__device__ __forceinline__ uint32_t route_key(float z) {
+    if (z != z) return 1u;
+    const uint32_t b = __float_as_uint(z + 0.0f);
+    return (b >> 31) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float route_unkey(uint32_t k) {
+    return __uint_as_float((k >> 31) ? k & 0x7FFFFFFFu : ~k);
+}
+
+// One warp, one token: lane l holds experts l, l + 32, ...  (V of them).  topk rounds of a warp-wide maximum of the
+// keys and a minimum of the indices that have it.
+template <int V>
+__device__ __forceinline__ void route_token(const RouteParams& p, int t, int lane) {
+    uint32_t key[V];
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = lane + 32 * i;
+        key[i] = 0u;
+        if (e < p.experts) {
+            const float z = route_load(p, t, e);
+            nan |= z != z;
+            key[i] = route_key(z);
+        }
+    }
+    nan = __any_sync(~0u, nan);
+    uint32_t own_key = 0u;                     // lane j keeps choice j
+    int own = 0;
+    uint32_t first_key = 0u;
+    uint32_t live[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) live[i] = key[i];
+    for (int j = 0; j < p.topk; ++j) {
+        uint32_t best = 0u;
+#pragma unroll
+        for (int i = 0; i < V; ++i) best = max(best, live[i]);
+        const uint32_t top = __reduce_max_sync(~0u, best);
+        uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+        for (int i = V - 1; i >= 0; --i)
+            if (live[i] == top) at = lane + 32 * i;
+        const uint32_t e = __reduce_min_sync(~0u, at);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (static_cast<uint32_t>(lane + 32 * i) == e) live[i] = 0u;
+        if (lane == j) { own_key = top; own = static_cast<int>(e); }
+        if (j == 0) first_key = top;
+    }
+    // weights: exp(z - max) over the sum
+    const float m = route_unkey(first_key);
+    const float mine = lane < p.topk && own_key > 1u ? expf(route_unkey(own_key) - m) : 0.0f;
+    float sum = 0.0f;
+    if (p.renormalise) {
+        sum = mine;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (key[i] > 1u) sum += expf(route_unkey(key[i]) - m);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+    if (lane < p.topk) {
+        const size_t o = static_cast<size_t>(t) * p.topk + lane;
+        const bool none = m == -INFINITY;      // nothing may be chosen
+        p.gates[o] = nan ? __int_as_float(0x7FC00000) : none ? 0.0f : mine / sum;
+        p.chosen[o] = own;
+    }
+}
+
+// exclusive scan of s[0..n) in place by the whole block (n <= 1024, at least 32 threads); returns the total
+__device__ __forceinline__ int block_scan(int* s, int n, int* part) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int chunks = (n + 31) / 32;
+    for (int c = warp; c < chunks; c += warps) {
+        const int i = c * 32 + lane;
+        const int x = i < n ? s[i] : 0;
+        int v = x;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(~0u, v, d);
+            if (lane >= d) v += o;
+        }
+        if (i < n) s[i] = v - x;
+        if (lane == 31) part[c] = v;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        const int x = lane < chunks ? part[lane] : 0;
+        int v = x;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(~0u, v, d);
+            if (lane >= d) v += o;
+        }
+        if (lane < chunks) part[lane] = v - x;
+        if (lane == 31) part[32] = v;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += blockDim.x) s[i] += part[i >> 5];
+    __syncthreads();
+    return part[32];
+}
+
+// The places of the tokens [t0, t1) of one block: `base[e]` is the place of its first pair of expert e.  Each warp
+// has a contiguous run of tokens and a row of counts; after a scan over the warps it walks its tokens in order.
+__device__ __forceinline__ void route_places(const RouteParams& p, int t0, int t1, const int* base, int* rows) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int E = p.experts, run = (t1 - t0 + warps - 1) / warps;
+    const int lo = min(t1, t0 + warp * run), hi = min(t1, lo + run);
+    int* mine = rows + warp * E;
+    for (int e = lane; e < E; e += 32) mine[e] = 0;
+    __syncwarp();
+    for (int i = lo * p.topk + lane; i < hi * p.topk; i += 32) atomicAdd(mine + p.chosen[i], 1);
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        int at = base[e];
+        for (int w = 0; w < warps; ++w) {
+            const int n = rows[w * E + e];
+            rows[w * E + e] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+    for (int t = lo; t < hi; ++t) {
+        if (lane < p.topk) {
+            const size_t o = static_cast<size_t>(t) * p.topk + lane;
+            p.slots[o] = mine[p.chosen[o]]++;      // a token's experts are distinct
+        }
+        __syncwarp();
+    }
+}
+
+constexpr int ROUTE_THREADS = 512;                 // both kernels; 16 warps
+constexpr int ROUTE_ONE_BLOCK = 64;                // up to this many tokens one block does everything
+__host__ __device__ constexpr int route_smem(int experts) { return (16 * experts + 2 * experts + 64) * 4; }
+
+// A block of tokens: choices, weights, and the block's counts by expert.  ONE: the only block; it goes on to the places.
+template <int V, bool ONE>
+__global__ void __launch_bounds__(ROUTE_THREADS) route_select_kernel(const RouteParams p) {
+    extern __shared__ int route_sm[];
+    int* hist = route_sm;                          // [experts]
+    int* part = hist + p.experts;                  // [64]
+    int* rows = part + 64;                         // [16][experts] (ONE)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int t0 = blockIdx.x * p.per_block, t1 = min(p.tokens, t0 + p.per_block);
+    for (int e = threadIdx.x; e < p.experts; e += ROUTE_THREADS) hist[e] = 0;
+    __syncthreads();
+    for (int t = t0 + warp; t < t1; t += ROUTE_THREADS / 32) {
+        route_token<V>(p, t, lane);
+        __syncwarp();
+        if (lane < p.topk) atomicAdd(hist + p.chosen[static_cast<size_t>(t) * p.topk + lane], 1);
+    }
+    __syncthreads();
+    if (ONE) {
+        const int total = block_scan(hist, p.experts, part);
+        for (int e = threadIdx.x; e < p.experts; e += ROUTE_THREADS) p.offsets[e] = hist[e];
+        if (threadIdx.x == 0) p.offsets[p.experts] = total;
+        route_places(p, t0, t1, hist, rows);
+    } else {
+        for (int e = threadIdx.x; e < p.experts; e += ROUTE_THREADS) p.counts[static_cast<size_t>(blockIdx.x) * p.experts + e] = hist[e];
+    }
+}
+
+// The places of a block's pairs from every block's counts: the pairs of lower experts, then those of earlier blocks.
+__global__ void __launch_bounds__(ROUTE_THREADS) route_place_kernel(const RouteParams p) {
+    extern __shared__ int route_sm[];
+    int* total = route_sm;                         // [experts]
+    int* part = total + p.experts;                 // [64]
+    int* rows = part + 64;                         // [16][experts]
+    int* before = rows + 16 * p.experts;           // [experts]
+    const int blocks = gridDim.x, E = p.experts;
+    for (int e = threadIdx.x; e < E; e += ROUTE_THREADS) total[e] = before[e] = 0;
+    __syncthreads();
+    // threads of a row of counts side by side, rows dealt out over what threads are left (integer sums: any order)
+    const int lanes = min(E, ROUTE_THREADS), rowsets = ROUTE_THREADS / lanes;
+    const int set = threadIdx.x / lanes;
+    if (set < rowsets) {
+        for (int e = threadIdx.x - set * lanes; e < E; e += lanes) {
+            int all = 0, early = 0;
+#pragma unroll 8
+            for (int b = set; b < blocks; b += rowsets) {
+                const int n = p.counts[static_cast<size_t>(b) * E + e];
+                all += n;
+                if (b < static_cast<int>(blockIdx.x)) early += n;
+            }
+            atomicAdd(total + e, all);
+            atomicAdd(before + e, early);
+        }
+    }
+    __syncthreads();
+    const int sum = block_scan(total, E, part);
+    if (blockIdx.x == 0) {
+        for (int e = threadIdx.x; e < E; e += ROUTE_THREADS) p.offsets[e] = total[e];
+        if (threadIdx.x == 0) p.offsets[E] = sum;
+    }
+    for (int e = threadIdx.x; e < E; e += ROUTE_THREADS) total[e] += before[e];
+    __syncthreads();
+    const int t0 = blockIdx.x * p.per_block, t1 = min(p.tokens, t0 + p.per_block);
+    route_places(p, t0, t1, total, rows);
+}
+
+// dz_e = p_e (d_e - sum_j d_j g_j): one warp per token, the row's softmax taken again (cheaper than keeping it)
+template <int V>
+__global__ void __launch_bounds__(256) route_backward_kernel(const RouteParams p, const float* dgates, float* dlogits) {
+    const int lane = threadIdx.x & 31;
+    const int t = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (t >= p.tokens) return;
+    float z[V], d[V];
+    float m = -INFINITY;
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = lane + 32 * i;
+        z[i] = e < p.experts ? route_load(p, t, e) : -INFINITY;
+        d[i] = 0.0f;
+        nan |= z[i] != z[i];
+        m = fmaxf(m, z[i]);
+    }
+    nan = __any_sync(~0u, nan);
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, s));
+    const size_t o = static_cast<size_t>(t) * p.topk;
+    uint32_t taken = 0u;                           // bit i: this lane's expert i is one of the chosen
+    const int own = lane < p.topk ? p.chosen[o + lane] : -1;
+    const float own_d = lane < p.topk ? dgates[o + lane] : 0.0f;
+    for (int j = 0; j < p.topk; ++j) {
+        const int e = __shfl_sync(~0u, own, j);
+        const float g = __shfl_sync(~0u, own_d, j);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (e == lane + 32 * i) { d[i] = g; taken |= 1u << i; }
+    }
+    float sum = 0.0f, inner = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const bool in = !p.renormalise || ((taken >> i) & 1u);
+        z[i] = in ? expf(z[i] - m) : 0.0f;
+        sum += z[i];
+        inner += z[i] * d[i];
+    }
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+        sum += __shfl_xor_sync(~0u, sum, s);
+        inner += __shfl_xor_sync(~0u, inner, s);
+    }
+    const bool none = m == -INFINITY && !nan;
+    const float inv = 1.0f / sum;
+    inner *= inv;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = lane + 32 * i;
+        if (e < p.experts) {
+            float x = z[i] * inv * (d[i] - inner);
+            if (p.renormalise && !((taken >> i) & 1u)) x = 0.0f;
+            dlogits[static_cast<size_t>(t) * p.experts + e] = nan ? __int_as_float(0x7FC00000) : none ? 0.0f : x;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- rows to their experts' order and back
+struct ExchangeParams {
+    int tokens, topk, vecs;     // vecs: 16-byte pieces of a row
+    int f16;
+    long long ld_tokens, ld_slots;   // in 16-byte pieces
+    const int* slots;
+    const float* gates;
+};
+
+__device__ __forceinline__ void unpack8(const uint4& v, int f16, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = half_bits_to_f32(w[i] & 0xFFFFu, f16);
+        x[2 * i + 1] = half_bits_to_f32(w[i] >> 16, f16);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float (&x)[8], int f16) {
+    return make_uint4(pack_half2(x[0], x[1], f16), pack_half2(x[2], x[3], f16), pack_half2(x[4], x[5], f16), pack_half2(x[6], x[7], f16));
+}
+
+// a thread reads one piece of a token's row and writes it to the topk places
+__global__ void __launch_bounds__(256) dispatch_kernel(const ExchangeParams p, const uint4* x, uint4* xs) {
+    const long long n = static_cast<long long>(p.tokens) * p.vecs, pairs = static_cast<long long>(p.tokens) * p.topk;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+        const long long t = i / p.vecs;
+        const int v = static_cast<int>(i - t * p.vecs);
+        const uint4 r = x[t * p.ld_tokens + v];
+        for (int j = 0; j < p.topk; ++j) {
+            const int s = __ldg(p.slots + t * p.topk + j);
+            if (s >= 0 && s < pairs) xs[s * p.ld_slots + v] = r;
+        }
+    }
+}
+
+// a thread adds one piece of the topk rows of a token
+__global__ void __launch_bounds__(256) combine_kernel(const ExchangeParams p, const uint4* ys, uint4* y) {
+    const long long n = static_cast<long long>(p.tokens) * p.vecs, pairs = static_cast<long long>(p.tokens) * p.topk;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+        const long long t = i / p.vecs;
+        const int v = static_cast<int>(i - t * p.vecs);
+        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < p.topk; ++j) {
+            const int s = __ldg(p.slots + t * p.topk + j);
+            if (s < 0 || s >= pairs) continue;
+            const float g = p.gates ? __ldg(p.gates + t * p.topk + j) : 1.0f;
+            float r[8];
+            unpack8(ys[s * p.ld_slots + v], p.f16, r);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q] += g * r[q];
+        }
+        y[t * p.ld_tokens + v] = pack8(sum, p.f16);
+    }
+}
+
+// a warp per (token, j): the pair's row of dYs, and the product of two rows for its dgates
+__global__ void __launch_bounds__(256) combine_backward_kernel(const ExchangeParams p, const uint4* dy, const uint4* ys, uint4* dys, float* dgates) {
+    const int lane = threadIdx.x & 31;
+    const long long pairs = static_cast<long long>(p.tokens) * p.topk;
+    const long long i = blockIdx.x * 8ll + (threadIdx.x >> 5);
+    if (i >= pairs) return;
+    const long long t = i / p.topk;
+    const int s = p.slots[i];
+    if (s < 0 || s >= pairs) {
+        if (lane == 0) dgates[i] = 0.0f;
+        return;
+    }
+    const float g = p.gates[i];
+    float dot = 0.0f;
+#pragma unroll 4
+    for (int v = lane; v < p.vecs; v += 32) {
+        float a[8], b[8];
+        unpack8(dy[t * p.ld_tokens + v], p.f16, a);
+        unpack8(ys[s * p.ld_slots + v], p.f16, b);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            dot += a[q] * b[q];
+            a[q] *= g;
+        }
+        dys[s * p.ld_slots + v] = pack8(a, p.f16);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) dot += __shfl_xor_sync(~0u, dot, d);
+    if (lane == 0) dgates[i] = dot;
+}
+
+}  // namespace nk

@@ -10,13 +10,21 @@ from .binding import BF16, F32, ROW_MAJOR, NkError, _ptr
 GROUPED_ROWS, GROUPED_WEIGHTS = 0, 1
 
 EXPORTS = ["nk_grouped_create", "nk_grouped_workspace_bytes", "nk_grouped_run", "nk_grouped_check",
-           "nk_grouped_kernel_name", "nk_grouped_last_cuda_error", "nk_grouped_destroy"]
+           "nk_grouped_kernel_name", "nk_grouped_last_cuda_error", "nk_grouped_destroy",
+           "nk_route_create", "nk_route_workspace_bytes", "nk_route_run", "nk_route_backward", "nk_route_dispatch",
+           "nk_route_combine", "nk_route_combine_backward", "nk_route_check", "nk_route_kernel_name",
+           "nk_route_last_cuda_error", "nk_route_destroy"]
 
 
 class GroupedDesc(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int64) for n in ("groups", "rows", "N", "K")]
                 + [(n, ctypes.c_int32) for n in ("kind", "in_dtype", "out_dtype", "layout_b", "beta", "device")]
                 + [(n, ctypes.c_int64) for n in ("lda", "ldb", "ldc", "stride_g")])
+
+
+class RouteDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("tokens", "experts", "topk", "width", "ld_logits", "ld_tokens", "ld_slots")]
+                + [(n, ctypes.c_int32) for n in ("logits_dtype", "dtype", "renormalise", "device")])
 
 
 _lib = None
@@ -27,7 +35,7 @@ def lib():
     if _lib is None:
         L = binding.lib()
         vp, sz = ctypes.c_void_p, ctypes.c_size_t
-        for family, desc in (("grouped", GroupedDesc),):
+        for family, desc in (("grouped", GroupedDesc), ("route", RouteDesc)):
             create = getattr(L, f"nk_{family}_create")
             create.restype, create.argtypes = ctypes.c_int, [ctypes.POINTER(desc), ctypes.POINTER(vp)]
             for name, result in (("workspace_bytes", sz), ("check", ctypes.c_int), ("destroy", ctypes.c_int),
@@ -36,6 +44,11 @@ def lib():
                 f.restype, f.argtypes = result, [vp]
         L.nk_grouped_run.restype = ctypes.c_int
         L.nk_grouped_run.argtypes = [vp] * 6 + [sz, vp]
+        L.nk_route_run.restype = ctypes.c_int
+        L.nk_route_run.argtypes = [vp] * 7 + [sz, vp]
+        for name, pointers in (("backward", 4), ("dispatch", 3), ("combine", 4), ("combine_backward", 6)):
+            f = getattr(L, f"nk_route_{name}")
+            f.restype, f.argtypes = ctypes.c_int, [vp] * (pointers + 2)
         _lib = L
     return _lib
 
@@ -106,5 +119,43 @@ class GroupedPlan(_Handle):
         """offsets: device INT32 [groups + 1]; never read by the host."""
         status = lib().nk_grouped_run(self._h, _ptr(A), _ptr(B), _ptr(C), _ptr(offsets), _ptr(workspace),
                                       _bytes(workspace, workspace_bytes), stream)
+        if status:
+            self._check(status)
+
+
+class RoutePlan(_Handle):
+    """nk_route: choice of experts and gates, the rows' way to their experts' order and back, and the gradients."""
+    family = "route"
+
+    def __init__(self, tokens, experts, topk, width=0, logits_dtype=F32, dtype=BF16, renormalise=1, device=0,
+                 ld_logits=0, ld_tokens=0, ld_slots=0):
+        self._create(RouteDesc(tokens, experts, topk, width, ld_logits, ld_tokens, ld_slots, logits_dtype, dtype,
+                               renormalise, device))
+
+    def run(self, logits, gates, experts, offsets, slots, workspace=None, workspace_bytes=None, stream=None):
+        status = lib().nk_route_run(self._h, _ptr(logits), _ptr(gates), _ptr(experts), _ptr(offsets), _ptr(slots),
+                                    _ptr(workspace), _bytes(workspace, workspace_bytes), stream)
+        if status:
+            self._check(status)
+
+    def backward(self, logits, experts, dgates, dlogits, stream=None):
+        status = lib().nk_route_backward(self._h, _ptr(logits), _ptr(experts), _ptr(dgates), _ptr(dlogits), stream)
+        if status:
+            self._check(status)
+
+    def dispatch(self, X, slots, Xs, stream=None):
+        status = lib().nk_route_dispatch(self._h, _ptr(X), _ptr(slots), _ptr(Xs), stream)
+        if status:
+            self._check(status)
+
+    def combine(self, Ys, slots, Y, gates=None, stream=None):
+        """gates None: plain sum, the gradient of dispatch."""
+        status = lib().nk_route_combine(self._h, _ptr(Ys), _ptr(slots), _ptr(gates), _ptr(Y), stream)
+        if status:
+            self._check(status)
+
+    def combine_backward(self, dY, Ys, slots, gates, dYs, dgates, stream=None):
+        status = lib().nk_route_combine_backward(self._h, _ptr(dY), _ptr(Ys), _ptr(slots), _ptr(gates), _ptr(dYs),
+                                                 _ptr(dgates), stream)
         if status:
             self._check(status)
