@@ -5,6 +5,7 @@
  *   nk_route     which experts a row goes to and with what weight, the rows' way to their experts' order and
  *                back, and the gradients of both
  *   nk_grouped   products grouped by expert over ragged groups of rows, and their gradients
+ *   nk_lora      a shared projection with the low-rank adapters of many requests beside it
  *
  * Conventions are those of nk_gemm.h: DEVICE pointers on the plan's device, nothing is allocated on the
  * device, nothing synchronises inside a run call, failures are status codes, and a plan (with its workspace)
@@ -128,6 +129,51 @@ nk_status_t nk_route_check(nk_route_t plan); /* synchronises the device */
 const char* nk_route_kernel_name(nk_route_t plan);
 const char* nk_route_last_cuda_error(nk_route_t plan);
 nk_status_t nk_route_destroy(nk_route_t plan);
+
+/* ------------------------------------------------------------------ low-rank adapters of many requests
+ *
+ *   Y[t] = X[t] . W + scale[a] * (X[t] . A_a) . B_a        a = adapter[q] of the request q that row t belongs to
+ *
+ * `offsets` is a device array of requests + 1 non-decreasing INT32 row numbers as for nk_grouped: request q owns the
+ * rows offsets[q] .. offsets[q+1]-1 (one row each in a decoding step, many for a prompt, none is fine; any mix).
+ * `adapter` is a device array of `requests` INT32 numbers; a number outside [0, adapters) means no adapter.  Rows
+ * outside all requests get the shared projection alone.  `scale` is a device array of `adapters` FP32 numbers.
+ *
+ *   layout NK_ROW_MAJOR    W [K][N],  A [adapters][K][rank],  B [adapters][rank][N]
+ *   layout NK_TRANSPOSED   W [N][K],  A [adapters][rank][K],  B [adapters][N][rank]   (linear layers' [out][in])
+ *
+ * Adapters of a lower rank are padded with zeros.  16-bit operands of one type, FP32 accumulation, Y in FP32 or rounded
+ * once to the operands' type.  X . A_a is held in FP32, or as the sum of two 16-bit numbers (good to 2^-16 of it with
+ * NK_BF16, 2^-21 with NK_F16) where the tensor cores multiply it by B_a; with NK_F16 |scale * X . A_a| has to stay within
+ * the type's range then.
+ * Offsets that break the rule are clamped and reported by nk_lora_check, as for nk_grouped.
+ */
+typedef struct nk_lora_s* nk_lora_t;
+#define NK_LORA_MAX_RANK 128
+#define NK_LORA_MAX_REQUESTS 1024
+
+typedef struct {
+    int64_t rows;      /* extent of X and Y; 0 is allowed */
+    int64_t N, K;      /* multiples of 8 */
+    int64_t rank;      /* a multiple of 8, up to NK_LORA_MAX_RANK */
+    int64_t adapters;  /* 1 .. 65535 */
+    int64_t requests;  /* 1 .. NK_LORA_MAX_REQUESTS */
+    int32_t in_dtype;  /* NK_BF16 or NK_F16: X, W, A, B */
+    int32_t out_dtype; /* NK_F32, or the operands' type */
+    int32_t layout;    /* NK_ROW_MAJOR or NK_TRANSPOSED, of W, A and B alike */
+    int32_t device;
+    int64_t ldx, ldw, ldy; /* row strides of X, W and Y; multiples of 8; 0: dense.  A and B are dense */
+} nk_lora_desc_t;
+
+nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out);
+size_t nk_lora_workspace_bytes(nk_lora_t plan); /* contents need no initialisation */
+nk_status_t nk_lora_run(nk_lora_t plan, const void* X, const void* W, const void* A, const void* B, const float* scale,
+                        const int32_t* offsets, const int32_t* adapter, void* Y, void* workspace, size_t workspace_bytes,
+                        void* cuda_stream);
+nk_status_t nk_lora_check(nk_lora_t plan); /* as nk_grouped_check */
+const char* nk_lora_kernel_name(nk_lora_t plan);
+const char* nk_lora_last_cuda_error(nk_lora_t plan);
+nk_status_t nk_lora_destroy(nk_lora_t plan);
 
 #ifdef __cplusplus
 }

@@ -7,4 +7,4 @@ from .binding import (  # noqa: F401
     FLAG_SCALAR_FMA, FLAG_SEPARATE_REDUCE, FLAG_LSU_STORE, FLAG_NO_TAIL_SPLIT, FLAG_F32_TENSOR,
     flag_splitk, flag_tile_n, flag_tail_split, flag_raster, plan_for, quantize_s8, STATIC_SCRATCH_BYTES,
 )
-from .rows import GroupedPlan, RoutePlan, GROUPED_ROWS, GROUPED_WEIGHTS  # noqa: F401
+from .rows import GroupedPlan, LoraPlan, RoutePlan, GROUPED_ROWS, GROUPED_WEIGHTS  # noqa: F401

@@ -19,38 +19,11 @@
 // ones), 10 (WEIGHTS) clears the rows of a group's last k-block that belong to the next group.
 // All waits are bounded (see mbar_wait).
 #pragma once
-#include <cuda.h>
+#include "grouped_launch.cuh"
 #include "half.cuh"
 #include "ptx.cuh"
 
 namespace nk {
-
-constexpr int GRP_THREADS = 352;
-constexpr int GRP_MAX_GROUPS = 1024;
-constexpr int GRP_STAGES = 6;
-constexpr int GRP_A_BYTES = 128 * 64 * 2;
-constexpr int GRP_STAGE = 2 * GRP_A_BYTES;             // 16 KB of features, up to 16 KB of rows, per CTA
-constexpr int GRP_BK = 64;
-constexpr int GRP_TILE = 256;                          // features of a tile, and the most rows of one
-constexpr int GRP_MAX_SPLITS = 16;
-constexpr int GRP_SMEM = GRP_STAGES * GRP_STAGE + 1024 + 2 * 4 * (GRP_MAX_GROUPS + 1) + 512;
-
-struct GroupedParams {
-    int groups, rows;      // rows: extent of the row arrays; offsets are clamped to it
-    int I, J;              // features (contiguous in C); WEIGHTS: rows of each C_g
-    int kb_total;          // ROWS: k-blocks of the contraction
-    int tiles_i;           // ceil(I / 256)
-    int tiles_j;           // WEIGHTS: ceil(J / 256)
-    int beta, out16, f16;
-    uint32_t idesc;        // without the N field
-    const int* offsets;    // [groups + 1]; null: one group of all rows
-    void* C;
-    const float* add;      // ROWS: FP32 [rows][I], added before the rounding; null: none
-    long long ldc, stride_c;
-    float* partial;        // K splits: [unit][split][CTA of the pair][column][128 features]
-    unsigned int* counter; // one per (unit, CTA of the pair); zero before and after every launch
-    unsigned int* status;
-};
 
 // Work of one unit.
 struct GroupedUnit {

@@ -1,0 +1,273 @@
+// The adapters' part of nk_lora for requests of few rows: D[t] = scale_a (X[t] . A_a) . B_a in FP32.
+//
+// With a row or a few per request this is two reads, of A_a and B_a, and next to no arithmetic: each weight is
+// used for up to eight rows at a time on the FMA units.  A cluster of eight CTAs takes eight rows of one request:
+// every CTA multiplies its eighth of K, the eight partial results are added (in the order of the CTAs) through
+// distributed shared memory, and every CTA then multiplies its eighth of N.  So even sixteen requests spread their
+// weights' reads over 128 SMs, and X . A_a never leaves the cluster.
+#pragma once
+#include "half.cuh"
+#include "ptx.cuh"
+
+namespace nk {
+
+constexpr int LORA_CLUSTER = 8, LORA_THREADS = 256, LORA_ROWS = 8;
+constexpr int LORA_MAX_RANK = 128, LORA_MAX_REQUESTS = 1024;
+constexpr int LORA_KSTEP = 512;                 // k of X kept in shared memory at a time
+
+struct LoraParams {
+    int rows, N, K, rank, adapters, requests;
+    int transposed, f16;
+    long long ldx;
+    const void *X, *A, *B;
+    const float* scale;
+    const int *offsets, *adapter;
+    float* D;                                   // [rows][N]
+    unsigned int* status;
+};
+
+// Rows of the requests, clamped and monotone, and the chunks of LORA_ROWS rows before each request.
+__device__ __forceinline__ void lora_prefix(const LoraParams& p, int* s_row, int* s_pre) {
+    const int lane = threadIdx.x & 31;
+    for (int q = threadIdx.x; q <= p.requests; q += LORA_THREADS) s_row[q] = p.offsets[q];
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        int top = 0, chunks = 0;
+        bool bad = false;
+        for (int base = 0; base <= p.requests; base += 32) {
+            const int q = base + lane;
+            const int raw = q <= p.requests ? s_row[q] : 0;
+            int v = min(max(raw, 0), p.rows);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(~0u, v, d);
+                if (lane >= d) v = max(v, o);
+            }
+            v = max(v, top);
+            if (q <= p.requests) {
+                bad |= v != raw;
+                s_row[q] = v;
+            }
+            top = __shfl_sync(~0u, v, 31);
+        }
+        if (__any_sync(~0u, bad) && lane == 0 && blockIdx.x == 0 && p.status) atomicCAS(p.status, 0u, 0x10000u);
+        __syncwarp();
+        for (int base = 0; base <= p.requests; base += 32) {
+            const int q = base + lane;
+            int n = 0;
+            if (q < p.requests) {
+                const int a = p.adapter[q];
+                if (a >= 0 && a < p.adapters) n = (s_row[q + 1] - s_row[q] + LORA_ROWS - 1) / LORA_ROWS;
+            }
+            int v = n;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(~0u, v, d);
+                if (lane >= d) v += o;
+            }
+            if (q <= p.requests) s_pre[q] = chunks + v - n;
+            chunks += __shfl_sync(~0u, v, 31);
+        }
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void lora_unpack8(const uint4& v, int f16, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = half_bits_to_f32(w[i] & 0xFFFFu, f16);
+        x[2 * i + 1] = half_bits_to_f32(w[i] >> 16, f16);
+    }
+}
+
+// RT rows (1 or LORA_ROWS) of one request; `n` of them exist.  h: this CTA's share of X . A_a, then the whole of it.
+template <int RT>
+__device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n, int a, uint32_t crank, float* xs, float* part,
+                                           float* share, float* h) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int R = p.rank;
+    const uint16_t* X = static_cast<const uint16_t*>(p.X);
+    const uint16_t* A = static_cast<const uint16_t*>(p.A) + static_cast<size_t>(a) * R * p.K;
+    const uint16_t* B = static_cast<const uint16_t*>(p.B) + static_cast<size_t>(a) * R * p.N;
+    // this CTA's share of K and N, in steps of 8
+    const int kw = ((p.K + LORA_CLUSTER * 8 - 1) / (LORA_CLUSTER * 8)) * 8, k_lo = min(p.K, static_cast<int>(crank) * kw), k_hi = min(p.K, k_lo + kw);
+    const int nw = ((p.N + LORA_CLUSTER * 8 - 1) / (LORA_CLUSTER * 8)) * 8, n_lo = min(p.N, static_cast<int>(crank) * nw), n_hi = min(p.N, n_lo + nw);
+
+    for (int i = threadIdx.x; i < RT * R; i += LORA_THREADS) share[i] = 0.0f;
+    // part[warp][r][RT] (row-major weights only): each warp's sums
+    for (int k0 = k_lo; k0 < k_hi; k0 += LORA_KSTEP) {
+        const int kn = min(LORA_KSTEP, k_hi - k0);
+        __syncthreads();
+        // X as FP32, [k][RT]
+        for (int i = threadIdx.x; i < kn * RT; i += LORA_THREADS) {
+            const int t = i / kn, k = i - t * kn;
+            xs[k * RT + t] = t < n ? half_bits_to_f32(X[static_cast<size_t>(row0 + t) * p.ldx + k0 + k], p.f16) : 0.0f;
+        }
+        __syncthreads();
+        if (p.transposed) {
+            // a warp per rank, lanes along k
+            for (int r = warp; r < R; r += LORA_THREADS / 32) {
+                float acc[RT];
+#pragma unroll
+                for (int t = 0; t < RT; ++t) acc[t] = 0.0f;
+#pragma unroll 2
+                for (int k = lane * 8; k < kn; k += 256) {
+                    float w[8];
+                    lora_unpack8(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k0 + k)), p.f16, w);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) acc[t] += w[q] * xs[(k + q) * RT + t];
+                }
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) acc[t] += __shfl_xor_sync(~0u, acc[t], d);
+                    if (lane == 0) share[r * RT + t] += acc[t];
+                }
+            }
+        } else {
+            // lanes along pairs of ranks, then along k; warps along k; the warps' sums meet in shared memory
+            const int pairs = R / 2;
+            int wide = 4;
+            while (wide < pairs && wide < 32) wide *= 2;            // lanes for one k
+            const int kl = lane / wide, deep = 32 / wide;
+            for (int r0 = 0; r0 < pairs; r0 += wide) {
+                const int pr = r0 + lane % wide;
+                float acc0[RT], acc1[RT];
+#pragma unroll
+                for (int t = 0; t < RT; ++t) acc0[t] = acc1[t] = 0.0f;
+                if (pr < pairs) {
+#pragma unroll 8
+                    for (int k = warp * deep + kl; k < kn; k += deep * (LORA_THREADS / 32)) {
+                        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(A + static_cast<size_t>(k0 + k) * R) + pr);
+                        const float w0 = half_bits_to_f32(w & 0xFFFFu, p.f16), w1 = half_bits_to_f32(w >> 16, p.f16);
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) {
+                            acc0[t] += w0 * xs[k * RT + t];
+                            acc1[t] += w1 * xs[k * RT + t];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    for (int d = wide; d < 32; d <<= 1) {
+                        acc0[t] += __shfl_xor_sync(~0u, acc0[t], d);
+                        acc1[t] += __shfl_xor_sync(~0u, acc1[t], d);
+                    }
+                    if (kl == 0 && pr < pairs) {
+                        part[(warp * R + 2 * pr) * RT + t] = acc0[t];
+                        part[(warp * R + 2 * pr + 1) * RT + t] = acc1[t];
+                    }
+                }
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < R * RT; i += LORA_THREADS) {
+                float s = share[i];
+#pragma unroll
+                for (int w = 0; w < LORA_THREADS / 32; ++w) s += part[w * R * RT + i];
+                share[i] = s;
+            }
+        }
+    }
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    const float scale = __ldg(p.scale + a);
+    const uint32_t share_addr = smem_u32(share);
+    for (int i = threadIdx.x; i < R * RT; i += LORA_THREADS) {
+        float v[LORA_CLUSTER];
+#pragma unroll
+        for (int c = 0; c < LORA_CLUSTER; ++c)
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c]) : "r"(map_to_cta(share_addr + 4 * i, c)) : "memory");
+        float s = v[0];
+#pragma unroll
+        for (int c = 1; c < LORA_CLUSTER; ++c) s += v[c];
+        h[i] = s * scale;
+    }
+    cluster_arrive();          // `share` may be written again once every CTA has read it
+    cluster_wait();
+    __syncthreads();
+    if (p.transposed) {
+        for (int i = n_lo + threadIdx.x; i < n_hi; i += LORA_THREADS) {
+            float acc[RT];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) acc[t] = 0.0f;
+#pragma unroll 4
+            for (int r = 0; r < R; r += 8) {
+                float w[8];
+                lora_unpack8(__ldg(reinterpret_cast<const uint4*>(B + static_cast<size_t>(i) * R + r)), p.f16, w);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) acc[t] += w[q] * h[(r + q) * RT + t];
+            }
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+                if (t < n) p.D[static_cast<size_t>(row0 + t) * p.N + i] = acc[t];
+        }
+    } else {
+        for (int i = n_lo + 2 * threadIdx.x; i < n_hi; i += 2 * LORA_THREADS) {
+            float acc0[RT], acc1[RT];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) acc0[t] = acc1[t] = 0.0f;
+#pragma unroll 8
+            for (int r = 0; r < R; ++r) {
+                const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(B + static_cast<size_t>(r) * p.N + i));
+                const float w0 = half_bits_to_f32(w & 0xFFFFu, p.f16), w1 = half_bits_to_f32(w >> 16, p.f16);
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    acc0[t] += w0 * h[r * RT + t];
+                    acc1[t] += w1 * h[r * RT + t];
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+                if (t < n) *reinterpret_cast<float2*>(p.D + static_cast<size_t>(row0 + t) * p.N + i) = make_float2(acc0[t], acc1[t]);
+        }
+    }
+    __syncthreads();
+}
+
+constexpr int LORA_SMEM = 4 * (LORA_KSTEP * LORA_ROWS + (LORA_THREADS / 32) * LORA_MAX_RANK * LORA_ROWS + 2 * LORA_MAX_RANK * LORA_ROWS +
+                               2 * (LORA_MAX_REQUESTS + 1));
+
+__global__ void __launch_bounds__(LORA_THREADS) __cluster_dims__(LORA_CLUSTER, 1, 1) lora_delta_kernel(const LoraParams p) {
+    extern __shared__ float lora_sm[];
+    float* xs = lora_sm;
+    float* part = xs + LORA_KSTEP * LORA_ROWS;
+    float* share = part + (LORA_THREADS / 32) * LORA_MAX_RANK * LORA_ROWS;
+    float* h = share + LORA_MAX_RANK * LORA_ROWS;
+    int* s_row = reinterpret_cast<int*>(h + LORA_MAX_RANK * LORA_ROWS);
+    int* s_pre = s_row + LORA_MAX_REQUESTS + 1;
+    lora_prefix(p, s_row, s_pre);
+    const uint32_t crank = cluster_ctarank();
+    const int clusters = gridDim.x / LORA_CLUSTER, chunks = s_pre[p.requests];
+    // rows without an adapter add nothing: zeros, all threads of the grid (rows of no request among them)
+    const int stride = gridDim.x * LORA_THREADS;
+    for (int q = -1; q <= p.requests; ++q) {
+        if (q >= 0 && q < p.requests) {
+            if (s_pre[q + 1] > s_pre[q] || s_row[q + 1] == s_row[q]) continue;
+        }
+        const int lo = q < 0 ? 0 : s_row[q], hi = q < 0 ? s_row[0] : q == p.requests ? p.rows : s_row[q + 1];
+        const size_t first = static_cast<size_t>(lo) * p.N / 4, last = static_cast<size_t>(hi) * p.N / 4;
+        for (size_t i = first + blockIdx.x * LORA_THREADS + threadIdx.x; i < last; i += stride)
+            reinterpret_cast<float4*>(p.D)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int c = blockIdx.x / LORA_CLUSTER; c < chunks; c += clusters) {
+        int lo = 0, hi = p.requests;                       // s_pre[lo] <= c < s_pre[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s_pre[mid] <= c) lo = mid;
+            else hi = mid;
+        }
+        const int row0 = s_row[lo] + (c - s_pre[lo]) * LORA_ROWS;
+        const int n = min(LORA_ROWS, s_row[lo + 1] - row0);
+        const int a = p.adapter[lo];
+        if (n == 1) lora_chunk<1>(p, row0, n, a, crank, xs, part, share, h);
+        else lora_chunk<LORA_ROWS>(p, row0, n, a, crank, xs, part, share, h);
+    }
+}
+
+}  // namespace nk

@@ -4,26 +4,45 @@
 
 namespace nk {
 
-// Arrival counters of the K splits, zero between launches (the last arriver of a tile clears its own).  A plan
-// holds a slot of this table from create to destroy; where none is free it runs without K splits.
-constexpr int SPLIT_SLOTS = 1024, SPLIT_COUNTERS = 128;
+constexpr int SPLIT_SLOTS = 1024;
 __device__ unsigned int g_split_counter[SPLIT_SLOTS][SPLIT_COUNTERS];
 static std::mutex g_split_mutex;
 static bool g_split_taken[SPLIT_SLOTS];
 
-static int take_split_slot() {
+int take_split_slot(unsigned int** counters) {
+    *counters = nullptr;
+    void* sym = nullptr;
+    if (cudaGetSymbolAddress(&sym, g_split_counter) != cudaSuccess) {
+        cudaGetLastError();
+        return -1;
+    }
     std::lock_guard<std::mutex> lock(g_split_mutex);
     for (int i = 0; i < SPLIT_SLOTS; ++i)
         if (!g_split_taken[i]) {
             g_split_taken[i] = true;
+            *counters = static_cast<unsigned int*>(sym) + i * SPLIT_COUNTERS;
             return i;
         }
     return -1;
 }
-static void give_split_slot(int slot) {
+void give_split_slot(int slot) {
     if (slot < 0) return;
     std::lock_guard<std::mutex> lock(g_split_mutex);
     g_split_taken[slot] = false;
+}
+
+typedef void (*GroupedKernel)(CUtensorMap, CUtensorMap, CUtensorMap, GroupedParams);
+static GroupedKernel grouped_kernel_for(bool weights, bool a_mn) {
+    if (weights) return grouped_kernel<true, true>;
+    return a_mn ? grouped_kernel<false, true> : grouped_kernel<false, false>;
+}
+cudaError_t grouped_prepare(bool weights, bool a_mn) {
+    return cudaFuncSetAttribute(grouped_kernel_for(weights, a_mn), cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM);
+}
+cudaError_t grouped_launch(bool weights, bool a_mn, int pairs, cudaStream_t st, const CUtensorMap& a, const CUtensorMap& b,
+                           const CUtensorMap& b16, const GroupedParams& p) {
+    grouped_kernel_for(weights, a_mn)<<<2 * pairs, GRP_THREADS, GRP_SMEM, st>>>(a, b, b16, p);
+    return cudaGetLastError();
 }
 
 }  // namespace nk
@@ -39,24 +58,6 @@ struct nk_grouped_s : nk::PlanBase {
 };
 
 using namespace nk;
-
-namespace nk {
-
-// tcgen05 instruction descriptor without N: kind::f16, FP32 accumulator, M = 256 over the pair
-static uint32_t grouped_idesc(bool a_mn, bool b_mn, bool f16) {
-    uint32_t d = 1u << 4;
-    d |= (f16 ? 0u : 1u) << 7 | (f16 ? 0u : 1u) << 10;
-    d |= (a_mn ? 1u : 0u) << 15 | (b_mn ? 1u : 0u) << 16;
-    return d | (256u >> 4) << 24;
-}
-
-typedef void (*GroupedKernel)(CUtensorMap, CUtensorMap, CUtensorMap, GroupedParams);
-static GroupedKernel grouped_kernel_for(const nk_grouped_desc_t& d) {
-    if (d.kind == NK_GROUPED_WEIGHTS) return grouped_kernel<true, true>;
-    return d.layout_b == NK_TRANSPOSED ? grouped_kernel<false, false> : grouped_kernel<false, true>;
-}
-
-}  // namespace nk
 
 extern "C" {
 
@@ -99,17 +100,9 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     DeviceGuard guard(d.device);
     if (!encode_tiled()) { delete p; return NK_ERR_CUDA; }
-    const void* kernel = reinterpret_cast<const void*>(grouped_kernel_for(d));
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
+    if (grouped_prepare(weights, weights || d.layout_b == NK_ROW_MAJOR) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
-    if (!weights) {
-        void* sym = nullptr;
-        p->split_slot = take_split_slot();
-        if (p->split_slot >= 0) {
-            if (cudaGetSymbolAddress(&sym, g_split_counter) != cudaSuccess) { give_split_slot(p->split_slot); delete p; return NK_ERR_CUDA; }
-            p->counters = static_cast<unsigned int*>(sym) + p->split_slot * SPLIT_COUNTERS;
-        }
-    }
+    if (!weights) p->split_slot = take_split_slot(&p->counters);
     snprintf(p->name, sizeof(p->name), "grouped_%s_256x256x64_s%d_pair", weights ? "weights" : d.layout_b == NK_TRANSPOSED ? "rows_t" : "rows", GRP_STAGES);
     *out = p;
     return NK_OK;
@@ -118,7 +111,7 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
 // partial sums: one slab of 256 x 256 FP32 per (tile, split); there are at most as many as pairs
 size_t nk_grouped_workspace_bytes(nk_grouped_t p) {
     if (!p || p->split_slot < 0) return 0;
-    return static_cast<size_t>(p->pairs) * GRP_TILE * GRP_TILE * sizeof(float);
+    return grouped_partial_bytes(p->pairs);
 }
 
 nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C, const int32_t* offsets, void* workspace,
@@ -179,8 +172,8 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     int64_t most = weights ? d.groups * g.tiles_i * g.tiles_j : (d.rows / 256 + (d.rows < d.groups ? d.rows : d.groups)) * g.tiles_i;
     if (!weights) most *= GRP_MAX_SPLITS;
     const int pairs = static_cast<int>(most < p->pairs ? most : p->pairs);
-    grouped_kernel_for(d)<<<2 * pairs, GRP_THREADS, GRP_SMEM, static_cast<cudaStream_t>(cuda_stream)>>>(p->map_a, p->map_b, p->map_b16, g);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = grouped_launch(weights, weights || d.layout_b == NK_ROW_MAJOR, pairs, static_cast<cudaStream_t>(cuda_stream),
+                                         p->map_a, p->map_b, p->map_b16, g);
     return e == cudaSuccess ? NK_OK : p->cuda("grouped launch", e);
 }
 

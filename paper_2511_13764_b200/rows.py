@@ -13,7 +13,9 @@ EXPORTS = ["nk_grouped_create", "nk_grouped_workspace_bytes", "nk_grouped_run", 
            "nk_grouped_kernel_name", "nk_grouped_last_cuda_error", "nk_grouped_destroy",
            "nk_route_create", "nk_route_workspace_bytes", "nk_route_run", "nk_route_backward", "nk_route_dispatch",
            "nk_route_combine", "nk_route_combine_backward", "nk_route_check", "nk_route_kernel_name",
-           "nk_route_last_cuda_error", "nk_route_destroy"]
+           "nk_route_last_cuda_error", "nk_route_destroy",
+           "nk_lora_create", "nk_lora_workspace_bytes", "nk_lora_run", "nk_lora_check", "nk_lora_kernel_name",
+           "nk_lora_last_cuda_error", "nk_lora_destroy"]
 
 
 class GroupedDesc(ctypes.Structure):
@@ -27,6 +29,12 @@ class RouteDesc(ctypes.Structure):
                 + [(n, ctypes.c_int32) for n in ("logits_dtype", "dtype", "renormalise", "device")])
 
 
+class LoraDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "N", "K", "rank", "adapters", "requests")]
+                + [(n, ctypes.c_int32) for n in ("in_dtype", "out_dtype", "layout", "device")]
+                + [(n, ctypes.c_int64) for n in ("ldx", "ldw", "ldy")])
+
+
 _lib = None
 
 
@@ -35,7 +43,7 @@ def lib():
     if _lib is None:
         L = binding.lib()
         vp, sz = ctypes.c_void_p, ctypes.c_size_t
-        for family, desc in (("grouped", GroupedDesc), ("route", RouteDesc)):
+        for family, desc in (("grouped", GroupedDesc), ("route", RouteDesc), ("lora", LoraDesc)):
             create = getattr(L, f"nk_{family}_create")
             create.restype, create.argtypes = ctypes.c_int, [ctypes.POINTER(desc), ctypes.POINTER(vp)]
             for name, result in (("workspace_bytes", sz), ("check", ctypes.c_int), ("destroy", ctypes.c_int),
@@ -44,6 +52,8 @@ def lib():
                 f.restype, f.argtypes = result, [vp]
         L.nk_grouped_run.restype = ctypes.c_int
         L.nk_grouped_run.argtypes = [vp] * 6 + [sz, vp]
+        L.nk_lora_run.restype = ctypes.c_int
+        L.nk_lora_run.argtypes = [vp] * 10 + [sz, vp]
         L.nk_route_run.restype = ctypes.c_int
         L.nk_route_run.argtypes = [vp] * 7 + [sz, vp]
         for name, pointers in (("backward", 4), ("dispatch", 3), ("combine", 4), ("combine_backward", 6)):
@@ -157,5 +167,21 @@ class RoutePlan(_Handle):
     def combine_backward(self, dY, Ys, slots, gates, dYs, dgates, stream=None):
         status = lib().nk_route_combine_backward(self._h, _ptr(dY), _ptr(Ys), _ptr(slots), _ptr(gates), _ptr(dYs),
                                                  _ptr(dgates), stream)
+        if status:
+            self._check(status)
+
+
+class LoraPlan(_Handle):
+    """nk_lora: a shared projection with the low-rank adapters of many requests beside it."""
+    family = "lora"
+
+    def __init__(self, rows, N, K, rank, adapters, requests, in_dtype=BF16, out_dtype=F32, layout=ROW_MAJOR, device=0,
+                 ldx=0, ldw=0, ldy=0):
+        self._create(LoraDesc(rows, N, K, rank, adapters, requests, in_dtype, out_dtype, layout, device, ldx, ldw, ldy))
+
+    def run(self, X, W, A, B, scale, offsets, adapter, Y, workspace=None, workspace_bytes=None, stream=None):
+        """offsets (INT32 [requests + 1]), adapter (INT32 [requests]) and scale (FP32 [adapters]) are on the device."""
+        status = lib().nk_lora_run(self._h, _ptr(X), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(offsets), _ptr(adapter),
+                                   _ptr(Y), _ptr(workspace), _bytes(workspace, workspace_bytes), stream)
         if status:
             self._check(status)

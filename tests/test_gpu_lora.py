@@ -1,0 +1,219 @@
+"""The adapters of many requests beside a shared projection (nk_lora) against the formula in 64 bits.
+
+Tolerance: that of the dense GEMM (1e-5 of the largest sum of |products|, half a unit in the last place of a 16-bit
+result) on both products; X . A_a enters the second product as FP32 or as two 16-bit numbers, off by at most 2^-16 of
+itself, so 2^-16 * scale * sum |X . A_a| |B_a| is added."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_13764_b200 as nk
+from nk_testlib import TOL_BF16_REL, TOL_F16_ABS, TOL_F16_REL, TOL_REL_SMAX
+
+TYPES = {"bf16": (nk.BF16, torch.bfloat16), "f16": (nk.F16, torch.float16), "f32": (nk.F32, torch.float32)}
+SENTINEL = 7.0
+
+
+def rand(shape, kind, gen, scale=1.0):
+    return (torch.randn(shape, generator=gen, dtype=torch.float32) * scale).to(TYPES[kind][1])
+
+
+def strided(x, ld):
+    buf = torch.full((x.shape[0], ld), float("nan"), dtype=x.dtype)
+    buf[:, : x.shape[1]] = x
+    return buf.cuda()
+
+
+def make(sizes, N, K, r, L, kind, first=0, spare=0, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    rows = first + sum(sizes) + spare
+    off = torch.tensor(np.concatenate([[first], first + np.cumsum(sizes)]), dtype=torch.int32)
+    which = torch.randint(0, L, (len(sizes),), generator=gen, dtype=torch.int32)
+    return (rand((rows, K), kind, gen), rand((K, N), kind, gen, K ** -0.5), rand((L, K, r), kind, gen, K ** -0.5),
+            rand((L, r, N), kind, gen, r ** -0.5), 0.5 + torch.rand(L, generator=gen), off, which)
+
+
+def run(data, layout="row", out="f32", ldx=0, ldw=0, ldy=0, check=True):
+    X, W, A, B, scale, off, which = data
+    rows, K = X.shape
+    N, r, L = W.shape[1], A.shape[2], A.shape[0]
+    kind = "bf16" if X.dtype == torch.bfloat16 else "f16"
+    t = layout == "transposed"
+    Ws, As, Bs = (m.transpose(-1, -2).contiguous() if t else m for m in (W, A, B))
+    plan = nk.LoraPlan(rows, N, K, r, L, len(which), in_dtype=TYPES[kind][0], out_dtype=TYPES[out][0],
+                       layout=nk.TRANSPOSED if t else nk.ROW_MAJOR, ldx=ldx, ldw=ldw, ldy=ldy)
+    Y = torch.full((rows, ldy or N), SENTINEL, dtype=TYPES[out][1], device="cuda")
+    ws = torch.full((plan.workspace_bytes,), 255, dtype=torch.uint8, device="cuda")
+    args = (strided(X, ldx or K), strided(Ws, ldw or Ws.shape[1]), As.cuda(), Bs.cuda(), scale.cuda(), off.cuda(), which.cuda())
+    plan.run(*args, Y, workspace=ws, stream=torch.cuda.current_stream().cuda_stream)
+    if check:
+        plan.check()
+    assert (Y[:, N:] == SENTINEL).all()
+    return Y[:, :N].cpu(), plan
+
+
+def want_of(data):
+    """Formula, and the tolerance's size terms."""
+    X, W, A, B, scale, off, which = data
+    x, w = X.double().cuda(), W.double().cuda()
+    y, size, h16 = x @ w, x.abs() @ w.abs(), torch.zeros(X.shape[0], W.shape[1], dtype=torch.float64, device="cuda")
+    for q, a in enumerate(which.tolist()):
+        lo, hi = int(off[q]), int(off[q + 1])
+        if 0 <= a < A.shape[0] and hi > lo:
+            f, g, s = A[a].double().cuda(), B[a].double().cuda(), float(scale[a])
+            h = x[lo:hi] @ f
+            y[lo:hi] += s * h @ g
+            size[lo:hi] += s * (x[lo:hi].abs() @ f.abs()) @ g.abs()
+            h16[lo:hi] = 2.0 ** -16 * s * h.abs() @ g.abs()
+    return y.cpu(), float(size.max()), h16.cpu()
+
+
+def close(got, data, out):
+    y, size, h16 = want_of(data)
+    tol = TOL_REL_SMAX * size + h16 + {"bf16": TOL_BF16_REL, "f16": TOL_F16_REL, "f32": 0.0}[out] * y.abs() + (TOL_F16_ABS if out == "f16" else 0)
+    bad = ~((got.double() - y).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, first at {bad.nonzero()[0].tolist()}: got {got[bad][0]} want {y[bad][0]}"
+
+
+SHAPES = {
+    "one_row": [1],
+    "step": [1] * 16,
+    "step_many": [1] * 300,
+    "one_prompt": [700],
+    "mixed": [1, 1, 200, 0, 1, 1, 1, 90, 1, 17, 1],
+    "edges": [255, 1, 256, 257, 0, 8, 9, 7],
+    "short": [5, 8, 3, 0, 0, 12, 2, 9],
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(SHAPES))
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("rank", [8, 16, 40, 128])
+def test_requests(name, layout, rank):
+    data = make(SHAPES[name], 264, 328, rank, 5, "bf16", seed=1)
+    got, _ = run(data, layout)
+    close(got, data, "f32")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,out", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")])
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("name", ["step", "mixed"])
+def test_types_strides_and_rows_outside(kind, out, layout, name):
+    data = make(SHAPES[name], 520, 136, 24, 3, kind, first=7, spare=5, seed=2)
+    got, _ = run(data, layout, out, ldx=152, ldw=544 if layout == "row" else 144, ldy=536)
+    close(got, data, out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,K", [(8, 8), (8, 4096), (1000, 8), (4096, 1024), (1032, 2056)])
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("sizes", [[1, 1, 1, 1], [60, 1, 130]])
+def test_sizes(N, K, layout, sizes):
+    data = make(sizes, N, K, 16, 2, "bf16", seed=3)
+    got, _ = run(data, layout)
+    close(got, data, "f32")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["step", "mixed", "one_prompt"])
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+def test_requests_without_an_adapter(name, layout):
+    data = make(SHAPES[name], 264, 328, 16, 4, "bf16", seed=4)
+    which = data[6]
+    which[::2] = -1
+    which[-1] = 4                                    # one past the last adapter
+    got, _ = run(data, layout)
+    close(got, data, "f32")
+    which[:] = -1
+    got, _ = run(data, layout)
+    close(got, data, "f32")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["step", "mixed"])
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+def test_nan_stays_with_its_request(name, layout):
+    """An adapter of infinities or NaN reaches the rows of its own requests only, and no row without one."""
+    data = make(SHAPES[name], 264, 328, 16, 6, "bf16", seed=5)
+    X, W, A, B, scale, off, which = data
+    A[1] = float("nan")
+    B[2] = float("inf")
+    which[0] = -1
+    which[1] = 1
+    X[int(off[4]):int(off[5])] = float("nan")
+    got, _ = run(data, layout)
+    bad = torch.zeros(X.shape[0], dtype=torch.bool)
+    for q, a in enumerate(which.tolist()):
+        if a in (1, 2) or q == 4:
+            bad[int(off[q]):int(off[q + 1])] = True
+    assert got[~bad].isfinite().all()
+    assert not got[bad].isfinite().any()
+
+
+@pytest.mark.gpu
+def test_same_bits_every_time():
+    data = make(SHAPES["mixed"], 264, 4096, 16, 4, "bf16", seed=6)
+    first, _ = run(data)
+    for _ in range(10):
+        again, _ = run(data)
+        assert torch.equal(first, again)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("off", [[0, 50, 20, 90], [-5, 30, 60, 90], [0, 30, 60, 95], [90, 60, 30, 0]])
+def test_offsets_that_break_the_rule_are_reported(off):
+    data = list(make([30, 30, 30], 72, 64, 16, 2, "bf16", seed=7))
+    data[5] = torch.tensor(off, dtype=torch.int32)
+    _, plan = run(data, check=False)
+    with pytest.raises(nk.NkError) as e:
+        plan.check()
+    assert e.value.status == 1 and "offsets" in str(e.value)
+    plan.check()
+
+
+@pytest.mark.gpu
+def test_no_rows():
+    plan = nk.LoraPlan(0, 64, 32, 8, 2, 3)
+    plan.run(*[None] * 8)
+    plan.check()
+
+
+@pytest.mark.gpu
+def test_run_refusals():
+    plan = nk.LoraPlan(50, 64, 32, 8, 2, 3)
+    x = torch.zeros(1 << 16, dtype=torch.bfloat16, device="cuda")
+    f, i = torch.zeros(1 << 14, device="cuda"), torch.zeros(64, dtype=torch.int32, device="cuda")
+    ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    good = [x, x, x, x, f, i, i, f]
+    for pos in range(8):
+        args = list(good)
+        args[pos] = None
+        with pytest.raises(nk.NkError) as e:
+            plan.run(*args, workspace=ws)
+        assert e.value.status == 1
+    for pos in (0, 1, 2, 3, 7):
+        args = list(good)
+        args[pos] = args[pos][1:]
+        with pytest.raises(nk.NkError) as e:
+            plan.run(*args, workspace=ws)
+        assert e.value.status == 3
+    for kw in (dict(), dict(workspace=ws, workspace_bytes=ws.numel() - 1)):
+        with pytest.raises(nk.NkError) as e:
+            plan.run(*good, **kw)
+        assert e.value.status == 4
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rows=-1), 1), (dict(N=0), 1), (dict(K=0), 1), (dict(rank=0), 1), (dict(adapters=0), 1), (dict(requests=0), 1),
+    (dict(in_dtype=nk.F32), 2), (dict(in_dtype=33), 1), (dict(out_dtype=nk.F16), 1), (dict(layout=nk.BLOCKED32), 2), (dict(layout=9), 1),
+    (dict(rank=136), 2), (dict(rank=12), 3), (dict(requests=1025), 2), (dict(adapters=65536), 2), (dict(N=68), 3), (dict(K=36), 3),
+    (dict(ldx=24), 1), (dict(ldx=36), 3), (dict(ldw=8), 1), (dict(ldy=8), 1), (dict(rows=(1 << 24) + 1), 2),
+])
+def test_descriptor_refusals_need_no_device(kw, status):
+    args = dict(rows=50, N=64, K=32, rank=8, adapters=2, requests=3)
+    args.update(kw)
+    with pytest.raises(nk.NkError) as e:
+        nk.LoraPlan(**args)
+    assert e.value.status == status
