@@ -14,24 +14,40 @@ constexpr int GRP_A_BYTES = 128 * 64 * 2;
 constexpr int GRP_STAGE = 2 * GRP_A_BYTES;             // 16 KB of features, up to 16 KB of rows, per CTA
 constexpr int GRP_BK = 64;
 constexpr int GRP_TILE = 256;                          // features of a tile, and the most rows of one
-constexpr int GRP_MAX_SPLITS = 16;
-constexpr int GRP_SMEM = GRP_STAGES * GRP_STAGE + 1024 + 2 * 4 * (GRP_MAX_GROUPS + 1) + 512;
+constexpr int GRP_TABLE = 4 * (GRP_MAX_GROUPS + 1);    // bytes of a table by group
+constexpr int GRP_SMEM = GRP_STAGES * GRP_STAGE + 1024 + 3 * GRP_TABLE + 512;
+
+constexpr int GRP_CHUNK = 4;                           // k-blocks between additions to the FP32 sums of FP32 results
+
+enum GroupedMode { GRP_ROWS = 0, GRP_WEIGHTS = 1, GRP_LORA = 2 };
 
 struct GroupedParams {
     int groups, rows;      // rows: extent of the row arrays; offsets are clamped to it
     int I, J;              // features (contiguous in C); WEIGHTS: rows of each C_g
-    int kb_total;          // ROWS: k-blocks of the contraction
+    int kb_total;          // ROWS, LORA: k-blocks of the contraction
     int tiles_i;           // ceil(I / 256)
     int tiles_j;           // WEIGHTS: ceil(J / 256)
     int beta, out16, f16;
+    int chunk;             // k-blocks summed in tensor memory before they are added to an FP32 sum in registers; 0: all
     uint32_t idesc;        // without the N field
     const int* offsets;    // [groups + 1]; null: one group of all rows
+    const int* index;      // ROWS: weight of each group (outside [0, index_max): the group is skipped); null: its number
+    int index_max;
     void* C;
-    const float* add;      // ROWS: FP32 [rows][I], added before the rounding; null: none
+    const float* add;      // FP32 [rows][I], added before the rounding; null: none
     long long ldc, stride_c;
-    float* partial;        // K splits: [unit][split][CTA of the pair][column][128 features]
-    unsigned int* counter; // one per (unit, CTA of the pair); zero before and after every launch
+    float* partial;        // slabs of tiles cut along k, two per CTA pair; null: no tile is cut
+    int slab_cols;         // columns of a slab
+    unsigned int* counter; // arrivals, a byte per (cut tile, CTA of the pair, 32-column piece, warp); zero before and after
     unsigned int* status;
+    // adapters.  ROWS with h16: instead of C the product times scale[weight] is stored as two 16-bit numbers whose sum is
+    // good to twice their precision, [row][rank block of 32][32 leading parts, 32 remainders].  LORA: each request's
+    // rows of h16 times its B_a are further k-blocks of a tile.
+    uint16_t* h16;
+    const float* scale;
+    int rank_blocks, rank;
+    int requests;
+    const int* request_offsets;
 };
 
 // tcgen05 instruction descriptor without N: kind::f16, FP32 accumulator, M = 256 over the pair
@@ -42,15 +58,25 @@ inline uint32_t grouped_idesc(bool a_mn, bool b_mn, bool f16) {
     return d | (256u >> 4) << 24;
 }
 
+struct GroupedMaps {
+    CUtensorMap a;         // the features' operand
+    CUtensorMap b, b16;    // the rows' operand in boxes of 128 (WEIGHTS: 64) and of 16 rows
+    CUtensorMap c, h, h16; // LORA: the adapters' B, and h16 in boxes of 128 and of 16 rows
+};
+
 // (nk_grouped.cu)
-cudaError_t grouped_prepare(bool weights, bool a_mn);     // once per kernel and device: its shared memory
-cudaError_t grouped_launch(bool weights, bool a_mn, int pairs, cudaStream_t st, const CUtensorMap& a, const CUtensorMap& b,
-                           const CUtensorMap& b16, const GroupedParams& p);
-// Arrival counters of the K splits, zero between launches (the last arriver of a tile clears its own).  A plan holds a
-// slot of a static table from create to destroy; where none is free (null) it runs without K splits.
-constexpr int SPLIT_COUNTERS = 128;
+cudaError_t grouped_prepare(GroupedMode mode, bool a_mn);     // once per kernel and device: its shared memory
+// `after_start`: the launch may begin while the kernel before it in the stream still runs (which has to allow it)
+cudaError_t grouped_launch(GroupedMode mode, bool a_mn, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p,
+                           bool after_start);
+// Arrival counters of the tiles cut along k, zero between launches (the last arriver clears its own).  A plan holds a
+// slot of a static table from create to destroy; where none is free (null) it cuts no tile.
+constexpr int SPLIT_COUNTERS = 4096;
 int take_split_slot(unsigned int** counters);
 void give_split_slot(int slot);
-inline size_t grouped_partial_bytes(int pairs) { return static_cast<size_t>(pairs) * GRP_TILE * GRP_TILE * sizeof(float); }
+inline size_t grouped_partial_bytes(int pairs, int slab_cols) {
+    return static_cast<size_t>(pairs) * 2 * GRP_TILE * slab_cols * sizeof(float);
+}
+inline int grouped_slab_cols(int64_t most_rows) { return most_rows >= GRP_TILE ? GRP_TILE : static_cast<int>((most_rows + 31) / 32 * 32); }
 
 }  // namespace nk

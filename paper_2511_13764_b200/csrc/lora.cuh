@@ -241,6 +241,7 @@ __global__ void __launch_bounds__(LORA_THREADS) __cluster_dims__(LORA_CLUSTER, 1
     float* h = share + LORA_MAX_RANK * LORA_ROWS;
     int* s_row = reinterpret_cast<int*>(h + LORA_MAX_RANK * LORA_ROWS);
     int* s_pre = s_row + LORA_MAX_REQUESTS + 1;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     lora_prefix(p, s_row, s_pre);
     const uint32_t crank = cluster_ctarank();
     const int clusters = gridDim.x / LORA_CLUSTER, chunks = s_pre[p.requests];

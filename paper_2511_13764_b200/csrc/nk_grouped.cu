@@ -31,18 +31,28 @@ void give_split_slot(int slot) {
     g_split_taken[slot] = false;
 }
 
-typedef void (*GroupedKernel)(CUtensorMap, CUtensorMap, CUtensorMap, GroupedParams);
-static GroupedKernel grouped_kernel_for(bool weights, bool a_mn) {
-    if (weights) return grouped_kernel<true, true>;
-    return a_mn ? grouped_kernel<false, true> : grouped_kernel<false, false>;
+typedef void (*GroupedKernel)(GroupedMaps, GroupedParams);
+static GroupedKernel grouped_kernel_for(GroupedMode mode, bool a_mn) {
+    if (mode == GRP_WEIGHTS) return grouped_kernel<GRP_WEIGHTS, true>;
+    if (mode == GRP_LORA) return a_mn ? grouped_kernel<GRP_LORA, true> : grouped_kernel<GRP_LORA, false>;
+    return a_mn ? grouped_kernel<GRP_ROWS, true> : grouped_kernel<GRP_ROWS, false>;
 }
-cudaError_t grouped_prepare(bool weights, bool a_mn) {
-    return cudaFuncSetAttribute(grouped_kernel_for(weights, a_mn), cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM);
+cudaError_t grouped_prepare(GroupedMode mode, bool a_mn) {
+    return cudaFuncSetAttribute(grouped_kernel_for(mode, a_mn), cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM);
 }
-cudaError_t grouped_launch(bool weights, bool a_mn, int pairs, cudaStream_t st, const CUtensorMap& a, const CUtensorMap& b,
-                           const CUtensorMap& b16, const GroupedParams& p) {
-    grouped_kernel_for(weights, a_mn)<<<2 * pairs, GRP_THREADS, GRP_SMEM, st>>>(a, b, b16, p);
-    return cudaGetLastError();
+cudaError_t grouped_launch(GroupedMode mode, bool a_mn, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p,
+                           bool after_start) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * pairs);
+    cfg.blockDim = dim3(GRP_THREADS);
+    cfg.dynamicSmemBytes = GRP_SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = after_start ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, grouped_kernel_for(mode, a_mn), maps, p);
 }
 
 }  // namespace nk
@@ -52,7 +62,8 @@ struct nk_grouped_s : nk::PlanBase {
     int pairs;                    // CTA pairs that fit the device
     int split_slot;
     unsigned int* counters;
-    CUtensorMap map_a, map_b, map_b16;
+    nk::GroupedMaps maps;
+    int slab_cols;                // columns of a slab of partial sums
     const void *cached_a, *cached_b, *cached_c;
     char name[64];
 };
@@ -89,6 +100,7 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
     if (d.lda >= (1ll << 38) || d.ldb >= (1ll << 38) || d.stride_g >= (1ll << 38)) return NK_ERR_UNSUPPORTED;
     const int64_t tiles = weights ? d.groups * div_up(d.N, 256) * div_up(d.K, 256) : (d.rows / 256 + d.groups) * div_up(d.N, 256);
     if (tiles >= (1 << 24)) return NK_ERR_UNSUPPORTED;
+    if (weights && (d.rows / 64 + d.groups) * div_up(d.N, 256) * div_up(d.K, 256) >= (1ll << 31)) return NK_ERR_UNSUPPORTED;   // k-blocks of all tiles
 
     int sms = 0;
     nk_status_t s = usable_device(d.device, &sms);
@@ -100,18 +112,19 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     DeviceGuard guard(d.device);
     if (!encode_tiled()) { delete p; return NK_ERR_CUDA; }
-    if (grouped_prepare(weights, weights || d.layout_b == NK_ROW_MAJOR) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
+    if (grouped_prepare(weights ? GRP_WEIGHTS : GRP_ROWS, weights || d.layout_b == NK_ROW_MAJOR) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
-    if (!weights) p->split_slot = take_split_slot(&p->counters);
+    p->slab_cols = grouped_slab_cols(weights ? d.K : d.rows);
+    p->split_slot = take_split_slot(&p->counters);
     snprintf(p->name, sizeof(p->name), "grouped_%s_256x256x64_s%d_pair", weights ? "weights" : d.layout_b == NK_TRANSPOSED ? "rows_t" : "rows", GRP_STAGES);
     *out = p;
     return NK_OK;
 }
 
-// partial sums: one slab of 256 x 256 FP32 per (tile, split); there are at most as many as pairs
+// partial sums of cut tiles: two FP32 slabs for each pair
 size_t nk_grouped_workspace_bytes(nk_grouped_t p) {
     if (!p || p->split_slot < 0) return 0;
-    return grouped_partial_bytes(p->pairs);
+    return grouped_partial_bytes(p->pairs, p->slab_cols);
 }
 
 nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C, const int32_t* offsets, void* workspace,
@@ -133,12 +146,12 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
         const bool f16 = d.in_dtype == NK_F16;
         bool ok;
         if (weights) {
-            ok = encode_map(&p->map_a, B, f16, d.N, rows, 1, d.ldb, 0, 64) && encode_map(&p->map_b, A, f16, d.K, rows, 1, d.lda, 0, 64);
-            p->map_b16 = p->map_b;
+            ok = encode_map(&p->maps.a, B, f16, d.N, rows, 1, d.ldb, 0, 64) && encode_map(&p->maps.b, A, f16, d.K, rows, 1, d.lda, 0, 64);
+            p->maps.b16 = p->maps.b;
         } else {
-            ok = (d.layout_b == NK_ROW_MAJOR ? encode_map(&p->map_a, B, f16, d.N, d.K, d.groups, d.ldb, d.stride_g, 64)
-                                             : encode_map(&p->map_a, B, f16, d.K, d.N, d.groups, d.ldb, d.stride_g, 128)) &&
-                 encode_map(&p->map_b, A, f16, d.K, rows, 1, d.lda, 0, 128) && encode_map(&p->map_b16, A, f16, d.K, rows, 1, d.lda, 0, 16);
+            ok = (d.layout_b == NK_ROW_MAJOR ? encode_map(&p->maps.a, B, f16, d.N, d.K, d.groups, d.ldb, d.stride_g, 64)
+                                             : encode_map(&p->maps.a, B, f16, d.K, d.N, d.groups, d.ldb, d.stride_g, 128)) &&
+                 encode_map(&p->maps.b, A, f16, d.K, rows, 1, d.lda, 0, 128) && encode_map(&p->maps.b16, A, f16, d.K, rows, 1, d.lda, 0, 16);
         }
         if (!ok) {
             p->cached_c = nullptr;
@@ -168,12 +181,10 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     g.partial = need ? static_cast<float*>(workspace) : nullptr;
     g.counter = p->counters;
     g.status = p->status_dev;
-    // no more pairs than units can exist (a few rows of many groups: one tile column per row) times K splits
-    int64_t most = weights ? d.groups * g.tiles_i * g.tiles_j : (d.rows / 256 + (d.rows < d.groups ? d.rows : d.groups)) * g.tiles_i;
-    if (!weights) most *= GRP_MAX_SPLITS;
-    const int pairs = static_cast<int>(most < p->pairs ? most : p->pairs);
-    const cudaError_t e = grouped_launch(weights, weights || d.layout_b == NK_ROW_MAJOR, pairs, static_cast<cudaStream_t>(cuda_stream),
-                                         p->map_a, p->map_b, p->map_b16, g);
+    g.slab_cols = p->slab_cols;
+    g.chunk = g.out16 ? 0 : GRP_CHUNK;
+    const cudaError_t e = grouped_launch(weights ? GRP_WEIGHTS : GRP_ROWS, weights || d.layout_b == NK_ROW_MAJOR, p->pairs,
+                                         static_cast<cudaStream_t>(cuda_stream), p->maps, g, false);
     return e == cudaSuccess ? NK_OK : p->cuda("grouped launch", e);
 }
 

@@ -5,10 +5,13 @@
 
 struct nk_lora_s : nk::PlanBase {
     nk_lora_desc_t d;             // strides filled in
-    int pairs, split_slot;
-    unsigned int* counters;
-    CUtensorMap map_w, map_x, map_x16;
-    const void *cached_x, *cached_w;
+    bool few;                     // few rows to a request: FP32 contributions from lora_delta_kernel
+    int pairs, rank_blocks;
+    int split_slot[2];            // of X . A and of the projection: the two overlap
+    unsigned int* counters[2];
+    size_t part_bytes[2], side_bytes;   // partial sums of the two; FP32 contributions or X . A
+    nk::GroupedMaps maps, shrink; // of the projection and of X . A
+    const void *cached_x, *cached_w, *cached_a, *cached_b, *cached_ws;
     char name[64];
 };
 
@@ -17,7 +20,11 @@ using namespace nk;
 namespace nk {
 
 static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-static size_t lora_delta_bytes(const nk_lora_desc_t& d) { return align256(static_cast<size_t>(d.rows) * d.N * sizeof(float)); }
+
+// Which way the adapters' part goes.  Up to about LORA_FEW_ROWS rows to a request its weights are all that counts, and
+// the clusters of lora_delta_kernel read them at the speed of memory; beyond that the rows' arithmetic wants
+// the tensor cores: X . A_a as a grouped product, (X . A_a) . B_a as further k-blocks of the projection.
+constexpr int64_t LORA_FEW_ROWS = 8;
 
 }  // namespace nk
 
@@ -49,24 +56,30 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     nk_lora_s* p = new (std::nothrow) nk_lora_s();
     if (!p) return NK_ERR_INVALID_ARG;
     p->d = d;
-    p->split_slot = -1;
+    p->split_slot[0] = p->split_slot[1] = -1;
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     DeviceGuard guard(d.device);
-    if (!encode_tiled() || grouped_prepare(false, d.layout == NK_ROW_MAJOR) != cudaSuccess ||
-        cudaFuncSetAttribute(lora_delta_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LORA_SMEM) != cudaSuccess) {
-        delete p;
-        return NK_ERR_CUDA;
-    }
+    const bool row = d.layout == NK_ROW_MAJOR;
+    p->few = d.rows <= LORA_FEW_ROWS * d.requests;
+    cudaError_t e = grouped_prepare(GRP_ROWS, row);
+    if (e == cudaSuccess) e = p->few ? cudaFuncSetAttribute(lora_delta_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LORA_SMEM)
+                                     : grouped_prepare(GRP_LORA, row);
+    if (e != cudaSuccess || !encode_tiled()) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
-    p->split_slot = take_split_slot(&p->counters);
-    snprintf(p->name, sizeof(p->name), "lora_delta_%s", d.layout == NK_TRANSPOSED ? "rows_t" : "rows");
+    p->rank_blocks = static_cast<int>(div_up(d.rank, 32));
+    p->side_bytes = align256(p->few ? static_cast<size_t>(d.rows) * d.N * sizeof(float) : static_cast<size_t>(d.rows) * p->rank_blocks * 128);
+    for (int i = p->few ? 1 : 0; i < 2; ++i) {
+        p->split_slot[i] = take_split_slot(&p->counters[i]);
+        p->part_bytes[i] = p->split_slot[i] < 0 ? 0 : grouped_partial_bytes(p->pairs, grouped_slab_cols(d.rows));
+    }
+    snprintf(p->name, sizeof(p->name), "lora_%s_%s", p->few ? "few" : "many", row ? "rows" : "rows_t");
     *out = p;
     return NK_OK;
 }
 
 size_t nk_lora_workspace_bytes(nk_lora_t p) {
     if (!p) return 0;
-    return lora_delta_bytes(p->d) + (p->split_slot < 0 ? 0 : grouped_partial_bytes(p->pairs));
+    return p->side_bytes + p->part_bytes[0] + p->part_bytes[1];
 }
 
 nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A, const void* B, const float* scale,
@@ -82,73 +95,111 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     if (!workspace || workspace_bytes < nk_lora_workspace_bytes(p)) return NK_ERR_WORKSPACE;
     DeviceGuard guard(d.device);
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
-    const bool f16 = d.in_dtype == NK_F16;
-    if (p->cached_x != X || p->cached_w != W) {
+    const bool f16 = d.in_dtype == NK_F16, row = d.layout == NK_ROW_MAJOR;
+    if (p->cached_x != X || p->cached_w != W || p->cached_a != A || p->cached_b != B || p->cached_ws != workspace) {
         p->cached_x = nullptr;
-        const bool ok = (d.layout == NK_ROW_MAJOR ? encode_map(&p->map_w, W, f16, d.N, d.K, 1, d.ldw, 0, 64)
-                                                  : encode_map(&p->map_w, W, f16, d.K, d.N, 1, d.ldw, 0, 128)) &&
-                        encode_map(&p->map_x, X, f16, d.K, d.rows, 1, d.ldx, 0, 128) &&
-                        encode_map(&p->map_x16, X, f16, d.K, d.rows, 1, d.ldx, 0, 16);
+        GroupedMaps &m = p->maps, &s = p->shrink;
+        bool ok = (row ? encode_map(&m.a, W, f16, d.N, d.K, 1, d.ldw, 0, 64) : encode_map(&m.a, W, f16, d.K, d.N, 1, d.ldw, 0, 128)) &&
+                  encode_map(&m.b, X, f16, d.K, d.rows, 1, d.ldx, 0, 128) && encode_map(&m.b16, X, f16, d.K, d.rows, 1, d.ldx, 0, 16);
+        if (!p->few) {
+            const int64_t r = d.rank, h = p->rank_blocks * 64;
+            ok = ok && (row ? encode_map(&s.a, A, f16, r, d.K, d.adapters, r, r * d.K, 64) : encode_map(&s.a, A, f16, d.K, r, d.adapters, d.K, r * d.K, 128)) &&
+                 (row ? encode_map(&m.c, B, f16, d.N, r, d.adapters, d.N, r * d.N, 32) : encode_map(&m.c, B, f16, r, d.N, d.adapters, r, r * d.N, 128)) &&
+                 encode_map(&m.h, workspace, f16, h, d.rows, 1, h, 0, 128) && encode_map(&m.h16, workspace, f16, h, d.rows, 1, h, 0, 16);
+            s.b = m.b;
+            s.b16 = m.b16;
+        }
         if (!ok) {
             snprintf(p->cuda_err, sizeof(p->cuda_err), "cuTensorMapEncodeTiled failed");
             return NK_ERR_CUDA;
         }
         p->cached_x = X;
         p->cached_w = W;
+        p->cached_a = A;
+        p->cached_b = B;
+        p->cached_ws = workspace;
     }
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    float* delta = static_cast<float*>(workspace);
-    LoraParams l = {};
-    l.rows = static_cast<int>(d.rows);
-    l.N = static_cast<int>(d.N);
-    l.K = static_cast<int>(d.K);
-    l.rank = static_cast<int>(d.rank);
-    l.adapters = static_cast<int>(d.adapters);
-    l.requests = static_cast<int>(d.requests);
-    l.transposed = d.layout == NK_TRANSPOSED;
-    l.f16 = f16;
-    l.ldx = d.ldx;
-    l.X = X;
-    l.A = A;
-    l.B = B;
-    l.scale = scale;
-    l.offsets = offsets;
-    l.adapter = adapter;
-    l.D = delta;
-    l.status = p->status_dev;
-    // clusters: no more than there can be chunks of rows, and a few for every SM
-    const int64_t chunks = d.rows / LORA_ROWS + (d.rows < d.requests ? d.rows : d.requests);
-    const int64_t most = 4 * p->sm_count / LORA_CLUSTER;
-    lora_delta_kernel<<<static_cast<unsigned>((chunks < most ? chunks : most) * LORA_CLUSTER), LORA_THREADS, LORA_SMEM, st>>>(l);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return p->cuda("lora delta launch", e);
-
+    char* ws = static_cast<char*>(workspace);
+    float* partial[2];
+    for (int i = 0; i < 2; ++i) partial[i] = p->part_bytes[i] ? reinterpret_cast<float*>(ws + p->side_bytes + (i ? p->part_bytes[0] : 0)) : nullptr;
     GroupedParams g = {};
-    g.groups = 1;
-    g.rows = l.rows;
-    g.I = l.N;
-    g.J = l.K;
+    g.rows = static_cast<int>(d.rows);
     g.kb_total = static_cast<int>(div_up(d.K, GRP_BK));
+    g.f16 = f16;
+    g.idesc = grouped_idesc(row, false, f16);
+    g.slab_cols = grouped_slab_cols(d.rows);
+    g.status = p->status_dev;
+    g.rank = static_cast<int>(d.rank);
+    g.rank_blocks = p->rank_blocks;
+    g.scale = scale;
+    cudaError_t e;
+    if (p->few) {
+        LoraParams l = {};
+        l.rows = g.rows;
+        l.N = static_cast<int>(d.N);
+        l.K = static_cast<int>(d.K);
+        l.rank = g.rank;
+        l.adapters = static_cast<int>(d.adapters);
+        l.requests = static_cast<int>(d.requests);
+        l.transposed = !row;
+        l.f16 = f16;
+        l.ldx = d.ldx;
+        l.X = X;
+        l.A = A;
+        l.B = B;
+        l.scale = scale;
+        l.offsets = offsets;
+        l.adapter = adapter;
+        l.D = reinterpret_cast<float*>(ws);
+        l.status = p->status_dev;
+        // clusters: no more than there can be chunks of rows, and a few for every SM
+        const int64_t chunks = d.rows / LORA_ROWS + (d.rows < d.requests ? d.rows : d.requests);
+        const int64_t most = 4 * p->sm_count / LORA_CLUSTER;
+        lora_delta_kernel<<<static_cast<unsigned>((chunks < most ? chunks : most) * LORA_CLUSTER), LORA_THREADS, LORA_SMEM, st>>>(l);
+        if ((e = cudaGetLastError()) != cudaSuccess) return p->cuda("lora delta launch", e);
+        g.add = l.D;
+    } else {
+        // X . A_a: the requests are the groups, their adapters the weights
+        GroupedParams h = g;
+        h.groups = static_cast<int>(d.requests);
+        h.offsets = offsets;
+        h.index = adapter;
+        h.index_max = static_cast<int>(d.adapters);
+        h.I = g.rank;
+        h.tiles_i = 1;
+        h.chunk = GRP_CHUNK;
+        h.h16 = reinterpret_cast<uint16_t*>(ws);
+        h.partial = partial[0];
+        h.counter = p->counters[0];
+        e = grouped_launch(GRP_ROWS, row, p->pairs, st, p->shrink, h, false);
+        if (e != cudaSuccess) return p->cuda("lora shrink launch", e);
+        g.requests = h.groups;
+        g.request_offsets = offsets;
+        g.index = adapter;
+        g.index_max = h.index_max;
+    }
+    g.groups = 1;
+    g.I = static_cast<int>(d.N);
     g.tiles_i = static_cast<int>(div_up(d.N, GRP_TILE));
     g.out16 = d.out_dtype != NK_F32;
-    g.f16 = f16;
-    g.idesc = grouped_idesc(d.layout == NK_ROW_MAJOR, false, f16);
+    g.chunk = g.out16 ? 0 : GRP_CHUNK;
     g.C = Y;
     g.ldc = d.ldy;
-    g.add = delta;
-    g.partial = p->split_slot < 0 ? nullptr : reinterpret_cast<float*>(static_cast<char*>(workspace) + lora_delta_bytes(d));
-    g.counter = p->counters;
-    g.status = p->status_dev;
-    e = grouped_launch(false, d.layout == NK_ROW_MAJOR, p->pairs, st, p->map_w, p->map_x, p->map_x16, g);
+    g.partial = partial[1];
+    g.counter = p->counters[1];
+    // the projection starts while the adapters' kernel runs, and waits for it where it needs its result
+    e = grouped_launch(p->few ? GRP_ROWS : GRP_LORA, row, p->pairs, st, p->maps, g, true);
     return e == cudaSuccess ? NK_OK : p->cuda("lora projection launch", e);
 }
 
 nk_status_t nk_lora_check(nk_lora_t p) {
     if (!p) return NK_ERR_INVALID_ARG;
     const nk_status_t s = base_check(p);
-    if (s == NK_ERR_TIMEOUT && p->counters) {
+    if (s == NK_ERR_TIMEOUT) {
         DeviceGuard guard(p->device);
-        cudaMemset(p->counters, 0, SPLIT_COUNTERS * sizeof(unsigned int));   // an abandoned tile may have left a count
+        for (unsigned int* c : p->counters)
+            if (c) cudaMemset(c, 0, SPLIT_COUNTERS * sizeof(unsigned int));   // an abandoned tile may have left a count
     }
     return s;
 }
@@ -157,7 +208,10 @@ const char* nk_lora_kernel_name(nk_lora_t p) { return p ? p->name : ""; }
 const char* nk_lora_last_cuda_error(nk_lora_t p) { return p ? p->cuda_err : ""; }
 
 nk_status_t nk_lora_destroy(nk_lora_t p) {
-    if (p) give_split_slot(p->split_slot);
+    if (p) {
+        give_split_slot(p->split_slot[0]);
+        give_split_slot(p->split_slot[1]);
+    }
     delete p;
     return NK_OK;
 }
