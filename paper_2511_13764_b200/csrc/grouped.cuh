@@ -51,45 +51,42 @@ struct GroupedRequests {
 
 __device__ __forceinline__ int round32(int x) { return (x + 31) & ~31; }
 
-// 16-bit results: two rows of 32 features each per store.  Even lanes take row j of features (lane, lane + 1), odd
-// lanes row j + 1 of (lane - 1, lane): a warp's store is two whole 64-byte pieces instead of one.
-__device__ __forceinline__ void grouped_store16(const GroupedParams& p, const float (&v)[32], size_t base, int i, int cols, const float* add) {
-    const int odd = threadIdx.x & 1;
-    uint16_t* C = static_cast<uint16_t*>(p.C);
+// One 32 x 32 piece of C, lane l holding feature l, v[j] row j.  Where all of its rows are stored it goes through
+// shared memory: a TMA store writes the box (and clips what lies beyond C's edges), which takes a third of the
+// instructions of stores from registers; with a short contraction the epilogue's issue slots bound the kernel.
+//
+// 16-bit results: a lane packs its feature of rows j and j + 1 and exchanges words with its neighbour; even lanes then
+// hold row j of features (l, l + 1), odd lanes row j + 1 of (l - 1, l): two rows of 64 bytes per store, no bank twice.
+template <bool F16>
+__device__ __forceinline__ void grouped_stage16(const float (&v)[32], uint32_t dst) {
+    const uint32_t odd = threadIdx.x & 1, l = threadIdx.x & 31;
+    const uint32_t pick = odd ? 0x3276u : 0x5410u;
+    dst += odd * 64 + (l >> 1) * 4;
 #pragma unroll
-    for (int j = 0; j < 32; j += 2) {
-        if (j >= cols) break;                            // warp-uniform
-        const float give = odd ? v[j] : v[j + 1], keep = odd ? v[j + 1] : v[j];
-        const float got = __shfl_xor_sync(~0u, give, 1);
-        float lo = odd ? got : keep, hi = odd ? keep : got;
-        const int row = j + odd;
-        if (row >= cols || i >= p.I) continue;           // (I is even: both features of a pair exist or neither)
-        const size_t o = base + static_cast<size_t>(row) * p.ldc + (i & ~1);
-        if (add) {
-            const float2 a = *reinterpret_cast<const float2*>(add + static_cast<size_t>(row) * p.I + (i & ~1));
-            lo += a.x;
-            hi += a.y;
-        }
-        uint32_t* c = reinterpret_cast<uint32_t*>(C + o);
-        if (p.beta) {
-            const uint32_t old = *c;
-            lo += half_bits_to_f32(old & 0xFFFFu, p.f16);
-            hi += half_bits_to_f32(old >> 16, p.f16);
-        }
-        *c = pack_half2(lo, hi, p.f16);
+    for (int j = 0; j < 16; ++j) {
+        const uint32_t w = pack_half2(v[2 * j], v[2 * j + 1], F16);
+        const uint32_t got = __shfl_xor_sync(~0u, w, 1);
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + j * 128), "r"(__byte_perm(w, got, pick)) : "memory");
     }
 }
-
-__device__ __forceinline__ void grouped_store32(const GroupedParams& p, const float (&v)[32], size_t base, int i, int cols, const float* add) {
-    if (i >= p.I) return;
-    float* C = static_cast<float*>(p.C) + base + i;
+__device__ __forceinline__ void grouped_stage32(const float (&v)[32], uint32_t dst) {
+    dst += (threadIdx.x & 31) * 4;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        if (j >= cols) break;
-        float x = v[j];
-        if (add) x += add[static_cast<size_t>(j) * p.I + i];
-        if (p.beta) x += C[static_cast<size_t>(j) * p.ldc];
-        C[static_cast<size_t>(j) * p.ldc] = x;
+    for (int j = 0; j < 32; ++j) asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + j * 128), "r"(__float_as_uint(v[j])) : "memory");
+}
+
+// The rows [0, rows) of a piece from registers; c points at row 0, this lane's feature.
+__device__ __forceinline__ void grouped_store_rows(const GroupedParams& p, const float (&v)[32], size_t at, int rows) {
+    if (p.out16) {
+        uint16_t* c = static_cast<uint16_t*>(p.C) + at;
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < rows) c[j * p.ldc] = static_cast<uint16_t>(pack_half2(v[j], 0.0f, p.f16) & 0xFFFFu);
+    } else {
+        float* c = static_cast<float*>(p.C) + at;
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < rows) c[j * p.ldc] = v[j];
     }
 }
 
@@ -119,10 +116,10 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
-    int* s_row = reinterpret_cast<int*>(gen_base + GRP_STAGES * GRP_STAGE);   // first row of each group (LORA: request), clamped and monotone
+    int* s_row = reinterpret_cast<int*>(gen_base + GRP_STAGES * GRP_STAGE + GRP_STAGING);   // first row of each group (LORA: request), clamped and monotone
     int* s_pre = s_row + GRP_MAX_GROUPS + 1;                                  // tiles before each group
     int* s_alt = s_pre + GRP_MAX_GROUPS + 1;                                  // ROWS: weight of the group; LORA: adapter of the request; -1: none.  WEIGHTS: k-blocks before each group
-    const uint32_t bar_base = smem_base + GRP_STAGES * GRP_STAGE + 3 * GRP_TABLE + 4;   // (8-byte aligned: a table is 4 mod 8 bytes)
+    const uint32_t bar_base = smem_base + GRP_STAGES * GRP_STAGE + GRP_STAGING + 3 * GRP_TABLE + 4;   // (8-byte aligned: a table is 4 mod 8 bytes)
     constexpr int S = GRP_STAGES;
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
     auto empty_bar = [&](int s) { return bar_base + 8u * (S + s); };
@@ -170,7 +167,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         __syncwarp();
     } else if (warp == 2 && lane == 0) {
         tma_prefetch_desc(&maps.a);
-        tma_prefetch_desc(&maps.b);
+        tma_prefetch_desc(&maps.b[0]);
     } else if (warp == 1) {
         tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
         tmem_relinquish_pair();
@@ -393,8 +390,19 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             const int half = u.jn >> 1;
             const int i = u.i0 + static_cast<int>(rank) * 128;
             const int c = u.c0 + static_cast<int>(rank) * half;      // first column of this CTA's B operand
-            const int boxes = WEIGHTS ? (half + 63) >> 6 : half >> 4;
+            const int boxes = (half + 63) >> 6;                       // WEIGHTS
             const uint32_t b_bytes = WEIGHTS ? boxes * 8192u : half * 128u;
+            // half rows (a multiple of 16, up to 128) of 128 bytes each, in the fewest boxes of 16, 32, 64 or 128 rows
+            auto rows_boxes = [&](const CUtensorMap (&map)[4], uint32_t dst, uint32_t bar, int x0) {
+                int row = c;
+#pragma unroll
+                for (int z = 3; z >= 0; --z)
+                    if (half & (16 << z)) {
+                        tma_load_3d_pair_if(dst, &map[z], bar, x0, row, 0, elected);
+                        dst += 2048u << z;
+                        row += 16 << z;
+                    }
+            };
             auto acquire = [&]() {
                 if (mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) return true;
                 if (lane == 0) give_up(0x100u + stage);
@@ -416,29 +424,39 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         mbar_arrive_expect_tx_if(raw_bar(stage), bytes, elected);
                         if (rank == 0 && elected) mbar_arrive(fb);
                         __syncwarp();
-                        tma_load_3d_if(sa, &maps.a, raw_bar(stage), i, t, 0, elected);
-                        tma_load_3d_if(sa + 8192, &maps.a, raw_bar(stage), i + 64, t, 0, elected);
-                        for (int b = 0; b < boxes; ++b) tma_load_3d_if(sb + b * 8192, &maps.b, raw_bar(stage), c + b * 64, t, 0, elected);
+                        if (p.a_slabs) {
+                            tma_load_4d_if(sa, &maps.a, raw_bar(stage), 0, t, i >> 6, 0, elected);
+                        } else {
+                            tma_load_3d_if(sa, &maps.a, raw_bar(stage), i, t, 0, elected);
+                            tma_load_3d_if(sa + 8192, &maps.a, raw_bar(stage), i + 64, t, 0, elected);
+                        }
+                        for (int b = 0; b < boxes; ++b) tma_load_3d_if(sb + b * 8192, &maps.b[0], raw_bar(stage), c + b * 64, t, 0, elected);
                     } else {
                         mbar_arrive_expect_tx_if(fb, 2u * bytes, lead_elected);
-                        tma_load_3d_pair_if(sa, &maps.a, lfb, i, t, 0, elected);
-                        tma_load_3d_pair_if(sa + 8192, &maps.a, lfb, i + 64, t, 0, elected);
-                        for (int b = 0; b < boxes; ++b) tma_load_3d_pair_if(sb + b * 8192, &maps.b, lfb, c + b * 64, t, 0, elected);
+                        if (p.a_slabs) {
+                            tma_load_4d_pair_if(sa, &maps.a, lfb, 0, t, i >> 6, 0, elected);
+                        } else {
+                            tma_load_3d_pair_if(sa, &maps.a, lfb, i, t, 0, elected);
+                            tma_load_3d_pair_if(sa + 8192, &maps.a, lfb, i + 64, t, 0, elected);
+                        }
+                        if (p.b_slabs && half == 128) {
+                            tma_load_4d_pair_if(sb, &maps.b[1], lfb, 0, t, c >> 6, 0, elected);
+                        } else {
+                            for (int b = 0; b < boxes; ++b) tma_load_3d_pair_if(sb + b * 8192, &maps.b[0], lfb, c + b * 64, t, 0, elected);
+                        }
                     }
                 } else {
                     const int kx = kb * GRP_BK;
                     mbar_arrive_expect_tx_if(fb, 2u * bytes, lead_elected);
-                    if (A_MN) {
+                    if (A_MN && p.a_slabs) {
+                        tma_load_4d_pair_if(sa, &maps.a, lfb, 0, kx, i >> 6, u.w, elected);
+                    } else if (A_MN) {
                         tma_load_3d_pair_if(sa, &maps.a, lfb, i, kx, u.w, elected);
                         tma_load_3d_pair_if(sa + 8192, &maps.a, lfb, i + 64, kx, u.w, elected);
                     } else {
                         tma_load_3d_pair_if(sa, &maps.a, lfb, kx, i, u.w, elected);
                     }
-                    if (half == 128) {
-                        tma_load_3d_pair_if(sb, &maps.b, lfb, kx, c, 0, elected);
-                    } else {
-                        for (int b = 0; b < boxes; ++b) tma_load_3d_pair_if(sb + b * 2048, &maps.b16, lfb, kx, c + b * 16, 0, elected);
-                    }
+                    rows_boxes(maps.b, sb, lfb, kx);
                 }
                 advance();
             }
@@ -461,11 +479,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         } else {
                             tma_load_3d_pair_if(sa, &maps.c, lfb, rb * 32, i, s_alt[q], elected);
                         }
-                        if (half == 128) {
-                            tma_load_3d_pair_if(sb, &maps.h, lfb, rb * 64, c, 0, elected);
-                        } else {
-                            for (int b = 0; b < boxes; ++b) tma_load_3d_pair_if(sb + b * 2048, &maps.h16, lfb, rb * 64, c + b * 16, 0, elected);
-                        }
+                        rows_boxes(maps.h, sb, lfb, rb * 64);
                         advance();
                     }
                 }
@@ -579,6 +593,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         const int set = warp >= 6 ? 1 : 0;
         const int quarter = warp & 3;
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
+        const uint32_t staging = smem_base + S * GRP_STAGE + (warp - 2) * 4096;
+        uint32_t parity = 0;
         int local = 0;
         bool ok = true, waited = false;
         GroupedUnit u = {};
@@ -597,92 +613,105 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             if (lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(tempty_bar(local & 1), 0));
             ++local;
         };
-        // one finished 32 x 32 piece (columns c .. c + 31 of the tile, this warp's 32 features) of a whole tile
-        auto store = [&](const float (&v)[32], int c) {
+        // one 32 x 32 piece (columns c .. c + 31 of the tile, this warp's 32 features) of a tile or of one part of a cut one
+        auto deliver = [&](float (&v)[32], int c) {
+            if (u.parts > 1) {
+                const size_t slab = static_cast<size_t>(GRP_TILE) * p.slab_cols;
+                const size_t at = (rank * static_cast<size_t>(p.slab_cols) + c) * 128 + quarter * 32 + lane;
+                // the slab of a pair: 0 for the tile its share begins in, 1 for the one it ends in
+                auto slab_of = [&](int part) { return p.partial + (2 * (u.first_pair + part) + (part > 0 ? 0 : 1)) * slab + at; };
+                float* mine = slab_of(u.part);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) __stcg(mine + j * 128, v[j]);
+                __threadfence();
+                __syncwarp();
+                unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + (c >> 5);
+                unsigned int old = 0;
+                if (lane == 0) old = (atomicAdd(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
+                old = __shfl_sync(~0u, old, 0);
+                if (old != static_cast<unsigned>(u.parts) - 1u) return;
+                if (lane == 0) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
+                __threadfence();
+                const float* src = slab_of(0);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = __ldcg(src + j * 128);
+#pragma unroll 1
+                for (int s = 1; s < u.parts; ++s) {
+                    src = slab_of(s);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] += __ldcg(src + j * 128);
+                }
+            }
             const int i = u.i0 + static_cast<int>(rank) * 128 + quarter * 32 + lane;
             const int n = min(32, u.cols - c);
             if (MODE == GRP_ROWS && p.h16) {
                 grouped_store_h(p, v, u.c0 + c, i, n, __ldg(p.scale + u.w));
                 return;
             }
-            const float* add = p.add ? p.add + static_cast<size_t>(u.c0 + c) * p.I : nullptr;
-            if (add && !waited) {
-                asm volatile("griddepcontrol.wait;" ::: "memory");   // `add` comes from the kernel before this one
+            const bool live = i < p.I;
+            if (MODE == GRP_ROWS && p.add) {
+                if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // `add` comes from the kernel before this one
                 waited = true;
+                const float* add = p.add + static_cast<size_t>(u.c0 + c) * p.I + i;
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (live && j < n) v[j] += add[static_cast<size_t>(j) * p.I];
             }
-            const size_t base = (WEIGHTS ? static_cast<size_t>(u.g) * p.stride_c : 0) + static_cast<size_t>(u.c0 + c) * p.ldc;
-            if (p.out16) grouped_store16(p, v, base, i, n, add);
-            else grouped_store32(p, v, base, i, n, add);
-        };
-        // ... or of one part of a cut tile
-        auto deliver = [&](const float (&v)[32], int c) {
-            if (u.parts == 1) {
-                store(v, c);
+            const size_t base = (WEIGHTS ? static_cast<size_t>(u.g) * p.stride_c : 0) + static_cast<size_t>(u.c0 + c) * p.ldc + i;
+            if (p.beta && live) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j < n)
+                        v[j] += p.out16 ? half_bits_to_f32(static_cast<const uint16_t*>(p.C)[base + j * p.ldc], p.f16)
+                                        : static_cast<const float*>(p.C)[base + j * p.ldc];
+            }
+            if (!WEIGHTS && n < 32) {                     // the next row is another group's
+                grouped_store_rows(p, v, base, live ? n : 0);
                 return;
             }
-            const size_t slab = static_cast<size_t>(GRP_TILE) * p.slab_cols;
-            const size_t at = (rank * static_cast<size_t>(p.slab_cols) + c) * 128 + quarter * 32 + lane;
-            // the slab of a pair: 0 for the tile its share begins in, 1 for the one it ends in
-            auto slab_of = [&](int part) {
-                const int pair = u.first_pair + part;
-                return p.partial + (2 * pair + (part > 0 ? 0 : 1)) * slab + at;
-            };
-            float* mine = slab_of(u.part);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) __stcg(mine + j * 128, v[j]);
-            __threadfence();
-            __syncwarp();
-            unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + (c >> 5);
-            unsigned int old = 0;
-            if (lane == 0) old = (atomicAdd(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
-            old = __shfl_sync(~0u, old, 0);
-            if (old != static_cast<unsigned>(u.parts) - 1u) return;
-            if (lane == 0) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
-            __threadfence();
-            float sum[32];
-            const float* src = slab_of(0);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) sum[j] = __ldcg(src + j * 128);
-            for (int s = 1; s < u.parts; ++s) {
-                src = slab_of(s);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) sum[j] += __ldcg(src + j * 128);
+            // two boxes of 16-bit, one of 32-bit results fit this warp's 4 KB: wait until the store of the one before has been read
+            const uint32_t box = staging + (p.out16 ? parity * 2048 : 0);
+            if (lane == 0) {
+                if (p.out16) bulk_wait_read<1>();
+                else bulk_wait_read<0>();
             }
-            store(sum, c);
+            __syncwarp();
+            if (!p.out16) grouped_stage32(v, box);
+            else if (p.f16) grouped_stage16<true>(v, box);
+            else grouped_stage16<false>(v, box);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                tma_store_3d(&maps.out, box, i - lane, u.c0 + c, WEIGHTS ? u.g : 0);
+                bulk_commit();
+            }
+            parity ^= 1u;
         };
         reset();
         while (ok && next(u)) {
             const GroupedRequests r = look(u);
-            if (p.chunk || r.parts > 0) {
-                // the accumulators of the chunks, and the requests' columns of theirs, are added in registers
-                const int blocks = u.kb1 - u.kb0 + r.whole;
-                const int chunks = p.chunk ? max(1, (blocks + p.chunk - 1) / p.chunk) : 1;
+            // the accumulators that make up the tile: chunks of its own k-blocks, then one for each request with some of its rows
+            const int blocks = u.kb1 - u.kb0 + r.whole;
+            const int chunks = p.chunk ? max(1, (blocks + p.chunk - 1) / p.chunk) : 1, all = chunks + r.parts;
+            if (!await()) break;
+            if (all > 1) {
+                // all but the last are added in registers, and the sum goes back to the last one's place
                 float sum[4][32];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) sum[q][j] = 0.0f;
-                for (int ch = 0; ch < chunks; ++ch) {
-                    if (!await()) { ok = false; break; }
-                    const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int c = set * 32 + q * 64;
-                        if (c < u.cols && blocks > 0) {
-                            uint32_t v[32];
-                            tmem_ld_32x32(taddr + c, v);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[q][j] += __uint_as_float(v[j]);
-                        }
+                int at = r.first;
+#pragma unroll 1
+                for (int n = 0; n < all; ++n) {
+                    int lo = 0, hi = u.cols;              // the columns this accumulator has something for
+                    if (LORA && n >= chunks) {
+                        while (!has_part(at)) ++at;
+                        lo = s_row[at] - u.c0;
+                        hi = min(hi, s_row[at + 1] - u.c0);
+                        ++at;
                     }
-                    release();
-                }
-                for (int n = 0, at = r.first; LORA && ok && n < r.parts; ++n, ++at) {
-                    while (!has_part(at)) ++at;
-                    if (!await()) { ok = false; break; }
                     const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
-                    const int lo = s_row[at] - u.c0, hi = s_row[at + 1] - u.c0;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int c = set * 32 + q * 64;
@@ -690,40 +719,59 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                             uint32_t v[32];
                             tmem_ld_32x32(taddr + c, v);
                             tmem_ld_wait();
+                            if (!LORA || (c >= lo && c + 32 <= hi)) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (c + j >= lo && c + j < hi) sum[q][j] += __uint_as_float(v[j]);
+                                for (int j = 0; j < 32; ++j) sum[q][j] += __uint_as_float(v[j]);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (c + j >= lo && c + j < hi) sum[q][j] += __uint_as_float(v[j]);
+                            }
                         }
                     }
-                    release();
+                    if (n < all - 1) {
+                        release();
+                        if (!await()) { ok = false; break; }
+                    }
                 }
                 if (!ok) break;
+                const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = set * 32 + q * 64;
-                    if (c < u.cols) deliver(sum[q], c);
-                }
-            } else {
-                if (!await()) break;
-                const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
-                const bool none = u.kb1 <= u.kb0;
-                // the parts of a cut tile begin with different columns, so that each finishes some of them last
-                const int mine = (u.cols - set * 32 + 63) >> 6;
-                for (int r = 0; r < mine; ++r) {
-                    int q = r + u.part;
-                    while (q >= mine) q -= mine;
-                    const int c = set * 32 + q * 64;
-                    uint32_t v[32];
-                    float f[32];
-                    tmem_ld_32x32(taddr + c, v);
-                    tmem_ld_wait();
+                    if (c < u.cols) {
+                        uint32_t v[32];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = none ? 0.0f : __uint_as_float(v[j]);
-                    deliver(f, c);
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[q][j]);
+                        tmem_st_32x32(taddr + c, v);
+                    }
                 }
-                release();
+                tmem_st_wait();
             }
+            const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
+            // the parts of a cut tile begin with different columns, so that each finishes some of them last
+            const int mine = (u.cols - set * 32 + 63) >> 6;
+#pragma unroll 1
+            for (int n = 0; n < mine; ++n) {
+                int q = n + u.part;
+                while (q >= mine) q -= mine;
+                const int c = set * 32 + q * 64;
+                uint32_t v[32];
+                float f[32];
+                tmem_ld_32x32(taddr + c, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                if (WEIGHTS && blocks == 0) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[j] = 0.0f;
+                }
+                deliver(f, c);
+            }
+            release();
         }
+        if (lane == 0) bulk_wait_read<0>();               // the stores are done with this CTA's shared memory
+        __syncwarp();
     } else if (WEIGHTS) {
         // ------------------------------------------------ rows of the next group in a group's last k-block
         const uint32_t lead_tail0 = map_to_cta(tail_bar(0), 0);

@@ -9,13 +9,14 @@ namespace nk {
 
 constexpr int GRP_THREADS = 352;
 constexpr int GRP_MAX_GROUPS = 1024;
-constexpr int GRP_STAGES = 6;
+constexpr int GRP_STAGES = 5;
 constexpr int GRP_A_BYTES = 128 * 64 * 2;
 constexpr int GRP_STAGE = 2 * GRP_A_BYTES;             // 16 KB of features, up to 16 KB of rows, per CTA
 constexpr int GRP_BK = 64;
 constexpr int GRP_TILE = 256;                          // features of a tile, and the most rows of one
 constexpr int GRP_TABLE = 4 * (GRP_MAX_GROUPS + 1);    // bytes of a table by group
-constexpr int GRP_SMEM = GRP_STAGES * GRP_STAGE + 1024 + 3 * GRP_TABLE + 512;
+constexpr int GRP_STAGING = 8 * 4096;                  // of the stores: 4 KB for each epilogue warp
+constexpr int GRP_SMEM = GRP_STAGES * GRP_STAGE + GRP_STAGING + 1024 + 3 * GRP_TABLE + 512;
 
 constexpr int GRP_CHUNK = 4;                           // k-blocks between additions to the FP32 sums of FP32 results
 
@@ -30,6 +31,7 @@ struct GroupedParams {
     int beta, out16, f16;
     int chunk;             // k-blocks summed in tensor memory before they are added to an FP32 sum in registers; 0: all
     uint32_t idesc;        // without the N field
+    int a_slabs, b_slabs;  // MN-major operands of whole 64-feature slabs: a CTA's 128 features in one box
     const int* offsets;    // [groups + 1]; null: one group of all rows
     const int* index;      // ROWS: weight of each group (outside [0, index_max): the group is skipped); null: its number
     int index_max;
@@ -59,9 +61,10 @@ inline uint32_t grouped_idesc(bool a_mn, bool b_mn, bool f16) {
 }
 
 struct GroupedMaps {
-    CUtensorMap a;         // the features' operand
-    CUtensorMap b, b16;    // the rows' operand in boxes of 128 (WEIGHTS: 64) and of 16 rows
-    CUtensorMap c, h, h16; // LORA: the adapters' B, and h16 in boxes of 128 and of 16 rows
+    CUtensorMap a;         // the features' operand: boxes of 128 features x 64 of k; with a_slabs one box, else two
+    CUtensorMap b[4];      // the rows' operand in boxes of 16, 32, 64 and 128 rows; WEIGHTS: [0] 64 features, [1] 128 of them (b_slabs)
+    CUtensorMap out;       // C in boxes of 32 features x 32 rows (not with h16)
+    CUtensorMap c, h[4];   // LORA: the adapters' B, and h16 in boxes like b's
 };
 
 // (nk_grouped.cu)

@@ -142,16 +142,19 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     if (d.rows == 0) A = B = C;        // no row is loaded; the maps only need an address
     const int64_t rows = d.rows ? d.rows : 1;
-    if (!p->cached_c || p->cached_a != A || p->cached_b != B) {
+    if (p->cached_c != C || p->cached_a != A || p->cached_b != B) {
         const bool f16 = d.in_dtype == NK_F16;
         bool ok;
+        GroupedMaps& m = p->maps;
         if (weights) {
-            ok = encode_map(&p->maps.a, B, f16, d.N, rows, 1, d.ldb, 0, 64) && encode_map(&p->maps.b, A, f16, d.K, rows, 1, d.lda, 0, 64);
-            p->maps.b16 = p->maps.b;
+            ok = encode_out(&m.out, C, d.out_dtype, d.N, d.K, d.groups, d.ldc, d.stride_g) &&
+                 (d.N % 64 == 0 ? encode_slabs(&m.a, B, f16, d.N, rows, 1, d.ldb, 0) : encode_map(&m.a, B, f16, d.N, rows, 1, d.ldb, 0, 64)) &&
+                 encode_map(&m.b[0], A, f16, d.K, rows, 1, d.lda, 0, 64) && (d.K % 64 != 0 || encode_slabs(&m.b[1], A, f16, d.K, rows, 1, d.lda, 0));
         } else {
-            ok = (d.layout_b == NK_ROW_MAJOR ? encode_map(&p->maps.a, B, f16, d.N, d.K, d.groups, d.ldb, d.stride_g, 64)
-                                             : encode_map(&p->maps.a, B, f16, d.K, d.N, d.groups, d.ldb, d.stride_g, 128)) &&
-                 encode_map(&p->maps.b, A, f16, d.K, rows, 1, d.lda, 0, 128) && encode_map(&p->maps.b16, A, f16, d.K, rows, 1, d.lda, 0, 16);
+            ok = encode_rows(m.b, A, f16, d.K, rows, d.lda) && encode_out(&m.out, C, d.out_dtype, d.N, rows, 1, d.ldc, 0) &&
+                 (d.layout_b == NK_TRANSPOSED ? encode_map(&m.a, B, f16, d.K, d.N, d.groups, d.ldb, d.stride_g, 128)
+                  : d.N % 64 == 0             ? encode_slabs(&m.a, B, f16, d.N, d.K, d.groups, d.ldb, d.stride_g)
+                                              : encode_map(&m.a, B, f16, d.N, d.K, d.groups, d.ldb, d.stride_g, 64));
         }
         if (!ok) {
             p->cached_c = nullptr;
@@ -160,7 +163,7 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
         }
         p->cached_a = A;
         p->cached_b = B;
-        p->cached_c = C;               // (set: the maps are valid)
+        p->cached_c = C;
     }
     GroupedParams g = {};
     g.groups = static_cast<int>(d.groups);
@@ -182,6 +185,8 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     g.counter = p->counters;
     g.status = p->status_dev;
     g.slab_cols = p->slab_cols;
+    g.a_slabs = d.N % 64 == 0;
+    g.b_slabs = d.K % 64 == 0;
     g.chunk = g.out16 ? 0 : GRP_CHUNK;
     const cudaError_t e = grouped_launch(weights ? GRP_WEIGHTS : GRP_ROWS, weights || d.layout_b == NK_ROW_MAJOR, p->pairs,
                                          static_cast<cudaStream_t>(cuda_stream), p->maps, g, false);

@@ -11,7 +11,7 @@ struct nk_lora_s : nk::PlanBase {
     unsigned int* counters[2];
     size_t part_bytes[2], side_bytes;   // partial sums of the two; FP32 contributions or X . A
     nk::GroupedMaps maps, shrink; // of the projection and of X . A
-    const void *cached_x, *cached_w, *cached_a, *cached_b, *cached_ws;
+    const void *cached_x, *cached_w, *cached_a, *cached_b, *cached_ws, *cached_y;
     char name[64];
 };
 
@@ -96,18 +96,18 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     DeviceGuard guard(d.device);
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     const bool f16 = d.in_dtype == NK_F16, row = d.layout == NK_ROW_MAJOR;
-    if (p->cached_x != X || p->cached_w != W || p->cached_a != A || p->cached_b != B || p->cached_ws != workspace) {
+    if (p->cached_x != X || p->cached_w != W || p->cached_a != A || p->cached_b != B || p->cached_ws != workspace || p->cached_y != Y) {
         p->cached_x = nullptr;
         GroupedMaps &m = p->maps, &s = p->shrink;
-        bool ok = (row ? encode_map(&m.a, W, f16, d.N, d.K, 1, d.ldw, 0, 64) : encode_map(&m.a, W, f16, d.K, d.N, 1, d.ldw, 0, 128)) &&
-                  encode_map(&m.b, X, f16, d.K, d.rows, 1, d.ldx, 0, 128) && encode_map(&m.b16, X, f16, d.K, d.rows, 1, d.ldx, 0, 16);
+        bool ok = encode_rows(m.b, X, f16, d.K, d.rows, d.ldx) && encode_out(&m.out, Y, d.out_dtype, d.N, d.rows, 1, d.ldy, 0) &&
+                  (!row ? encode_map(&m.a, W, f16, d.K, d.N, 1, d.ldw, 0, 128)
+                   : d.N % 64 == 0 ? encode_slabs(&m.a, W, f16, d.N, d.K, 1, d.ldw, 0) : encode_map(&m.a, W, f16, d.N, d.K, 1, d.ldw, 0, 64));
         if (!p->few) {
             const int64_t r = d.rank, h = p->rank_blocks * 64;
-            ok = ok && (row ? encode_map(&s.a, A, f16, r, d.K, d.adapters, r, r * d.K, 64) : encode_map(&s.a, A, f16, d.K, r, d.adapters, d.K, r * d.K, 128)) &&
-                 (row ? encode_map(&m.c, B, f16, d.N, r, d.adapters, d.N, r * d.N, 32) : encode_map(&m.c, B, f16, r, d.N, d.adapters, r, r * d.N, 128)) &&
-                 encode_map(&m.h, workspace, f16, h, d.rows, 1, h, 0, 128) && encode_map(&m.h16, workspace, f16, h, d.rows, 1, h, 0, 16);
-            s.b = m.b;
-            s.b16 = m.b16;
+            ok = ok && encode_rows(m.h, workspace, f16, h, d.rows, h) &&
+                 (row ? encode_map(&s.a, A, f16, r, d.K, d.adapters, r, r * d.K, 64) : encode_map(&s.a, A, f16, d.K, r, d.adapters, d.K, r * d.K, 128)) &&
+                 (row ? encode_map(&m.c, B, f16, d.N, r, d.adapters, d.N, r * d.N, 32) : encode_map(&m.c, B, f16, r, d.N, d.adapters, r, r * d.N, 128));
+            memcpy(s.b, m.b, sizeof(s.b));
         }
         if (!ok) {
             snprintf(p->cuda_err, sizeof(p->cuda_err), "cuTensorMapEncodeTiled failed");
@@ -118,6 +118,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
         p->cached_a = A;
         p->cached_b = B;
         p->cached_ws = workspace;
+        p->cached_y = Y;
     }
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(workspace);
@@ -182,6 +183,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     g.groups = 1;
     g.I = static_cast<int>(d.N);
     g.tiles_i = static_cast<int>(div_up(d.N, GRP_TILE));
+    g.a_slabs = d.N % 64 == 0;
     g.out16 = d.out_dtype != NK_F32;
     g.chunk = g.out16 ? 0 : GRP_CHUNK;
     g.C = Y;

@@ -100,4 +100,36 @@ static inline bool encode_map(CUtensorMap* m, const void* base, bool f16, int64_
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same array with rows of whole slabs of 64 elements seen as [outer][slab][mid][64]: a box is 64 rows of two slabs,
+// one slab behind the other.
+static inline bool encode_slabs(CUtensorMap* m, const void* base, bool f16, int64_t inner, int64_t mid, int64_t outer,
+                                int64_t ld, int64_t stride) {
+    cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(mid), static_cast<cuuint64_t>(inner / 64), static_cast<cuuint64_t>(outer)};
+    cuuint64_t strides[3] = {static_cast<cuuint64_t>(ld) * 2, 128, static_cast<cuuint64_t>(outer > 1 ? stride : ld) * 2};
+    cuuint32_t box[4] = {64, 64, 2, 1};
+    cuuint32_t es[4] = {1, 1, 1, 1};
+    return encode_tiled()(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base),
+                          dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// C as boxes of 32 x 32 elements, rows of a box behind one another.
+static inline bool encode_out(CUtensorMap* m, void* base, int dtype, int64_t inner, int64_t mid, int64_t outer, int64_t ld, int64_t stride) {
+    const int64_t esz = dtype == NK_F32 ? 4 : 2;
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(mid), static_cast<cuuint64_t>(outer)};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * esz), static_cast<cuuint64_t>((outer > 1 ? stride : ld) * esz)};
+    cuuint32_t box[3] = {32, 32, 1};
+    cuuint32_t es[3] = {1, 1, 1};
+    return encode_tiled()(m, dtype == NK_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == NK_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                          3, base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                          CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The four box heights of a rows' operand.
+static inline bool encode_rows(CUtensorMap (&m)[4], const void* base, bool f16, int64_t inner, int64_t rows, int64_t ld) {
+    for (int z = 0; z < 4; ++z)
+        if (!encode_map(&m[z], base, f16, inner, rows, 1, ld, 0, 16 << z)) return false;
+    return true;
+}
+
 }  // namespace nk
