@@ -11,7 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libnk_gemm.so")
-SOURCES = ["nk_gemm.cu", "nk_grouped.cu", "nk_route.cu", "nk_lora.cu"]
+SOURCES = ["nk_gemm.cu", "nk_grouped.cu", "grouped_rows.cu", "grouped_weights.cu", "grouped_lora.cu",
+           "nk_route.cu", "nk_lora.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 

@@ -13,8 +13,8 @@
 //
 // A CTA pair (cta_group::2) computes a tile of 256 features x up to 256 rows: each CTA holds 128 features
 // of the MMA's A operand and half of the columns of its B operand, and drains 128 accumulator lanes.  The
-// groups' offsets are read on the device: every CTA turns them into a prefix of tile counts at its start
-// (a few hundred clocks), so no launch, size or plan depends on how the rows are spread.
+// groups' offsets are read on the device: every CTA turns them into a prefix of tile counts at its start,
+// so no launch, size or plan depends on how the rows are spread.
 //
 // Schedule.  Whole waves of tiles go to the pairs in turn.  What is left (less than two waves) is laid end to
 // end along k and shared out evenly, where that saves more k-blocks than a cut tile costs; the pieces of a
@@ -26,7 +26,9 @@
 // the epilogue's registers while the other accumulator is being filled.  16-bit results do not need it.
 //
 // Warps: 0 TMA producer, 1 MMA issuer, 2-9 epilogue (warps 2-5 take the even 32-column chunks, 6-9 the odd
-// ones), 10 (WEIGHTS) clears the rows of a group's last k-block that belong to the next group.
+// ones), 10 (WEIGHTS) clears the rows of a group's last k-block that belong to the next group, 11 scheduler: it alone
+// reads the offsets and hands out the work (inlined in every role the schedule made the kernel's code several times
+// as long, and a launch that does little pays for code that is not in the instruction cache yet).
 // All waits are bounded (see mbar_wait).
 #pragma once
 #include "grouped_launch.cuh"
@@ -35,106 +37,54 @@
 
 namespace nk {
 
-// One piece of work: k-blocks kb0 .. kb1-1 of a tile.
-struct GroupedUnit {
-    int g, w, i0, c0;      // group, its weight, first feature, first row of C (ROWS: in the whole array, WEIGHTS: in C_g)
-    int cols, jn;          // rows of C in the tile, and the MMA's N (cols rounded up to 32)
-    int kb0, kb1, kbs;     // k-blocks of this piece, and of the whole tile
+// One piece of work: k-blocks kb0 .. kb1-1 of a tile.  Made by the scheduler warp, handed to the others in shared memory.
+struct __align__(16) GroupedUnit {
+    int some;              // 0: no more work
+    int g, w, i0;          // group, its weight, first feature
+    int c0, cols, jn;      // first row of C (ROWS: in the whole array, WEIGHTS: in C_g), rows of C in the tile, the MMA's N (cols rounded up to 32)
+    int kb0, kb1;
     int row0, rows;        // the group's rows
     int cut, parts, part, first_pair;   // a cut tile: its number among the tail's tiles, its parts, this one, the pair of part 0
+    int req, req_whole, req_parts;      // LORA: the first request of the tile, k-blocks of the one with all of its rows, how many have some of them
+    int pad[2];
 };
-
-// LORA: the first request of a tile, the k-blocks of the one that has all of its rows, how many have some of them
-struct GroupedRequests {
-    int first, whole, parts;
-};
+constexpr int GRP_UNITS = 4;            // of them on the way
 
 __device__ __forceinline__ int round32(int x) { return (x + 31) & ~31; }
 
-// One 32 x 32 piece of C, lane l holding feature l, v[j] row j.  Where all of its rows are stored it goes through
-// shared memory: a TMA store writes the box (and clips what lies beyond C's edges), which takes a third of the
-// instructions of stores from registers; with a short contraction the epilogue's issue slots bound the kernel.
-//
-// 16-bit results: a lane packs its feature of rows j and j + 1 and exchanges words with its neighbour; even lanes then
-// hold row j of features (l, l + 1), odd lanes row j + 1 of (l - 1, l): two rows of 64 bytes per store, no bank twice.
-template <bool F16>
-__device__ __forceinline__ void grouped_stage16(const float (&v)[32], uint32_t dst) {
-    const uint32_t odd = threadIdx.x & 1, l = threadIdx.x & 31;
-    const uint32_t pick = odd ? 0x3276u : 0x5410u;
-    dst += odd * 64 + (l >> 1) * 4;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const uint32_t w = pack_half2(v[2 * j], v[2 * j + 1], F16);
-        const uint32_t got = __shfl_xor_sync(~0u, w, 1);
-        asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + j * 128), "r"(__byte_perm(w, got, pick)) : "memory");
-    }
-}
-__device__ __forceinline__ void grouped_stage32(const float (&v)[32], uint32_t dst) {
-    dst += (threadIdx.x & 31) * 4;
-#pragma unroll
-    for (int j = 0; j < 32; ++j) asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + j * 128), "r"(__float_as_uint(v[j])) : "memory");
-}
-
-// The rows [0, rows) of a piece from registers; c points at row 0, this lane's feature.
-__device__ __forceinline__ void grouped_store_rows(const GroupedParams& p, const float (&v)[32], size_t at, int rows) {
-    if (p.out16) {
-        uint16_t* c = static_cast<uint16_t*>(p.C) + at;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < rows) c[j * p.ldc] = static_cast<uint16_t>(pack_half2(v[j], 0.0f, p.f16) & 0xFFFFu);
-    } else {
-        float* c = static_cast<float*>(p.C) + at;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < rows) c[j * p.ldc] = v[j];
-    }
-}
-
-// h16: leading part and remainder of the scaled product; an infinite leading part has no remainder
-__device__ __forceinline__ void grouped_store_h(const GroupedParams& p, const float (&v)[32], int row0, int i, int cols, float scale) {
-    if (i >= p.rank_blocks * 32) return;
-    uint16_t* h = p.h16 + static_cast<size_t>(row0) * (p.rank_blocks * 64) + (i >> 5) * 64 + (i & 31);
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        if (j >= cols) break;
-        const float x = i < p.I ? v[j] * scale : 0.0f;
-        const uint32_t hi = pack_half2(x, 0.0f, p.f16) & 0xFFFFu;
-        const float back = half_bits_to_f32(hi, p.f16);
-        const uint32_t lo = fabsf(back) <= 3.4028235e38f ? pack_half2(x - back, 0.0f, p.f16) & 0xFFFFu : 0u;
-        h[static_cast<size_t>(j) * (p.rank_blocks * 64)] = static_cast<uint16_t>(hi);
-        h[static_cast<size_t>(j) * (p.rank_blocks * 64) + 32] = static_cast<uint16_t>(lo);
-    }
-}
-
 // MODE: GroupedMode.  A_MN: the features' operand is MN-major (row-major weights [K][I], or rows [t][I]), else
 // K-major (weights [I][K]).
-template <int MODE, bool A_MN>
+// OUT: type of C (GroupedOut).
+template <int MODE, bool A_MN, int OUT>
 __global__ void __launch_bounds__(GRP_THREADS, 1) __cluster_dims__(2, 1, 1)
 grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__ GroupedParams p) {
     constexpr bool WEIGHTS = MODE == GRP_WEIGHTS, LORA = MODE == GRP_LORA;
+    constexpr bool OUT16 = OUT != GRP_OUT_F32, F16 = OUT == GRP_OUT_F16;
     static_assert(!WEIGHTS || A_MN, "rows are contiguous in their features");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
-    int* s_row = reinterpret_cast<int*>(gen_base + GRP_STAGES * GRP_STAGE + GRP_STAGING);   // first row of each group (LORA: request), clamped and monotone
+    int* s_row = reinterpret_cast<int*>(gen_base + GRP_RING + GRP_STAGING);   // first row of each group (LORA: request), clamped and monotone
     int* s_pre = s_row + GRP_MAX_GROUPS + 1;                                  // tiles before each group
     int* s_alt = s_pre + GRP_MAX_GROUPS + 1;                                  // ROWS: weight of the group; LORA: adapter of the request; -1: none.  WEIGHTS: k-blocks before each group
-    const uint32_t bar_base = smem_base + GRP_STAGES * GRP_STAGE + GRP_STAGING + 3 * GRP_TABLE + 4;   // (8-byte aligned: a table is 4 mod 8 bytes)
-    constexpr int S = GRP_STAGES;
+    const uint32_t bar_base = smem_base + GRP_RING + GRP_STAGING + 3 * GRP_TABLE + 4;   // (8-byte aligned: a table is 4 mod 8 bytes)
+    constexpr int MS = GRP_MAX_STAGES, WS = 5;            // (WEIGHTS: always five stages)
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
-    auto empty_bar = [&](int s) { return bar_base + 8u * (S + s); };
-    auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * S + a); };
-    auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * S + 2 + a); };
-    auto raw_bar = [&](int s) { return bar_base + 8u * (2 * S + 4 + s); };    // a block with rows to clear: this CTA's boxes have landed
-    auto tail_bar = [&](int s) { return bar_base + 8u * (3 * S + 4 + s); };   // leader: both CTAs have cleared theirs
-    constexpr int NB = 4 * S + 4;
-    static_assert(NB <= 32, "one barrier per lane");
+    auto empty_bar = [&](int s) { return bar_base + 8u * (MS + s); };
+    auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * MS + a); };
+    auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * MS + 2 + a); };
+    auto raw_bar = [&](int s) { return bar_base + 8u * (2 * MS + 4 + s); };   // a block with rows to clear: this CTA's boxes have landed
+    auto tail_bar = [&](int s) { return bar_base + 8u * (2 * MS + 4 + WS + s); };   // leader: both CTAs have cleared theirs
+    auto ufull_bar = [&](int n) { return bar_base + 8u * (2 * MS + 4 + 2 * WS + n); };    // a unit is there
+    auto uempty_bar = [&](int n) { return bar_base + 8u * (2 * MS + 4 + 2 * WS + GRP_UNITS + n); };   // every role has read it
+    constexpr int NB = 2 * MS + 4 + 2 * WS + 2 * GRP_UNITS;
     static_assert((3 * GRP_TABLE + 4) % 8 == 0, "barriers are 8-byte aligned");
     const uint32_t peer_ready_bar = bar_base + 8u * NB;
     uint8_t* after = gen_base + (bar_base - smem_base) + 8 * (NB + 1);
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(after);
     volatile uint32_t* abort_flag = tmem_slot + 1;
-    volatile int* s_most = reinterpret_cast<volatile int*>(after + 8);       // rows of the largest group
+    volatile int* s_width = reinterpret_cast<volatile int*>(after + 8);      // rows of a tile at most
+    GroupedUnit* s_unit = reinterpret_cast<GroupedUnit*>(gen_base + ((GRP_RING + GRP_STAGING + 3 * GRP_TABLE + 4 + 8 * (NB + 1) + 12 + 15) & ~15));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -156,10 +106,14 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         }
     }
     if (warp == 0) {
-        if (lane < NB) {
-            // tempty: one arrival per epilogue warp of both CTAs; tail: one per CTA
-            const uint32_t count = lane >= 2 * S + 2 && lane < 2 * S + 4 ? 16 : lane >= 3 * S + 4 ? 2 : 1;
-            mbar_init(bar_base + 8u * lane, count);
+        for (int n = lane; n < NB; n += 32) {
+            // tempty: one arrival per epilogue warp of both CTAs; tail: one per CTA; uempty: producer, epilogue warps, the leader's
+            // MMA issuer and (WEIGHTS) the warp that clears rows
+            const uint32_t count = n >= 2 * MS + 2 && n < 2 * MS + 4                            ? 16
+                                   : n >= 2 * MS + 4 + WS && n < 2 * MS + 4 + 2 * WS            ? 2
+                                   : n >= 2 * MS + 4 + 2 * WS + GRP_UNITS ? 9 + (rank == 0) + WEIGHTS
+                                                                                                : 1;
+            mbar_init(bar_base + 8u * n, count);
         }
         if (lane == 31) mbar_init(peer_ready_bar, 1);
         if (lane == 0) *abort_flag = 0;
@@ -174,175 +128,32 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 2) {
-        // running maximum of the clamped offsets, then the prefix of the tile counts
-        int top = 0, units = 0, blocks = 0, most = 0;
-        bool bad = false;
-        for (int base = 0; base <= entries; base += 32) {
-            const int g = base + lane;
-            const int raw = g <= entries ? s_row[g] : 0;
-            int v = min(max(raw, 0), p.rows);
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(~0u, v, d);
-                if (lane >= d) v = max(v, o);
-            }
-            v = max(v, top);
-            if (g <= entries) {
-                bad |= v != raw;
-                s_row[g] = v;
-            }
-            top = __shfl_sync(~0u, v, 31);
-        }
-        if (__any_sync(~0u, bad) && lane == 0 && blockIdx.x == 0 && p.status) atomicCAS(p.status, 0u, 0x10000u);
-        __syncwarp();
-        for (int base = 0; !LORA && base <= p.groups; base += 32) {
-            const int g = base + lane;
-            const int rows = g < p.groups ? s_row[g + 1] - s_row[g] : 0;
-            most = max(most, rows);
-            const int n = g >= p.groups ? 0 : WEIGHTS ? p.tiles_i * p.tiles_j : s_alt[g] < 0 ? 0 : (rows + GRP_TILE - 1) / GRP_TILE * p.tiles_i;
-            const int b = WEIGHTS ? n * max(1, (rows + GRP_BK - 1) / GRP_BK) : 0;
-            int v = n, w = b;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(~0u, v, d), x = __shfl_up_sync(~0u, w, d);
-                if (lane >= d) { v += o; w += x; }
-            }
-            if (g <= p.groups) {
-                s_pre[g] = units + v - n;
-                if (WEIGHTS) s_alt[g] = blocks + w - b;
-            }
-            units += __shfl_sync(~0u, v, 31);
-            blocks += __shfl_sync(~0u, w, 31);
-        }
-        if (LORA) {
-            most = p.rows;
-            if (lane == 0) { s_pre[0] = 0; s_pre[1] = (p.rows + GRP_TILE - 1) / GRP_TILE * p.tiles_i; }
-        }
-        most = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(most)));
-        if (lane == 0) *s_most = most;
-    }
     cluster_arrive();
     cluster_wait();          // the barriers of both CTAs are initialised
-    __syncthreads();         // the prefix is there
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
     if (warp == 1 && rank == 1 && lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(peer_ready_bar, 0));
 
-    // ---------------------------------------------------- the schedule
-    const int tiles = s_pre[p.groups];
-    const int most_kbs = WEIGHTS ? (*s_most + GRP_BK - 1) / GRP_BK : p.kb_total;      // k-blocks of the longest tile
-    // whole tiles in turn, then the tail [tail_from, tiles): `tail_len` k-blocks, `share` of them to each pair
-    const int full_waves = tiles / num_pairs;
-    int tail_from = tiles, tail_len = 0, share = 0, tail_base = 0;
-    if (p.partial && tiles > full_waves * num_pairs) {
-        const int from = full_waves > 1 ? (full_waves - 1) * num_pairs : 0;
-        if (WEIGHTS) {
-            int lo = 0, hi = p.groups;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (s_pre[mid] <= from) lo = mid;
-                else hi = mid;
-            }
-            tail_base = s_alt[lo] + (from - s_pre[lo]) * max(1, (s_row[lo + 1] - s_row[lo] + GRP_BK - 1) / GRP_BK);
-            tail_len = s_alt[p.groups] - tail_base;
-        } else {
-            tail_len = (tiles - from) * p.kb_total;
-        }
-        share = max(4, (tail_len + num_pairs - 1) / num_pairs);
-        // a cut tile writes its sums to memory and reads them back: about as long as 8 k-blocks, and one more for
-        // every 32 columns
-        const int rounds = (tiles - from + num_pairs - 1) / num_pairs;
-        const int columns = WEIGHTS ? min(p.J, GRP_TILE) : min(*s_most, GRP_TILE);
-        if (rounds * most_kbs - share > 8 + columns / 32) tail_from = from;
-    }
-    const int tail_lo = pair_id * share, tail_hi = min(tail_lo + share, tail_len);
-    // n counts this pair's whole tiles, x is its place in the tail
-    int next_tile = pair_id, x = tail_lo;
-    auto reset = [&]() { next_tile = pair_id; x = tail_lo; };
+    // the roles' view of the schedule: wait for the next unit, read it, give its place back
+    int unit_at = 0;
+    uint32_t unit_phase = 0;
     auto next = [&](GroupedUnit& u) -> bool {
-        int tile;
-        u.cut = -1;
-        u.parts = 1;
-        u.part = 0;
-        u.first_pair = 0;
-        int at = 0;                                       // k-block of the tile to begin with
-        if (next_tile < tail_from) {
-            tile = next_tile;
-            next_tile += num_pairs;
-        } else {
-            if (tail_from == tiles || x >= tail_hi) return false;
-            if (WEIGHTS) {
-                const int y = tail_base + x;
-                int lo = 0, hi = p.groups;                // s_alt[lo] <= y < s_alt[hi]
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (s_alt[mid] <= y) lo = mid;
-                    else hi = mid;
-                }
-                const int len = max(1, (s_row[lo + 1] - s_row[lo] + GRP_BK - 1) / GRP_BK);
-                const int rel = (y - s_alt[lo]) / len;
-                tile = s_pre[lo] + rel;
-                at = y - s_alt[lo] - rel * len;
-            } else {
-                const int rel = x / p.kb_total;
-                tile = tail_from + rel;
-                at = x - rel * p.kb_total;
-            }
+        if (!mbar_wait(ufull_bar(unit_at), unit_phase, abort_flag)) {
+            if (lane == 0) give_up(0x800u + warp);
+            return false;
         }
-        if (WEIGHTS) {
-            const int per = p.tiles_i * p.tiles_j;
-            u.g = div_small(tile, per);
-            u.w = 0;
-            const int rel = tile - u.g * per;
-            const int ti = div_small(rel, p.tiles_j);
-            u.i0 = ti * GRP_TILE;
-            u.c0 = (rel - ti * p.tiles_j) * GRP_TILE;
-            u.cols = min(GRP_TILE, p.J - u.c0);
-            u.row0 = s_row[u.g];
-            u.rows = s_row[u.g + 1] - u.row0;
-            u.kbs = (u.rows + GRP_BK - 1) / GRP_BK;
-        } else {
-            int lo = 0, hi = p.groups;                    // s_pre[lo] <= tile < s_pre[hi]
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (s_pre[mid] <= tile) lo = mid;
-                else hi = mid;
-            }
-            u.g = lo;
-            u.w = LORA ? 0 : s_alt[lo];
-            const int rel = tile - s_pre[lo];
-            u.row0 = LORA ? 0 : s_row[lo];
-            u.rows = LORA ? p.rows : s_row[lo + 1] - u.row0;
-            // the group's rows cut into equal tiles; eight of them sweep the features together
-            const int nt = (u.rows + GRP_TILE - 1) / GRP_TILE;
-            const int jt = round32((u.rows + nt - 1) / nt);
-            const int per = 8 * p.tiles_i;
-            const int block = div_small(rel, per);
-            const int within = rel - block * per;
-            const int wide = min(8, nt - block * 8);
-            const int ti = div_small(within, wide);
-            const int tj = block * 8 + within - ti * wide;
-            u.i0 = ti * GRP_TILE;
-            u.c0 = u.row0 + tj * jt;
-            u.cols = min(jt, u.row0 + u.rows - u.c0);
-            u.kbs = p.kb_total;
-        }
-        u.jn = round32(u.cols);
-        u.kb0 = 0;
-        u.kb1 = u.kbs;
-        if (tile >= tail_from) {
-            const int len = max(1, u.kbs), start = x - at;            // the tile's place in the tail
-            u.kb0 = min(at, u.kbs);
-            u.kb1 = min(u.kbs, at + tail_hi - x);
-            x += min(len - at, tail_hi - x);
-            u.first_pair = start / share;
-            const int last_pair = (start + len - 1) / share;
-            u.parts = last_pair - u.first_pair + 1;
-            u.part = pair_id - u.first_pair;
-            u.cut = tile - tail_from;
-        }
-        return true;
+        u = s_unit[unit_at];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(uempty_bar(unit_at));
+        if (++unit_at == GRP_UNITS) { unit_at = 0; unit_phase ^= 1u; }
+        return u.some != 0;
+    };
+    // stages of the ring: as many as tiles of the schedule's width leave room for
+    int stage_bytes = 2 * GRP_A_BYTES, S = WS;
+    auto ring = [&]() {
+        if (WEIGHTS) return;
+        stage_bytes = GRP_A_BYTES + *s_width * 64;
+        S = min(MS, GRP_RING / stage_bytes);
     };
     // WEIGHTS: rows of the group in k-block kb
     auto rows_of = [&](const GroupedUnit& u, int kb) { return min(GRP_BK, u.rows - kb * GRP_BK); };
@@ -350,33 +161,206 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     // LORA: the requests' blocks follow the last k-block of a tile.  A request that has all of the tile's rows goes into
     // the tile's own accumulator.  Of the others each gets an accumulator of its own, of which the epilogue adds the
     // request's columns to the tile's sum: an adapter of infinities or NaN cannot reach another request's rows.
-    auto first_request = [&](const GroupedUnit& u) {
-        int lo = 0, hi = p.requests;                      // the first q with s_row[q + 1] > c0
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (s_row[mid + 1] > u.c0) hi = mid;
-            else lo = mid + 1;
-        }
-        return lo;
-    };
-    auto in_tile = [&](const GroupedUnit& u, int q) { return q < p.requests && s_row[q] < u.c0 + u.cols; };
     auto has_part = [&](int q) { return s_alt[q] >= 0 && s_row[q + 1] > s_row[q]; };
-    auto look = [&](const GroupedUnit& u) {
-        GroupedRequests r = {0, 0, 0};
-        if (!LORA || u.kb1 != u.kbs) return r;
-        r.first = first_request(u);
-        if (r.first >= p.requests) return r;
-        if (s_row[r.first] <= u.c0 && s_row[r.first + 1] >= u.c0 + u.cols) {
-            r.whole = s_alt[r.first] >= 0 ? p.rank_blocks : 0;
-            return r;
-        }
-        int n = 0;
-        for (int q = r.first + lane; in_tile(u, q); q += 32) n += has_part(q) ? 1 : 0;
-        r.parts = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(n)));
-        return r;
-    };
 
-    if (warp == 0) {
+    if (warp == GRP_THREADS / 32 - 1) {
+        // ------------------------------------------------ scheduler (both CTAs of a pair come to the same schedule)
+        // offsets that break their rule are clamped to the running maximum
+        bool bad = false;
+        for (int g = lane; g <= entries; g += 32) bad |= s_row[g] < (g ? s_row[g - 1] : 0) || s_row[g] > p.rows;
+        if (__any_sync(~0u, bad)) {
+            if (lane == 0) {
+                if (blockIdx.x == 0 && p.status) atomicCAS(p.status, 0u, 0x10000u);
+                int top = 0;
+                for (int g = 0; g <= entries; ++g) s_row[g] = top = max(top, min(s_row[g], p.rows));
+            }
+            __syncwarp();
+        }
+        auto rows_in = [&](int g) { return LORA ? p.rows : !WEIGHTS && s_alt[g] < 0 ? 0 : s_row[g + 1] - s_row[g]; };
+        // k-blocks of a tile of group g
+        auto length = [&](int g) { return WEIGHTS ? max(1, (rows_in(g) + GRP_BK - 1) / GRP_BK) : p.kb_total; };
+        int most = 0;
+        for (int g = lane; g < p.groups; g += 32) most = max(most, rows_in(g));
+        most = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(most)));
+        // Estimated time, in clocks, of n tiles of w rows: with whole tiles, and with the tail cut.  A k-block of a tile costs the tensor
+        // core 2 w, and never less than 400 (operand feed); a cut tile's parts are written to memory and read back at the
+        // end, about GRP_CUT_FIXED + GRP_CUT_ROW w.
+        const float fpairs = static_cast<float>(num_pairs), fk = static_cast<float>(p.kb_total);
+        auto estimate = [&](int n, int w, bool& cut) {
+            const float kb = static_cast<float>(max(400, 2 * w)), share = __fdividef(static_cast<float>(n), fpairs);
+            const float whole = ceilf(share) * fk * kb, even = fmaxf(share * fk, 4.0f) * kb + GRP_CUT_FIXED + GRP_CUT_ROW * w;
+            cut = p.partial && even < whole;
+            return cut ? even : whole;
+        };
+        int width = WEIGHTS ? GRP_TILE : max(32, min(GRP_TILE, round32(most)));
+        if (!WEIGHTS && width > 32) {
+            // the width of least estimated time: lane l looks at 32 (l + 1); narrower than the widest has to promise a tenth
+            const int w = min(32 * ((lane & 7) + 1), width);
+            int n = 0;
+            for (int g = lane >> 3; g < p.groups; g += 4) n += (rows_in(g) + w - 1) / w;
+            n += __shfl_xor_sync(~0u, n, 8);
+            n += __shfl_xor_sync(~0u, n, 16);
+            bool c;
+            const float t = estimate(n * p.tiles_i, w, c) * (w == width ? 0.9f : 1.0f);
+            // the smallest; of equals the widest: a time's upper bits, then the width
+            const unsigned won = __reduce_min_sync(~0u, (__float_as_uint(t) & ~15u) | (8u - static_cast<unsigned>(w >> 5)));
+            width = static_cast<int>(8u - (won & 15u)) << 5;
+        }
+        if (lane == 0) *s_width = width;
+        // tiles (and k-blocks) before each group
+        int tiles = 0, blocks = 0;
+        for (int base = 0; base <= p.groups; base += 32) {
+            const int g = base + lane;
+            int n = g >= p.groups ? 0 : WEIGHTS ? p.tiles_i * p.tiles_j : (rows_in(g) + width - 1) / width * p.tiles_i;
+            const int m = WEIGHTS && g < p.groups ? n * length(g) : 0;
+            int v = n, w = m;
+#pragma unroll 1
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(~0u, v, d), y = WEIGHTS ? __shfl_up_sync(~0u, w, d) : 0;
+                if (lane >= d) { v += o; w += y; }
+            }
+            if (g <= p.groups) {
+                s_pre[g] = tiles + v - n;
+                if (WEIGHTS) s_alt[g] = blocks + w - m;
+            }
+            tiles += __shfl_sync(~0u, v, 31);
+            if (WEIGHTS) blocks += __shfl_sync(~0u, w, 31);
+        }
+        __syncwarp();
+        // the last i of [0, n) with table[i] <= x
+        auto find = [&](const int* table, int n, int x) {
+            int lo = 0, hi = n;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (table[mid] <= x) lo = mid;
+                else hi = mid;
+            }
+            return lo;
+        };
+        // Whole tiles in turn, then the tail [tail_from, tiles): `tail_len` k-blocks from `tail_base` on, `share` of them to each pair.
+        // A tail of at most half as many tiles as pairs is cut into equal parts (a tile then counts `padded` k-blocks, a whole
+        // number of shares), so that no pair has parts of two tiles.
+        int tail_from = tiles, tail_len = 0, share = 1, tail_base = 0, padded = p.kb_total;
+        const int full_waves = tiles / num_pairs, from = full_waves > 1 ? (full_waves - 1) * num_pairs : 0;
+        if (p.partial && tiles > full_waves * num_pairs) {
+            bool cut = false;
+            if (WEIGHTS) {
+                const int g = find(s_pre, p.groups, from);
+                tail_base = s_alt[g] + (from - s_pre[g]) * length(g);
+                tail_len = blocks - tail_base;
+                share = max(4, (tail_len + num_pairs - 1) / num_pairs);
+                // (as for the rows)
+                const int rounds = (tiles - from + num_pairs - 1) / num_pairs;
+                const int whole = rounds > 1 ? rounds * (tail_len / (tiles - from)) : (most + GRP_BK - 1) / GRP_BK;
+                cut = (whole - share) * 512 > GRP_CUT_FIXED + GRP_CUT_ROW * min(p.J, GRP_TILE);
+            } else {
+                estimate(tiles, width, cut);
+                if (cut) {
+                    const int n = tiles - from;
+                    if (2 * n <= num_pairs) {
+                        const int parts = min(num_pairs / n, max(1, p.kb_total / 4));
+                        share = (p.kb_total + parts - 1) / parts;
+                        padded = (p.kb_total + share - 1) / share * share;
+                    } else {
+                        share = max(4, (n * p.kb_total + num_pairs - 1) / num_pairs);
+                    }
+                    tail_len = n * padded;
+                }
+            }
+            if (cut) tail_from = from;
+        }
+        int next_tile = pair_id, x = pair_id * share;     // this pair's next whole tile, its place in the tail
+        const int tail_hi = min(x + share, tail_len);
+        GroupedUnit u = {};
+        for (u.some = 1; u.some;) {
+            int tile = 0, at = 0;                         // `at`: the tile's k-block to begin with
+            if (next_tile < tail_from) {
+                tile = next_tile;
+                next_tile += num_pairs;
+                u.g = find(s_pre, p.groups, tile);
+            } else if (tail_from < tiles && x < tail_hi) {
+                if (WEIGHTS) {
+                    const int y = tail_base + x;
+                    u.g = find(s_alt, p.groups, y);
+                    const int rel = (y - s_alt[u.g]) / length(u.g);
+                    tile = s_pre[u.g] + rel;
+                    at = y - s_alt[u.g] - rel * length(u.g);
+                } else {
+                    const int rel = x / padded;
+                    tile = tail_from + rel;
+                    at = x - rel * padded;
+                    u.g = find(s_pre, p.groups, tile);
+                }
+            } else {
+                u.some = 0;
+            }
+            if (u.some) {
+                const int rel = tile - s_pre[u.g], len = length(u.g);
+                u.row0 = LORA ? 0 : s_row[u.g];
+                u.rows = rows_in(u.g);
+                int ti, kbs = len;
+                if (WEIGHTS) {
+                    ti = div_small(rel, p.tiles_j);
+                    u.c0 = (rel - ti * p.tiles_j) * GRP_TILE;
+                    u.cols = min(GRP_TILE, p.J - u.c0);
+                    kbs = u.rows > 0 ? len : 0;
+                } else {
+                    u.w = LORA ? 0 : s_alt[u.g];
+                    // the group's rows cut into equal tiles; eight of them sweep the features together
+                    const int nt = (u.rows + width - 1) / width;
+                    const int jt = round32((u.rows + nt - 1) / nt);
+                    const int block = div_small(rel, 8 * p.tiles_i);
+                    const int within = rel - block * 8 * p.tiles_i;
+                    const int wide = min(8, nt - block * 8);
+                    ti = div_small(within, wide);
+                    u.c0 = u.row0 + (block * 8 + within - ti * wide) * jt;
+                    u.cols = min(jt, u.row0 + u.rows - u.c0);
+                }
+                u.i0 = ti * GRP_TILE;
+                u.jn = round32(u.cols);
+                u.kb0 = 0;
+                u.kb1 = kbs;
+                u.parts = 1;
+                u.part = 0;
+                if (tile >= tail_from) {
+                    const int start = x - at, whole = WEIGHTS ? len : padded;    // the tile's place and extent in the tail
+                    u.kb0 = min(at, kbs);
+                    u.kb1 = min(kbs, at + tail_hi - x);
+                    x += min(whole - at, tail_hi - x);
+                    u.first_pair = start / share;
+                    u.parts = (start + len - 1) / share - u.first_pair + 1;
+                    u.part = pair_id - u.first_pair;
+                    u.cut = tile - tail_from;
+                }
+                if (LORA) {
+                    u.req_whole = u.req_parts = 0;
+                    if (u.kb1 == kbs) {
+                        // the first request with rows at or behind the tile's first
+                        u.req = s_row[0] > u.c0 ? 0 : find(s_row, p.requests + 1, u.c0);
+                        if (u.req < p.requests) {
+                            if (s_row[u.req] <= u.c0 && s_row[u.req + 1] >= u.c0 + u.cols) {
+                                u.req_whole = s_alt[u.req] >= 0 ? p.rank_blocks : 0;
+                            } else {
+                                int n = 0;
+                                for (int q = u.req + lane; q < p.requests && s_row[q] < u.c0 + u.cols; q += 32) n += has_part(q) ? 1 : 0;
+                                u.req_parts = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(n)));
+                            }
+                        }
+                    }
+                }
+            }
+            if (!mbar_wait(uempty_bar(unit_at), unit_phase ^ 1u, abort_flag)) {
+                if (lane == 0) give_up(0x900u);
+                break;
+            }
+            if (lane == 0) {
+                s_unit[unit_at] = u;
+                mbar_arrive(ufull_bar(unit_at));
+            }
+            __syncwarp();
+            if (++unit_at == GRP_UNITS) { unit_at = 0; unit_phase ^= 1u; }
+        }
+    } else if (warp == 0) {
         // ------------------------------------------------ TMA producer (both CTAs)
         const uint32_t lead_full0 = map_to_cta(full_bar(0), 0);
         const uint32_t elected = elect_one();
@@ -385,8 +369,8 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         uint32_t phase = 0;
         bool ok = true, waited = false;
         GroupedUnit u = {};
-        reset();
         while (ok && next(u)) {
+            ring();
             const int half = u.jn >> 1;
             const int i = u.i0 + static_cast<int>(rank) * 128;
             const int c = u.c0 + static_cast<int>(rank) * half;      // first column of this CTA's B operand
@@ -414,7 +398,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             };
             for (int kb = u.kb0; kb < u.kb1; ++kb) {
                 if (!acquire()) { ok = false; break; }
-                const uint32_t sa = smem_base + stage * GRP_STAGE, sb = sa + GRP_A_BYTES;
+                const uint32_t sa = smem_base + stage * stage_bytes, sb = sa + GRP_A_BYTES;
                 const uint32_t fb = full_bar(stage), lfb = lead_full0 + 8u * stage;
                 const uint32_t bytes = GRP_A_BYTES + b_bytes;
                 if (WEIGHTS) {
@@ -460,18 +444,17 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 }
                 advance();
             }
-            const GroupedRequests r = look(u);
-            if (LORA && ok && r.whole + r.parts > 0) {
+            if (LORA && ok && u.req_whole + u.req_parts > 0) {
                 // h16 comes from the kernel before this one
                 if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
                 waited = true;
                 const uint32_t bytes = (A_MN ? 8192u : GRP_A_BYTES) + b_bytes;
-                int q = r.first;
-                for (int n = 0; ok && n < max(1, r.parts); ++n, ++q) {
-                    while (!r.whole && !has_part(q)) ++q;
+                int q = u.req;
+                for (int n = 0; ok && n < max(1, u.req_parts); ++n, ++q) {
+                    while (!u.req_whole && !has_part(q)) ++q;
                     for (int rb = 0; rb < p.rank_blocks; ++rb) {
                         if (!acquire()) { ok = false; break; }
-                        const uint32_t sa = smem_base + stage * GRP_STAGE, sb = sa + GRP_A_BYTES, lfb = lead_full0 + 8u * stage;
+                        const uint32_t sa = smem_base + stage * stage_bytes, sb = sa + GRP_A_BYTES, lfb = lead_full0 + 8u * stage;
                         mbar_arrive_expect_tx_if(full_bar(stage), 2u * bytes, lead_elected);
                         if (A_MN) {
                             tma_load_3d_pair_if(sa, &maps.c, lfb, i, rb * 32, s_alt[q], elected);
@@ -509,11 +492,10 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 ok = false;
             }
             GroupedUnit u;
-            reset();
             while (ok && next(u)) {
+                ring();
                 const uint32_t idesc = p.idesc | (static_cast<uint32_t>(u.jn >> 3) << 17);
-                const GroupedRequests r = look(u);
-                const int base = u.kb1 - u.kb0, own = base + r.whole, blocks = own + r.parts * p.rank_blocks;
+                const int base = u.kb1 - u.kb0, own = base + u.req_whole, blocks = own + u.req_parts * p.rank_blocks;
                 const int chunk = p.chunk ? p.chunk : own;
                 int in_chunk = 0, rb = 0;
                 uint32_t d_tmem = 0;
@@ -565,7 +547,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         tail_phase ^= 1u << stage;
                     }
                     tc_fence_after_sync();
-                    const uint32_t a_lo = a_lo0 + stage * (GRP_STAGE >> 4), b_lo = b_lo0 + stage * (GRP_STAGE >> 4);
+                    const uint32_t a_lo = a_lo0 + stage * (stage_bytes >> 4), b_lo = b_lo0 + stage * (stage_bytes >> 4);
                     umma_pair_if<0>(d_tmem, a_lo, a_hi, b_lo, b_hi, idesc, accumulate, elected);
                     if (low_rank) {
                         // 32 ranks: leading parts of h16 in the first 64 bytes of a row, remainders in the second
@@ -593,7 +575,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         const int set = warp >= 6 ? 1 : 0;
         const int quarter = warp & 3;
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
-        const uint32_t staging = smem_base + S * GRP_STAGE + (warp - 2) * 4096;
+        const uint32_t staging = smem_base + GRP_RING + (warp - 2) * 4096;
         uint32_t parity = 0;
         int local = 0;
         bool ok = true, waited = false;
@@ -613,95 +595,120 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             if (lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(tempty_bar(local & 1), 0));
             ++local;
         };
-        // one 32 x 32 piece (columns c .. c + 31 of the tile, this warp's 32 features) of a tile or of one part of a cut one
+        // Cut tiles.  The slab of a pair: 0 for the tile its share begins in, 1 for the one it ends in.  A piece is 4 KB of it,
+        // lane after lane.
+        auto slab_of = [&](int part, int c) {
+            return reinterpret_cast<float4*>(p.partial) + (2 * (u.first_pair + part) + (part > 0 ? 0 : 1)) * (static_cast<size_t>(GRP_TILE / 4) * p.slab_cols) +
+                   ((rank * p.slab_cols + c) / 32 * 4 + quarter) * 256 + lane;
+        };
+        // One 32 x 32 piece of C (columns c .. c + 31 of the tile, this warp's 32 features): lane l has feature l, v[j] is row j.
+        // It goes through two 2 KB buffers of shared memory, from where a TMA store writes it (and clips what lies beyond C's
+        // edges); of a piece that ends inside the box, because the next row is another group's, lanes write 16 bytes each.
         auto deliver = [&](float (&v)[32], int c) {
-            if (u.parts > 1) {
-                const size_t slab = static_cast<size_t>(GRP_TILE) * p.slab_cols;
-                const size_t at = (rank * static_cast<size_t>(p.slab_cols) + c) * 128 + quarter * 32 + lane;
-                // the slab of a pair: 0 for the tile its share begins in, 1 for the one it ends in
-                auto slab_of = [&](int part) { return p.partial + (2 * (u.first_pair + part) + (part > 0 ? 0 : 1)) * slab + at; };
-                float* mine = slab_of(u.part);
+            const int n = min(32, u.cols - c), i0 = u.i0 + static_cast<int>(rank) * 128 + quarter * 32;
+            const size_t row0 = static_cast<size_t>(u.c0 + c);
+            if (MODE == GRP_ROWS && !OUT16 && p.h16) {
+                // X . A_a for the adapters: the scaled product as a leading 16-bit part and a remainder (none behind an infinite
+                // leading part); ranks beyond the last are zeros
+                const float scale = __ldg(p.scale + u.w);
+                const int pitch = p.rank_blocks * 64;
+                uint16_t* h = p.h16 + row0 * pitch + (i0 >> 5) * 64 + lane;
+                if (i0 < p.rank_blocks * 32) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) __stcg(mine + j * 128, v[j]);
-                __threadfence();
-                __syncwarp();
-                unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + (c >> 5);
-                unsigned int old = 0;
-                if (lane == 0) old = (atomicAdd(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
-                old = __shfl_sync(~0u, old, 0);
-                if (old != static_cast<unsigned>(u.parts) - 1u) return;
-                if (lane == 0) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
-                __threadfence();
-                const float* src = slab_of(0);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = __ldcg(src + j * 128);
-#pragma unroll 1
-                for (int s = 1; s < u.parts; ++s) {
-                    src = slab_of(s);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] += __ldcg(src + j * 128);
+                    for (int j = 0; j < 32; ++j) {
+                        const float x = i0 + lane < p.I ? v[j] * scale : 0.0f;
+                        const uint32_t hi = pack_half2(x, 0.0f, p.f16) & 0xFFFFu;
+                        const float lead = half_bits_to_f32(hi, p.f16);
+                        if (j < n) {
+                            h[0] = static_cast<uint16_t>(hi);
+                            h[32] = static_cast<uint16_t>(pack_half2(fabsf(lead) <= 3.4028235e38f ? x - lead : 0.0f, 0.0f, p.f16) & 0xFFFFu);
+                        }
+                        h += pitch;
+                    }
                 }
-            }
-            const int i = u.i0 + static_cast<int>(rank) * 128 + quarter * 32 + lane;
-            const int n = min(32, u.cols - c);
-            if (MODE == GRP_ROWS && p.h16) {
-                grouped_store_h(p, v, u.c0 + c, i, n, __ldg(p.scale + u.w));
                 return;
             }
-            const bool live = i < p.I;
+            const bool live = i0 + lane < p.I;
             if (MODE == GRP_ROWS && p.add) {
                 if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // `add` comes from the kernel before this one
                 waited = true;
-                const float* add = p.add + static_cast<size_t>(u.c0 + c) * p.I + i;
+                const float* add = p.add + row0 * p.I + i0 + lane;
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (live && j < n) v[j] += add[static_cast<size_t>(j) * p.I];
+                for (int j = 0; j < 32; ++j) {
+                    if (live && j < n) v[j] += __ldcg(add);
+                    add += p.I;
+                }
             }
-            const size_t base = (WEIGHTS ? static_cast<size_t>(u.g) * p.stride_c : 0) + static_cast<size_t>(u.c0 + c) * p.ldc + i;
-            if (p.beta && live) {
+            const size_t base = (WEIGHTS ? static_cast<size_t>(u.g) * p.stride_c : 0) + row0 * p.ldc + i0;
+            if (p.beta) {
+                const uint16_t* c16 = static_cast<const uint16_t*>(p.C) + base + lane;
+                const float* c32 = static_cast<const float*>(p.C) + base + lane;
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (j < n)
-                        v[j] += p.out16 ? half_bits_to_f32(static_cast<const uint16_t*>(p.C)[base + j * p.ldc], p.f16)
-                                        : static_cast<const float*>(p.C)[base + j * p.ldc];
+                for (int j = 0; j < 32; ++j) {
+                    if (live && j < n) v[j] += OUT16 ? half_bits_to_f32(*c16, F16) : *c32;
+                    c16 += p.ldc;
+                    c32 += p.ldc;
+                }
             }
-            if (!WEIGHTS && n < 32) {                     // the next row is another group's
-                grouped_store_rows(p, v, base, live ? n : 0);
-                return;
+            constexpr int ROWS = OUT16 ? 32 : 16, PITCH = 2048 / ROWS;    // of a buffer; 64 or 128 bytes
+#pragma unroll
+            for (int half = 0; half < 32; half += ROWS) {
+                if (half > 0 && half >= n) break;
+                const uint32_t box = staging + parity * 2048;
+                parity ^= 1u;
+                if (lane == 0) bulk_wait_read<1>();       // the store before the last has read this buffer
+                __syncwarp();
+                if (OUT16) {
+                    // a lane packs its feature of rows j and j + 1 and exchanges words with its neighbour: even lanes then hold row j of
+                    // features (l, l + 1), odd lanes row j + 1 of (l - 1, l): two rows of 64 bytes per store, no bank twice
+                    const uint32_t odd = lane & 1, pick = odd ? 0x3276u : 0x5410u, dst = box + odd * 64 + (lane >> 1) * 4;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const uint32_t w = pack_half2(v[2 * j], v[2 * j + 1], F16);
+                        const uint32_t got = __shfl_xor_sync(~0u, w, 1);
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + j * 128), "r"(__byte_perm(w, got, pick)) : "memory");
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < ROWS; ++j)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(box + lane * 4 + j * PITCH), "f"(v[half + j]) : "memory");
+                }
+                if (WEIGHTS || n >= half + ROWS) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) tma_store_3d(&maps.out, box, i0, static_cast<int>(row0) + half, WEIGHTS ? u.g : 0);
+                } else {
+                    __syncwarp();
+                    constexpr int LANES = PITCH / 16, WIDE = OUT16 ? 8 : 4;       // lanes of a row, elements of a lane
+                    const int f = (lane % LANES) * WIDE;
+                    if (i0 + f < p.I) {                   // (the number of features is a multiple of 8)
+#pragma unroll 1
+                        for (int r = lane / LANES; r < n - half; r += 32 / LANES) {
+                            uint32_t x[4];
+                            ld_shared_v4(box + r * PITCH + (lane % LANES) * 16, x);
+                            const size_t o = base + (half + r) * p.ldc + f;
+                            uint4* dst = OUT16 ? reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.C) + o) : reinterpret_cast<uint4*>(static_cast<float*>(p.C) + o);
+                            *dst = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (lane == 0) bulk_commit();             // (an empty group where nothing was stored: the buffers take turns)
             }
-            // two boxes of 16-bit, one of 32-bit results fit this warp's 4 KB: wait until the store of the one before has been read
-            const uint32_t box = staging + (p.out16 ? parity * 2048 : 0);
-            if (lane == 0) {
-                if (p.out16) bulk_wait_read<1>();
-                else bulk_wait_read<0>();
-            }
-            __syncwarp();
-            if (!p.out16) grouped_stage32(v, box);
-            else if (p.f16) grouped_stage16<true>(v, box);
-            else grouped_stage16<false>(v, box);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                tma_store_3d(&maps.out, box, i - lane, u.c0 + c, WEIGHTS ? u.g : 0);
-                bulk_commit();
-            }
-            parity ^= 1u;
         };
-        reset();
         while (ok && next(u)) {
-            const GroupedRequests r = look(u);
             // the accumulators that make up the tile: chunks of its own k-blocks, then one for each request with some of its rows
-            const int blocks = u.kb1 - u.kb0 + r.whole;
-            const int chunks = p.chunk ? max(1, (blocks + p.chunk - 1) / p.chunk) : 1, all = chunks + r.parts;
+            const int blocks = u.kb1 - u.kb0 + u.req_whole;
+            const int chunks = p.chunk ? max(1, (blocks + p.chunk - 1) / p.chunk) : 1, all = chunks + u.req_parts;
             if (!await()) break;
-            if (all > 1) {
+            if ((!OUT16 || LORA) && all > 1) {
                 // all but the last are added in registers, and the sum goes back to the last one's place
                 float sum[4][32];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) sum[q][j] = 0.0f;
-                int at = r.first;
+                int at = u.req;
 #pragma unroll 1
                 for (int n = 0; n < all; ++n) {
                     int lo = 0, hi = u.cols;              // the columns this accumulator has something for
@@ -749,26 +756,66 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 tmem_st_wait();
             }
             const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
-            // the parts of a cut tile begin with different columns, so that each finishes some of them last
             const int mine = (u.cols - set * 32 + 63) >> 6;
+            unsigned int last = (1u << max(0, mine)) - 1u;    // the pieces this warp stores
+            if (u.parts > 1) {
+                // this part's pieces go to its slab; then one count for each of them says which have all their parts
 #pragma unroll 1
-            for (int n = 0; n < mine; ++n) {
-                int q = n + u.part;
-                while (q >= mine) q -= mine;
-                const int c = set * 32 + q * 64;
-                uint32_t v[32];
-                float f[32];
-                tmem_ld_32x32(taddr + c, v);
-                tmem_ld_wait();
+                for (int q = 0; q < mine; ++q) {
+                    const int c = set * 32 + q * 64;
+                    uint32_t v[32];
+                    tmem_ld_32x32(taddr + c, v);
+                    tmem_ld_wait();
+                    float4* dst = slab_of(u.part, c);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
-                if (WEIGHTS && blocks == 0) {
+                    for (int j = 0; j < 8; ++j)
+                        __stcg(dst + j * 32, make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]),
+                                                         __uint_as_float(v[4 * j + 3])));
+                }
+                release();
+                __threadfence();
+                __syncwarp();
+                bool done = false;
+                if (lane < mine) {
+                    unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + set + 2 * lane;
+                    const unsigned int old = (atomicAdd(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
+                    done = old == static_cast<unsigned>(u.parts) - 1u;
+                    if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
+                }
+                last = __ballot_sync(~0u, done);
+                __threadfence();
+            }
+#pragma unroll 1
+            for (int q = 0; q < mine; ++q) {
+                if (!((last >> q) & 1u)) continue;
+                const int c = set * 32 + q * 64;
+                float f[32];
+                if (u.parts > 1) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) f[j] = 0.0f;
+#pragma unroll 2
+                    for (int s = 0; s < u.parts; ++s) {
+                        const float4* src = slab_of(s, c);
+                        float4 y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = __ldcg(src + j * 32);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[4 * j] += y[j].x, f[4 * j + 1] += y[j].y, f[4 * j + 2] += y[j].z, f[4 * j + 3] += y[j].w;
+                    }
+                } else {
+                    uint32_t v[32];
+                    tmem_ld_32x32(taddr + c, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                    if (WEIGHTS && blocks == 0) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[j] = 0.0f;
+                    }
                 }
                 deliver(f, c);
             }
-            release();
+            if (u.parts == 1) release();
         }
         if (lane == 0) bulk_wait_read<0>();               // the stores are done with this CTA's shared memory
         __syncwarp();
@@ -778,7 +825,6 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         int stage = 0;
         uint32_t raw_phase = 0;
         GroupedUnit u = {};
-        reset();
         while (next(u)) {
             if (u.kb1 <= u.kb0) continue;
             stage = (stage + u.kb1 - u.kb0 - 1) % S;
@@ -793,7 +839,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 const int first = rem * 8, last = ((rem + 15) & ~15) * 8;   // 16-byte pieces of a box's rows of 128 bytes
                 for (int b = 0; b < boxes; ++b)
                     for (int y = first + lane; y < last; y += 32)
-                        st_shared_v4(smem_base + stage * GRP_STAGE + b * 8192 + y * 16, 0u, 0u, 0u, 0u);
+                        st_shared_v4(smem_base + stage * stage_bytes + b * 8192 + y * 16, 0u, 0u, 0u, 0u);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster_cta_release(lead_tail0 + 8u * stage);

@@ -7,20 +7,22 @@
 
 namespace nk {
 
-constexpr int GRP_THREADS = 352;
+constexpr int GRP_THREADS = 384;
 constexpr int GRP_MAX_GROUPS = 1024;
-constexpr int GRP_STAGES = 5;
-constexpr int GRP_A_BYTES = 128 * 64 * 2;
-constexpr int GRP_STAGE = 2 * GRP_A_BYTES;             // 16 KB of features, up to 16 KB of rows, per CTA
+constexpr int GRP_A_BYTES = 128 * 64 * 2;              // a stage: 16 KB of features, up to 16 KB of rows, per CTA
+constexpr int GRP_RING = 5 * 2 * GRP_A_BYTES;          // five stages of 256 rows, more where the tiles are narrower
+constexpr int GRP_MAX_STAGES = 8;
 constexpr int GRP_BK = 64;
 constexpr int GRP_TILE = 256;                          // features of a tile, and the most rows of one
 constexpr int GRP_TABLE = 4 * (GRP_MAX_GROUPS + 1);    // bytes of a table by group
-constexpr int GRP_STAGING = 8 * 4096;                  // of the stores: 4 KB for each epilogue warp
-constexpr int GRP_SMEM = GRP_STAGES * GRP_STAGE + GRP_STAGING + 1024 + 3 * GRP_TABLE + 512;
+constexpr int GRP_STAGING = 8 * 4096;                  // of the stores: two buffers of 2 KB for each epilogue warp
+constexpr int GRP_CUT_FIXED = 5000, GRP_CUT_ROW = 24;  // estimated clocks of cutting a tile (see grouped.cuh)
+constexpr int GRP_SMEM = GRP_RING + GRP_STAGING + 1024 + 3 * GRP_TABLE + 1024;
 
-constexpr int GRP_CHUNK = 4;                           // k-blocks between additions to the FP32 sums of FP32 results
+constexpr int GRP_CHUNK = 8;                           // k-blocks between additions to the FP32 sums of FP32 results
 
 enum GroupedMode { GRP_ROWS = 0, GRP_WEIGHTS = 1, GRP_LORA = 2 };
+enum GroupedOut { GRP_OUT_F32 = 0, GRP_OUT_BF16 = 1, GRP_OUT_F16 = 2 };
 
 struct GroupedParams {
     int groups, rows;      // rows: extent of the row arrays; offsets are clamped to it
@@ -28,7 +30,7 @@ struct GroupedParams {
     int kb_total;          // ROWS, LORA: k-blocks of the contraction
     int tiles_i;           // ceil(I / 256)
     int tiles_j;           // WEIGHTS: ceil(J / 256)
-    int beta, out16, f16;
+    int beta, f16;
     int chunk;             // k-blocks summed in tensor memory before they are added to an FP32 sum in registers; 0: all
     uint32_t idesc;        // without the N field
     int a_slabs, b_slabs;  // MN-major operands of whole 64-feature slabs: a CTA's 128 features in one box
@@ -63,14 +65,24 @@ inline uint32_t grouped_idesc(bool a_mn, bool b_mn, bool f16) {
 struct GroupedMaps {
     CUtensorMap a;         // the features' operand: boxes of 128 features x 64 of k; with a_slabs one box, else two
     CUtensorMap b[4];      // the rows' operand in boxes of 16, 32, 64 and 128 rows; WEIGHTS: [0] 64 features, [1] 128 of them (b_slabs)
-    CUtensorMap out;       // C in boxes of 32 features x 32 rows (not with h16)
+    CUtensorMap out;       // C in boxes of 2 KB: 32 features x 32 (16-bit) or 16 (FP32) rows (not with h16)
     CUtensorMap c, h[4];   // LORA: the adapters' B, and h16 in boxes like b's
 };
 
-// (nk_grouped.cu)
-cudaError_t grouped_prepare(GroupedMode mode, bool a_mn);     // once per kernel and device: its shared memory
+// (grouped_rows.cu, grouped_weights.cu, grouped_lora.cu: the instantiations; nk_grouped.cu: the rest)
+typedef void (*GroupedFunction)(GroupedMaps, GroupedParams);
+GroupedFunction grouped_rows_kernel(bool a_mn, GroupedOut out);
+GroupedFunction grouped_weights_kernel(GroupedOut out);
+GroupedFunction grouped_lora_kernel(bool a_mn, GroupedOut out);
+struct GroupedKernel {     // one instantiation
+    GroupedMode mode;
+    bool a_mn;
+    GroupedOut out;
+};
+inline GroupedOut grouped_out(bool out16, bool f16) { return !out16 ? GRP_OUT_F32 : f16 ? GRP_OUT_F16 : GRP_OUT_BF16; }
+cudaError_t grouped_prepare(const GroupedKernel& k);     // once per kernel and device: its shared memory
 // `after_start`: the launch may begin while the kernel before it in the stream still runs (which has to allow it)
-cudaError_t grouped_launch(GroupedMode mode, bool a_mn, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p,
+cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p,
                            bool after_start);
 // Arrival counters of the tiles cut along k, zero between launches (the last arriver clears its own).  A plan holds a
 // slot of a static table from create to destroy; where none is free (null) it cuts no tile.

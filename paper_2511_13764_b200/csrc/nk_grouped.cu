@@ -1,6 +1,6 @@
 // Host side of nk_grouped: descriptor validation, TMA maps, the launch.
 #include "rows_host.cuh"
-#include "grouped.cuh"
+#include "grouped_launch.cuh"
 
 namespace nk {
 
@@ -31,17 +31,13 @@ void give_split_slot(int slot) {
     g_split_taken[slot] = false;
 }
 
-typedef void (*GroupedKernel)(GroupedMaps, GroupedParams);
-static GroupedKernel grouped_kernel_for(GroupedMode mode, bool a_mn) {
-    if (mode == GRP_WEIGHTS) return grouped_kernel<GRP_WEIGHTS, true>;
-    if (mode == GRP_LORA) return a_mn ? grouped_kernel<GRP_LORA, true> : grouped_kernel<GRP_LORA, false>;
-    return a_mn ? grouped_kernel<GRP_ROWS, true> : grouped_kernel<GRP_ROWS, false>;
+static GroupedFunction function_of(const GroupedKernel& k) {
+    return k.mode == GRP_WEIGHTS ? grouped_weights_kernel(k.out) : k.mode == GRP_LORA ? grouped_lora_kernel(k.a_mn, k.out) : grouped_rows_kernel(k.a_mn, k.out);
 }
-cudaError_t grouped_prepare(GroupedMode mode, bool a_mn) {
-    return cudaFuncSetAttribute(grouped_kernel_for(mode, a_mn), cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM);
+cudaError_t grouped_prepare(const GroupedKernel& k) {
+    return cudaFuncSetAttribute(function_of(k), cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM);
 }
-cudaError_t grouped_launch(GroupedMode mode, bool a_mn, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p,
-                           bool after_start) {
+cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p, bool after_start) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * pairs);
     cfg.blockDim = dim3(GRP_THREADS);
@@ -52,7 +48,7 @@ cudaError_t grouped_launch(GroupedMode mode, bool a_mn, int pairs, cudaStream_t 
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = after_start ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, grouped_kernel_for(mode, a_mn), maps, p);
+    return cudaLaunchKernelEx(&cfg, function_of(k), maps, p);
 }
 
 }  // namespace nk
@@ -60,6 +56,7 @@ cudaError_t grouped_launch(GroupedMode mode, bool a_mn, int pairs, cudaStream_t 
 struct nk_grouped_s : nk::PlanBase {
     nk_grouped_desc_t d;          // strides filled in
     int pairs;                    // CTA pairs that fit the device
+    nk::GroupedKernel kernel;
     int split_slot;
     unsigned int* counters;
     nk::GroupedMaps maps;
@@ -97,8 +94,8 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
     if (d.stride_g == 0) d.stride_g = item;
     if (d.stride_g < item) return NK_ERR_INVALID_ARG;                               // items overlap
     // TMA strides are below 2^40 bytes; unit numbers stay below 2^24
-    if (d.lda >= (1ll << 38) || d.ldb >= (1ll << 38) || d.stride_g >= (1ll << 38)) return NK_ERR_UNSUPPORTED;
-    const int64_t tiles = weights ? d.groups * div_up(d.N, 256) * div_up(d.K, 256) : (d.rows / 256 + d.groups) * div_up(d.N, 256);
+    if (d.lda >= (1ll << 37) || d.ldb >= (1ll << 37) || d.ldc >= (1ll << 37) || d.stride_g >= (1ll << 37)) return NK_ERR_UNSUPPORTED;
+    const int64_t tiles = weights ? d.groups * div_up(d.N, 256) * div_up(d.K, 256) : (d.rows / 32 + d.groups) * div_up(d.N, 256);
     if (tiles >= (1 << 24)) return NK_ERR_UNSUPPORTED;
     if (weights && (d.rows / 64 + d.groups) * div_up(d.N, 256) * div_up(d.K, 256) >= (1ll << 31)) return NK_ERR_UNSUPPORTED;   // k-blocks of all tiles
 
@@ -112,11 +109,12 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     DeviceGuard guard(d.device);
     if (!encode_tiled()) { delete p; return NK_ERR_CUDA; }
-    if (grouped_prepare(weights ? GRP_WEIGHTS : GRP_ROWS, weights || d.layout_b == NK_ROW_MAJOR) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
+    p->kernel = {weights ? GRP_WEIGHTS : GRP_ROWS, weights || d.layout_b == NK_ROW_MAJOR, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
+    if (grouped_prepare(p->kernel) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
     p->slab_cols = grouped_slab_cols(weights ? d.K : d.rows);
     p->split_slot = take_split_slot(&p->counters);
-    snprintf(p->name, sizeof(p->name), "grouped_%s_256x256x64_s%d_pair", weights ? "weights" : d.layout_b == NK_TRANSPOSED ? "rows_t" : "rows", GRP_STAGES);
+    snprintf(p->name, sizeof(p->name), "grouped_%s_256x256x64_pair", weights ? "weights" : d.layout_b == NK_TRANSPOSED ? "rows_t" : "rows");
     *out = p;
     return NK_OK;
 }
@@ -163,7 +161,7 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
         }
         p->cached_a = A;
         p->cached_b = B;
-        p->cached_c = C;
+        p->cached_c = C;               // (C is never null: the maps are valid)
     }
     GroupedParams g = {};
     g.groups = static_cast<int>(d.groups);
@@ -174,7 +172,6 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     g.tiles_i = static_cast<int>(div_up(d.N, GRP_TILE));
     g.tiles_j = static_cast<int>(div_up(d.K, GRP_TILE));
     g.beta = d.beta;
-    g.out16 = d.out_dtype != NK_F32;
     g.f16 = d.in_dtype == NK_F16;
     g.idesc = grouped_idesc(weights || d.layout_b == NK_ROW_MAJOR, weights, g.f16);
     g.offsets = offsets;
@@ -187,9 +184,8 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     g.slab_cols = p->slab_cols;
     g.a_slabs = d.N % 64 == 0;
     g.b_slabs = d.K % 64 == 0;
-    g.chunk = g.out16 ? 0 : GRP_CHUNK;
-    const cudaError_t e = grouped_launch(weights ? GRP_WEIGHTS : GRP_ROWS, weights || d.layout_b == NK_ROW_MAJOR, p->pairs,
-                                         static_cast<cudaStream_t>(cuda_stream), p->maps, g, false);
+    g.chunk = d.out_dtype == NK_F32 ? GRP_CHUNK : 0;
+    const cudaError_t e = grouped_launch(p->kernel, p->pairs, static_cast<cudaStream_t>(cuda_stream), p->maps, g, false);
     return e == cudaSuccess ? NK_OK : p->cuda("grouped launch", e);
 }
 

@@ -10,6 +10,7 @@ struct nk_lora_s : nk::PlanBase {
     int split_slot[2];            // of X . A and of the projection: the two overlap
     unsigned int* counters[2];
     size_t part_bytes[2], side_bytes;   // partial sums of the two; FP32 contributions or X . A
+    nk::GroupedKernel projection, shrinking;
     nk::GroupedMaps maps, shrink; // of the projection and of X . A
     const void *cached_x, *cached_w, *cached_a, *cached_b, *cached_ws, *cached_y;
     char name[64];
@@ -48,8 +49,8 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     if (d.ldw == 0) d.ldw = w_cols;
     if (d.ldy == 0) d.ldy = d.N;
     if (d.ldx < d.K || d.ldw < w_cols || d.ldy < d.N) return NK_ERR_INVALID_ARG;
-    if (d.ldx >= (1ll << 38) || d.ldw >= (1ll << 38)) return NK_ERR_UNSUPPORTED;
-    if ((d.rows / 256 + 1) * div_up(d.N, 256) >= (1 << 24)) return NK_ERR_UNSUPPORTED;
+    if (d.ldx >= (1ll << 37) || d.ldw >= (1ll << 37) || d.ldy >= (1ll << 37)) return NK_ERR_UNSUPPORTED;
+    if ((d.rows / 32 + 1) * div_up(d.N, 256) >= (1 << 24)) return NK_ERR_UNSUPPORTED;
     int sms = 0;
     nk_status_t s = usable_device(d.device, &sms);
     if (s != NK_OK) return s;
@@ -61,9 +62,11 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     DeviceGuard guard(d.device);
     const bool row = d.layout == NK_ROW_MAJOR;
     p->few = d.rows <= LORA_FEW_ROWS * d.requests;
-    cudaError_t e = grouped_prepare(GRP_ROWS, row);
+    p->projection = {p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
+    p->shrinking = {GRP_ROWS, row, GRP_OUT_F32};
+    cudaError_t e = grouped_prepare(p->projection);
     if (e == cudaSuccess) e = p->few ? cudaFuncSetAttribute(lora_delta_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LORA_SMEM)
-                                     : grouped_prepare(GRP_LORA, row);
+                                     : grouped_prepare(p->shrinking);
     if (e != cudaSuccess || !encode_tiled()) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
     p->rank_blocks = static_cast<int>(div_up(d.rank, 32));
@@ -173,7 +176,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
         h.h16 = reinterpret_cast<uint16_t*>(ws);
         h.partial = partial[0];
         h.counter = p->counters[0];
-        e = grouped_launch(GRP_ROWS, row, p->pairs, st, p->shrink, h, false);
+        e = grouped_launch(p->shrinking, p->pairs, st, p->shrink, h, false);
         if (e != cudaSuccess) return p->cuda("lora shrink launch", e);
         g.requests = h.groups;
         g.request_offsets = offsets;
@@ -184,14 +187,13 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     g.I = static_cast<int>(d.N);
     g.tiles_i = static_cast<int>(div_up(d.N, GRP_TILE));
     g.a_slabs = d.N % 64 == 0;
-    g.out16 = d.out_dtype != NK_F32;
-    g.chunk = g.out16 ? 0 : GRP_CHUNK;
+    g.chunk = d.out_dtype == NK_F32 ? GRP_CHUNK : 0;
     g.C = Y;
     g.ldc = d.ldy;
     g.partial = partial[1];
     g.counter = p->counters[1];
     // the projection starts while the adapters' kernel runs, and waits for it where it needs its result
-    e = grouped_launch(p->few ? GRP_ROWS : GRP_LORA, row, p->pairs, st, p->maps, g, true);
+    e = grouped_launch(p->projection, p->pairs, st, p->maps, g, true);
     return e == cudaSuccess ? NK_OK : p->cuda("lora projection launch", e);
 }
 

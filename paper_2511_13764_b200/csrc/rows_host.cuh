@@ -113,12 +113,12 @@ static inline bool encode_slabs(CUtensorMap* m, const void* base, bool f16, int6
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// C as boxes of 32 x 32 elements, rows of a box behind one another.
+// C as boxes of 2 KB: 32 elements by 32 (16-bit) or 16 (FP32) rows, rows of a box behind one another.
 static inline bool encode_out(CUtensorMap* m, void* base, int dtype, int64_t inner, int64_t mid, int64_t outer, int64_t ld, int64_t stride) {
     const int64_t esz = dtype == NK_F32 ? 4 : 2;
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(mid), static_cast<cuuint64_t>(outer)};
     cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * esz), static_cast<cuuint64_t>((outer > 1 ? stride : ld) * esz)};
-    cuuint32_t box[3] = {32, 32, 1};
+    cuuint32_t box[3] = {32, dtype == NK_F32 ? 16u : 32u, 1};
     cuuint32_t es[3] = {1, 1, 1};
     return encode_tiled()(m, dtype == NK_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == NK_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
                           3, base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,

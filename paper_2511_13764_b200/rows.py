@@ -71,7 +71,7 @@ def exported_symbols():
 def _bytes(workspace, workspace_bytes):
     if workspace_bytes is not None:
         return workspace_bytes
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return 0 if workspace is None else workspace.nbytes
 
 
 class _Handle:
@@ -82,6 +82,7 @@ class _Handle:
         self.desc = desc
         self._h = ctypes.c_void_p()
         self._check(getattr(lib(), f"nk_{self.family}_create")(ctypes.byref(desc), ctypes.byref(self._h)))
+        self._raw = self._h.value
 
     def _check(self, status):
         if status != 0:
@@ -107,6 +108,7 @@ class _Handle:
         if self._h:
             getattr(lib(), f"nk_{self.family}_destroy")(self._h)
             self._h = ctypes.c_void_p()
+            self._raw = None
 
     def __del__(self):
         try:
@@ -127,7 +129,7 @@ class GroupedPlan(_Handle):
 
     def run(self, A, B, C, offsets, workspace=None, workspace_bytes=None, stream=None):
         """offsets: device INT32 [groups + 1]; never read by the host."""
-        status = lib().nk_grouped_run(self._h, _ptr(A), _ptr(B), _ptr(C), _ptr(offsets), _ptr(workspace),
+        status = _lib.nk_grouped_run(self._raw, _ptr(A), _ptr(B), _ptr(C), _ptr(offsets), _ptr(workspace),
                                       _bytes(workspace, workspace_bytes), stream)
         if status:
             self._check(status)
@@ -143,29 +145,29 @@ class RoutePlan(_Handle):
                                renormalise, device))
 
     def run(self, logits, gates, experts, offsets, slots, workspace=None, workspace_bytes=None, stream=None):
-        status = lib().nk_route_run(self._h, _ptr(logits), _ptr(gates), _ptr(experts), _ptr(offsets), _ptr(slots),
+        status = _lib.nk_route_run(self._raw, _ptr(logits), _ptr(gates), _ptr(experts), _ptr(offsets), _ptr(slots),
                                     _ptr(workspace), _bytes(workspace, workspace_bytes), stream)
         if status:
             self._check(status)
 
     def backward(self, logits, experts, dgates, dlogits, stream=None):
-        status = lib().nk_route_backward(self._h, _ptr(logits), _ptr(experts), _ptr(dgates), _ptr(dlogits), stream)
+        status = _lib.nk_route_backward(self._raw, _ptr(logits), _ptr(experts), _ptr(dgates), _ptr(dlogits), stream)
         if status:
             self._check(status)
 
     def dispatch(self, X, slots, Xs, stream=None):
-        status = lib().nk_route_dispatch(self._h, _ptr(X), _ptr(slots), _ptr(Xs), stream)
+        status = _lib.nk_route_dispatch(self._raw, _ptr(X), _ptr(slots), _ptr(Xs), stream)
         if status:
             self._check(status)
 
     def combine(self, Ys, slots, Y, gates=None, stream=None):
         """gates None: plain sum, the gradient of dispatch."""
-        status = lib().nk_route_combine(self._h, _ptr(Ys), _ptr(slots), _ptr(gates), _ptr(Y), stream)
+        status = _lib.nk_route_combine(self._raw, _ptr(Ys), _ptr(slots), _ptr(gates), _ptr(Y), stream)
         if status:
             self._check(status)
 
     def combine_backward(self, dY, Ys, slots, gates, dYs, dgates, stream=None):
-        status = lib().nk_route_combine_backward(self._h, _ptr(dY), _ptr(Ys), _ptr(slots), _ptr(gates), _ptr(dYs),
+        status = _lib.nk_route_combine_backward(self._raw, _ptr(dY), _ptr(Ys), _ptr(slots), _ptr(gates), _ptr(dYs),
                                                  _ptr(dgates), stream)
         if status:
             self._check(status)
@@ -181,7 +183,7 @@ class LoraPlan(_Handle):
 
     def run(self, X, W, A, B, scale, offsets, adapter, Y, workspace=None, workspace_bytes=None, stream=None):
         """offsets (INT32 [requests + 1]), adapter (INT32 [requests]) and scale (FP32 [adapters]) are on the device."""
-        status = lib().nk_lora_run(self._h, _ptr(X), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(offsets), _ptr(adapter),
+        status = _lib.nk_lora_run(self._raw, _ptr(X), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(offsets), _ptr(adapter),
                                    _ptr(Y), _ptr(workspace), _bytes(workspace, workspace_bytes), stream)
         if status:
             self._check(status)
