@@ -46,17 +46,30 @@ struct __align__(16) GroupedUnit {
     int row0, rows;        // the group's rows
     int cut, parts, part, first_pair;   // a cut tile: its number among the tail's tiles, its parts, this one, the pair of part 0
     int req, req_whole, req_parts;      // LORA: the first request of the tile, k-blocks of the one with all of its rows, how many have some of them
-    int pad[2];
+    int shorts;            // LORA: short requests with rows in the tile
+    int pad;
 };
 constexpr int GRP_UNITS = 4;            // of them on the way
+
+// the last i of [0, n) with table[i] <= x (0 if there is none)
+__device__ __forceinline__ int find_last(const int* table, int n, int x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (table[mid] <= x) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
 
 __device__ __forceinline__ int round32(int x) { return (x + 31) & ~31; }
 
 // MODE: GroupedMode.  A_MN: the features' operand is MN-major (row-major weights [K][I], or rows [t][I]), else
 // K-major (weights [I][K]).
-// OUT: type of C (GroupedOut).
+// OUT: type of C (GroupedOut).  (The bound of 512 threads keeps the 16-bit ROWS kernels at 128 registers, which leaves an
+// SM room for a block of the adapters' kernel beside them.)
 template <int MODE, bool A_MN, int OUT>
-__global__ void __launch_bounds__(GRP_THREADS, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(MODE == GRP_ROWS && OUT != GRP_OUT_F32 ? 512 : GRP_THREADS, 1) __cluster_dims__(2, 1, 1)
 grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__ GroupedParams p) {
     constexpr bool WEIGHTS = MODE == GRP_WEIGHTS, LORA = MODE == GRP_LORA;
     constexpr bool OUT16 = OUT != GRP_OUT_F32, F16 = OUT == GRP_OUT_F16;
@@ -97,14 +110,6 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     // offsets -> shared memory (LORA: the requests'; its one group is all the rows)
     const int* offsets = LORA ? p.request_offsets : p.offsets;
     const int entries = LORA ? p.requests : p.groups;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    for (int g = threadIdx.x; g <= entries; g += GRP_THREADS) {
-        s_row[g] = offsets ? offsets[g] : g == 0 ? 0 : p.rows;
-        if (!WEIGHTS) {
-            const int a = p.index && g < entries ? p.index[g] : g;
-            s_alt[g] = p.index && (a < 0 || a >= p.index_max) ? -1 : a;
-        }
-    }
     if (warp == 0) {
         for (int n = lane; n < NB; n += 32) {
             // tempty: one arrival per epilogue warp of both CTAs; tail: one per CTA; uempty: producer, epilogue warps, the leader's
@@ -127,8 +132,18 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         tmem_relinquish_pair();
     }
     tc_fence_before_sync();
-    __syncthreads();
     cluster_arrive();
+    // up to here the launch may have run beside the end of the one before it in the stream
+    if (!p.late) launch_wait();
+    launch_next();
+    for (int g = threadIdx.x; g <= entries; g += GRP_THREADS) {
+        s_row[g] = offsets ? offsets[g] : g == 0 ? 0 : p.rows;
+        if (!WEIGHTS) {
+            const int a = p.index && g < entries ? p.index[g] : g;
+            s_alt[g] = p.index && (a < 0 || a >= p.index_max) ? -1 : a;
+        }
+    }
+    __syncthreads();
     cluster_wait();          // the barriers of both CTAs are initialised
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
@@ -160,8 +175,10 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
 
     // LORA: the requests' blocks follow the last k-block of a tile.  A request that has all of the tile's rows goes into
     // the tile's own accumulator.  Of the others each gets an accumulator of its own, of which the epilogue adds the
-    // request's columns to the tile's sum: an adapter of infinities or NaN cannot reach another request's rows.
-    auto has_part = [&](int q) { return s_alt[q] >= 0 && s_row[q + 1] > s_row[q]; };
+    // request's columns to the tile's sum: an adapter of infinities or NaN cannot reach another request's rows.  Requests
+    // of p.min_rows rows or fewer are not worth an accumulator: theirs comes in FP32 from the kernel before (`add`).
+    auto has_part = [&](int q) { return s_alt[q] >= 0 && s_row[q + 1] - s_row[q] > p.min_rows; };
+    auto is_short = [&](int q) { return s_alt[q] >= 0 && s_row[q + 1] > s_row[q] && s_row[q + 1] - s_row[q] <= p.min_rows; };
 
     if (warp == GRP_THREADS / 32 - 1) {
         // ------------------------------------------------ scheduler (both CTAs of a pair come to the same schedule)
@@ -176,32 +193,39 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             }
             __syncwarp();
         }
-        auto rows_in = [&](int g) { return LORA ? p.rows : !WEIGHTS && s_alt[g] < 0 ? 0 : s_row[g + 1] - s_row[g]; };
+        auto rows_in = [&](int g) {
+            if (LORA) return p.rows;
+            const int rows = s_row[g + 1] - s_row[g];
+            return !WEIGHTS && (s_alt[g] < 0 || rows <= p.min_rows) ? 0 : rows;
+        };
         // k-blocks of a tile of group g
         auto length = [&](int g) { return WEIGHTS ? max(1, (rows_in(g) + GRP_BK - 1) / GRP_BK) : p.kb_total; };
         int most = 0;
         for (int g = lane; g < p.groups; g += 32) most = max(most, rows_in(g));
         most = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(most)));
-        // Estimated time, in clocks, of n tiles of w rows: with whole tiles, and with the tail cut.  A k-block of a tile costs the tensor
-        // core 2 w, and never less than 400 (operand feed); a cut tile's parts are written to memory and read back at the
-        // end, about GRP_CUT_FIXED + GRP_CUT_ROW w.
-        const float fpairs = static_cast<float>(num_pairs), fk = static_cast<float>(p.kb_total);
-        auto estimate = [&](int n, int w, bool& cut) {
-            const float kb = static_cast<float>(max(400, 2 * w)), share = __fdividef(static_cast<float>(n), fpairs);
-            const float whole = ceilf(share) * fk * kb, even = fmaxf(share * fk, 4.0f) * kb + GRP_CUT_FIXED + GRP_CUT_ROW * w;
-            cut = p.partial && even < whole;
-            return cut ? even : whole;
+        // Estimated time, in clocks, of n tiles of w rows, and into how many parts (1: none) the tiles of the last, partial wave are cut:
+        // equal parts, so that no pair has parts of two tiles, where they fill at most half a wave.  A k-block of a tile costs about
+        // GRP_BLOCK + w / 8 whatever its width (operand feed; the tensor core alone would need 2 w); parts are written to memory
+        // and read back at the end, GRP_CUT_FIXED + GRP_CUT_ROW w if all pairs have one.
+        auto estimate = [&](int n, int w, int& parts) {
+            const int waves = n / num_pairs, rest = n - waves * num_pairs;
+            const float kb = GRP_BLOCK + w * 0.125f, k = static_cast<float>(p.kb_total), whole = (waves + (rest ? 1 : 0)) * k * kb;
+            parts = rest && p.partial ? min(num_pairs / rest, max(1, p.kb_total / 4)) : 1;
+            if (parts < 2) { parts = 1; return whole; }
+            const float cut = (waves * k + (p.kb_total + parts - 1) / parts) * kb + GRP_CUT_FIXED + __fdividef(GRP_CUT_ROW * w * rest * parts, static_cast<float>(num_pairs));
+            if (cut < whole) return cut;
+            parts = 1;
+            return whole;
         };
-        int width = WEIGHTS ? GRP_TILE : max(32, min(GRP_TILE, round32(most)));
+        int width = WEIGHTS ? GRP_TILE : max(32, min(GRP_TILE, round32(most))), parts = 1;
         if (!WEIGHTS && width > 32) {
-            // the width of least estimated time: lane l looks at 32 (l + 1); narrower than the widest has to promise a tenth
+            // the width of least estimated time: lane l looks at 32 (l + 1)
             const int w = min(32 * ((lane & 7) + 1), width);
             int n = 0;
             for (int g = lane >> 3; g < p.groups; g += 4) n += (rows_in(g) + w - 1) / w;
             n += __shfl_xor_sync(~0u, n, 8);
             n += __shfl_xor_sync(~0u, n, 16);
-            bool c;
-            const float t = estimate(n * p.tiles_i, w, c) * (w == width ? 0.9f : 1.0f);
+            const float t = estimate(n * p.tiles_i, w, parts);
             // the smallest; of equals the widest: a time's upper bits, then the width
             const unsigned won = __reduce_min_sync(~0u, (__float_as_uint(t) & ~15u) | (8u - static_cast<unsigned>(w >> 5)));
             width = static_cast<int>(8u - (won & 15u)) << 5;
@@ -219,55 +243,53 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 const int o = __shfl_up_sync(~0u, v, d), y = WEIGHTS ? __shfl_up_sync(~0u, w, d) : 0;
                 if (lane >= d) { v += o; w += y; }
             }
-            if (g <= p.groups) {
+            if (!LORA && g <= p.groups) {
                 s_pre[g] = tiles + v - n;
                 if (WEIGHTS) s_alt[g] = blocks + w - m;
             }
             tiles += __shfl_sync(~0u, v, 31);
             if (WEIGHTS) blocks += __shfl_sync(~0u, w, 31);
         }
-        __syncwarp();
-        // the last i of [0, n) with table[i] <= x
-        auto find = [&](const int* table, int n, int x) {
-            int lo = 0, hi = n;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (table[mid] <= x) lo = mid;
-                else hi = mid;
+        if (LORA) {
+            // rows of short requests before each request
+            int sum = 0;
+            for (int base = 0; base < p.requests; base += 32) {
+                const int q = base + lane, n = q < p.requests && is_short(q) ? s_row[q + 1] - s_row[q] : 0;
+                int v = n;
+#pragma unroll 1
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int o = __shfl_up_sync(~0u, v, d);
+                    if (lane >= d) v += o;
+                }
+                if (q < p.requests) s_pre[q] = sum + v - n;
+                sum += __shfl_sync(~0u, v, 31);
             }
-            return lo;
-        };
-        // Whole tiles in turn, then the tail [tail_from, tiles): `tail_len` k-blocks from `tail_base` on, `share` of them to each pair.
-        // A tail of at most half as many tiles as pairs is cut into equal parts (a tile then counts `padded` k-blocks, a whole
-        // number of shares), so that no pair has parts of two tiles.
+        }
+        __syncwarp();
+        // Whole tiles in turn, then the tail [tail_from, tiles), the last, partial wave: `tail_len` k-blocks from `tail_base` on, `share` of them
+        // to each pair.  (ROWS, LORA: a tile counts `padded` k-blocks there, a whole number of shares.)
+        const int full_waves = tiles / num_pairs, from = full_waves * num_pairs;
         int tail_from = tiles, tail_len = 0, share = 1, tail_base = 0, padded = p.kb_total;
-        const int full_waves = tiles / num_pairs, from = full_waves > 1 ? (full_waves - 1) * num_pairs : 0;
-        if (p.partial && tiles > full_waves * num_pairs) {
-            bool cut = false;
-            if (WEIGHTS) {
-                const int g = find(s_pre, p.groups, from);
+        if (WEIGHTS) {
+            if (p.partial && tiles > from) {
+                // tiles of different lengths: the wave's k-blocks laid end to end and shared out evenly (as long as the longest, uncut)
+                const int g = find_last(s_pre, p.groups, from);
                 tail_base = s_alt[g] + (from - s_pre[g]) * length(g);
                 tail_len = blocks - tail_base;
                 share = max(4, (tail_len + num_pairs - 1) / num_pairs);
-                // (as for the rows)
-                const int rounds = (tiles - from + num_pairs - 1) / num_pairs;
-                const int whole = rounds > 1 ? rounds * (tail_len / (tiles - from)) : (most + GRP_BK - 1) / GRP_BK;
-                cut = (whole - share) * 512 > GRP_CUT_FIXED + GRP_CUT_ROW * min(p.J, GRP_TILE);
-            } else {
-                estimate(tiles, width, cut);
-                if (cut) {
-                    const int n = tiles - from;
-                    if (2 * n <= num_pairs) {
-                        const int parts = min(num_pairs / n, max(1, p.kb_total / 4));
-                        share = (p.kb_total + parts - 1) / parts;
-                        padded = (p.kb_total + share - 1) / share * share;
-                    } else {
-                        share = max(4, (n * p.kb_total + num_pairs - 1) / num_pairs);
-                    }
-                    tail_len = n * padded;
-                }
+                int longest = 0;
+                for (int h = g + lane; h < p.groups; h += 32) longest = max(longest, length(h));
+                longest = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(longest)));
+                if ((longest - share) * (GRP_BLOCK + GRP_TILE / 8) > GRP_CUT_FIXED + GRP_CUT_ROW * min(p.J, GRP_TILE)) tail_from = from;
             }
-            if (cut) tail_from = from;
+        } else {
+            estimate(tiles, width, parts);
+            if (parts > 1) {
+                tail_from = from;
+                share = (p.kb_total + parts - 1) / parts;
+                padded = (p.kb_total + share - 1) / share * share;
+                tail_len = (tiles - from) * padded;
+            }
         }
         int next_tile = pair_id, x = pair_id * share;     // this pair's next whole tile, its place in the tail
         const int tail_hi = min(x + share, tail_len);
@@ -277,11 +299,11 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             if (next_tile < tail_from) {
                 tile = next_tile;
                 next_tile += num_pairs;
-                u.g = find(s_pre, p.groups, tile);
+                u.g = LORA ? 0 : find_last(s_pre, p.groups, tile);
             } else if (tail_from < tiles && x < tail_hi) {
                 if (WEIGHTS) {
                     const int y = tail_base + x;
-                    u.g = find(s_alt, p.groups, y);
+                    u.g = find_last(s_alt, p.groups, y);
                     const int rel = (y - s_alt[u.g]) / length(u.g);
                     tile = s_pre[u.g] + rel;
                     at = y - s_alt[u.g] - rel * length(u.g);
@@ -289,13 +311,13 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     const int rel = x / padded;
                     tile = tail_from + rel;
                     at = x - rel * padded;
-                    u.g = find(s_pre, p.groups, tile);
+                    u.g = LORA ? 0 : find_last(s_pre, p.groups, tile);
                 }
             } else {
                 u.some = 0;
             }
             if (u.some) {
-                const int rel = tile - s_pre[u.g], len = length(u.g);
+                const int rel = LORA ? tile : tile - s_pre[u.g], len = length(u.g);
                 u.row0 = LORA ? 0 : s_row[u.g];
                 u.rows = rows_in(u.g);
                 int ti, kbs = len;
@@ -333,19 +355,19 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     u.cut = tile - tail_from;
                 }
                 if (LORA) {
-                    u.req_whole = u.req_parts = 0;
-                    if (u.kb1 == kbs) {
-                        // the first request with rows at or behind the tile's first
-                        u.req = s_row[0] > u.c0 ? 0 : find(s_row, p.requests + 1, u.c0);
-                        if (u.req < p.requests) {
-                            if (s_row[u.req] <= u.c0 && s_row[u.req + 1] >= u.c0 + u.cols) {
-                                u.req_whole = s_alt[u.req] >= 0 ? p.rank_blocks : 0;
-                            } else {
-                                int n = 0;
-                                for (int q = u.req + lane; q < p.requests && s_row[q] < u.c0 + u.cols; q += 32) n += has_part(q) ? 1 : 0;
-                                u.req_parts = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(n)));
-                            }
-                        }
+                    u.req_whole = u.req_parts = u.shorts = 0;
+                    // (the first request with rows at or behind the tile's first; before the first request's rows it is that one)
+                    u.req = find_last(s_row, p.requests + 1, u.c0);
+                    int parts_of = 0, shorts = 0;
+                    for (int q = u.req + lane; q < p.requests && s_row[q] < u.c0 + u.cols; q += 32) {
+                        parts_of += has_part(q) ? 1 : 0;
+                        shorts += is_short(q) ? 1 : 0;
+                    }
+                    parts_of = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(parts_of)));
+                    u.shorts = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(shorts)));
+                    if (u.kb1 == kbs && parts_of) {
+                        if (s_row[u.req] <= u.c0 && s_row[u.req + 1] >= u.c0 + u.cols) u.req_whole = p.rank_blocks;
+                        else u.req_parts = parts_of;
                     }
                 }
             }
@@ -446,7 +468,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             }
             if (LORA && ok && u.req_whole + u.req_parts > 0) {
                 // h16 comes from the kernel before this one
-                if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+                if (!waited) launch_wait();
                 waited = true;
                 const uint32_t bytes = (A_MN ? 8192u : GRP_A_BYTES) + b_bytes;
                 int q = u.req;
@@ -601,6 +623,11 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             return reinterpret_cast<float4*>(p.partial) + (2 * (u.first_pair + part) + (part > 0 ? 0 : 1)) * (static_cast<size_t>(GRP_TILE / 4) * p.slab_cols) +
                    ((rank * p.slab_cols + c) / 32 * 4 + quarter) * 256 + lane;
         };
+        auto to_slab = [&](const float (&v)[32], int c) {
+            float4* dst = slab_of(u.part, c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) __stcg(dst + j * 32, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+        };
         // One 32 x 32 piece of C (columns c .. c + 31 of the tile, this warp's 32 features): lane l has feature l, v[j] is row j.
         // It goes through two 2 KB buffers of shared memory, from where a TMA store writes it (and clips what lies beyond C's
         // edges); of a piece that ends inside the box, because the next row is another group's, lanes write 16 bytes each.
@@ -630,13 +657,32 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             }
             const bool live = i0 + lane < p.I;
             if (MODE == GRP_ROWS && p.add) {
-                if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // `add` comes from the kernel before this one
+                if (!waited) launch_wait();
                 waited = true;
                 const float* add = p.add + row0 * p.I + i0 + lane;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
                     if (live && j < n) v[j] += __ldcg(add);
                     add += p.I;
+                }
+            }
+            if (LORA && u.shorts) {
+                // rows of short requests have theirs in `add`, in the order of the rows: which of these 32, and where the first is
+                const int row = u.c0 + c + lane;
+                const int q = find_last(s_row, p.requests + 1, row);
+                const bool has = lane < n && row >= s_row[0] && q < p.requests && is_short(q);
+                const unsigned mask = __ballot_sync(~0u, has);
+                if (mask) {
+                    if (!waited) launch_wait();
+                    waited = true;
+                    const int first = __shfl_sync(~0u, has ? s_pre[q] + row - s_row[q] : 0, __ffs(mask) - 1);
+                    const float* add = p.add + static_cast<size_t>(first) * p.I + i0 + lane;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if ((mask >> j) & 1u) {
+                            if (live) v[j] += __ldcg(add);
+                            add += p.I;
+                        }
                 }
             }
             const size_t base = (WEIGHTS ? static_cast<size_t>(u.g) * p.stride_c : 0) + row0 * p.ldc + i0;
@@ -698,11 +744,12 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         };
         while (ok && next(u)) {
             // the accumulators that make up the tile: chunks of its own k-blocks, then one for each request with some of its rows
+            bool held = true;                             // the sum is in tensor memory, not stored yet
             const int blocks = u.kb1 - u.kb0 + u.req_whole;
             const int chunks = p.chunk ? max(1, (blocks + p.chunk - 1) / p.chunk) : 1, all = chunks + u.req_parts;
             if (!await()) break;
             if ((!OUT16 || LORA) && all > 1) {
-                // all but the last are added in registers, and the sum goes back to the last one's place
+                // they are added in registers
                 float sum[4][32];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
@@ -742,18 +789,15 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     }
                 }
                 if (!ok) break;
-                const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
+                release();                                // the next tile may have this accumulator while the sums are stored
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = set * 32 + q * 64;
-                    if (c < u.cols) {
-                        uint32_t v[32];
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[q][j]);
-                        tmem_st_32x32(taddr + c, v);
-                    }
+                    if (c >= u.cols) continue;
+                    if (u.parts > 1) to_slab(sum[q], c);
+                    else deliver(sum[q], c);
                 }
-                tmem_st_wait();
+                held = false;
             }
             const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
             const int mine = (u.cols - set * 32 + 63) >> 6;
@@ -761,18 +805,16 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             if (u.parts > 1) {
                 // this part's pieces go to its slab; then one count for each of them says which have all their parts
 #pragma unroll 1
-                for (int q = 0; q < mine; ++q) {
-                    const int c = set * 32 + q * 64;
+                for (int q = 0; held && q < mine; ++q) {
                     uint32_t v[32];
-                    tmem_ld_32x32(taddr + c, v);
+                    float f[32];
+                    tmem_ld_32x32(taddr + set * 32 + q * 64, v);
                     tmem_ld_wait();
-                    float4* dst = slab_of(u.part, c);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        __stcg(dst + j * 32, make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]),
-                                                         __uint_as_float(v[4 * j + 3])));
+                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                    to_slab(f, set * 32 + q * 64);
                 }
-                release();
+                if (held) release();
                 __threadfence();
                 __syncwarp();
                 bool done = false;
@@ -787,7 +829,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             }
 #pragma unroll 1
             for (int q = 0; q < mine; ++q) {
-                if (!((last >> q) & 1u)) continue;
+                if (!((last >> q) & 1u) || !(held || u.parts > 1)) continue;
                 const int c = set * 32 + q * 64;
                 float f[32];
                 if (u.parts > 1) {
@@ -815,7 +857,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 }
                 deliver(f, c);
             }
-            if (u.parts == 1) release();
+            if (held && u.parts == 1) release();
         }
         if (lane == 0) bulk_wait_read<0>();               // the stores are done with this CTA's shared memory
         __syncwarp();
@@ -848,7 +890,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         }
     }
 
-    if (warp == 0) asm volatile("griddepcontrol.wait;" ::: "memory");   // this launch ends after the one before it, whatever it read
+    if (warp == 0) launch_wait();        // this launch ends after the one before it, whatever it read
     tc_fence_before_sync();
     __syncthreads();
     cluster_sync_all();

@@ -16,7 +16,7 @@ constexpr int GRP_BK = 64;
 constexpr int GRP_TILE = 256;                          // features of a tile, and the most rows of one
 constexpr int GRP_TABLE = 4 * (GRP_MAX_GROUPS + 1);    // bytes of a table by group
 constexpr int GRP_STAGING = 8 * 4096;                  // of the stores: two buffers of 2 KB for each epilogue warp
-constexpr int GRP_CUT_FIXED = 5000, GRP_CUT_ROW = 24;  // estimated clocks of cutting a tile (see grouped.cuh)
+constexpr int GRP_BLOCK = 600, GRP_CUT_FIXED = 3000, GRP_CUT_ROW = 80;   // estimated clocks (see grouped.cuh)
 constexpr int GRP_SMEM = GRP_RING + GRP_STAGING + 1024 + 3 * GRP_TABLE + 1024;
 
 constexpr int GRP_CHUNK = 8;                           // k-blocks between additions to the FP32 sums of FP32 results
@@ -38,7 +38,9 @@ struct GroupedParams {
     const int* index;      // ROWS: weight of each group (outside [0, index_max): the group is skipped); null: its number
     int index_max;
     void* C;
-    const float* add;      // FP32 [rows][I], added before the rounding; null: none
+    const float* add;      // FP32 [rows][I], added before the rounding; null: none.  LORA: rows of short requests only, one behind the other
+    int late;              // what `add` and h16 hold comes from the kernel before this one, nothing else does: wait for it there only
+    int min_rows;          // ROWS with index: groups of so few rows are skipped; LORA: such requests' part is in `add`
     long long ldc, stride_c;
     float* partial;        // slabs of tiles cut along k, two per CTA pair; null: no tile is cut
     int slab_cols;         // columns of a slab
@@ -81,9 +83,7 @@ struct GroupedKernel {     // one instantiation
 };
 inline GroupedOut grouped_out(bool out16, bool f16) { return !out16 ? GRP_OUT_F32 : f16 ? GRP_OUT_F16 : GRP_OUT_BF16; }
 cudaError_t grouped_prepare(const GroupedKernel& k);     // once per kernel and device: its shared memory
-// `after_start`: the launch may begin while the kernel before it in the stream still runs (which has to allow it)
-cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p,
-                           bool after_start);
+cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p);
 // Arrival counters of the tiles cut along k, zero between launches (the last arriver clears its own).  A plan holds a
 // slot of a static table from create to destroy; where none is free (null) it cuts no tile.
 constexpr int SPLIT_COUNTERS = 4096;

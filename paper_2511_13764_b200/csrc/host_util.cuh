@@ -29,6 +29,23 @@ struct DeviceGuard {
     }
 };
 
+// Launch that may begin while the kernel before it in the stream ends.  Every kernel launched this way waits for that
+// one (griddepcontrol.wait) before it touches global memory, unless it says otherwise, and again before it ends.
+template <typename... P, typename... A>
+static cudaError_t launch_beside(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // The next slot of the current device's table of status words, cleared (see nk_gemm_check).
 nk_status_t take_status_slot(unsigned int** slot);
 

@@ -4,7 +4,8 @@
 // used for up to eight rows at a time on the FMA units.  A cluster of eight CTAs takes eight rows of one request:
 // every CTA multiplies its eighth of K, the eight partial results are added (in the order of the CTAs) through
 // distributed shared memory, and every CTA then multiplies its eighth of N.  So even sixteen requests spread their
-// weights' reads over 128 SMs, and X . A_a never leaves the cluster.
+// weights' reads over 128 SMs, and X . A_a never leaves the cluster.  Small in registers and shared memory, so that
+// the projection's blocks can start beside it: its time hides behind theirs.
 #pragma once
 #include "half.cuh"
 #include "ptx.cuh"
@@ -13,11 +14,13 @@ namespace nk {
 
 constexpr int LORA_CLUSTER = 8, LORA_THREADS = 256, LORA_ROWS = 8;
 constexpr int LORA_MAX_RANK = 128, LORA_MAX_REQUESTS = 1024;
-constexpr int LORA_KSTEP = 512;                 // k of X kept in shared memory at a time
+constexpr int LORA_KSTEP = 256;                 // k of X kept in shared memory at a time
 
 struct LoraParams {
     int rows, N, K, rank, adapters, requests;
     int transposed, f16;
+    int few;                                    // 0: requests of up to LORA_ROWS rows, their rows one behind the other in D
+                                                // 1: all requests, D like Y, rows without an adapter zero
     long long ldx;
     const void *X, *A, *B;
     const float* scale;
@@ -26,50 +29,43 @@ struct LoraParams {
     unsigned int* status;
 };
 
-// Rows of the requests, clamped and monotone, and the chunks of LORA_ROWS rows before each request.
-__device__ __forceinline__ void lora_prefix(const LoraParams& p, int* s_row, int* s_pre) {
+// Rows of the requests, clamped and monotone, and before each request the chunks of LORA_ROWS rows and (few = 0) the rows
+// of D.  (few = 0: one chunk to a short request, so `s_pre` counts rows and a request's chunk begins where they change.)
+__device__ __forceinline__ int lora_prefix(const LoraParams& p, int* s_row, int* s_pre) {
     const int lane = threadIdx.x & 31;
     for (int q = threadIdx.x; q <= p.requests; q += LORA_THREADS) s_row[q] = p.offsets[q];
     __syncthreads();
     if (threadIdx.x < 32) {
-        int top = 0, chunks = 0;
         bool bad = false;
-        for (int base = 0; base <= p.requests; base += 32) {
-            const int q = base + lane;
-            const int raw = q <= p.requests ? s_row[q] : 0;
-            int v = min(max(raw, 0), p.rows);
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(~0u, v, d);
-                if (lane >= d) v = max(v, o);
+        for (int q = lane; q <= p.requests; q += 32) bad |= s_row[q] < (q ? s_row[q - 1] : 0) || s_row[q] > p.rows;
+        if (__any_sync(~0u, bad)) {
+            if (lane == 0) {
+                if (blockIdx.x == 0 && p.status) atomicCAS(p.status, 0u, 0x10000u);
+                int top = 0;
+                for (int q = 0; q <= p.requests; ++q) s_row[q] = top = max(top, min(s_row[q], p.rows));
             }
-            v = max(v, top);
-            if (q <= p.requests) {
-                bad |= v != raw;
-                s_row[q] = v;
-            }
-            top = __shfl_sync(~0u, v, 31);
+            __syncwarp();
         }
-        if (__any_sync(~0u, bad) && lane == 0 && blockIdx.x == 0 && p.status) atomicCAS(p.status, 0u, 0x10000u);
-        __syncwarp();
+        int sum = 0;
         for (int base = 0; base <= p.requests; base += 32) {
             const int q = base + lane;
             int n = 0;
             if (q < p.requests) {
-                const int a = p.adapter[q];
-                if (a >= 0 && a < p.adapters) n = (s_row[q + 1] - s_row[q] + LORA_ROWS - 1) / LORA_ROWS;
+                const int a = p.adapter[q], rows = s_row[q + 1] - s_row[q];
+                if (a >= 0 && a < p.adapters) n = p.few ? (rows + LORA_ROWS - 1) / LORA_ROWS : rows <= LORA_ROWS ? rows : 0;
             }
             int v = n;
-#pragma unroll
+#pragma unroll 1
             for (int d = 1; d < 32; d <<= 1) {
                 const int o = __shfl_up_sync(~0u, v, d);
                 if (lane >= d) v += o;
             }
-            if (q <= p.requests) s_pre[q] = chunks + v - n;
-            chunks += __shfl_sync(~0u, v, 31);
+            if (q <= p.requests) s_pre[q] = sum + v - n;
+            sum += __shfl_sync(~0u, v, 31);
         }
     }
     __syncthreads();
+    return s_pre[p.requests];
 }
 
 __device__ __forceinline__ void lora_unpack8(const uint4& v, int f16, float (&x)[8]) {
@@ -83,7 +79,7 @@ __device__ __forceinline__ void lora_unpack8(const uint4& v, int f16, float (&x)
 
 // RT rows (1 or LORA_ROWS) of one request; `n` of them exist.  h: this CTA's share of X . A_a, then the whole of it.
 template <int RT>
-__device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n, int a, uint32_t crank, float* xs, float* part,
+__device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n, int a, size_t d_row, uint32_t crank, float* xs, float* part,
                                            float* share, float* h) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int R = p.rank;
@@ -99,10 +95,14 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
     for (int k0 = k_lo; k0 < k_hi; k0 += LORA_KSTEP) {
         const int kn = min(LORA_KSTEP, k_hi - k0);
         __syncthreads();
-        // X as FP32, [k][RT]
-        for (int i = threadIdx.x; i < kn * RT; i += LORA_THREADS) {
-            const int t = i / kn, k = i - t * kn;
-            xs[k * RT + t] = t < n ? half_bits_to_f32(X[static_cast<size_t>(row0 + t) * p.ldx + k0 + k], p.f16) : 0.0f;
+        // X as FP32, [k][RT]; eight of k to a thread
+        for (int i = threadIdx.x; i < RT * (LORA_KSTEP / 8); i += LORA_THREADS) {
+            const int t = i / (LORA_KSTEP / 8), k = (i - t * (LORA_KSTEP / 8)) * 8;
+            if (k >= kn) continue;
+            float x[8];
+            lora_unpack8(t < n ? *reinterpret_cast<const uint4*>(X + static_cast<size_t>(row0 + t) * p.ldx + k0 + k) : make_uint4(0, 0, 0, 0), p.f16, x);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) xs[(k + q) * RT + t] = x[q];
         }
         __syncthreads();
         if (p.transposed) {
@@ -205,7 +205,7 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
             }
 #pragma unroll
             for (int t = 0; t < RT; ++t)
-                if (t < n) p.D[static_cast<size_t>(row0 + t) * p.N + i] = acc[t];
+                if (t < n) p.D[(d_row + t) * p.N + i] = acc[t];
         }
     } else {
         for (int i = n_lo + 2 * threadIdx.x; i < n_hi; i += 2 * LORA_THREADS) {
@@ -224,50 +224,61 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
             }
 #pragma unroll
             for (int t = 0; t < RT; ++t)
-                if (t < n) *reinterpret_cast<float2*>(p.D + static_cast<size_t>(row0 + t) * p.N + i) = make_float2(acc0[t], acc1[t]);
+                if (t < n) *reinterpret_cast<float2*>(p.D + (d_row + t) * p.N + i) = make_float2(acc0[t], acc1[t]);
         }
     }
     __syncthreads();
 }
 
-constexpr int LORA_SMEM = 4 * (LORA_KSTEP * LORA_ROWS + (LORA_THREADS / 32) * LORA_MAX_RANK * LORA_ROWS + 2 * LORA_MAX_RANK * LORA_ROWS +
-                               2 * (LORA_MAX_REQUESTS + 1));
+// Shared memory: X, the warps' sums (row-major weights), the CTA's share and the whole of X . A_a, the two tables.
+__host__ __device__ inline int lora_smem(int rank, int requests, bool transposed) {
+    return 4 * (LORA_KSTEP * LORA_ROWS + (transposed ? 0 : LORA_THREADS / 32 * rank * LORA_ROWS) + 2 * rank * LORA_ROWS + 2 * (requests + 1));
+}
 
-__global__ void __launch_bounds__(LORA_THREADS) __cluster_dims__(LORA_CLUSTER, 1, 1) lora_delta_kernel(const LoraParams p) {
+__global__ void __launch_bounds__(LORA_THREADS, 4) __cluster_dims__(LORA_CLUSTER, 1, 1) lora_delta_kernel(const LoraParams p) {
     extern __shared__ float lora_sm[];
     float* xs = lora_sm;
     float* part = xs + LORA_KSTEP * LORA_ROWS;
-    float* share = part + (LORA_THREADS / 32) * LORA_MAX_RANK * LORA_ROWS;
-    float* h = share + LORA_MAX_RANK * LORA_ROWS;
-    int* s_row = reinterpret_cast<int*>(h + LORA_MAX_RANK * LORA_ROWS);
-    int* s_pre = s_row + LORA_MAX_REQUESTS + 1;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    lora_prefix(p, s_row, s_pre);
+    float* share = part + (p.transposed ? 0 : LORA_THREADS / 32 * p.rank * LORA_ROWS);
+    float* h = share + p.rank * LORA_ROWS;
+    int* s_row = reinterpret_cast<int*>(h + p.rank * LORA_ROWS);
+    int* s_pre = s_row + p.requests + 1;
+    launch_wait();
+    launch_next();
+    const int chunks = lora_prefix(p, s_row, s_pre);
     const uint32_t crank = cluster_ctarank();
-    const int clusters = gridDim.x / LORA_CLUSTER, chunks = s_pre[p.requests];
-    // rows without an adapter add nothing: zeros, all threads of the grid (rows of no request among them)
-    const int stride = gridDim.x * LORA_THREADS;
-    for (int q = -1; q <= p.requests; ++q) {
-        if (q >= 0 && q < p.requests) {
-            if (s_pre[q + 1] > s_pre[q] || s_row[q + 1] == s_row[q]) continue;
+    const int clusters = gridDim.x / LORA_CLUSTER, cluster = blockIdx.x / LORA_CLUSTER;
+    if (p.few) {
+        // rows without an adapter add nothing: zeros (rows of no request among them)
+        const int stride = gridDim.x * LORA_THREADS;
+        for (int q = -1; q <= p.requests; ++q) {
+            if (q >= 0 && q < p.requests && (s_pre[q + 1] > s_pre[q] || s_row[q + 1] == s_row[q])) continue;
+            const int lo = q < 0 ? 0 : s_row[q], hi = q < 0 ? s_row[0] : q == p.requests ? p.rows : s_row[q + 1];
+            const size_t first = static_cast<size_t>(lo) * p.N / 4, last = static_cast<size_t>(hi) * p.N / 4;
+            for (size_t i = first + blockIdx.x * LORA_THREADS + threadIdx.x; i < last; i += stride)
+                reinterpret_cast<float4*>(p.D)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        const int lo = q < 0 ? 0 : s_row[q], hi = q < 0 ? s_row[0] : q == p.requests ? p.rows : s_row[q + 1];
-        const size_t first = static_cast<size_t>(lo) * p.N / 4, last = static_cast<size_t>(hi) * p.N / 4;
-        for (size_t i = first + blockIdx.x * LORA_THREADS + threadIdx.x; i < last; i += stride)
-            reinterpret_cast<float4*>(p.D)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    for (int c = blockIdx.x / LORA_CLUSTER; c < chunks; c += clusters) {
-        int lo = 0, hi = p.requests;                       // s_pre[lo] <= c < s_pre[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (s_pre[mid] <= c) lo = mid;
-            else hi = mid;
+    // few: chunk after chunk; else request after request
+    for (int c = cluster; c < (p.few ? chunks : p.requests); c += clusters) {
+        int q = c;
+        if (p.few) {
+            int lo = 0, hi = p.requests;                   // s_pre[lo] <= c < s_pre[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s_pre[mid] <= c) lo = mid;
+                else hi = mid;
+            }
+            q = lo;
+        } else if (s_pre[q + 1] == s_pre[q]) {
+            continue;
         }
-        const int row0 = s_row[lo] + (c - s_pre[lo]) * LORA_ROWS;
-        const int n = min(LORA_ROWS, s_row[lo + 1] - row0);
-        const int a = p.adapter[lo];
-        if (n == 1) lora_chunk<1>(p, row0, n, a, crank, xs, part, share, h);
-        else lora_chunk<LORA_ROWS>(p, row0, n, a, crank, xs, part, share, h);
+        const int row0 = s_row[q] + (p.few ? (c - s_pre[q]) * LORA_ROWS : 0);
+        const int n = min(LORA_ROWS, s_row[q + 1] - row0);
+        const size_t d_row = p.few ? row0 : s_pre[q];
+        const int a = p.adapter[q];
+        if (n == 1) lora_chunk<1>(p, row0, n, a, d_row, crank, xs, part, share, h);
+        else lora_chunk<LORA_ROWS>(p, row0, n, a, d_row, crank, xs, part, share, h);
     }
 }
 

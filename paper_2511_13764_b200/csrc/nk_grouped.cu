@@ -37,18 +37,8 @@ static GroupedFunction function_of(const GroupedKernel& k) {
 cudaError_t grouped_prepare(const GroupedKernel& k) {
     return cudaFuncSetAttribute(function_of(k), cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM);
 }
-cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p, bool after_start) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * pairs);
-    cfg.blockDim = dim3(GRP_THREADS);
-    cfg.dynamicSmemBytes = GRP_SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = after_start ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, function_of(k), maps, p);
+cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p) {
+    return launch_beside(function_of(k), 2 * pairs, GRP_THREADS, GRP_SMEM, st, maps, p);
 }
 
 }  // namespace nk
@@ -185,7 +175,7 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     g.a_slabs = d.N % 64 == 0;
     g.b_slabs = d.K % 64 == 0;
     g.chunk = d.out_dtype == NK_F32 ? GRP_CHUNK : 0;
-    const cudaError_t e = grouped_launch(p->kernel, p->pairs, static_cast<cudaStream_t>(cuda_stream), p->maps, g, false);
+    const cudaError_t e = grouped_launch(p->kernel, p->pairs, static_cast<cudaStream_t>(cuda_stream), p->maps, g);
     return e == cudaSuccess ? NK_OK : p->cuda("grouped launch", e);
 }
 

@@ -9,7 +9,7 @@ struct nk_lora_s : nk::PlanBase {
     int pairs, rank_blocks;
     int split_slot[2];            // of X . A and of the projection: the two overlap
     unsigned int* counters[2];
-    size_t part_bytes[2], side_bytes;   // partial sums of the two; FP32 contributions or X . A
+    size_t part_bytes[2], h_bytes, side_bytes;   // partial sums of the two; X . A; it and the FP32 contributions
     nk::GroupedKernel projection, shrinking;
     nk::GroupedMaps maps, shrink; // of the projection and of X . A
     const void *cached_x, *cached_w, *cached_a, *cached_b, *cached_ws, *cached_y;
@@ -22,10 +22,10 @@ namespace nk {
 
 static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Which way the adapters' part goes.  Up to about LORA_FEW_ROWS rows to a request its weights are all that counts, and
-// the clusters of lora_delta_kernel read them at the speed of memory; beyond that the rows' arithmetic wants
-// the tensor cores: X . A_a as a grouped product, (X . A_a) . B_a as further k-blocks of the projection.
-constexpr int64_t LORA_FEW_ROWS = 8;
+// Which way the adapters' part goes.  Requests of up to LORA_ROWS rows are lora_delta_kernel's: their weights are all that
+// counts, and its clusters read them at the speed of memory; more rows want the tensor cores: X . A_a as a grouped
+// product, (X . A_a) . B_a as further k-blocks of the projection.  Where a plan's requests have so few rows on average,
+// lora_delta_kernel takes all of them, and the launch of the grouped product is saved.
 
 }  // namespace nk
 
@@ -61,16 +61,18 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     DeviceGuard guard(d.device);
     const bool row = d.layout == NK_ROW_MAJOR;
-    p->few = d.rows <= LORA_FEW_ROWS * d.requests;
+    p->few = d.rows <= LORA_ROWS * d.requests;
     p->projection = {p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
     p->shrinking = {GRP_ROWS, row, GRP_OUT_F32};
     cudaError_t e = grouped_prepare(p->projection);
-    if (e == cudaSuccess) e = p->few ? cudaFuncSetAttribute(lora_delta_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LORA_SMEM)
-                                     : grouped_prepare(p->shrinking);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_delta_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lora_smem(LORA_MAX_RANK, LORA_MAX_REQUESTS, false));
+    if (e == cudaSuccess && !p->few) e = grouped_prepare(p->shrinking);
     if (e != cudaSuccess || !encode_tiled()) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
     p->rank_blocks = static_cast<int>(div_up(d.rank, 32));
-    p->side_bytes = align256(p->few ? static_cast<size_t>(d.rows) * d.N * sizeof(float) : static_cast<size_t>(d.rows) * p->rank_blocks * 128);
+    p->h_bytes = p->few ? 0 : align256(static_cast<size_t>(d.rows) * p->rank_blocks * 128);
+    const int64_t short_rows = d.rows < LORA_ROWS * d.requests ? d.rows : LORA_ROWS * d.requests;
+    p->side_bytes = p->h_bytes + align256(static_cast<size_t>(short_rows) * d.N * sizeof(float));
     for (int i = p->few ? 1 : 0; i < 2; ++i) {
         p->split_slot[i] = take_split_slot(&p->counters[i]);
         p->part_bytes[i] = p->split_slot[i] < 0 ? 0 : grouped_partial_bytes(p->pairs, grouped_slab_cols(d.rows));
@@ -137,51 +139,57 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     g.rank = static_cast<int>(d.rank);
     g.rank_blocks = p->rank_blocks;
     g.scale = scale;
-    cudaError_t e;
-    if (p->few) {
-        LoraParams l = {};
-        l.rows = g.rows;
-        l.N = static_cast<int>(d.N);
-        l.K = static_cast<int>(d.K);
-        l.rank = g.rank;
-        l.adapters = static_cast<int>(d.adapters);
-        l.requests = static_cast<int>(d.requests);
-        l.transposed = !row;
-        l.f16 = f16;
-        l.ldx = d.ldx;
-        l.X = X;
-        l.A = A;
-        l.B = B;
-        l.scale = scale;
-        l.offsets = offsets;
-        l.adapter = adapter;
-        l.D = reinterpret_cast<float*>(ws);
-        l.status = p->status_dev;
-        // clusters: no more than there can be chunks of rows, and a few for every SM
-        const int64_t chunks = d.rows / LORA_ROWS + (d.rows < d.requests ? d.rows : d.requests);
-        const int64_t most = 4 * p->sm_count / LORA_CLUSTER;
-        lora_delta_kernel<<<static_cast<unsigned>((chunks < most ? chunks : most) * LORA_CLUSTER), LORA_THREADS, LORA_SMEM, st>>>(l);
-        if ((e = cudaGetLastError()) != cudaSuccess) return p->cuda("lora delta launch", e);
-        g.add = l.D;
-    } else {
+    LoraParams l = {};
+    l.rows = g.rows;
+    l.N = static_cast<int>(d.N);
+    l.K = static_cast<int>(d.K);
+    l.rank = g.rank;
+    l.adapters = static_cast<int>(d.adapters);
+    l.requests = static_cast<int>(d.requests);
+    l.transposed = !row;
+    l.f16 = f16;
+    l.few = p->few;
+    l.ldx = d.ldx;
+    l.X = X;
+    l.A = A;
+    l.B = B;
+    l.scale = scale;
+    l.offsets = offsets;
+    l.adapter = adapter;
+    l.D = reinterpret_cast<float*>(ws + p->h_bytes);
+    l.status = p->status_dev;
+    // clusters: no more than there can be chunks of rows, and a few for every SM
+    const int64_t chunks = p->few ? d.rows / LORA_ROWS + (d.rows < d.requests ? d.rows : d.requests) : d.requests;
+    const int64_t most = 4 * p->sm_count / LORA_CLUSTER;
+    cudaError_t e = launch_beside(lora_delta_kernel, static_cast<unsigned>((chunks < most ? chunks : most) * LORA_CLUSTER), LORA_THREADS,
+                                  lora_smem(l.rank, l.requests, l.transposed), st, l);
+    if (e != cudaSuccess) return p->cuda("lora delta launch", e);
+    // The two products start beside it.  Neither touches what it writes before they wait for it, and what it waited for
+    // before its start has ended before theirs.
+    g.late = 1;
+    g.add = l.D;
+    if (!p->few) {
         // X . A_a: the requests are the groups, their adapters the weights
         GroupedParams h = g;
-        h.groups = static_cast<int>(d.requests);
+        h.add = nullptr;
+        h.groups = l.requests;
         h.offsets = offsets;
         h.index = adapter;
-        h.index_max = static_cast<int>(d.adapters);
+        h.index_max = l.adapters;
+        h.min_rows = LORA_ROWS;
         h.I = g.rank;
         h.tiles_i = 1;
         h.chunk = GRP_CHUNK;
         h.h16 = reinterpret_cast<uint16_t*>(ws);
         h.partial = partial[0];
         h.counter = p->counters[0];
-        e = grouped_launch(p->shrinking, p->pairs, st, p->shrink, h, false);
+        e = grouped_launch(p->shrinking, p->pairs, st, p->shrink, h);
         if (e != cudaSuccess) return p->cuda("lora shrink launch", e);
         g.requests = h.groups;
         g.request_offsets = offsets;
         g.index = adapter;
         g.index_max = h.index_max;
+        g.min_rows = LORA_ROWS;
     }
     g.groups = 1;
     g.I = static_cast<int>(d.N);
@@ -192,8 +200,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     g.ldc = d.ldy;
     g.partial = partial[1];
     g.counter = p->counters[1];
-    // the projection starts while the adapters' kernel runs, and waits for it where it needs its result
-    e = grouped_launch(p->projection, p->pairs, st, p->maps, g, true);
+    e = grouped_launch(p->projection, p->pairs, st, p->maps, g);
     return e == cudaSuccess ? NK_OK : p->cuda("lora projection launch", e);
 }
 

@@ -19,25 +19,25 @@ static int route_width(int64_t experts) {
 }
 
 template <bool ONE>
-static const void* select_kernel(int v) {
+static void (*select_kernel(int v))(RouteParams) {
     switch (v) {
-        case 1: return reinterpret_cast<const void*>(route_select_kernel<1, ONE>);
-        case 2: return reinterpret_cast<const void*>(route_select_kernel<2, ONE>);
-        case 4: return reinterpret_cast<const void*>(route_select_kernel<4, ONE>);
-        case 8: return reinterpret_cast<const void*>(route_select_kernel<8, ONE>);
-        case 16: return reinterpret_cast<const void*>(route_select_kernel<16, ONE>);
+        case 1: return route_select_kernel<1, ONE>;
+        case 2: return route_select_kernel<2, ONE>;
+        case 4: return route_select_kernel<4, ONE>;
+        case 8: return route_select_kernel<8, ONE>;
+        case 16: return route_select_kernel<16, ONE>;
     }
-    return reinterpret_cast<const void*>(route_select_kernel<32, ONE>);
+    return route_select_kernel<32, ONE>;
 }
-static const void* backward_kernel(int v) {
+static void (*backward_kernel(int v))(RouteParams, const float*, float*) {
     switch (v) {
-        case 1: return reinterpret_cast<const void*>(route_backward_kernel<1>);
-        case 2: return reinterpret_cast<const void*>(route_backward_kernel<2>);
-        case 4: return reinterpret_cast<const void*>(route_backward_kernel<4>);
-        case 8: return reinterpret_cast<const void*>(route_backward_kernel<8>);
-        case 16: return reinterpret_cast<const void*>(route_backward_kernel<16>);
+        case 1: return route_backward_kernel<1>;
+        case 2: return route_backward_kernel<2>;
+        case 4: return route_backward_kernel<4>;
+        case 8: return route_backward_kernel<8>;
+        case 16: return route_backward_kernel<16>;
     }
-    return reinterpret_cast<const void*>(route_backward_kernel<32>);
+    return route_backward_kernel<32>;
 }
 
 static RouteParams route_params(const nk_route_s* p) {
@@ -97,14 +97,13 @@ nk_status_t nk_route_create(const nk_route_desc_t* desc, nk_route_t* out) {
     p->per_block = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? ROUTE_ONE_BLOCK : div_up(d.tokens, sms) < 16 ? 16 : div_up(d.tokens, sms));
     p->blocks = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? 1 : div_up(d.tokens, p->per_block));
     DeviceGuard guard(d.device);
-    const int v = route_width(d.experts), smem = route_smem(static_cast<int>(d.experts));
-    const void* first = p->blocks == 1 ? select_kernel<true>(v) : select_kernel<false>(v);
+    const int v = route_width(d.experts);
+    const auto first = p->blocks == 1 ? select_kernel<true>(v) : select_kernel<false>(v);
     if (cudaFuncSetAttribute(first, cudaFuncAttributeMaxDynamicSharedMemorySize, route_smem(NK_ROUTE_MAX_EXPERTS)) != cudaSuccess ||
         cudaFuncSetAttribute(route_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, route_smem(NK_ROUTE_MAX_EXPERTS)) != cudaSuccess) {
         delete p;
         return NK_ERR_CUDA;
     }
-    (void)smem;
     *out = p;
     return NK_OK;
 }
@@ -134,13 +133,10 @@ nk_status_t nk_route_run(nk_route_t p, const void* logits, float* gates, int32_t
     r.counts = static_cast<int*>(workspace);
     const int v = route_width(p->d.experts), smem = route_smem(r.experts);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    void* args[] = {&r};
-    cudaError_t e = cudaLaunchKernel(p->blocks == 1 ? select_kernel<true>(v) : select_kernel<false>(v), dim3(p->blocks),
-                                     dim3(ROUTE_THREADS), args, smem, st);
+    cudaError_t e = launch_beside(p->blocks == 1 ? select_kernel<true>(v) : select_kernel<false>(v), p->blocks, ROUTE_THREADS, smem, st, r);
     if (e != cudaSuccess) return p->cuda("route select launch", e);
     if (p->blocks > 1) {
-        route_place_kernel<<<p->blocks, ROUTE_THREADS, smem, st>>>(r);
-        if ((e = cudaGetLastError()) != cudaSuccess) return p->cuda("route place launch", e);
+        if ((e = launch_beside(route_place_kernel, p->blocks, ROUTE_THREADS, smem, st, r)) != cudaSuccess) return p->cuda("route place launch", e);
     }
     return NK_OK;
 }
@@ -158,9 +154,8 @@ nk_status_t nk_route_backward(nk_route_t p, const void* logits, const int32_t* e
     RouteParams r = route_params(p);
     r.logits = logits;
     r.chosen = const_cast<int32_t*>(experts);
-    void* args[] = {&r, &dgates, &dlogits};
-    const cudaError_t e = cudaLaunchKernel(backward_kernel(route_width(p->d.experts)), dim3(static_cast<unsigned>(div_up(r.tokens, 8))), dim3(256),
-                                           args, 0, static_cast<cudaStream_t>(cuda_stream));
+    const cudaError_t e = launch_beside(backward_kernel(route_width(p->d.experts)), static_cast<unsigned>(div_up(r.tokens, 8)), 256, 0,
+                                        static_cast<cudaStream_t>(cuda_stream), r, dgates, dlogits);
     return e == cudaSuccess ? NK_OK : p->cuda("route backward launch", e);
 }
 
@@ -173,9 +168,8 @@ nk_status_t nk_route_dispatch(nk_route_t p, const void* X, const int32_t* slots,
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     const ExchangeParams x = exchange_params(p, slots, nullptr);
     const int64_t blocks = div_up(p->d.tokens * x.vecs, 256);
-    dispatch_kernel<<<static_cast<unsigned>(blocks < (1 << 30) ? blocks : 1 << 30), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
-        x, static_cast<const uint4*>(X), static_cast<uint4*>(Xs));
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_beside(dispatch_kernel, static_cast<unsigned>(blocks < (1 << 30) ? blocks : 1 << 30), 256, 0, static_cast<cudaStream_t>(cuda_stream),
+                                        x, static_cast<const uint4*>(X), static_cast<uint4*>(Xs));
     return e == cudaSuccess ? NK_OK : p->cuda("dispatch launch", e);
 }
 
@@ -188,9 +182,8 @@ nk_status_t nk_route_combine(nk_route_t p, const void* Ys, const int32_t* slots,
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     const ExchangeParams x = exchange_params(p, slots, gates);
     const int64_t blocks = div_up(p->d.tokens * x.vecs, 256);
-    combine_kernel<<<static_cast<unsigned>(blocks < (1 << 30) ? blocks : 1 << 30), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
-        x, static_cast<const uint4*>(Ys), static_cast<uint4*>(Y));
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_beside(combine_kernel, static_cast<unsigned>(blocks < (1 << 30) ? blocks : 1 << 30), 256, 0, static_cast<cudaStream_t>(cuda_stream),
+                                        x, static_cast<const uint4*>(Ys), static_cast<uint4*>(Y));
     return e == cudaSuccess ? NK_OK : p->cuda("combine launch", e);
 }
 
@@ -204,9 +197,8 @@ nk_status_t nk_route_combine_backward(nk_route_t p, const void* dY, const void* 
     DeviceGuard guard(p->device);
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     const ExchangeParams x = exchange_params(p, slots, gates);
-    combine_backward_kernel<<<static_cast<unsigned>(div_up(p->d.tokens * p->d.topk, 8)), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
-        x, static_cast<const uint4*>(dY), static_cast<const uint4*>(Ys), static_cast<uint4*>(dYs), dgates);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_beside(combine_backward_kernel, static_cast<unsigned>(div_up(p->d.tokens * p->d.topk, 8)), 256, 0, static_cast<cudaStream_t>(cuda_stream),
+                                        x, static_cast<const uint4*>(dY), static_cast<const uint4*>(Ys), static_cast<uint4*>(dYs), dgates);
     return e == cudaSuccess ? NK_OK : p->cuda("combine backward launch", e);
 }
 

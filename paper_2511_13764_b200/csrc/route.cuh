@@ -3,6 +3,7 @@
 // floating-point atomics, and every sum in an order that does not depend on timing.
 #pragma once
 #include "half.cuh"
+#include "ptx.cuh"
 
 namespace nk {
 
@@ -172,6 +173,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_select_kernel(const Route
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t0 = blockIdx.x * p.per_block, t1 = min(p.tokens, t0 + p.per_block);
     for (int e = threadIdx.x; e < p.experts; e += ROUTE_THREADS) hist[e] = 0;
+    launch_wait();
+    launch_next();
     __syncthreads();
     for (int t = t0 + warp; t < t1; t += ROUTE_THREADS / 32) {
         route_token<V>(p, t, lane);
@@ -198,6 +201,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_place_kernel(const RouteP
     int* before = rows + 16 * p.experts;           // [experts]
     const int blocks = gridDim.x, E = p.experts;
     for (int e = threadIdx.x; e < E; e += ROUTE_THREADS) total[e] = before[e] = 0;
+    launch_wait();
+    launch_next();
     __syncthreads();
     // threads of a row of counts side by side, rows dealt out over what threads are left (integer sums: any order)
     const int lanes = min(E, ROUTE_THREADS), rowsets = ROUTE_THREADS / lanes;
@@ -232,6 +237,8 @@ template <int V>
 __global__ void __launch_bounds__(256) route_backward_kernel(const RouteParams p, const float* dgates, float* dlogits) {
     const int lane = threadIdx.x & 31;
     const int t = blockIdx.x * 8 + (threadIdx.x >> 5);
+    launch_wait();
+    launch_next();
     if (t >= p.tokens) return;
     float z[V], d[V];
     float m = -INFINITY;
@@ -309,6 +316,8 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8], int f16) {
 // a thread reads one piece of a token's row and writes it to the topk places
 __global__ void __launch_bounds__(256) dispatch_kernel(const ExchangeParams p, const uint4* x, uint4* xs) {
     const long long n = static_cast<long long>(p.tokens) * p.vecs, pairs = static_cast<long long>(p.tokens) * p.topk;
+    launch_wait();
+    launch_next();
     for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
         const long long t = i / p.vecs;
         const int v = static_cast<int>(i - t * p.vecs);
@@ -323,6 +332,8 @@ __global__ void __launch_bounds__(256) dispatch_kernel(const ExchangeParams p, c
 // a thread adds one piece of the topk rows of a token
 __global__ void __launch_bounds__(256) combine_kernel(const ExchangeParams p, const uint4* ys, uint4* y) {
     const long long n = static_cast<long long>(p.tokens) * p.vecs, pairs = static_cast<long long>(p.tokens) * p.topk;
+    launch_wait();
+    launch_next();
     for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
         const long long t = i / p.vecs;
         const int v = static_cast<int>(i - t * p.vecs);
@@ -345,6 +356,8 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const ExchangePar
     const int lane = threadIdx.x & 31;
     const long long pairs = static_cast<long long>(p.tokens) * p.topk;
     const long long i = blockIdx.x * 8ll + (threadIdx.x >> 5);
+    launch_wait();
+    launch_next();
     if (i >= pairs) return;
     const long long t = i / p.topk;
     const int s = p.slots[i];
