@@ -205,15 +205,20 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         most = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(most)));
         // Estimated time, in clocks, of n tiles of w rows, and into how many parts (1: none) the tiles of the last, partial wave are cut:
         // equal parts, so that no pair has parts of two tiles, where they fill at most half a wave.  A k-block of a tile costs about
-        // GRP_BLOCK + w / 8 whatever its width (operand feed; the tensor core alone would need 2 w); parts are written to memory
-        // and read back at the end, GRP_CUT_FIXED + GRP_CUT_ROW w if all pairs have one.
+        // GRP_BLOCK + w / 8 whatever its width (operand feed; the tensor core alone would need 2 w).  Parts are written to memory
+        // at the end and the last to arrive reads them all: about 4000 clocks, and for every part and row (64 at least: a warp's
+        // pieces follow one another) 10 + t^2 / 450, t being the parts of all tiles, which share the way to memory and back.
+        // So the best number of parts goes with the root of the contraction's length.
+        auto share_of = [&](int w, int t) { return static_cast<float>(max(64, w)) * (10.0f + static_cast<float>(t) * t * (1.0f / 450)); };
+        auto best_parts = [&](int kbs, int w, int t) {
+            return max(1, min(__float2int_rn(sqrtf(__fdividef(static_cast<float>(kbs) * GRP_BLOCK, share_of(w, t)))), kbs / 4));
+        };
         auto estimate = [&](int n, int w, int& parts) {
-            const int waves = n / num_pairs, rest = n - waves * num_pairs;
+            const int waves = n / num_pairs, rest = n - waves * num_pairs, most_parts = rest ? num_pairs / rest : 1;
             const float kb = GRP_BLOCK + w * 0.125f, k = static_cast<float>(p.kb_total), whole = (waves + (rest ? 1 : 0)) * k * kb;
-            parts = rest && p.partial ? min(num_pairs / rest, max(1, p.kb_total / 4)) : 1;
-            if (parts < 2) { parts = 1; return whole; }
-            const float cut = (waves * k + (p.kb_total + parts - 1) / parts) * kb + GRP_CUT_FIXED + __fdividef(GRP_CUT_ROW * w * rest * parts, static_cast<float>(num_pairs));
-            if (cut < whole) return cut;
+            parts = p.partial && most_parts > 1 ? min(most_parts, best_parts(p.kb_total, w, rest * most_parts)) : 1;
+            const float cut = (waves * k + (p.kb_total + parts - 1) / parts) * kb + 4000.0f + share_of(w, rest * parts) * parts;
+            if (parts > 1 && cut < whole) return cut;
             parts = 1;
             return whole;
         };
@@ -276,11 +281,14 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 const int g = find_last(s_pre, p.groups, from);
                 tail_base = s_alt[g] + (from - s_pre[g]) * length(g);
                 tail_len = blocks - tail_base;
-                share = max(4, (tail_len + num_pairs - 1) / num_pairs);
                 int longest = 0;
                 for (int h = g + lane; h < p.groups; h += 32) longest = max(longest, length(h));
                 longest = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(longest)));
-                if ((longest - share) * (GRP_BLOCK + GRP_TILE / 8) > GRP_CUT_FIXED + GRP_CUT_ROW * min(p.J, GRP_TILE)) tail_from = from;
+                const int w = min(p.J, GRP_TILE), n = tiles - from;
+                const int most_parts = best_parts(longest, w, min(2 * n, num_pairs + n));
+                share = max(max(4, (tail_len + num_pairs - 1) / num_pairs), (longest + most_parts - 1) / most_parts);
+                const int tile_parts = (longest + share - 1) / share + 1, all_parts = min(n * tile_parts, num_pairs + n);
+                if (static_cast<float>((longest - share) * GRP_BLOCK) > 4000.0f + share_of(w, all_parts) * tile_parts) tail_from = from;
             }
         } else {
             estimate(tiles, width, parts);

@@ -16,7 +16,7 @@ constexpr int GRP_BK = 64;
 constexpr int GRP_TILE = 256;                          // features of a tile, and the most rows of one
 constexpr int GRP_TABLE = 4 * (GRP_MAX_GROUPS + 1);    // bytes of a table by group
 constexpr int GRP_STAGING = 8 * 4096;                  // of the stores: two buffers of 2 KB for each epilogue warp
-constexpr int GRP_BLOCK = 600, GRP_CUT_FIXED = 3000, GRP_CUT_ROW = 80;   // estimated clocks (see grouped.cuh)
+constexpr int GRP_BLOCK = 600;                         // estimated clocks of a k-block (see grouped.cuh)
 constexpr int GRP_SMEM = GRP_RING + GRP_STAGING + 1024 + 3 * GRP_TABLE + 1024;
 
 constexpr int GRP_CHUNK = 8;                           // k-blocks between additions to the FP32 sums of FP32 results
