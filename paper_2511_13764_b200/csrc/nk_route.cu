@@ -57,7 +57,8 @@ static ExchangeParams exchange_params(const nk_route_s* p, const int32_t* slots,
     x.tokens = static_cast<int>(p->d.tokens);
     x.topk = static_cast<int>(p->d.topk);
     x.vecs = static_cast<int>(p->d.width / 8);
-    x.f16 = p->d.dtype == NK_F16;
+    // four pieces to a thread, but eight threads (128 bytes) to a row at least
+    while (x.lanes_log2 < 8 && (1 << x.lanes_log2) < x.vecs && (x.lanes_log2 < 3 || (4 << x.lanes_log2) < x.vecs)) ++x.lanes_log2;
     x.ld_tokens = p->d.ld_tokens / 8;
     x.ld_slots = p->d.ld_slots / 8;
     x.slots = slots;
@@ -81,6 +82,7 @@ nk_status_t nk_route_create(const nk_route_desc_t* desc, nk_route_t* out) {
     if (d.logits_dtype != NK_F32 && !is_half_type(d.logits_dtype)) return NK_ERR_UNSUPPORTED;
     if (!is_half_type(d.dtype)) return NK_ERR_UNSUPPORTED;
     if (d.tokens > (1 << 24) || d.experts > NK_ROUTE_MAX_EXPERTS || d.topk > NK_ROUTE_MAX_TOPK || d.width > (1 << 24)) return NK_ERR_UNSUPPORTED;
+    // (2^24 tokens of 32 choices: pairs stay below 2^31)
     if (d.width % 8 || d.ld_tokens % 8 || d.ld_slots % 8) return NK_ERR_MISALIGNED;
     if (d.ld_logits == 0) d.ld_logits = d.experts;
     if (d.ld_tokens == 0) d.ld_tokens = d.width;
@@ -94,7 +96,7 @@ nk_status_t nk_route_create(const nk_route_desc_t* desc, nk_route_t* out) {
     if (!p) return NK_ERR_INVALID_ARG;
     p->d = d;
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
-    p->per_block = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? ROUTE_ONE_BLOCK : div_up(d.tokens, sms) < 16 ? 16 : div_up(d.tokens, sms));
+    p->per_block = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? ROUTE_ONE_BLOCK : div_up(d.tokens, sms) < 32 ? 32 : div_up(d.tokens, sms));
     p->blocks = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? 1 : div_up(d.tokens, p->per_block));
     DeviceGuard guard(d.device);
     const int v = route_width(d.experts);
@@ -133,7 +135,7 @@ nk_status_t nk_route_run(nk_route_t p, const void* logits, float* gates, int32_t
     r.counts = static_cast<int*>(workspace);
     const int v = route_width(p->d.experts), smem = route_smem(r.experts);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    cudaError_t e = launch_beside(p->blocks == 1 ? select_kernel<true>(v) : select_kernel<false>(v), p->blocks, ROUTE_THREADS, smem, st, r);
+    cudaError_t e = launch_beside(p->blocks == 1 ? select_kernel<true>(v) : select_kernel<false>(v), p->blocks, route_threads(v), smem, st, r);
     if (e != cudaSuccess) return p->cuda("route select launch", e);
     if (p->blocks > 1) {
         if ((e = launch_beside(route_place_kernel, p->blocks, ROUTE_THREADS, smem, st, r)) != cudaSuccess) return p->cuda("route place launch", e);
@@ -167,9 +169,8 @@ nk_status_t nk_route_dispatch(nk_route_t p, const void* X, const int32_t* slots,
     DeviceGuard guard(p->device);
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     const ExchangeParams x = exchange_params(p, slots, nullptr);
-    const int64_t blocks = div_up(p->d.tokens * x.vecs, 256);
-    const cudaError_t e = launch_beside(dispatch_kernel, static_cast<unsigned>(blocks < (1 << 30) ? blocks : 1 << 30), 256, 0, static_cast<cudaStream_t>(cuda_stream),
-                                        x, static_cast<const uint4*>(X), static_cast<uint4*>(Xs));
+    const cudaError_t e = launch_beside(dispatch_kernel, static_cast<unsigned>(div_up(x.tokens, 256 >> x.lanes_log2)), 256, 0,
+                                        static_cast<cudaStream_t>(cuda_stream), x, static_cast<const uint4*>(X), static_cast<uint4*>(Xs));
     return e == cudaSuccess ? NK_OK : p->cuda("dispatch launch", e);
 }
 
@@ -181,9 +182,9 @@ nk_status_t nk_route_combine(nk_route_t p, const void* Ys, const int32_t* slots,
     DeviceGuard guard(p->device);
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     const ExchangeParams x = exchange_params(p, slots, gates);
-    const int64_t blocks = div_up(p->d.tokens * x.vecs, 256);
-    const cudaError_t e = launch_beside(combine_kernel, static_cast<unsigned>(blocks < (1 << 30) ? blocks : 1 << 30), 256, 0, static_cast<cudaStream_t>(cuda_stream),
-                                        x, static_cast<const uint4*>(Ys), static_cast<uint4*>(Y));
+    const cudaError_t e = launch_beside(p->d.dtype == NK_F16 ? combine_kernel<true> : combine_kernel<false>,
+                                        static_cast<unsigned>(div_up(x.tokens, 256 >> x.lanes_log2)), 256, 0, static_cast<cudaStream_t>(cuda_stream), x,
+                                        static_cast<const uint4*>(Ys), static_cast<uint4*>(Y));
     return e == cudaSuccess ? NK_OK : p->cuda("combine launch", e);
 }
 
@@ -197,7 +198,7 @@ nk_status_t nk_route_combine_backward(nk_route_t p, const void* dY, const void* 
     DeviceGuard guard(p->device);
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     const ExchangeParams x = exchange_params(p, slots, gates);
-    const cudaError_t e = launch_beside(combine_backward_kernel, static_cast<unsigned>(div_up(p->d.tokens * p->d.topk, 8)), 256, 0, static_cast<cudaStream_t>(cuda_stream),
+    const cudaError_t e = launch_beside(p->d.dtype == NK_F16 ? combine_backward_kernel<true> : combine_backward_kernel<false>, static_cast<unsigned>(div_up(p->d.tokens * p->d.topk, 8)), 256, 0, static_cast<cudaStream_t>(cuda_stream),
                                         x, static_cast<const uint4*>(dY), static_cast<const uint4*>(Ys), static_cast<uint4*>(dYs), dgates);
     return e == cudaSuccess ? NK_OK : p->cuda("combine backward launch", e);
 }

@@ -39,18 +39,19 @@ __device__ __forceinline__ float route_unkey(uint32_t k) {
 // One warp, one token: lane l holds experts l, l + 32, ...  (V of them).  topk rounds of a warp-wide maximum of the
 // keys and a minimum of the indices that have it.
 template <int V>
-__device__ __forceinline__ void route_token(const RouteParams& p, int t, int lane) {
+__device__ __forceinline__ void route_fetch(const RouteParams& p, int t, int lane, float (&z)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = lane + 32 * i < p.experts ? route_load(p, t, lane + 32 * i) : 0.0f;
+}
+template <int V>
+__device__ __forceinline__ int route_token(const RouteParams& p, int t, int lane, const float (&z)[V]) {
     uint32_t key[V];
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int e = lane + 32 * i;
-        key[i] = 0u;
-        if (e < p.experts) {
-            const float z = route_load(p, t, e);
-            nan |= z != z;
-            key[i] = route_key(z);
-        }
+        const bool there = lane + 32 * i < p.experts;
+        nan |= there && z[i] != z[i];
+        key[i] = there ? route_key(z[i]) : 0u;
     }
     nan = __any_sync(~0u, nan);
     uint32_t own_key = 0u;                     // lane j keeps choice j
@@ -94,6 +95,7 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int t, int lan
         p.gates[o] = nan ? __int_as_float(0x7FC00000) : none ? 0.0f : mine / sum;
         p.chosen[o] = own;
     }
+    return own;
 }
 
 // exclusive scan of s[0..n) in place by the whole block (n <= 1024, at least 32 threads); returns the total
@@ -150,45 +152,58 @@ __device__ __forceinline__ void route_places(const RouteParams& p, int t0, int t
         }
     }
     __syncthreads();
-    for (int t = lo; t < hi; ++t) {
-        if (lane < p.topk) {
-            const size_t o = static_cast<size_t>(t) * p.topk + lane;
-            p.slots[o] = mine[p.chosen[o]]++;      // a token's experts are distinct
+    for (int t = lo; t < hi; t += 4) {             // four tokens' choices on the way at a time
+        const size_t o = static_cast<size_t>(t) * p.topk + lane;
+        int e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = lane < p.topk && t + i < hi ? p.chosen[o + i * p.topk] : -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (e[i] >= 0) p.slots[o + i * p.topk] = mine[e[i]]++;      // a token's experts are distinct
+            __syncwarp();
         }
-        __syncwarp();
     }
 }
 
-constexpr int ROUTE_THREADS = 512;                 // both kernels; 16 warps
+constexpr int ROUTE_THREADS = 1024;                // of both kernels; a lane of route_select_kernel that holds 16 experts or more
+                                                   // needs the registers of 512
+__host__ __device__ constexpr int route_threads(int v) { return v >= 16 ? 512 : ROUTE_THREADS; }
 constexpr int ROUTE_ONE_BLOCK = 64;                // up to this many tokens one block does everything
-__host__ __device__ constexpr int route_smem(int experts) { return (16 * experts + 2 * experts + 64) * 4; }
+__host__ __device__ constexpr int route_smem(int experts) { return (ROUTE_THREADS / 32 * experts + 2 * experts + 64) * 4; }
 
 // A block of tokens: choices, weights, and the block's counts by expert.  ONE: the only block; it goes on to the places.
 template <int V, bool ONE>
-__global__ void __launch_bounds__(ROUTE_THREADS) route_select_kernel(const RouteParams p) {
+__global__ void __launch_bounds__(route_threads(V)) route_select_kernel(const RouteParams p) {
+    constexpr int THREADS = route_threads(V), WARPS = THREADS / 32;
     extern __shared__ int route_sm[];
     int* hist = route_sm;                          // [experts]
     int* part = hist + p.experts;                  // [64]
-    int* rows = part + 64;                         // [16][experts] (ONE)
+    int* rows = part + 64;                         // [warps][experts] (ONE)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t0 = blockIdx.x * p.per_block, t1 = min(p.tokens, t0 + p.per_block);
-    for (int e = threadIdx.x; e < p.experts; e += ROUTE_THREADS) hist[e] = 0;
+    for (int e = threadIdx.x; e < p.experts; e += THREADS) hist[e] = 0;
     launch_wait();
     launch_next();
     __syncthreads();
-    for (int t = t0 + warp; t < t1; t += ROUTE_THREADS / 32) {
-        route_token<V>(p, t, lane);
-        __syncwarp();
-        if (lane < p.topk) atomicAdd(hist + p.chosen[static_cast<size_t>(t) * p.topk + lane], 1);
+    // the next token's logits are on the way while one is worked on
+    float z[V];
+    if (t0 + warp < t1) route_fetch<V>(p, t0 + warp, lane, z);
+    for (int t = t0 + warp; t < t1; t += WARPS) {
+        float now[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) now[i] = z[i];
+        if (t + WARPS < t1) route_fetch<V>(p, t + WARPS, lane, z);
+        const int e = route_token<V>(p, t, lane, now);
+        if (lane < p.topk) atomicAdd(hist + e, 1);
     }
     __syncthreads();
     if (ONE) {
         const int total = block_scan(hist, p.experts, part);
-        for (int e = threadIdx.x; e < p.experts; e += ROUTE_THREADS) p.offsets[e] = hist[e];
+        for (int e = threadIdx.x; e < p.experts; e += THREADS) p.offsets[e] = hist[e];
         if (threadIdx.x == 0) p.offsets[p.experts] = total;
         route_places(p, t0, t1, hist, rows);
     } else {
-        for (int e = threadIdx.x; e < p.experts; e += ROUTE_THREADS) p.counts[static_cast<size_t>(blockIdx.x) * p.experts + e] = hist[e];
+        for (int e = threadIdx.x; e < p.experts; e += THREADS) p.counts[static_cast<size_t>(blockIdx.x) * p.experts + e] = hist[e];
     }
 }
 
@@ -197,8 +212,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_place_kernel(const RouteP
     extern __shared__ int route_sm[];
     int* total = route_sm;                         // [experts]
     int* part = total + p.experts;                 // [64]
-    int* rows = part + 64;                         // [16][experts]
-    int* before = rows + 16 * p.experts;           // [experts]
+    int* rows = part + 64;                         // [warps][experts]
+    int* before = rows + ROUTE_THREADS / 32 * p.experts;   // [experts]
     const int blocks = gridDim.x, E = p.experts;
     for (int e = threadIdx.x; e < E; e += ROUTE_THREADS) total[e] = before[e] = 0;
     launch_wait();
@@ -240,24 +255,26 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const RouteParams p
     launch_wait();
     launch_next();
     if (t >= p.tokens) return;
+    const size_t o = static_cast<size_t>(t) * p.topk;
+    uint32_t taken = 0u;                           // bit i: this lane's expert i is one of the chosen
+    const int own = lane < p.topk ? p.chosen[o + lane] : -1;
+    const float own_d = lane < p.topk ? dgates[o + lane] : 0.0f;
     float z[V], d[V];
-    float m = -INFINITY;
+    uint32_t top = 0u;
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int e = lane + 32 * i;
         z[i] = e < p.experts ? route_load(p, t, e) : -INFINITY;
         d[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
         nan |= z[i] != z[i];
-        m = fmaxf(m, z[i]);
+        top = max(top, route_key(z[i]));
     }
     nan = __any_sync(~0u, nan);
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, s));
-    const size_t o = static_cast<size_t>(t) * p.topk;
-    uint32_t taken = 0u;                           // bit i: this lane's expert i is one of the chosen
-    const int own = lane < p.topk ? p.chosen[o + lane] : -1;
-    const float own_d = lane < p.topk ? dgates[o + lane] : 0.0f;
+    const float m = route_unkey(__reduce_max_sync(~0u, top));
     for (int j = 0; j < p.topk; ++j) {
         const int e = __shfl_sync(~0u, own, j);
         const float g = __shfl_sync(~0u, own_d, j);
@@ -295,89 +312,130 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const RouteParams p
 // ---------------------------------------------------------------- rows to their experts' order and back
 struct ExchangeParams {
     int tokens, topk, vecs;     // vecs: 16-byte pieces of a row
-    int f16;
+    int lanes_log2;             // threads to a row of dispatch and combine
     long long ld_tokens, ld_slots;   // in 16-byte pieces
     const int* slots;
     const float* gates;
 };
 
-__device__ __forceinline__ void unpack8(const uint4& v, int f16, float (&x)[8]) {
+template <bool F16>
+__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        x[2 * i] = half_bits_to_f32(w[i] & 0xFFFFu, f16);
-        x[2 * i + 1] = half_bits_to_f32(w[i] >> 16, f16);
+        x[2 * i] = half_bits_to_f32(w[i] & 0xFFFFu, F16);
+        x[2 * i + 1] = half_bits_to_f32(w[i] >> 16, F16);
     }
 }
-__device__ __forceinline__ uint4 pack8(const float (&x)[8], int f16) {
-    return make_uint4(pack_half2(x[0], x[1], f16), pack_half2(x[2], x[3], f16), pack_half2(x[4], x[5], f16), pack_half2(x[6], x[7], f16));
+template <bool F16>
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+    return make_uint4(pack_half2(x[0], x[1], F16), pack_half2(x[2], x[3], F16), pack_half2(x[4], x[5], F16), pack_half2(x[6], x[7], F16));
 }
 
-// a thread reads one piece of a token's row and writes it to the topk places
+// A block of 256 threads has the rows of 256 >> p.lanes_log2 tokens, 1 << p.lanes_log2 threads to a row.  (One index over all
+// pieces of all rows and a division by a row's pieces cost as many instructions as the sum itself.)
+__device__ __forceinline__ int exchange_token(const ExchangeParams& p) {
+    return blockIdx.x * (256 >> p.lanes_log2) + (threadIdx.x >> p.lanes_log2);
+}
+
+// a thread reads four pieces of a token's row and writes them to the topk places
 __global__ void __launch_bounds__(256) dispatch_kernel(const ExchangeParams p, const uint4* x, uint4* xs) {
-    const long long n = static_cast<long long>(p.tokens) * p.vecs, pairs = static_cast<long long>(p.tokens) * p.topk;
+    const int t = exchange_token(p), lanes = 1 << p.lanes_log2;
     launch_wait();
     launch_next();
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-        const long long t = i / p.vecs;
-        const int v = static_cast<int>(i - t * p.vecs);
-        const uint4 r = x[t * p.ld_tokens + v];
+    if (t >= p.tokens) return;
+    const int* slots = p.slots + static_cast<size_t>(t) * p.topk;
+    const unsigned pairs = static_cast<unsigned>(p.tokens) * p.topk;
+    x += t * p.ld_tokens;
+    for (int v = threadIdx.x & (lanes - 1); v < p.vecs; v += 4 * lanes) {
+        uint4 piece[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+            if (v + n * lanes < p.vecs) piece[n] = __ldcs(x + v + n * lanes);
         for (int j = 0; j < p.topk; ++j) {
-            const int s = __ldg(p.slots + t * p.topk + j);
-            if (s >= 0 && s < pairs) xs[s * p.ld_slots + v] = r;
+            const unsigned s = __ldg(slots + j);
+            if (s >= pairs) continue;
+            uint4* row = xs + s * p.ld_slots + v;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                if (v + n * lanes < p.vecs) row[n * lanes] = piece[n];
         }
     }
 }
 
-// a thread adds one piece of the topk rows of a token
+// a thread adds four pieces of the topk rows of a token
+template <bool F16>
 __global__ void __launch_bounds__(256) combine_kernel(const ExchangeParams p, const uint4* ys, uint4* y) {
-    const long long n = static_cast<long long>(p.tokens) * p.vecs, pairs = static_cast<long long>(p.tokens) * p.topk;
+    const int t = exchange_token(p), lanes = 1 << p.lanes_log2;
     launch_wait();
     launch_next();
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-        const long long t = i / p.vecs;
-        const int v = static_cast<int>(i - t * p.vecs);
-        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int j = 0; j < p.topk; ++j) {
-            const int s = __ldg(p.slots + t * p.topk + j);
-            if (s < 0 || s >= pairs) continue;
-            const float g = p.gates ? __ldg(p.gates + t * p.topk + j) : 1.0f;
-            float r[8];
-            unpack8(ys[s * p.ld_slots + v], p.f16, r);
+    if (t >= p.tokens) return;
+    const int* slots = p.slots + static_cast<size_t>(t) * p.topk;
+    const float* gates = p.gates ? p.gates + static_cast<size_t>(t) * p.topk : nullptr;
+    const unsigned pairs = static_cast<unsigned>(p.tokens) * p.topk;
+    y += t * p.ld_tokens;
+    // four pieces of a row at a time: where the rows are is known only after the slots have come, and then every load
+    // that can be on the way has to be
+    for (int v = threadIdx.x & (lanes - 1); v < p.vecs; v += 4 * lanes) {
+        float sum[4][8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) sum[q] += g * r[q];
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[n][q] = 0.0f;
+#pragma unroll 2
+        for (int j = 0; j < p.topk; ++j) {
+            const unsigned s = __ldg(slots + j);
+            if (s >= pairs) continue;
+            const float g = gates ? __ldg(gates + j) : 1.0f;
+            const uint4* row = ys + s * p.ld_slots + v;
+            uint4 piece[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                if (v + n * lanes < p.vecs) piece[n] = __ldcs(row + n * lanes);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                float r[8];
+                unpack8<F16>(piece[n], r);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) sum[n][q] += g * r[q];
+            }
         }
-        y[t * p.ld_tokens + v] = pack8(sum, p.f16);
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+            if (v + n * lanes < p.vecs) y[v + n * lanes] = pack8<F16>(sum[n]);
     }
 }
 
 // a warp per (token, j): the pair's row of dYs, and the product of two rows for its dgates
+template <bool F16>
 __global__ void __launch_bounds__(256) combine_backward_kernel(const ExchangeParams p, const uint4* dy, const uint4* ys, uint4* dys, float* dgates) {
     const int lane = threadIdx.x & 31;
-    const long long pairs = static_cast<long long>(p.tokens) * p.topk;
-    const long long i = blockIdx.x * 8ll + (threadIdx.x >> 5);
+    const unsigned pairs = static_cast<unsigned>(p.tokens) * p.topk;
+    const unsigned i = blockIdx.x * 8u + (threadIdx.x >> 5);
     launch_wait();
     launch_next();
     if (i >= pairs) return;
-    const long long t = i / p.topk;
-    const int s = p.slots[i];
-    if (s < 0 || s >= pairs) {
+    const unsigned t = i / static_cast<unsigned>(p.topk), s = p.slots[i];
+    if (s >= pairs) {
         if (lane == 0) dgates[i] = 0.0f;
         return;
     }
     const float g = p.gates[i];
+    dy += t * p.ld_tokens;
+    ys += s * p.ld_slots;
+    dys += s * p.ld_slots;
     float dot = 0.0f;
 #pragma unroll 4
     for (int v = lane; v < p.vecs; v += 32) {
         float a[8], b[8];
-        unpack8(dy[t * p.ld_tokens + v], p.f16, a);
-        unpack8(ys[s * p.ld_slots + v], p.f16, b);
+        unpack8<F16>(dy[v], a);
+        unpack8<F16>(ys[v], b);
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             dot += a[q] * b[q];
             a[q] *= g;
         }
-        dys[s * p.ld_slots + v] = pack8(a, p.f16);
+        dys[v] = pack8<F16>(a);
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) dot += __shfl_xor_sync(~0u, dot, d);
