@@ -823,17 +823,15 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     to_slab(f, set * 32 + q * 64);
                 }
                 if (held) release();
-                __threadfence();
                 __syncwarp();
                 bool done = false;
                 if (lane < mine) {
                     unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + set + 2 * lane;
-                    const unsigned int old = (atomicAdd(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
+                    const unsigned int old = (atomic_add_acq_rel(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
                     done = old == static_cast<unsigned>(u.parts) - 1u;
                     if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
                 }
                 last = __ballot_sync(~0u, done);
-                __threadfence();
             }
 #pragma unroll 1
             for (int q = 0; q < mine; ++q) {

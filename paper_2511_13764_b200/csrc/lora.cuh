@@ -90,42 +90,36 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
     const int kw = ((p.K + LORA_CLUSTER * 8 - 1) / (LORA_CLUSTER * 8)) * 8, k_lo = min(p.K, static_cast<int>(crank) * kw), k_hi = min(p.K, k_lo + kw);
     const int nw = ((p.N + LORA_CLUSTER * 8 - 1) / (LORA_CLUSTER * 8)) * 8, n_lo = min(p.N, static_cast<int>(crank) * nw), n_hi = min(p.N, n_lo + nw);
 
-    for (int i = threadIdx.x; i < RT * R; i += LORA_THREADS) share[i] = 0.0f;
-    // part[warp][r][RT] (row-major weights only): each warp's sums
-    for (int k0 = k_lo; k0 < k_hi; k0 += LORA_KSTEP) {
-        const int kn = min(LORA_KSTEP, k_hi - k0);
-        __syncthreads();
-        // X as FP32, [k][RT]; eight of k to a thread
-        for (int i = threadIdx.x; i < RT * (LORA_KSTEP / 8); i += LORA_THREADS) {
-            const int t = i / (LORA_KSTEP / 8), k = (i - t * (LORA_KSTEP / 8)) * 8;
-            if (k >= kn) continue;
-            float x[8];
-            lora_unpack8(t < n ? *reinterpret_cast<const uint4*>(X + static_cast<size_t>(row0 + t) * p.ldx + k0 + k) : make_uint4(0, 0, 0, 0), p.f16, x);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) xs[(k + q) * RT + t] = x[q];
+    // B's part of this CTA is on its way to L2 while A is worked on
+    {
+        const size_t first = p.transposed ? static_cast<size_t>(n_lo) * R : n_lo, line = 64;   // elements of 128 bytes
+        if (p.transposed) {
+            for (size_t i = threadIdx.x * line; i < static_cast<size_t>(n_hi - n_lo) * R; i += LORA_THREADS * line)
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(B + first + i));
+        } else {
+            const int lines = (n_hi - n_lo + 63) / 64;
+            for (int i = threadIdx.x; i < R * lines; i += LORA_THREADS)
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(B + static_cast<size_t>(i / lines) * p.N + first + (i % lines) * line));
         }
-        __syncthreads();
+    }
+    if (RT == 1) {
+        // One row: X straight from memory, every load independent of the others.
+        const uint16_t* x = X + static_cast<size_t>(row0) * p.ldx;
         if (p.transposed) {
             // a warp per rank, lanes along k
             for (int r = warp; r < R; r += LORA_THREADS / 32) {
-                float acc[RT];
-#pragma unroll
-                for (int t = 0; t < RT; ++t) acc[t] = 0.0f;
+                float acc = 0.0f;
 #pragma unroll 2
-                for (int k = lane * 8; k < kn; k += 256) {
-                    float w[8];
-                    lora_unpack8(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k0 + k)), p.f16, w);
+                for (int k = k_lo + lane * 8; k < k_hi; k += 256) {
+                    float w[8], y[8];
+                    lora_unpack8(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k)), p.f16, w);
+                    lora_unpack8(__ldg(reinterpret_cast<const uint4*>(x + k)), p.f16, y);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-#pragma unroll
-                        for (int t = 0; t < RT; ++t) acc[t] += w[q] * xs[(k + q) * RT + t];
+                    for (int q = 0; q < 8; ++q) acc += w[q] * y[q];
                 }
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-#pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) acc[t] += __shfl_xor_sync(~0u, acc[t], d);
-                    if (lane == 0) share[r * RT + t] += acc[t];
-                }
+                for (int d = 16; d > 0; d >>= 1) acc += __shfl_xor_sync(~0u, acc, d);
+                if (lane == 0) share[r] = acc;
             }
         } else {
             // lanes along pairs of ranks, then along k; warps along k; the warps' sums meet in shared memory
@@ -135,39 +129,113 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
             const int kl = lane / wide, deep = 32 / wide;
             for (int r0 = 0; r0 < pairs; r0 += wide) {
                 const int pr = r0 + lane % wide;
-                float acc0[RT], acc1[RT];
-#pragma unroll
-                for (int t = 0; t < RT; ++t) acc0[t] = acc1[t] = 0.0f;
+                float acc0 = 0.0f, acc1 = 0.0f;
                 if (pr < pairs) {
 #pragma unroll 8
-                    for (int k = warp * deep + kl; k < kn; k += deep * (LORA_THREADS / 32)) {
-                        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(A + static_cast<size_t>(k0 + k) * R) + pr);
-                        const float w0 = half_bits_to_f32(w & 0xFFFFu, p.f16), w1 = half_bits_to_f32(w >> 16, p.f16);
-#pragma unroll
-                        for (int t = 0; t < RT; ++t) {
-                            acc0[t] += w0 * xs[k * RT + t];
-                            acc1[t] += w1 * xs[k * RT + t];
-                        }
+                    for (int k = k_lo + warp * deep + kl; k < k_hi; k += deep * (LORA_THREADS / 32)) {
+                        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(A + static_cast<size_t>(k) * R) + pr);
+                        const float y = half_bits_to_f32(__ldg(x + k), p.f16);
+                        acc0 += half_bits_to_f32(w & 0xFFFFu, p.f16) * y;
+                        acc1 += half_bits_to_f32(w >> 16, p.f16) * y;
                     }
                 }
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    for (int d = wide; d < 32; d <<= 1) {
-                        acc0[t] += __shfl_xor_sync(~0u, acc0[t], d);
-                        acc1[t] += __shfl_xor_sync(~0u, acc1[t], d);
-                    }
-                    if (kl == 0 && pr < pairs) {
-                        part[(warp * R + 2 * pr) * RT + t] = acc0[t];
-                        part[(warp * R + 2 * pr + 1) * RT + t] = acc1[t];
-                    }
+                for (int d = wide; d < 32; d <<= 1) {
+                    acc0 += __shfl_xor_sync(~0u, acc0, d);
+                    acc1 += __shfl_xor_sync(~0u, acc1, d);
+                }
+                if (kl == 0 && pr < pairs) {
+                    part[warp * R + 2 * pr] = acc0;
+                    part[warp * R + 2 * pr + 1] = acc1;
                 }
             }
             __syncthreads();
-            for (int i = threadIdx.x; i < R * RT; i += LORA_THREADS) {
-                float s = share[i];
+            for (int i = threadIdx.x; i < R; i += LORA_THREADS) {
+                float s = 0.0f;
 #pragma unroll
-                for (int w = 0; w < LORA_THREADS / 32; ++w) s += part[w * R * RT + i];
+                for (int w = 0; w < LORA_THREADS / 32; ++w) s += part[w * R + i];
                 share[i] = s;
+            }
+        }
+    } else {
+        for (int i = threadIdx.x; i < RT * R; i += LORA_THREADS) share[i] = 0.0f;
+        // part[warp][r][RT] (row-major weights only): each warp's sums
+        for (int k0 = k_lo; k0 < k_hi; k0 += LORA_KSTEP) {
+            const int kn = min(LORA_KSTEP, k_hi - k0);
+            __syncthreads();
+            // X as FP32, [k][RT]; eight of k to a thread
+            for (int i = threadIdx.x; i < RT * (LORA_KSTEP / 8); i += LORA_THREADS) {
+                const int t = i / (LORA_KSTEP / 8), k = (i - t * (LORA_KSTEP / 8)) * 8;
+                if (k >= kn) continue;
+                float x[8];
+                lora_unpack8(t < n ? *reinterpret_cast<const uint4*>(X + static_cast<size_t>(row0 + t) * p.ldx + k0 + k) : make_uint4(0, 0, 0, 0), p.f16, x);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) xs[(k + q) * RT + t] = x[q];
+            }
+            __syncthreads();
+            if (p.transposed) {
+                // a warp per rank, lanes along k
+                for (int r = warp; r < R; r += LORA_THREADS / 32) {
+                    float acc[RT];
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) acc[t] = 0.0f;
+#pragma unroll 2
+                    for (int k = lane * 8; k < kn; k += 256) {
+                        float w[8];
+                        lora_unpack8(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k0 + k)), p.f16, w);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+#pragma unroll
+                            for (int t = 0; t < RT; ++t) acc[t] += w[q] * xs[(k + q) * RT + t];
+                    }
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+                        for (int d = 16; d > 0; d >>= 1) acc[t] += __shfl_xor_sync(~0u, acc[t], d);
+                        if (lane == 0) share[r * RT + t] += acc[t];
+                    }
+                }
+            } else {
+                // lanes along pairs of ranks, then along k; warps along k; the warps' sums meet in shared memory
+                const int pairs = R / 2;
+                int wide = 4;
+                while (wide < pairs && wide < 32) wide *= 2;            // lanes for one k
+                const int kl = lane / wide, deep = 32 / wide;
+                for (int r0 = 0; r0 < pairs; r0 += wide) {
+                    const int pr = r0 + lane % wide;
+                    float acc0[RT], acc1[RT];
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) acc0[t] = acc1[t] = 0.0f;
+                    if (pr < pairs) {
+#pragma unroll 8
+                        for (int k = warp * deep + kl; k < kn; k += deep * (LORA_THREADS / 32)) {
+                            const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(A + static_cast<size_t>(k0 + k) * R) + pr);
+                            const float w0 = half_bits_to_f32(w & 0xFFFFu, p.f16), w1 = half_bits_to_f32(w >> 16, p.f16);
+#pragma unroll
+                            for (int t = 0; t < RT; ++t) {
+                                acc0[t] += w0 * xs[k * RT + t];
+                                acc1[t] += w1 * xs[k * RT + t];
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        for (int d = wide; d < 32; d <<= 1) {
+                            acc0[t] += __shfl_xor_sync(~0u, acc0[t], d);
+                            acc1[t] += __shfl_xor_sync(~0u, acc1[t], d);
+                        }
+                        if (kl == 0 && pr < pairs) {
+                            part[(warp * R + 2 * pr) * RT + t] = acc0[t];
+                            part[(warp * R + 2 * pr + 1) * RT + t] = acc1[t];
+                        }
+                    }
+                }
+                __syncthreads();
+                for (int i = threadIdx.x; i < R * RT; i += LORA_THREADS) {
+                    float s = share[i];
+#pragma unroll
+                    for (int w = 0; w < LORA_THREADS / 32; ++w) s += part[w * R * RT + i];
+                    share[i] = s;
+                }
             }
         }
     }
@@ -250,13 +318,16 @@ __global__ void __launch_bounds__(LORA_THREADS, 4) __cluster_dims__(LORA_CLUSTER
     const int clusters = gridDim.x / LORA_CLUSTER, cluster = blockIdx.x / LORA_CLUSTER;
     if (p.few) {
         // rows without an adapter add nothing: zeros (rows of no request among them)
-        const int stride = gridDim.x * LORA_THREADS;
-        for (int q = -1; q <= p.requests; ++q) {
-            if (q >= 0 && q < p.requests && (s_pre[q + 1] > s_pre[q] || s_row[q + 1] == s_row[q])) continue;
-            const int lo = q < 0 ? 0 : s_row[q], hi = q < 0 ? s_row[0] : q == p.requests ? p.rows : s_row[q + 1];
-            const size_t first = static_cast<size_t>(lo) * p.N / 4, last = static_cast<size_t>(hi) * p.N / 4;
-            for (size_t i = first + blockIdx.x * LORA_THREADS + threadIdx.x; i < last; i += stride)
-                reinterpret_cast<float4*>(p.D)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int t = blockIdx.x; t < p.rows; t += gridDim.x) {
+            int lo = 0, hi = p.requests + 1;               // the last request that begins at or before the row
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s_row[mid] <= t) lo = mid;
+                else hi = mid;
+            }
+            if (lo < p.requests && s_row[lo] <= t && s_pre[lo + 1] > s_pre[lo]) continue;
+            float4* d = reinterpret_cast<float4*>(p.D + static_cast<size_t>(t) * p.N);
+            for (int i = threadIdx.x; i < p.N / 4; i += LORA_THREADS) d[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
     // few: chunk after chunk; else request after request

@@ -102,6 +102,14 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t
 __device__ __forceinline__ void launch_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// Add to a counter in global memory; what this thread has seen before is visible to whoever sees the sum, and the other
+// way round (with a __syncwarp on the near side this holds for what the warp's other lanes wrote or read, too).
+__device__ __forceinline__ unsigned int atomic_add_acq_rel(unsigned int* p, unsigned int x) {
+    unsigned int old;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(x) : "memory");
+    return old;
+}
+
 // ---------------------------------------------------------------- cp.async
 // Asynchronous 4-byte copy global -> shared; `src_bytes` = 0 writes zeros instead.
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src, uint32_t src_bytes) {
