@@ -18,7 +18,7 @@ constexpr int LORA_KSTEP = 256;                 // k of X kept in shared memory 
 
 struct LoraParams {
     int rows, N, K, rank, adapters, requests;
-    int transposed, f16;
+    int transposed;
     int few;                                    // 0: requests of up to LORA_ROWS rows, their rows one behind the other in D
                                                 // 1: all requests, D like Y, rows without an adapter zero
     long long ldx;
@@ -68,17 +68,18 @@ __device__ __forceinline__ int lora_prefix(const LoraParams& p, int* s_row, int*
     return s_pre[p.requests];
 }
 
-__device__ __forceinline__ void lora_unpack8(const uint4& v, int f16, float (&x)[8]) {
+template <bool F16>
+__device__ __forceinline__ void lora_unpack8(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        x[2 * i] = half_bits_to_f32(w[i] & 0xFFFFu, f16);
-        x[2 * i + 1] = half_bits_to_f32(w[i] >> 16, f16);
+        x[2 * i] = half_bits_to_f32(w[i] & 0xFFFFu, F16);
+        x[2 * i + 1] = half_bits_to_f32(w[i] >> 16, F16);
     }
 }
 
 // RT rows (1 or LORA_ROWS) of one request; `n` of them exist.  h: this CTA's share of X . A_a, then the whole of it.
-template <int RT>
+template <int RT, bool F16>
 __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n, int a, size_t d_row, uint32_t crank, float* xs, float* part,
                                            float* share, float* h) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -112,8 +113,8 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
 #pragma unroll 2
                 for (int k = k_lo + lane * 8; k < k_hi; k += 256) {
                     float w[8], y[8];
-                    lora_unpack8(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k)), p.f16, w);
-                    lora_unpack8(__ldg(reinterpret_cast<const uint4*>(x + k)), p.f16, y);
+                    lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k)), w);
+                    lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(x + k)), y);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) acc += w[q] * y[q];
                 }
@@ -122,31 +123,29 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
                 if (lane == 0) share[r] = acc;
             }
         } else {
-            // lanes along pairs of ranks, then along k; warps along k; the warps' sums meet in shared memory
-            const int pairs = R / 2;
-            int wide = 4;
-            while (wide < pairs && wide < 32) wide *= 2;            // lanes for one k
-            const int kl = lane / wide, deep = 32 / wide;
-            for (int r0 = 0; r0 < pairs; r0 += wide) {
-                const int pr = r0 + lane % wide;
-                float acc0 = 0.0f, acc1 = 0.0f;
-                if (pr < pairs) {
-#pragma unroll 8
-                    for (int k = k_lo + warp * deep + kl; k < k_hi; k += deep * (LORA_THREADS / 32)) {
-                        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(A + static_cast<size_t>(k) * R) + pr);
-                        const float y = half_bits_to_f32(__ldg(x + k), p.f16);
-                        acc0 += half_bits_to_f32(w & 0xFFFFu, p.f16) * y;
-                        acc1 += half_bits_to_f32(w >> 16, p.f16) * y;
-                    }
+            // lanes along eights of ranks, then along k; warps along k; the warps' sums meet in shared memory
+            int wide = 1;
+            while (wide * 8 < R) wide *= 2;                         // lanes for one k
+            const int kl = lane / wide, deep = 32 / wide, r = (lane % wide) * 8;
+            float acc[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) acc[q] = 0.0f;
+            if (r < R) {
+#pragma unroll 4
+                for (int k = k_lo + warp * deep + kl; k < k_hi; k += deep * (LORA_THREADS / 32)) {
+                    float w[8];
+                    lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(k) * R + r)), w);
+                    const float y = half_bits_to_f32(__ldg(x + k), F16);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) acc[q] += w[q] * y;
                 }
-                for (int d = wide; d < 32; d <<= 1) {
-                    acc0 += __shfl_xor_sync(~0u, acc0, d);
-                    acc1 += __shfl_xor_sync(~0u, acc1, d);
-                }
-                if (kl == 0 && pr < pairs) {
-                    part[warp * R + 2 * pr] = acc0;
-                    part[warp * R + 2 * pr + 1] = acc1;
-                }
+            }
+            for (int d = wide; d < 32; d <<= 1)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) acc[q] += __shfl_xor_sync(~0u, acc[q], d);
+            if (kl == 0 && r < R) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) part[warp * R + r + q] = acc[q];
             }
             __syncthreads();
             for (int i = threadIdx.x; i < R; i += LORA_THREADS) {
@@ -167,7 +166,7 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
                 const int t = i / (LORA_KSTEP / 8), k = (i - t * (LORA_KSTEP / 8)) * 8;
                 if (k >= kn) continue;
                 float x[8];
-                lora_unpack8(t < n ? *reinterpret_cast<const uint4*>(X + static_cast<size_t>(row0 + t) * p.ldx + k0 + k) : make_uint4(0, 0, 0, 0), p.f16, x);
+                lora_unpack8<F16>(t < n ? *reinterpret_cast<const uint4*>(X + static_cast<size_t>(row0 + t) * p.ldx + k0 + k) : make_uint4(0, 0, 0, 0), x);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) xs[(k + q) * RT + t] = x[q];
             }
@@ -181,7 +180,7 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
 #pragma unroll 2
                     for (int k = lane * 8; k < kn; k += 256) {
                         float w[8];
-                        lora_unpack8(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k0 + k)), p.f16, w);
+                        lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k0 + k)), w);
 #pragma unroll
                         for (int q = 0; q < 8; ++q)
 #pragma unroll
@@ -209,7 +208,7 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
 #pragma unroll 8
                         for (int k = warp * deep + kl; k < kn; k += deep * (LORA_THREADS / 32)) {
                             const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(A + static_cast<size_t>(k0 + k) * R) + pr);
-                            const float w0 = half_bits_to_f32(w & 0xFFFFu, p.f16), w1 = half_bits_to_f32(w >> 16, p.f16);
+                            const float w0 = half_bits_to_f32(w & 0xFFFFu, F16), w1 = half_bits_to_f32(w >> 16, F16);
 #pragma unroll
                             for (int t = 0; t < RT; ++t) {
                                 acc0[t] += w0 * xs[k * RT + t];
@@ -257,7 +256,34 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
     cluster_arrive();          // `share` may be written again once every CTA has read it
     cluster_wait();
     __syncthreads();
-    if (p.transposed) {
+    if (RT == 1 && !p.transposed) {
+        // threads along eights of columns, the rest of them along the ranks; their sums meet in shared memory
+        const int eights = (n_hi - n_lo) / 8, groups = max(1, LORA_THREADS / max(1, eights));
+        for (int e0 = 0; e0 < eights; e0 += LORA_THREADS) {
+            const int wide = min(eights - e0, LORA_THREADS), g = threadIdx.x / wide, e = threadIdx.x - g * wide;
+            if (g < groups) {
+                float acc[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) acc[q] = 0.0f;
+#pragma unroll 4
+                for (int r = g; r < R; r += groups) {
+                    float w[8];
+                    lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(B + static_cast<size_t>(r) * p.N + n_lo + (e0 + e) * 8)), w);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) acc[q] += w[q] * h[r];
+                }
+#pragma unroll
+                for (int q = 0; q < 8; ++q) xs[(g * wide + e) * 8 + q] = acc[q];
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < wide * 8; i += LORA_THREADS) {
+                float s = xs[i];
+                for (int z = 1; z < groups; ++z) s += xs[z * wide * 8 + i];
+                p.D[d_row * p.N + n_lo + e0 * 8 + i] = s;
+            }
+            __syncthreads();
+        }
+    } else if (p.transposed) {
         for (int i = n_lo + threadIdx.x; i < n_hi; i += LORA_THREADS) {
             float acc[RT];
 #pragma unroll
@@ -265,7 +291,7 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
 #pragma unroll 4
             for (int r = 0; r < R; r += 8) {
                 float w[8];
-                lora_unpack8(__ldg(reinterpret_cast<const uint4*>(B + static_cast<size_t>(i) * R + r)), p.f16, w);
+                lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(B + static_cast<size_t>(i) * R + r)), w);
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
 #pragma unroll
@@ -283,7 +309,7 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
 #pragma unroll 8
             for (int r = 0; r < R; ++r) {
                 const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(B + static_cast<size_t>(r) * p.N + i));
-                const float w0 = half_bits_to_f32(w & 0xFFFFu, p.f16), w1 = half_bits_to_f32(w >> 16, p.f16);
+                const float w0 = half_bits_to_f32(w & 0xFFFFu, F16), w1 = half_bits_to_f32(w >> 16, F16);
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
                     acc0[t] += w0 * h[r * RT + t];
@@ -303,6 +329,7 @@ __host__ __device__ inline int lora_smem(int rank, int requests, bool transposed
     return 4 * (LORA_KSTEP * LORA_ROWS + (transposed ? 0 : LORA_THREADS / 32 * rank * LORA_ROWS) + 2 * rank * LORA_ROWS + 2 * (requests + 1));
 }
 
+template <bool F16>
 __global__ void __launch_bounds__(LORA_THREADS, 4) __cluster_dims__(LORA_CLUSTER, 1, 1) lora_delta_kernel(const LoraParams p) {
     extern __shared__ float lora_sm[];
     float* xs = lora_sm;
@@ -348,8 +375,8 @@ __global__ void __launch_bounds__(LORA_THREADS, 4) __cluster_dims__(LORA_CLUSTER
         const int n = min(LORA_ROWS, s_row[q + 1] - row0);
         const size_t d_row = p.few ? row0 : s_pre[q];
         const int a = p.adapter[q];
-        if (n == 1) lora_chunk<1>(p, row0, n, a, d_row, crank, xs, part, share, h);
-        else lora_chunk<LORA_ROWS>(p, row0, n, a, d_row, crank, xs, part, share, h);
+        if (n == 1) lora_chunk<1, F16>(p, row0, n, a, d_row, crank, xs, part, share, h);
+        else lora_chunk<LORA_ROWS, F16>(p, row0, n, a, d_row, crank, xs, part, share, h);
     }
 }
 

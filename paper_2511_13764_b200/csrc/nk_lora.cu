@@ -65,7 +65,7 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     p->projection = {p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
     p->shrinking = {GRP_ROWS, row, GRP_OUT_F32};
     cudaError_t e = grouped_prepare(p->projection);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_delta_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lora_smem(LORA_MAX_RANK, LORA_MAX_REQUESTS, false));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(d.in_dtype == NK_F16 ? lora_delta_kernel<true> : lora_delta_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, lora_smem(LORA_MAX_RANK, LORA_MAX_REQUESTS, false));
     if (e == cudaSuccess && !p->few) e = grouped_prepare(p->shrinking);
     if (e != cudaSuccess || !encode_tiled()) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
@@ -147,7 +147,6 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     l.adapters = static_cast<int>(d.adapters);
     l.requests = static_cast<int>(d.requests);
     l.transposed = !row;
-    l.f16 = f16;
     l.few = p->few;
     l.ldx = d.ldx;
     l.X = X;
@@ -161,7 +160,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     // clusters: no more than there can be chunks of rows, and a few for every SM
     const int64_t chunks = p->few ? d.rows / LORA_ROWS + (d.rows < d.requests ? d.rows : d.requests) : d.requests;
     const int64_t most = 4 * p->sm_count / LORA_CLUSTER;
-    cudaError_t e = launch_beside(lora_delta_kernel, static_cast<unsigned>((chunks < most ? chunks : most) * LORA_CLUSTER), LORA_THREADS,
+    cudaError_t e = launch_beside(f16 ? lora_delta_kernel<true> : lora_delta_kernel<false>, static_cast<unsigned>((chunks < most ? chunks : most) * LORA_CLUSTER), LORA_THREADS,
                                   lora_smem(l.rank, l.requests, l.transposed), st, l);
     if (e != cudaSuccess) return p->cuda("lora delta launch", e);
     // The two products start beside it.  Neither touches what it writes before they wait for it, and what it waited for
