@@ -72,15 +72,16 @@ template <int MODE, bool A_MN, int OUT>
 __global__ void __launch_bounds__(MODE == GRP_ROWS && OUT != GRP_OUT_F32 ? 512 : GRP_THREADS, 1) __cluster_dims__(2, 1, 1)
 grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__ GroupedParams p) {
     constexpr bool WEIGHTS = MODE == GRP_WEIGHTS, LORA = MODE == GRP_LORA;
-    constexpr bool OUT16 = OUT != GRP_OUT_F32, F16 = OUT == GRP_OUT_F16;
+    constexpr bool OUT16 = OUT == GRP_OUT_BF16 || OUT == GRP_OUT_F16, F16 = OUT == GRP_OUT_F16;
+    constexpr int STAGING = OUT == GRP_OUT_H ? 0 : GRP_STAGING;
     static_assert(!WEIGHTS || A_MN, "rows are contiguous in their features");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
-    int* s_row = reinterpret_cast<int*>(gen_base + GRP_RING + GRP_STAGING);   // first row of each group (LORA: request), clamped and monotone
+    int* s_row = reinterpret_cast<int*>(gen_base + GRP_RING + STAGING);   // first row of each group (LORA: request), clamped and monotone
     int* s_pre = s_row + GRP_MAX_GROUPS + 1;                                  // tiles before each group
     int* s_alt = s_pre + GRP_MAX_GROUPS + 1;                                  // ROWS: weight of the group; LORA: adapter of the request; -1: none.  WEIGHTS: k-blocks before each group
-    const uint32_t bar_base = smem_base + GRP_RING + GRP_STAGING + 3 * GRP_TABLE + 4;   // (8-byte aligned: a table is 4 mod 8 bytes)
+    const uint32_t bar_base = smem_base + GRP_RING + STAGING + 3 * GRP_TABLE + 4;   // (8-byte aligned: a table is 4 mod 8 bytes)
     constexpr int MS = GRP_MAX_STAGES, WS = 5;            // (WEIGHTS: always five stages)
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
     auto empty_bar = [&](int s) { return bar_base + 8u * (MS + s); };
@@ -97,7 +98,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(after);
     volatile uint32_t* abort_flag = tmem_slot + 1;
     volatile int* s_width = reinterpret_cast<volatile int*>(after + 8);      // rows of a tile at most
-    GroupedUnit* s_unit = reinterpret_cast<GroupedUnit*>(gen_base + ((GRP_RING + GRP_STAGING + 3 * GRP_TABLE + 4 + 8 * (NB + 1) + 12 + 15) & ~15));
+    GroupedUnit* s_unit = reinterpret_cast<GroupedUnit*>(gen_base + ((GRP_RING + STAGING + 3 * GRP_TABLE + 4 + 8 * (NB + 1) + 12 + 15) & ~15));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -642,7 +643,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         auto deliver = [&](float (&v)[32], int c) {
             const int n = min(32, u.cols - c), i0 = u.i0 + static_cast<int>(rank) * 128 + quarter * 32;
             const size_t row0 = static_cast<size_t>(u.c0 + c);
-            if (MODE == GRP_ROWS && !OUT16 && p.h16) {
+            if (OUT == GRP_OUT_H || (MODE == GRP_ROWS && OUT == GRP_OUT_F32 && p.h16)) {
                 // X . A_a for the adapters: the scaled product as a leading 16-bit part and a remainder (none behind an infinite
                 // leading part); ranks beyond the last are zeros
                 const float scale = __ldg(p.scale + u.w);
@@ -756,7 +757,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             const int blocks = u.kb1 - u.kb0 + u.req_whole;
             const int chunks = p.chunk ? max(1, (blocks + p.chunk - 1) / p.chunk) : 1, all = chunks + u.req_parts;
             if (!await()) break;
-            if ((!OUT16 || LORA) && all > 1) {
+            if ((OUT == GRP_OUT_F32 || LORA) && all > 1) {
                 // they are added in registers
                 float sum[4][32];
 #pragma unroll

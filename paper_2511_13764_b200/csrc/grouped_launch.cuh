@@ -17,12 +17,13 @@ constexpr int GRP_TILE = 256;                          // features of a tile, an
 constexpr int GRP_TABLE = 4 * (GRP_MAX_GROUPS + 1);    // bytes of a table by group
 constexpr int GRP_STAGING = 8 * 4096;                  // of the stores: two buffers of 2 KB for each epilogue warp
 constexpr int GRP_BLOCK = 600;                         // estimated clocks of a k-block (see grouped.cuh)
-constexpr int GRP_SMEM = GRP_RING + GRP_STAGING + 1024 + 3 * GRP_TABLE + 1024;
+// (a kernel that only writes h16 has no staging: more room for other blocks beside it)
+__host__ __device__ constexpr int grp_smem(bool staging) { return GRP_RING + (staging ? GRP_STAGING : 0) + 1024 + 3 * GRP_TABLE + 1024; }
 
 constexpr int GRP_CHUNK = 8;                           // k-blocks between additions to the FP32 sums of FP32 results
 
 enum GroupedMode { GRP_ROWS = 0, GRP_WEIGHTS = 1, GRP_LORA = 2 };
-enum GroupedOut { GRP_OUT_F32 = 0, GRP_OUT_BF16 = 1, GRP_OUT_F16 = 2 };
+enum GroupedOut { GRP_OUT_F32 = 0, GRP_OUT_BF16 = 1, GRP_OUT_F16 = 2, GRP_OUT_H = 3 };   // H: h16 only (see GroupedParams), from one accumulator
 
 struct GroupedParams {
     int groups, rows;      // rows: extent of the row arrays; offsets are clamped to it
@@ -46,7 +47,7 @@ struct GroupedParams {
     int slab_cols;         // columns of a slab
     unsigned int* counter; // arrivals, a byte per (cut tile, CTA of the pair, 32-column piece, warp); zero before and after
     unsigned int* status;
-    // adapters.  ROWS with h16: instead of C the product times scale[weight] is stored as two 16-bit numbers whose sum is
+    // adapters.  ROWS with h16 (out H, or F32: by chunks): instead of C the product times scale[weight] is stored as two 16-bit numbers whose sum is
     // good to twice their precision, [row][rank block of 32][32 leading parts, 32 remainders].  LORA: each request's
     // rows of h16 times its B_a are further k-blocks of a tile.
     uint16_t* h16;

@@ -4,6 +4,7 @@
 namespace nk {
 
 GroupedFunction grouped_rows_kernel(bool a_mn, GroupedOut out) {
+    if (out == GRP_OUT_H) return a_mn ? grouped_kernel<GRP_ROWS, true, GRP_OUT_H> : grouped_kernel<GRP_ROWS, false, GRP_OUT_H>;
     if (a_mn)
         return out == GRP_OUT_F32 ? grouped_kernel<GRP_ROWS, true, GRP_OUT_F32>
                : out == GRP_OUT_BF16 ? grouped_kernel<GRP_ROWS, true, GRP_OUT_BF16> : grouped_kernel<GRP_ROWS, true, GRP_OUT_F16>;

@@ -35,10 +35,10 @@ static GroupedFunction function_of(const GroupedKernel& k) {
     return k.mode == GRP_WEIGHTS ? grouped_weights_kernel(k.out) : k.mode == GRP_LORA ? grouped_lora_kernel(k.a_mn, k.out) : grouped_rows_kernel(k.a_mn, k.out);
 }
 cudaError_t grouped_prepare(const GroupedKernel& k) {
-    return cudaFuncSetAttribute(function_of(k), cudaFuncAttributeMaxDynamicSharedMemorySize, GRP_SMEM);
+    return cudaFuncSetAttribute(function_of(k), cudaFuncAttributeMaxDynamicSharedMemorySize, grp_smem(k.out != GRP_OUT_H));
 }
 cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p) {
-    return launch_beside(function_of(k), 2 * pairs, GRP_THREADS, GRP_SMEM, st, maps, p);
+    return launch_beside(function_of(k), 2 * pairs, GRP_THREADS, grp_smem(k.out != GRP_OUT_H), st, maps, p);
 }
 
 }  // namespace nk

@@ -63,7 +63,9 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     const bool row = d.layout == NK_ROW_MAJOR;
     p->few = d.rows <= LORA_ROWS * d.requests;
     p->projection = {p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
-    p->shrinking = {GRP_ROWS, row, GRP_OUT_F32};
+    // (one accumulator for all of K is cut short by up to K 2^-28 of itself, far below what a 16-bit Y keeps, and its kernel leaves
+    // room for lora_delta_kernel's blocks; an FP32 Y has X . A_a summed by chunks)
+    p->shrinking = {GRP_ROWS, row, d.out_dtype == NK_F32 ? GRP_OUT_F32 : GRP_OUT_H};
     cudaError_t e = grouped_prepare(p->projection);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(d.in_dtype == NK_F16 ? lora_delta_kernel<true> : lora_delta_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, lora_smem(LORA_MAX_RANK, LORA_MAX_REQUESTS, false));
     if (e == cudaSuccess && !p->few) e = grouped_prepare(p->shrinking);
@@ -178,7 +180,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
         h.min_rows = LORA_ROWS;
         h.I = g.rank;
         h.tiles_i = 1;
-        h.chunk = GRP_CHUNK;
+        h.chunk = d.out_dtype == NK_F32 ? GRP_CHUNK : 0;
         h.h16 = reinterpret_cast<uint16_t*>(ws);
         h.partial = partial[0];
         h.counter = p->counters[0];
