@@ -159,9 +159,11 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     l.adapter = adapter;
     l.D = reinterpret_cast<float*>(ws + p->h_bytes);
     l.status = p->status_dev;
-    // clusters: no more than there can be chunks of rows, and a few for every SM
+    // Clusters: no more than there can be chunks of rows.  Up to two rounds of them go to as many clusters as fit with one block
+    // to an SM (two in each of eight GPCs), beside which the projection's or X . A's blocks find room; more of them are bound by
+    // memory and get four blocks to an SM.
     const int64_t chunks = p->few ? d.rows / LORA_ROWS + (d.rows < d.requests ? d.rows : d.requests) : d.requests;
-    const int64_t most = 4 * p->sm_count / LORA_CLUSTER;
+    const int64_t single = p->sm_count / LORA_CLUSTER / 8 * 8, most = chunks <= 2 * single ? single : 4 * p->sm_count / LORA_CLUSTER;
     cudaError_t e = launch_beside(f16 ? lora_delta_kernel<true> : lora_delta_kernel<false>, static_cast<unsigned>((chunks < most ? chunks : most) * LORA_CLUSTER), LORA_THREADS,
                                   lora_smem(l.rank, l.requests, l.transposed), st, l);
     if (e != cudaSuccess) return p->cuda("lora delta launch", e);
