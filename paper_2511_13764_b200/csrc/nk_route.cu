@@ -100,6 +100,10 @@ nk_status_t nk_route_create(const nk_route_desc_t* desc, nk_route_t* out) {
     p->blocks = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? 1 : div_up(d.tokens, p->per_block));
     DeviceGuard guard(d.device);
     const int v = route_width(d.experts);
+    if (cudaFuncSetAttribute(backward_kernel(v), cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * 32 * 32 * sizeof(float2)) != cudaSuccess) {
+        delete p;
+        return NK_ERR_CUDA;
+    }
     const auto first = p->blocks == 1 ? select_kernel<true>(v) : select_kernel<false>(v);
     if (cudaFuncSetAttribute(first, cudaFuncAttributeMaxDynamicSharedMemorySize, route_smem(NK_ROUTE_MAX_EXPERTS)) != cudaSuccess ||
         cudaFuncSetAttribute(route_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, route_smem(NK_ROUTE_MAX_EXPERTS)) != cudaSuccess) {
@@ -156,7 +160,7 @@ nk_status_t nk_route_backward(nk_route_t p, const void* logits, const int32_t* e
     RouteParams r = route_params(p);
     r.logits = logits;
     r.chosen = const_cast<int32_t*>(experts);
-    const cudaError_t e = launch_beside(backward_kernel(route_width(p->d.experts)), static_cast<unsigned>(div_up(r.tokens, 8)), 256, 0,
+    const cudaError_t e = launch_beside(backward_kernel(route_width(p->d.experts)), static_cast<unsigned>(div_up(r.tokens, 8)), 256, 8 * 32 * route_width(p->d.experts) * sizeof(float2),
                                         static_cast<cudaStream_t>(cuda_stream), r, dgates, dlogits);
     return e == cudaSuccess ? NK_OK : p->cuda("route backward launch", e);
 }

@@ -20,10 +20,19 @@ struct RouteParams {
     int per_block;              // tokens of a block
 };
 
-__device__ __forceinline__ float route_load(const RouteParams& p, int t, int e) {
-    const size_t o = static_cast<size_t>(t) * p.ld_logits + e;
-    if (p.logits_type == 0) return static_cast<const float*>(p.logits)[o];
-    return half_bits_to_f32(static_cast<const uint16_t*>(p.logits)[o], p.logits_type == 2);
+// A token's logits: lane l holds experts l, l + 32, ...; `none` where there is no expert.
+template <int V>
+__device__ __forceinline__ void route_fetch(const RouteParams& p, int t, int lane, float none, float (&z)[V]) {
+    const size_t o = static_cast<size_t>(t) * p.ld_logits + lane;
+    if (p.logits_type == 0) {
+        const float* x = static_cast<const float*>(p.logits) + o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) z[i] = lane + 32 * i < p.experts ? x[32 * i] : none;
+    } else {
+        const uint16_t* x = static_cast<const uint16_t*>(p.logits) + o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) z[i] = lane + 32 * i < p.experts ? half_bits_to_f32(x[32 * i], p.logits_type == 2) : none;
+    }
 }
 
 // Unsigned key in the order of the numbers: both zeros alike, NaN below every number (1), 0 left for "taken".
@@ -38,11 +47,6 @@ __device__ __forceinline__ float route_unkey(uint32_t k) {
 
 // One warp, one token: lane l holds experts l, l + 32, ...  (V of them).  topk rounds of a warp-wide maximum of the
 // keys and a minimum of the indices that have it.
-template <int V>
-__device__ __forceinline__ void route_fetch(const RouteParams& p, int t, int lane, float (&z)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) z[i] = lane + 32 * i < p.experts ? route_load(p, t, lane + 32 * i) : 0.0f;
-}
 template <int V>
 __device__ __forceinline__ int route_token(const RouteParams& p, int t, int lane, const float (&z)[V]) {
     uint32_t key[V];
@@ -85,7 +89,7 @@ __device__ __forceinline__ int route_token(const RouteParams& p, int t, int lane
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (key[i] > 1u) sum += expf(route_unkey(key[i]) - m);
+            if (key[i]) sum += expf(z[i] - m);
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
@@ -187,12 +191,12 @@ __global__ void __launch_bounds__(route_threads(V)) route_select_kernel(const Ro
     __syncthreads();
     // the next token's logits are on the way while one is worked on
     float z[V];
-    if (t0 + warp < t1) route_fetch<V>(p, t0 + warp, lane, z);
+    if (t0 + warp < t1) route_fetch<V>(p, t0 + warp, lane, 0.0f, z);
     for (int t = t0 + warp; t < t1; t += WARPS) {
         float now[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) now[i] = z[i];
-        if (t + WARPS < t1) route_fetch<V>(p, t + WARPS, lane, z);
+        if (t + WARPS < t1) route_fetch<V>(p, t + WARPS, lane, 0.0f, z);
         const int e = route_token<V>(p, t, lane, now);
         if (lane < p.topk) atomicAdd(hist + e, 1);
     }
@@ -255,33 +259,31 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const RouteParams p
     launch_wait();
     launch_next();
     if (t >= p.tokens) return;
+    // the chosen experts' gradients by way of shared memory: a row of (gradient, 1) by expert for each warp
+    extern __shared__ float2 route_d[];
+    float2* row = route_d + (threadIdx.x >> 5) * (32 * V);
     const size_t o = static_cast<size_t>(t) * p.topk;
-    uint32_t taken = 0u;                           // bit i: this lane's expert i is one of the chosen
     const int own = lane < p.topk ? p.chosen[o + lane] : -1;
     const float own_d = lane < p.topk ? dgates[o + lane] : 0.0f;
     float z[V], d[V];
-    uint32_t top = 0u;
+    route_fetch<V>(p, t, lane, -INFINITY, z);
+#pragma unroll
+    for (int i = 0; i < V; ++i) row[lane + 32 * i] = make_float2(0.0f, 0.0f);
+    __syncwarp();
+    if (own >= 0 && own < p.experts) row[own] = make_float2(own_d, 1.0f);
+    __syncwarp();
+    uint32_t top = 0u, taken = 0u;                 // taken, bit i: this lane's expert i is one of the chosen
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int e = lane + 32 * i;
-        z[i] = e < p.experts ? route_load(p, t, e) : -INFINITY;
-        d[i] = 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
+        const float2 x = row[lane + 32 * i];
+        d[i] = x.x;
+        taken |= x.y != 0.0f ? 1u << i : 0u;
         nan |= z[i] != z[i];
         top = max(top, route_key(z[i]));
     }
     nan = __any_sync(~0u, nan);
     const float m = route_unkey(__reduce_max_sync(~0u, top));
-    for (int j = 0; j < p.topk; ++j) {
-        const int e = __shfl_sync(~0u, own, j);
-        const float g = __shfl_sync(~0u, own_d, j);
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (e == lane + 32 * i) { d[i] = g; taken |= 1u << i; }
-    }
     float sum = 0.0f, inner = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
