@@ -143,9 +143,9 @@ nk_status_t nk_route_destroy(nk_route_t plan);
  *   layout NK_TRANSPOSED   W [N][K],  A [adapters][rank][K],  B [adapters][N][rank]   (linear layers' [out][in])
  *
  * Adapters of a lower rank are padded with zeros.  16-bit operands of one type, FP32 accumulation, Y in FP32 or rounded
- * once to the operands' type.  X . A_a is held in FP32, or as the sum of two 16-bit numbers (good to 2^-16 of it with
- * NK_BF16, 2^-21 with NK_F16) where the tensor cores multiply it by B_a; with NK_F16 |scale * X . A_a| has to stay within
- * the type's range then.
+ * once to the operands' type.  X . A_a is held in FP32, or where the tensor cores multiply it by B_a as the sum of two 16-bit
+ * numbers (good to 2^-16 of it with NK_BF16, 2^-21 with NK_F16) or, for an FP32 Y of NK_BF16 operands, three (2^-24); with
+ * NK_F16 |scale * X . A_a| has to stay within the type's range.
  * Offsets that break the rule are clamped and reported by nk_lora_check, as for nk_grouped.
  */
 typedef struct nk_lora_s* nk_lora_t;

@@ -480,6 +480,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                 if (!waited) launch_wait();
                 waited = true;
                 const uint32_t bytes = (A_MN ? 8192u : GRP_A_BYTES) + b_bytes;
+                const int ranks = p.planes == 3 ? 16 : 32;    // of a block
                 int q = u.req;
                 for (int n = 0; ok && n < max(1, u.req_parts); ++n, ++q) {
                     while (!u.req_whole && !has_part(q)) ++q;
@@ -488,10 +489,10 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         const uint32_t sa = smem_base + stage * stage_bytes, sb = sa + GRP_A_BYTES, lfb = lead_full0 + 8u * stage;
                         mbar_arrive_expect_tx_if(full_bar(stage), 2u * bytes, lead_elected);
                         if (A_MN) {
-                            tma_load_3d_pair_if(sa, &maps.c, lfb, i, rb * 32, s_alt[q], elected);
-                            tma_load_3d_pair_if(sa + 8192, &maps.c, lfb, i + 64, rb * 32, s_alt[q], elected);
+                            tma_load_3d_pair_if(sa, &maps.c, lfb, i, rb * ranks, s_alt[q], elected);
+                            tma_load_3d_pair_if(sa + 8192, &maps.c, lfb, i + 64, rb * ranks, s_alt[q], elected);
                         } else {
-                            tma_load_3d_pair_if(sa, &maps.c, lfb, rb * 32, i, s_alt[q], elected);
+                            tma_load_3d_pair_if(sa, &maps.c, lfb, rb * ranks, i, s_alt[q], elected);
                         }
                         rows_boxes(maps.h, sb, lfb, rb * 64);
                         advance();
@@ -566,7 +567,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         cleared = rem & 15;
                     }
                     if (low_rank) {
-                        steps = min(2, (p.rank - 32 * rb + 15) >> 4);
+                        steps = p.planes == 3 ? 1 : min(2, (p.rank - 32 * rb + 15) >> 4);
                         if (++rb == p.rank_blocks) rb = 0;
                     }
                     if (WEIGHTS && cleared) {
@@ -581,9 +582,11 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     const uint32_t a_lo = a_lo0 + stage * (stage_bytes >> 4), b_lo = b_lo0 + stage * (stage_bytes >> 4);
                     umma_pair_if<0>(d_tmem, a_lo, a_hi, b_lo, b_hi, idesc, accumulate, elected);
                     if (low_rank) {
-                        // 32 ranks: leading parts of h16 in the first 64 bytes of a row, remainders in the second
+                        // 32 ranks: leading parts in the first 64 bytes of a row of h16, remainders in the second; or 16 ranks in 32 bytes each
+                        const uint32_t second = p.planes == 3 ? b_s : 2 * b_s;
                         if (steps > 1) umma_pair_if<0>(d_tmem, a_lo + a_s, a_hi, b_lo + b_s, b_hi, idesc, 1u, elected);
-                        umma_pair_if<0>(d_tmem, a_lo, a_hi, b_lo + 2 * b_s, b_hi, idesc, 1u, elected);
+                        umma_pair_if<0>(d_tmem, a_lo, a_hi, b_lo + second, b_hi, idesc, 1u, elected);
+                        if (p.planes == 3) umma_pair_if<0>(d_tmem, a_lo, a_hi, b_lo + 2 * b_s, b_hi, idesc, 1u, elected);
                         if (steps > 1) umma_pair_if<0>(d_tmem, a_lo + a_s, a_hi, b_lo + 3 * b_s, b_hi, idesc, 1u, elected);
                     } else {
                         if (!WEIGHTS || steps > 1) umma_pair_if<0>(d_tmem, a_lo + a_s, a_hi, b_lo + b_s, b_hi, idesc, 1u, elected);
@@ -644,20 +647,24 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             const int n = min(32, u.cols - c), i0 = u.i0 + static_cast<int>(rank) * 128 + quarter * 32;
             const size_t row0 = static_cast<size_t>(u.c0 + c);
             if (OUT == GRP_OUT_H || (MODE == GRP_ROWS && OUT == GRP_OUT_F32 && p.h16)) {
-                // X . A_a for the adapters: the scaled product as a leading 16-bit part and a remainder (none behind an infinite
-                // leading part); ranks beyond the last are zeros
+                // X . A_a for the adapters: the scaled product as a leading 16-bit part and one or two remainders (none behind an
+                // infinite leading part); ranks beyond the last are zeros
                 const float scale = __ldg(p.scale + u.w);
-                const int pitch = p.rank_blocks * 64;
-                uint16_t* h = p.h16 + row0 * pitch + (i0 >> 5) * 64 + lane;
-                if (i0 < p.rank_blocks * 32) {
+                const int pitch = p.rank_blocks * 64, per = p.planes == 3 ? 16 : 32, i = i0 + lane;
+                uint16_t* h = p.h16 + row0 * pitch + i / per * 64 + i % per;
+                if (i < p.rank_blocks * per) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        const float x = i0 + lane < p.I ? v[j] * scale : 0.0f;
-                        const uint32_t hi = pack_half2(x, 0.0f, p.f16) & 0xFFFFu;
-                        const float lead = half_bits_to_f32(hi, p.f16);
+                        float x = i < p.I ? v[j] * scale : 0.0f;
                         if (j < n) {
-                            h[0] = static_cast<uint16_t>(hi);
-                            h[32] = static_cast<uint16_t>(pack_half2(fabsf(lead) <= 3.4028235e38f ? x - lead : 0.0f, 0.0f, p.f16) & 0xFFFFu);
+#pragma unroll
+                            for (int z = 0; z < 3; ++z) {
+                                if (z == p.planes) break;
+                                const uint32_t bits = pack_half2(x, 0.0f, p.f16) & 0xFFFFu;
+                                const float lead = half_bits_to_f32(bits, p.f16);
+                                h[z * per] = static_cast<uint16_t>(bits);
+                                x = fabsf(lead) <= 3.4028235e38f ? x - lead : 0.0f;
+                            }
                         }
                         h += pitch;
                     }

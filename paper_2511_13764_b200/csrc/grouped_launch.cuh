@@ -47,12 +47,12 @@ struct GroupedParams {
     int slab_cols;         // columns of a slab
     unsigned int* counter; // arrivals, a byte per (cut tile, CTA of the pair, 32-column piece, warp); zero before and after
     unsigned int* status;
-    // adapters.  ROWS with h16 (out H, or F32: by chunks): instead of C the product times scale[weight] is stored as two 16-bit numbers whose sum is
-    // good to twice their precision, [row][rank block of 32][32 leading parts, 32 remainders].  LORA: each request's
-    // rows of h16 times its B_a are further k-blocks of a tile.
+    // adapters.  ROWS with h16 (out H, or F32: by chunks): instead of C the product times scale[weight] is stored as two or three
+    // 16-bit numbers (`planes`) that add up to it, each the rounding of what the ones before it leave: blocks of 64 to a row, of 32
+    // (two) or 16 (three) ranks, plane after plane.  LORA: each request's rows of h16 times its B_a are further k-blocks of a tile.
     uint16_t* h16;
     const float* scale;
-    int rank_blocks, rank;
+    int rank_blocks, rank, planes;
     int requests;
     const int* request_offsets;
 };

@@ -155,6 +155,42 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
                 share[i] = s;
             }
         }
+    } else if (p.transposed) {
+        // Up to eight rows: a lane has eight of k of four rows in registers while the ranks of its warp pass, lanes along k.
+        for (int i = threadIdx.x; i < RT * R; i += LORA_THREADS) share[i] = 0.0f;
+        __syncthreads();
+        for (int k0 = k_lo; k0 < k_hi; k0 += 256) {
+            const int k = k0 + lane * 8;
+            for (int t0 = 0; t0 < n; t0 += 4) {
+                uint4 x[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    x[t] = k < k_hi && t0 + t < n ? __ldg(reinterpret_cast<const uint4*>(X + static_cast<size_t>(row0 + t0 + t) * p.ldx + k)) : make_uint4(0, 0, 0, 0);
+#pragma unroll 2
+                for (int r = warp; r < R; r += LORA_THREADS / 32) {
+                    float w[8], acc[4];
+                    lora_unpack8<F16>(k < k_hi ? __ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k)) : make_uint4(0, 0, 0, 0), w);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        float y[8];
+                        lora_unpack8<F16>(x[t], y);
+                        acc[t] = 0.0f;
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) acc[t] += w[q] * y[q];
+                    }
+                    // four sums over 32 lanes: lanes of bits 4, 3 keep one of them each, then the rest add up
+                    const bool hi = lane & 16, odd = lane & 8;
+                    float a0 = hi ? acc[2] : acc[0], a1 = hi ? acc[3] : acc[1];
+                    a0 += __shfl_xor_sync(~0u, hi ? acc[0] : acc[2], 16);
+                    a1 += __shfl_xor_sync(~0u, hi ? acc[1] : acc[3], 16);
+                    float s = odd ? a1 : a0;
+                    s += __shfl_xor_sync(~0u, odd ? a0 : a1, 8);
+#pragma unroll
+                    for (int d = 4; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+                    if ((lane & 7) == 0) share[r * RT + t0 + (lane >> 3)] += s;
+                }
+            }
+        }
     } else {
         for (int i = threadIdx.x; i < RT * R; i += LORA_THREADS) share[i] = 0.0f;
         // part[warp][r][RT] (row-major weights only): each warp's sums
@@ -171,29 +207,7 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
                 for (int q = 0; q < 8; ++q) xs[(k + q) * RT + t] = x[q];
             }
             __syncthreads();
-            if (p.transposed) {
-                // a warp per rank, lanes along k
-                for (int r = warp; r < R; r += LORA_THREADS / 32) {
-                    float acc[RT];
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) acc[t] = 0.0f;
-#pragma unroll 2
-                    for (int k = lane * 8; k < kn; k += 256) {
-                        float w[8];
-                        lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k0 + k)), w);
-#pragma unroll
-                        for (int q = 0; q < 8; ++q)
-#pragma unroll
-                            for (int t = 0; t < RT; ++t) acc[t] += w[q] * xs[(k + q) * RT + t];
-                    }
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-#pragma unroll
-                        for (int d = 16; d > 0; d >>= 1) acc[t] += __shfl_xor_sync(~0u, acc[t], d);
-                        if (lane == 0) share[r * RT + t] += acc[t];
-                    }
-                }
-            } else {
+            {
                 // lanes along pairs of ranks, then along k; warps along k; the warps' sums meet in shared memory
                 const int pairs = R / 2;
                 int wide = 4;

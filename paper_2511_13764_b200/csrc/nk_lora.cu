@@ -6,7 +6,7 @@
 struct nk_lora_s : nk::PlanBase {
     nk_lora_desc_t d;             // strides filled in
     bool few;                     // few rows to a request: FP32 contributions from lora_delta_kernel
-    int pairs, rank_blocks;
+    int pairs, rank_blocks, planes;
     int split_slot[2];            // of X . A and of the projection: the two overlap
     unsigned int* counters[2];
     size_t part_bytes[2], h_bytes, side_bytes;   // partial sums of the two; X . A; it and the FP32 contributions
@@ -24,8 +24,10 @@ static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Which way the adapters' part goes.  Requests of up to LORA_ROWS rows are lora_delta_kernel's: their weights are all that
 // counts, and its clusters read them at the speed of memory; more rows want the tensor cores: X . A_a as a grouped
-// product, (X . A_a) . B_a as further k-blocks of the projection.  Where a plan's requests have so few rows on average,
-// lora_delta_kernel takes all of them, and the launch of the grouped product is saved.
+// product, (X . A_a) . B_a as further k-blocks of the projection.  Where a plan's requests have so few rows on average
+// lora_delta_kernel takes all of them, and the launch of the grouped product is saved.  So it does with longer requests where
+// its chunks of rows are a round or two of clusters and it reads A as rows of K, 16 bytes to a lane (59 rows of 2 requests, K =
+// 1240, N = 976, rank 8: 17 us against 27; but 465 rows of one, row-major, rank 104: 31 against 20, 12 rows, rank 112: 24 against 18).
 
 }  // namespace nk
 
@@ -61,7 +63,7 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     DeviceGuard guard(d.device);
     const bool row = d.layout == NK_ROW_MAJOR;
-    p->few = d.rows <= LORA_ROWS * d.requests;
+    p->few = d.rows <= LORA_ROWS * d.requests || (!row && d.rank <= 64 && d.rows / LORA_ROWS + d.requests <= 32);
     p->projection = {p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
     // (one accumulator for all of K is cut short by up to K 2^-28 of itself, far below what a 16-bit Y keeps, and its kernel leaves
     // room for lora_delta_kernel's blocks; an FP32 Y has X . A_a summed by chunks)
@@ -71,9 +73,11 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     if (e == cudaSuccess && !p->few) e = grouped_prepare(p->shrinking);
     if (e != cudaSuccess || !encode_tiled()) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
-    p->rank_blocks = static_cast<int>(div_up(d.rank, 32));
+    // two BF16 numbers hold X . A_a to 2^-16 of it: enough for a 16-bit Y, not for an FP32 one, which gets three (2^-24)
+    p->planes = d.out_dtype == NK_F32 && d.in_dtype == NK_BF16 ? 3 : 2;
+    p->rank_blocks = static_cast<int>(div_up(d.rank, p->planes == 3 ? 16 : 32));
     p->h_bytes = p->few ? 0 : align256(static_cast<size_t>(d.rows) * p->rank_blocks * 128);
-    const int64_t short_rows = d.rows < LORA_ROWS * d.requests ? d.rows : LORA_ROWS * d.requests;
+    const int64_t short_rows = p->few || d.rows < LORA_ROWS * d.requests ? d.rows : LORA_ROWS * d.requests;
     p->side_bytes = p->h_bytes + align256(static_cast<size_t>(short_rows) * d.N * sizeof(float));
     for (int i = p->few ? 1 : 0; i < 2; ++i) {
         p->split_slot[i] = take_split_slot(&p->counters[i]);
@@ -140,6 +144,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     g.status = p->status_dev;
     g.rank = static_cast<int>(d.rank);
     g.rank_blocks = p->rank_blocks;
+    g.planes = p->planes;
     g.scale = scale;
     LoraParams l = {};
     l.rows = g.rows;
