@@ -108,20 +108,36 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
         // One row: X straight from memory, every load independent of the others.
         const uint16_t* x = X + static_cast<size_t>(row0) * p.ldx;
         if (p.transposed) {
-            // a warp per rank, lanes along k
-            for (int r = warp; r < R; r += LORA_THREADS / 32) {
-                float acc = 0.0f;
-#pragma unroll 2
+            // a warp has every eighth rank, eight of them at a time with all their loads on the way; lanes along k
+            for (int r0 = warp; r0 < R; r0 += 8 * (LORA_THREADS / 32)) {
+                float acc[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
                 for (int k = k_lo + lane * 8; k < k_hi; k += 256) {
-                    float w[8], y[8];
-                    lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k)), w);
+                    uint4 w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int r = r0 + j * (LORA_THREADS / 32);
+                        w[j] = r < R ? __ldg(reinterpret_cast<const uint4*>(A + static_cast<size_t>(r) * p.K + k)) : make_uint4(0, 0, 0, 0);
+                    }
+                    float y[8];
                     lora_unpack8<F16>(__ldg(reinterpret_cast<const uint4*>(x + k)), y);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) acc += w[q] * y[q];
+                    for (int j = 0; j < 8; ++j) {
+                        float z[8];
+                        lora_unpack8<F16>(w[j], z);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) acc[j] += z[q] * y[q];
+                    }
                 }
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) acc += __shfl_xor_sync(~0u, acc, d);
-                if (lane == 0) share[r] = acc;
+                for (int j = 0; j < 8; ++j) {
+                    const int r = r0 + j * (LORA_THREADS / 32);
+                    if (r >= R) break;
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) acc[j] += __shfl_xor_sync(~0u, acc[j], d);
+                    if (lane == 0) share[r] = acc[j];
+                }
             }
         } else {
             // lanes along eights of ranks, then along k; warps along k; the warps' sums meet in shared memory
@@ -297,6 +313,24 @@ __device__ __forceinline__ void lora_chunk(const LoraParams& p, int row0, int n,
                 p.D[d_row * p.N + n_lo + e0 * 8 + i] = s;
             }
             __syncthreads();
+        }
+    } else if (RT == 1) {
+        // lanes along eights of ranks, then along columns: a load is 512 contiguous bytes of B where the rank is a power of two
+        int wide = 1;
+        while (wide * 8 < R) wide *= 2;                             // lanes for one column
+        const int per = 32 / wide, r = (lane % wide) * 8;
+        float g[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) g[q] = r < R ? h[r + q] : 0.0f;
+#pragma unroll 4
+        for (int i0 = n_lo + warp * per; i0 < n_hi; i0 += per * (LORA_THREADS / 32)) {
+            const int i = i0 + lane / wide;
+            float w[8], acc = 0.0f;
+            lora_unpack8<F16>(i < n_hi && r < R ? __ldg(reinterpret_cast<const uint4*>(B + static_cast<size_t>(i) * R + r)) : make_uint4(0, 0, 0, 0), w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) acc += w[q] * g[q];
+            for (int d = 1; d < wide; d <<= 1) acc += __shfl_xor_sync(~0u, acc, d);
+            if (lane % wide == 0 && i < n_hi) p.D[d_row * p.N + i] = acc;
         }
     } else if (p.transposed) {
         for (int i = n_lo + threadIdx.x; i < n_hi; i += LORA_THREADS) {
