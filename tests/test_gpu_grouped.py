@@ -202,6 +202,34 @@ def test_rows_cut_along_k(rows):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("sizes,N,K", [([2560], 2048, 2048), ([700, 1, 900, 0, 650, 300], 2048, 1536), ([9600, 40], 512, 4096)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_rows_last_wave_cut(sizes, N, K, out):
+    """A few tiles behind full waves of them: only the last wave's are cut along k."""
+    run_rows(sizes, N, K, out=out, seed=7)
+    run_rows(sizes, N, K, kind="f16", out="f16" if out == "bf16" else "f32", layout="transposed", beta=1, seed=8)
+
+
+@pytest.mark.gpu
+def test_more_plans_than_counters():
+    """A plan that finds no counters left runs without cutting tiles, and gives them back to nobody."""
+    plans = [nk.GroupedPlan(1, 40, 512, 8192, out_dtype=nk.F32) for _ in range(1030)]
+    assert plans[0].workspace_bytes > 0 and plans[-1].workspace_bytes == 0
+    gen = torch.Generator().manual_seed(9)
+    A, W = rand((40, 8192), "bf16", gen).cuda(), rand((1, 8192, 512), "bf16", gen, 0.01).cuda()
+    off = torch.tensor([0, 40], dtype=torch.int32).cuda()
+    want, size = A.double() @ W[0].double(), float((A.double().abs() @ W[0].double().abs()).max())
+    for plan in (plans[0], plans[-1]):
+        C = torch.full((40, 512), float("nan"), device="cuda")
+        plan.run(A, W, C, off, workspace=scratch(plan), stream=torch.cuda.current_stream().cuda_stream)
+        plan.check()
+        close(C, want, size, "f32")
+    for plan in plans:
+        plan.destroy()
+    assert nk.GroupedPlan(1, 40, 512, 8192).workspace_bytes > 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("name", list(GROUPS))
 def test_weights_of_ragged_groups(name):
     run_weights(GROUPS[name], 264, 200, seed=11)
@@ -231,6 +259,41 @@ def test_weights_neighbours_of_nan(sizes, poison):
 @pytest.mark.gpu
 def test_weights_many_tiles():
     run_weights([2049, 0, 700, 33, 1], 1288, 1032, out="bf16", seed=15)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes,N,K", [([16384], 256, 256), ([9001], 64, 520), ([3000, 0, 5000, 7], 304, 264), ([0, 4097, 0], 1032, 1032)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_weights_cut_along_the_rows(sizes, N, K, out):
+    """Few tiles and many rows: the parts of a tile are added in the same order on every run."""
+    run_weights(sizes, N, K, out=out, seed=16)
+    run_weights(sizes, N, K, kind="f16", out="f16" if out == "bf16" else "f32", beta=1, seed=17)
+    gen = torch.Generator().manual_seed(18)
+    rows, off = sum(sizes), offsets_of(sizes).cuda()
+    A, B = rand((rows, K), "bf16", gen).cuda(), rand((rows, N), "bf16", gen).cuda()
+    plan = nk.GroupedPlan(len(sizes), rows, N, K, kind=nk.GROUPED_WEIGHTS, out_dtype=nk.F32)
+    ws, outs = scratch(plan), []
+    for _ in range(10):
+        C = torch.full((len(sizes), K, N), float("nan"), device="cuda")
+        plan.run(A, B, C, off, workspace=ws, stream=torch.cuda.current_stream().cuda_stream)
+        outs.append(C)
+    plan.check()
+    assert all(torch.equal(outs[0], c) for c in outs)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1024, 8192])
+def test_fp32_sums_do_not_drift(rows):
+    """Sums of thousands of rows are as good as FP32 arithmetic: relative 2-norm error within 1e-6 (chunks of 512 rows, each
+    32 truncated additions of at most 2^-23 of the running sum, on average half of that over a sum that grows: 32 / 3 * 2^-23)."""
+    gen = torch.Generator().manual_seed(19)
+    A, B = rand((rows, 256), "bf16", gen).cuda(), rand((rows, 512), "bf16", gen).cuda()
+    plan = nk.GroupedPlan(1, rows, 512, 256, kind=nk.GROUPED_WEIGHTS, out_dtype=nk.F32)
+    C = torch.empty(1, 256, 512, device="cuda")
+    plan.run(A, B, C, torch.tensor([0, rows], dtype=torch.int32).cuda(), workspace=scratch(plan), stream=torch.cuda.current_stream().cuda_stream)
+    plan.check()
+    want = A.double().t() @ B.double()
+    assert float((C[0].double() - want).norm() / want.norm()) <= 32 / 3 * 2.0 ** -23
 
 
 @pytest.mark.gpu

@@ -117,6 +117,38 @@ def test_sizes(N, K, layout, sizes):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("name", ["one_prompt", "mixed", "edges", "short"])
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("rank", [8, 40, 128])
+def test_sixteen_bit_results(name, layout, kind, rank):
+    data = make(SHAPES[name], 264, 328, rank, 5, kind, seed=8)
+    got, _ = run(data, layout, kind)
+    close(got, data, kind)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_many_tiles_and_a_cut_last_wave(layout, out):
+    data = make([1, 1500, 1, 1, 3, 700, 9, 1, 360], 2056, 1096, 72, 4, "bf16", seed=9)
+    got, _ = run(data, layout, out)
+    close(got, data, out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+def test_most_requests(layout):
+    gen = np.random.default_rng(10)
+    data = make(gen.integers(0, 3, 1024).tolist(), 72, 136, 8, 60, "bf16", seed=10)
+    got, _ = run(data, layout)
+    close(got, data, "f32")
+    data = make([int(x) for x in gen.integers(0, 25, 400)], 72, 136, 24, 7, "bf16", seed=11)
+    got, _ = run(data, layout, "bf16")
+    close(got, data, "bf16")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("name", ["step", "mixed", "one_prompt"])
 @pytest.mark.parametrize("layout", ["row", "transposed"])
 def test_requests_without_an_adapter(name, layout):
