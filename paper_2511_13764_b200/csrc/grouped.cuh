@@ -39,6 +39,7 @@
 #include "grouped_launch.cuh"
 #include "half.cuh"
 #include "ptx.cuh"
+#include <type_traits>
 
 namespace nk {
 
@@ -75,7 +76,7 @@ __device__ __forceinline__ int round32(int x) { return (x + 31) & ~31; }
 // SM room for a block of the adapters' kernel beside them.)
 template <int MODE, bool A_MN, int OUT>
 __global__ void __launch_bounds__(MODE == GRP_ROWS && OUT != GRP_OUT_F32 ? 512 : GRP_THREADS, 1) __cluster_dims__(2, 1, 1)
-grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__ GroupedParams p) {
+grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, LoraMaps, GroupedMaps> maps, const __grid_constant__ GroupedParams p) {
     constexpr bool WEIGHTS = MODE == GRP_WEIGHTS, LORA = MODE == GRP_LORA;
     constexpr bool OUT16 = OUT == GRP_OUT_BF16 || OUT == GRP_OUT_F16, F16 = OUT == GRP_OUT_F16;
     constexpr int STAGING = OUT == GRP_OUT_H ? 0 : GRP_STAGING;
@@ -130,9 +131,9 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
         if (lane == 0) *abort_flag = 0;
         fence_mbar_init();
         __syncwarp();
-    } else if (warp == 2 && lane == 0) {
-        tma_prefetch_desc(&maps.a);
-        tma_prefetch_desc(&maps.b[0]);
+    } else if (warp == 2) {
+        if (lane < (WEIGHTS ? 1 : 8)) tma_prefetch_desc(&maps.b[lane]);
+        if (lane == 8) tma_prefetch_desc(&maps.a);
     } else if (warp == 1) {
         tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
         tmem_relinquish_pair();
@@ -413,17 +414,10 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
             const int c = u.c0 + static_cast<int>(rank) * half;      // first column of this CTA's B operand
             const int boxes = (half + 63) >> 6;                       // WEIGHTS
             const uint32_t b_bytes = WEIGHTS ? boxes * 8192u : half * 128u;
-            // half rows (a multiple of 16, up to 128) of 128 bytes each, in the fewest boxes of 16, 32, 64 or 128 rows
-            auto rows_boxes = [&](const CUtensorMap (&map)[4], uint32_t dst, uint32_t bar, int x0) {
-                int row = c;
-#pragma unroll
-                for (int z = 3; z >= 0; --z)
-                    if (half & (16 << z)) {
-                        tma_load_3d_pair_if(dst, &map[z], bar, x0, row, 0, elected);
-                        dst += 2048u << z;
-                        row += 16 << z;
-                    }
-            };
+            // Not WEIGHTS: half rows (a multiple of 16, up to 128) in one box, of the map that has them.  (Put together from boxes of 16, 32,
+            // 64 and 128 rows the loads kept this warp busy for 450 clocks a k-block, whatever the tile: 1024 rows,
+            // 4096 x 1024 took 20.6 us instead of 18.8; 32 rows, 8192 x 256 13.1 instead of 11.8.)
+            const int high = (half >> 4) - 1;
             auto acquire = [&]() {
                 if (mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) return true;
                 if (lane == 0) give_up(0x100u + stage);
@@ -477,11 +471,11 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                     } else {
                         tma_load_3d_pair_if(sa, &maps.a, lfb, kx, i, u.w, elected);
                     }
-                    rows_boxes(maps.b, sb, lfb, kx);
+                    tma_load_3d_pair_if(sb, &maps.b[high], lfb, kx, c, 0, elected);
                 }
                 advance();
             }
-            if (LORA && ok && u.req_whole + u.req_parts > 0) {
+            if constexpr (LORA) if (ok && u.req_whole + u.req_parts > 0) {
                 // h16 comes from the kernel before this one
                 if (!waited) launch_wait();
                 waited = true;
@@ -500,7 +494,7 @@ grouped_kernel(const __grid_constant__ GroupedMaps maps, const __grid_constant__
                         } else {
                             tma_load_3d_pair_if(sa, &maps.c, lfb, rb * ranks, i, s_alt[q], elected);
                         }
-                        rows_boxes(maps.h, sb, lfb, rb * 64);
+                        tma_load_3d_pair_if(sb, &maps.h[high], lfb, rb * 64, c, 0, elected);
                         advance();
                     }
                 }

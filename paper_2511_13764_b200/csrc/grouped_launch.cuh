@@ -67,16 +67,19 @@ inline uint32_t grouped_idesc(bool a_mn, bool b_mn, bool f16) {
 
 struct GroupedMaps {
     CUtensorMap a;         // the features' operand: boxes of 128 features x 64 of k; with a_slabs one box, else two
-    CUtensorMap b[4];      // the rows' operand in boxes of 16, 32, 64 and 128 rows; WEIGHTS: [0] 64 features, [1] 128 of them (b_slabs)
+    CUtensorMap b[8];      // the rows' operand in boxes of 16, 32, .. 128 rows; WEIGHTS: [0] 64 features, [1] 128 of them (b_slabs)
     CUtensorMap out;       // C in boxes of 2 KB: 32 features x 32 (16-bit) or 16 (FP32) rows (not with h16)
-    CUtensorMap c, h[4];   // LORA: the adapters' B, and h16 in boxes like b's
+};
+struct LoraMaps : GroupedMaps {    // (LORA alone: another KB of arguments costs a small launch 0.9 us)
+    CUtensorMap c, h[8];   // the adapters' B, and h16 in boxes like b's
 };
 
 // (grouped_rows.cu, grouped_weights.cu, grouped_lora.cu: the instantiations; nk_grouped.cu: the rest)
 typedef void (*GroupedFunction)(GroupedMaps, GroupedParams);
+typedef void (*LoraFunction)(LoraMaps, GroupedParams);
 GroupedFunction grouped_rows_kernel(bool a_mn, GroupedOut out);
 GroupedFunction grouped_weights_kernel(GroupedOut out);
-GroupedFunction grouped_lora_kernel(bool a_mn, GroupedOut out);
+LoraFunction grouped_lora_kernel(bool a_mn, GroupedOut out);
 struct GroupedKernel {     // one instantiation
     GroupedMode mode;
     bool a_mn;
@@ -84,7 +87,7 @@ struct GroupedKernel {     // one instantiation
 };
 inline GroupedOut grouped_out(bool out16, bool f16) { return !out16 ? GRP_OUT_F32 : f16 ? GRP_OUT_F16 : GRP_OUT_BF16; }
 cudaError_t grouped_prepare(const GroupedKernel& k);     // once per kernel and device: its shared memory
-cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p);
+cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p);   // (LORA: LoraMaps)
 // Arrival counters of the tiles cut along k, zero between launches (the last arriver clears its own).  A plan holds a
 // slot of a static table from create to destroy; where none is free (null) it cuts no tile.
 constexpr int SPLIT_COUNTERS = 4096;

@@ -3,7 +3,7 @@
 
 namespace nk {
 
-GroupedFunction grouped_lora_kernel(bool a_mn, GroupedOut out) {
+LoraFunction grouped_lora_kernel(bool a_mn, GroupedOut out) {
     if (a_mn)
         return out == GRP_OUT_F32 ? grouped_kernel<GRP_LORA, true, GRP_OUT_F32>
                : out == GRP_OUT_BF16 ? grouped_kernel<GRP_LORA, true, GRP_OUT_BF16> : grouped_kernel<GRP_LORA, true, GRP_OUT_F16>;

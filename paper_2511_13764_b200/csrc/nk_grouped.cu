@@ -32,12 +32,16 @@ void give_split_slot(int slot) {
 }
 
 static GroupedFunction function_of(const GroupedKernel& k) {
-    return k.mode == GRP_WEIGHTS ? grouped_weights_kernel(k.out) : k.mode == GRP_LORA ? grouped_lora_kernel(k.a_mn, k.out) : grouped_rows_kernel(k.a_mn, k.out);
+    return k.mode == GRP_WEIGHTS ? grouped_weights_kernel(k.out) : grouped_rows_kernel(k.a_mn, k.out);
 }
 cudaError_t grouped_prepare(const GroupedKernel& k) {
-    return cudaFuncSetAttribute(function_of(k), cudaFuncAttributeMaxDynamicSharedMemorySize, grp_smem(k.out != GRP_OUT_H));
+    const int smem = grp_smem(k.out != GRP_OUT_H);
+    if (k.mode == GRP_LORA) return cudaFuncSetAttribute(grouped_lora_kernel(k.a_mn, k.out), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return cudaFuncSetAttribute(function_of(k), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
 }
 cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p) {
+    if (k.mode == GRP_LORA)
+        return launch_beside(grouped_lora_kernel(k.a_mn, k.out), 2 * pairs, GRP_THREADS, grp_smem(true), st, static_cast<const LoraMaps&>(maps), p);
     return launch_beside(function_of(k), 2 * pairs, GRP_THREADS, grp_smem(k.out != GRP_OUT_H), st, maps, p);
 }
 

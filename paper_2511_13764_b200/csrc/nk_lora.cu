@@ -11,7 +11,8 @@ struct nk_lora_s : nk::PlanBase {
     unsigned int* counters[2];
     size_t part_bytes[2], h_bytes, side_bytes;   // partial sums of the two; X . A; it and the FP32 contributions
     nk::GroupedKernel projection, shrinking;
-    nk::GroupedMaps maps, shrink; // of the projection and of X . A
+    nk::LoraMaps maps;            // of the projection
+    nk::GroupedMaps shrink;       // of X . A
     const void *cached_x, *cached_w, *cached_a, *cached_b, *cached_ws, *cached_y;
     char name[64];
 };
@@ -109,7 +110,8 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     const bool f16 = d.in_dtype == NK_F16, row = d.layout == NK_ROW_MAJOR;
     if (p->cached_x != X || p->cached_w != W || p->cached_a != A || p->cached_b != B || p->cached_ws != workspace || p->cached_y != Y) {
         p->cached_x = nullptr;
-        GroupedMaps &m = p->maps, &s = p->shrink;
+        LoraMaps& m = p->maps;
+        GroupedMaps& s = p->shrink;
         bool ok = encode_rows(m.b, X, f16, d.K, d.rows, d.ldx) && encode_out(&m.out, Y, d.out_dtype, d.N, d.rows, 1, d.ldy, 0) &&
                   (!row ? encode_map(&m.a, W, f16, d.K, d.N, 1, d.ldw, 0, 128)
                    : d.N % 64 == 0 ? encode_slabs(&m.a, W, f16, d.N, d.K, 1, d.ldw, 0) : encode_map(&m.a, W, f16, d.N, d.K, 1, d.ldw, 0, 64));

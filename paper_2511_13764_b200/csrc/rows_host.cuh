@@ -125,10 +125,10 @@ static inline bool encode_out(CUtensorMap* m, void* base, int dtype, int64_t inn
                           CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The four box heights of a rows' operand.
-static inline bool encode_rows(CUtensorMap (&m)[4], const void* base, bool f16, int64_t inner, int64_t rows, int64_t ld) {
-    for (int z = 0; z < 4; ++z)
-        if (!encode_map(&m[z], base, f16, inner, rows, 1, ld, 0, 16 << z)) return false;
+// A rows' operand in boxes of 16, 32, .. 128 rows.
+static inline bool encode_rows(CUtensorMap (&m)[8], const void* base, bool f16, int64_t inner, int64_t rows, int64_t ld) {
+    for (int z = 0; z < 8; ++z)
+        if (!encode_map(&m[z], base, f16, inner, rows, 1, ld, 0, 16 * (z + 1))) return false;
     return true;
 }
 
