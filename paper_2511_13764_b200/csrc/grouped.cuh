@@ -212,18 +212,21 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
         most = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(most)));
         // Estimated time, in clocks, of n tiles of w rows, and into how many parts (1: none) the tiles of the last, partial wave are cut:
         // equal parts, so that no pair has parts of two tiles, where they fill at most half a wave.  A k-block of a tile costs about
-        // GRP_BLOCK + w / 8 whatever its width (operand feed; the tensor core alone would need 2 w).  Parts are written to memory
+        // 260 + 1.5 w (operand feed; the tensor core alone would need 2 w for w = 256), for which GRP_BLOCK stands where the width is
+        // settled.  (600 + w / 8 held for a slower producer; with it 4099 rows in 8 groups took 43.2 us instead of 38.9, 5000
+        // rows 43.1 instead of 37.1, 4096 x 1024 both, and 29 groups of 35 rows, 2048 x 32, 13.2 instead of 14.0; with 400 at
+        // least 32 groups of 64 rows, 2048 x 768, 28.6 instead of 27.0, those of 35 rows 13.2.)  Parts are written to memory
         // at the end and the last to arrive reads them all: about 4000 clocks, and for every part and row (64 at least: a warp's
         // pieces follow one another) 10 + t^2 / 450, t being the parts of all tiles, which share the way to memory and back.
-        // So the best number of parts goes with the root of the contraction's length.  (1024 rows, 4096 x 1024: whole tiles of 256 rows
-        // 28.8 us, in four parts 26.5, tiles of 128 in two parts 21.7; 48 tiles of 86 k-blocks in two or three parts each 44, whole 36.)
+        // So the best number of parts goes with the root of the contraction's length.  (Measured with the slower producer: 1024 rows, 4096 x 1024, whole tiles of 256
+        // rows 28.8 us, in four parts 26.5, tiles of 128 in two parts 21.7; 48 tiles of 86 k-blocks in two or three parts each 44, whole 36.)
         auto share_of = [&](int w, int t) { return static_cast<float>(max(64, w)) * (10.0f + static_cast<float>(t) * t * (1.0f / 450)); };
         auto best_parts = [&](int kbs, int w, int t) {
             return max(1, min(__float2int_rn(sqrtf(__fdividef(static_cast<float>(kbs) * GRP_BLOCK, share_of(w, t)))), kbs / 4));
         };
         auto estimate = [&](int n, int w, int& parts) {
             const int waves = n / num_pairs, rest = n - waves * num_pairs, most_parts = rest ? num_pairs / rest : 1;
-            const float kb = GRP_BLOCK + w * 0.125f, k = static_cast<float>(p.kb_total), whole = (waves + (rest ? 1 : 0)) * k * kb;
+            const float kb = 260.0f + w * 1.5f, k = static_cast<float>(p.kb_total), whole = (waves + (rest ? 1 : 0)) * k * kb;
             parts = p.partial && most_parts > 1 ? min(most_parts, best_parts(p.kb_total, w, rest * most_parts)) : 1;
             const float cut = (waves * k + (p.kb_total + parts - 1) / parts) * kb + 4000.0f + share_of(w, rest * parts) * parts;
             if (parts > 1 && cut < whole) return cut;

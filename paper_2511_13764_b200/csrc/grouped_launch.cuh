@@ -16,7 +16,7 @@ constexpr int GRP_BK = 64;
 constexpr int GRP_TILE = 256;                          // features of a tile, and the most rows of one
 constexpr int GRP_TABLE = 4 * (GRP_MAX_GROUPS + 1);    // bytes of a table by group
 constexpr int GRP_STAGING = 8 * 4096;                  // of the stores: two buffers of 2 KB for each epilogue warp
-constexpr int GRP_BLOCK = 600;                         // estimated clocks of a k-block (see grouped.cuh)
+constexpr int GRP_BLOCK = 600;                         // clocks of a k-block for the choice of parts (see grouped.cuh)
 // (a kernel that only writes h16 has no staging: more room for other blocks beside it)
 __host__ __device__ constexpr int grp_smem(bool staging) { return GRP_RING + (staging ? GRP_STAGING : 0) + 1024 + 3 * GRP_TABLE + 1024; }
 
