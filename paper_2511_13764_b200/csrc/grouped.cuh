@@ -597,7 +597,10 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                         if (!WEIGHTS || steps > 3) umma_pair_if<0>(d_tmem, a_lo + 3 * a_s, a_hi, b_lo + 3 * b_s, b_hi, idesc, 1u, elected);
                     }
                     umma_commit_pair_if(empty_bar(stage), 3, elected);
-                    if (++in_chunk == chunk || n == own - 1 || (LORA && n >= own && rb == 0)) {
+                    // (a request's accumulator has all of its ranks, however short the tile's own chunks are: one with K <= 64 and
+                    // ranks above 32 closed before its last block would leave the epilogue an accumulator nobody waits for)
+                    ++in_chunk;
+                    if (n < own ? in_chunk == chunk || n == own - 1 : rb == 0) {
                         umma_commit_pair_if(tfull_bar(acc), 3, elected);
                         in_chunk = 0;
                         ++local;

@@ -129,6 +129,33 @@ def test_sixteen_bit_results(name, layout, kind, rank):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("out", ["same", "f32"])
+@pytest.mark.parametrize("rank", [40, 72, 104, 128])
+@pytest.mark.parametrize("K", [8, 64, 72, 128, 192, 776, 832])
+def test_short_contraction_high_rank(layout, kind, out, rank, K):
+    """Fewer k-blocks in X . W than in the adapters' product, requests that share tiles, tiles of one request."""
+    out = kind if out == "same" else out
+    for sizes in (SHAPES["edges"], [40, 30, 25, 9, 300, 33]):
+        data = make(sizes, 264, K, rank, 5, kind, seed=12)
+        got, plan = run(data, layout, out)
+        assert plan.kernel_name.startswith("lora_many")
+        close(got, data, out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("K", [1344, 2112, 3200, 4160])
+def test_short_last_part_high_rank(K):
+    """Few tiles, cut along k, the last part the shortest."""
+    for sizes in ([20, 25], [12, 200, 33, 11]):
+        data = make(sizes, 264, K, 128, 3, "bf16", seed=13)
+        got, plan = run(data, "row", "bf16")
+        assert plan.kernel_name.startswith("lora_many")
+        close(got, data, "bf16")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["row", "transposed"])
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 def test_many_tiles_and_a_cut_last_wave(layout, out):
     data = make([1, 1500, 1, 1, 3, 700, 9, 1, 360], 2056, 1096, 72, 4, "bf16", seed=9)
