@@ -10,6 +10,9 @@
  * Conventions are those of nk_gemm.h: DEVICE pointers on the plan's device, nothing is allocated on the
  * device, nothing synchronises inside a run call, failures are status codes, and a plan (with its workspace)
  * serves one stream at a time: two runs of a plan whose work can overlap on the device race.
+ * A plan may be destroyed while runs of it are queued or are held by a CUDA graph: they keep what they need, and the
+ * counters they use in the library's static memory go to no other plan before they have ended (those of a captured run,
+ * never).  The caller's buffers have to live as long as the runs, as always.
  * Matrices are row-major; "ld" fields are row strides in elements (0: dense).
  */
 #ifndef NK_ROWS_H

@@ -89,10 +89,10 @@ inline GroupedOut grouped_out(bool out16, bool f16) { return !out16 ? GRP_OUT_F3
 cudaError_t grouped_prepare(const GroupedKernel& k);     // once per kernel and device: its shared memory
 cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p);   // (LORA: LoraMaps)
 // Arrival counters of the tiles cut along k, zero between launches (the last arriver clears its own).  A plan holds a
-// slot of a static table from create to destroy; where none is free (null) it cuts no tile.
+// slot of a static table from create until its last run has ended (see slot_table.h); where none is free (null) it cuts no tile.
 constexpr int SPLIT_COUNTERS = 4096;
-int take_split_slot(unsigned int** counters);
-void give_split_slot(int slot);
+int take_split_slot(int device, unsigned int** counters);      // (of the current device)
+void give_split_slot(int device, int slot, bool in_flight, bool captured);
 inline size_t grouped_partial_bytes(int pairs, int slab_cols) {
     return static_cast<size_t>(pairs) * 2 * GRP_TILE * slab_cols * sizeof(float);
 }

@@ -1,34 +1,31 @@
 // Host side of nk_grouped: descriptor validation, TMA maps, the launch.
 #include "rows_host.cuh"
 #include "grouped_launch.cuh"
+#include "slot_table.h"
 
 namespace nk {
 
-constexpr int SPLIT_SLOTS = 1024;
-__device__ unsigned int g_split_counter[SPLIT_SLOTS][SPLIT_COUNTERS];
-static std::mutex g_split_mutex;
-static bool g_split_taken[SPLIT_SLOTS];
+__device__ unsigned int g_split_counter[SlotTable::SLOTS][SPLIT_COUNTERS];
+constexpr int MAX_DEVICES = 64;
+static SlotTable g_split_slots[MAX_DEVICES];      // (the words are in every device's memory)
 
-int take_split_slot(unsigned int** counters) {
+int take_split_slot(int device, unsigned int** counters) {
     *counters = nullptr;
     void* sym = nullptr;
-    if (cudaGetSymbolAddress(&sym, g_split_counter) != cudaSuccess) {
+    if (device >= MAX_DEVICES || cudaGetSymbolAddress(&sym, g_split_counter) != cudaSuccess) {
         cudaGetLastError();
         return -1;
     }
-    std::lock_guard<std::mutex> lock(g_split_mutex);
-    for (int i = 0; i < SPLIT_SLOTS; ++i)
-        if (!g_split_taken[i]) {
-            g_split_taken[i] = true;
-            *counters = static_cast<unsigned int*>(sym) + i * SPLIT_COUNTERS;
-            return i;
-        }
-    return -1;
+    const int slot = g_split_slots[device].take([] { return cudaDeviceSynchronize() == cudaSuccess; });
+    if (slot < 0) {
+        cudaGetLastError();
+        return -1;
+    }
+    *counters = static_cast<unsigned int*>(sym) + slot * SPLIT_COUNTERS;
+    return slot;
 }
-void give_split_slot(int slot) {
-    if (slot < 0) return;
-    std::lock_guard<std::mutex> lock(g_split_mutex);
-    g_split_taken[slot] = false;
+void give_split_slot(int device, int slot, bool in_flight, bool captured) {
+    if (slot >= 0) g_split_slots[device].give(slot, in_flight, captured);
 }
 
 static GroupedFunction function_of(const GroupedKernel& k) {
@@ -107,7 +104,7 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
     if (grouped_prepare(p->kernel) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
     p->slab_cols = grouped_slab_cols(weights ? d.K : d.rows);
-    p->split_slot = take_split_slot(&p->counters);
+    p->split_slot = take_split_slot(d.device, &p->counters);
     snprintf(p->name, sizeof(p->name), "grouped_%s_256x256x64_pair", weights ? "weights" : d.layout_b == NK_TRANSPOSED ? "rows_t" : "rows");
     *out = p;
     return NK_OK;
@@ -179,6 +176,7 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     g.a_slabs = d.N % 64 == 0;
     g.b_slabs = d.K % 64 == 0;
     g.chunk = d.out_dtype == NK_F32 ? GRP_CHUNK : 0;
+    base_runs(p, static_cast<cudaStream_t>(cuda_stream));
     const cudaError_t e = grouped_launch(p->kernel, p->pairs, static_cast<cudaStream_t>(cuda_stream), p->maps, g);
     return e == cudaSuccess ? NK_OK : p->cuda("grouped launch", e);
 }
@@ -197,7 +195,7 @@ const char* nk_grouped_kernel_name(nk_grouped_t p) { return p ? p->name : ""; }
 const char* nk_grouped_last_cuda_error(nk_grouped_t p) { return p ? p->cuda_err : ""; }
 
 nk_status_t nk_grouped_destroy(nk_grouped_t p) {
-    if (p) give_split_slot(p->split_slot);
+    if (p) give_split_slot(p->device, p->split_slot, p->in_flight, p->captured);
     delete p;
     return NK_OK;
 }

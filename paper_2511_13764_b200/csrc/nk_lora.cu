@@ -81,7 +81,7 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     const int64_t short_rows = p->few || d.rows < LORA_ROWS * d.requests ? d.rows : LORA_ROWS * d.requests;
     p->side_bytes = p->h_bytes + align256(static_cast<size_t>(short_rows) * d.N * sizeof(float));
     for (int i = p->few ? 1 : 0; i < 2; ++i) {
-        p->split_slot[i] = take_split_slot(&p->counters[i]);
+        p->split_slot[i] = take_split_slot(d.device, &p->counters[i]);
         p->part_bytes[i] = p->split_slot[i] < 0 ? 0 : grouped_partial_bytes(p->pairs, grouped_slab_cols(d.rows));
     }
     snprintf(p->name, sizeof(p->name), "lora_%s_%s", p->few ? "few" : "many", row ? "rows" : "rows_t");
@@ -134,6 +134,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
         p->cached_y = Y;
     }
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    base_runs(p, st);
     char* ws = static_cast<char*>(workspace);
     float* partial[2];
     for (int i = 0; i < 2; ++i) partial[i] = p->part_bytes[i] ? reinterpret_cast<float*>(ws + p->side_bytes + (i ? p->part_bytes[0] : 0)) : nullptr;
@@ -230,8 +231,7 @@ const char* nk_lora_last_cuda_error(nk_lora_t p) { return p ? p->cuda_err : ""; 
 
 nk_status_t nk_lora_destroy(nk_lora_t p) {
     if (p) {
-        give_split_slot(p->split_slot[0]);
-        give_split_slot(p->split_slot[1]);
+        for (int slot : p->split_slot) give_split_slot(p->device, slot, p->in_flight, p->captured);
     }
     delete p;
     return NK_OK;

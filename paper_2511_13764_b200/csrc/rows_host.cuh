@@ -16,6 +16,7 @@ constexpr unsigned int STATUS_BAD_OFFSETS = 0x10000u;
 struct PlanBase {
     int device, sm_count;
     unsigned int* status_dev;
+    bool in_flight, captured;     // a run may not have ended; a graph holds one
     char cuda_err[256];
 
     nk_status_t cuda(const char* what, cudaError_t e) {
@@ -53,12 +54,21 @@ static inline nk_status_t base_init(PlanBase* p, int device, int sm_count) {
     return take_status_slot(&p->status_dev);
 }
 
+// What a run leaves to know for the plan's end.
+static inline void base_runs(PlanBase* p, cudaStream_t st) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &status) != cudaSuccess) cudaGetLastError();      // (the launch will say it)
+    if (status != cudaStreamCaptureStatusNone) p->captured = true;
+    p->in_flight = true;
+}
+
 // Synchronises and takes the status word: NK_OK, NK_ERR_INVALID_ARG (offsets) or NK_ERR_TIMEOUT.
 static inline nk_status_t base_check(PlanBase* p) {
     DeviceGuard guard(p->device);
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     cudaError_t e = cudaDeviceSynchronize();
     if (e != cudaSuccess) return p->cuda("cudaDeviceSynchronize", e);
+    p->in_flight = false;
     unsigned int w = 0;
     const unsigned int z = 0;
     if ((e = cudaMemcpy(&w, p->status_dev, sizeof(w), cudaMemcpyDeviceToHost)) != cudaSuccess) return p->cuda("status read", e);

@@ -230,6 +230,60 @@ def test_more_plans_than_counters():
 
 
 @pytest.mark.gpu
+def test_plan_destroyed_with_runs_queued():
+    """The next plan of cut tiles, on another stream, does not count in the words of the runs that are left."""
+    gen = torch.Generator().manual_seed(20)
+    W = rand((1, 8192, 512), "bf16", gen, 0.01).cuda()
+    A = [rand((40, 8192), "bf16", gen).cuda() for _ in range(2)]
+    off = torch.tensor([0, 40], dtype=torch.int32).cuda()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    bytes_ = nk.GroupedPlan(1, 40, 512, 8192, out_dtype=nk.F32).workspace_bytes
+    ws = [torch.full((bytes_,), 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    want = [a.double() @ W[0].double() for a in A]
+    size = [float((a.double().abs() @ W[0].double().abs()).max()) for a in A]
+    for _ in range(5):
+        outs = [[torch.full((40, 512), float("nan"), device="cuda") for _ in range(30)] for _ in range(2)]
+        torch.cuda.synchronize()
+        for i in range(2):
+            plan = nk.GroupedPlan(1, 40, 512, 8192, out_dtype=nk.F32)
+            for C in outs[i]:
+                plan.run(A[i], W, C, off, workspace=ws[i], stream=streams[i].cuda_stream)
+            plan.destroy()
+        torch.cuda.synchronize()
+        for i in range(2):
+            for C in outs[i]:
+                close(C, want[i], size[i], "f32")
+
+
+@pytest.mark.gpu
+def test_graph_outlives_its_plan():
+    """A captured run goes on working, and goes on counting in words of its own, when its plan is gone."""
+    gen = torch.Generator().manual_seed(21)
+    A, W = rand((40, 8192), "bf16", gen).cuda(), rand((1, 8192, 512), "bf16", gen, 0.01).cuda()
+    off = torch.tensor([0, 40], dtype=torch.int32).cuda()
+    want, size = A.double() @ W[0].double(), float((A.double().abs() @ W[0].double().abs()).max())
+    plan = nk.GroupedPlan(1, 40, 512, 8192, out_dtype=nk.F32)
+    ws, C, D = scratch(plan), torch.empty(40, 512, device="cuda"), torch.empty(40, 512, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.run(A, W, C, off, workspace=ws, stream=torch.cuda.current_stream().cuda_stream)
+    plan.destroy()
+    other, side = nk.GroupedPlan(1, 40, 512, 8192, out_dtype=nk.F32), torch.cuda.Stream()
+    ws2 = scratch(other)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        C.fill_(float("nan"))
+        D.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for _ in range(10):
+            graph.replay()
+            other.run(A, W, D, off, workspace=ws2, stream=side.cuda_stream)
+        torch.cuda.synchronize()
+        close(C, want, size, "f32")
+        close(D, want, size, "f32")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("name", list(GROUPS))
 def test_weights_of_ragged_groups(name):
     run_weights(GROUPS[name], 264, 200, seed=11)
