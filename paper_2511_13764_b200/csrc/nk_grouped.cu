@@ -21,7 +21,14 @@ int take_split_slot(int device, unsigned int** counters) {
         cudaGetLastError();
         return -1;
     }
-    *counters = static_cast<unsigned int*>(sym) + slot * SPLIT_COUNTERS;
+    // zero, whatever the plan before has left (a launch that gave up and was never checked leaves counts), and before any stream's run
+    unsigned int* words = static_cast<unsigned int*>(sym) + slot * SPLIT_COUNTERS;
+    if (cudaMemset(words, 0, SPLIT_COUNTERS * sizeof(unsigned int)) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) {
+        cudaGetLastError();
+        g_split_slots[device].give(slot, false, false);
+        return -1;
+    }
+    *counters = words;
     return slot;
 }
 void give_split_slot(int device, int slot, bool in_flight, bool captured) {
