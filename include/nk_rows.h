@@ -12,7 +12,10 @@
  * serves one stream at a time: two runs of a plan whose work can overlap on the device race.
  * A plan may be destroyed while runs of it are queued or are held by a CUDA graph: they keep what they need, and the
  * counters they use in the library's static memory go to no other plan before they have ended (those of a captured run,
- * never).  The caller's buffers have to live as long as the runs, as always.
+ * never).  A device has 1024 sets of counters: nk_grouped takes one, nk_lora one or two; a plan that finds none cuts no
+ * tile along its contraction, which costs time where there are few tiles and adds FP32 sums in another order: its kernel
+ * name ends in "_uncut", and its bits can differ from those of a plan with counters.  Bits of one plan are the same on every run.
+ * The caller's buffers have to live as long as the runs, as always.
  * Matrices are row-major; "ld" fields are row strides in elements (0: dense).
  */
 #ifndef NK_ROWS_H

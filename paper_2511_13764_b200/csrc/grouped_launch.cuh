@@ -90,8 +90,8 @@ cudaError_t grouped_prepare(const GroupedKernel& k);     // once per kernel and 
 cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p);   // (LORA: LoraMaps)
 // Arrival counters of the tiles cut along k, zero between launches (the last arriver clears its own).  A plan holds a
 // slot of a static table from create until its last run has ended (see slot_table.h); where none is free (null) it cuts no tile.
-constexpr int SPLIT_COUNTERS = 4096;
-int take_split_slot(int device, unsigned int** counters);      // (of the current device)
+constexpr int SPLIT_COUNTERS = 1280;           // 16 for each CTA pair of the device (a cut tile is one of the last wave)
+int take_split_slot(int device, int pairs, unsigned int** counters);      // (of the current device)
 void give_split_slot(int device, int slot, bool in_flight, bool captured);
 inline size_t grouped_partial_bytes(int pairs, int slab_cols) {
     return static_cast<size_t>(pairs) * 2 * GRP_TILE * slab_cols * sizeof(float);

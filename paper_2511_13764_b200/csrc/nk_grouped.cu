@@ -9,10 +9,10 @@ __device__ unsigned int g_split_counter[SlotTable::SLOTS][SPLIT_COUNTERS];
 constexpr int MAX_DEVICES = 64;
 static SlotTable g_split_slots[MAX_DEVICES];      // (the words are in every device's memory)
 
-int take_split_slot(int device, unsigned int** counters) {
+int take_split_slot(int device, int pairs, unsigned int** counters) {
     *counters = nullptr;
     void* sym = nullptr;
-    if (device >= MAX_DEVICES || cudaGetSymbolAddress(&sym, g_split_counter) != cudaSuccess) {
+    if (device >= MAX_DEVICES || 16 * pairs > SPLIT_COUNTERS || cudaGetSymbolAddress(&sym, g_split_counter) != cudaSuccess) {
         cudaGetLastError();
         return -1;
     }
@@ -111,8 +111,9 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
     if (grouped_prepare(p->kernel) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
     p->slab_cols = grouped_slab_cols(weights ? d.K : d.rows);
-    p->split_slot = take_split_slot(d.device, &p->counters);
-    snprintf(p->name, sizeof(p->name), "grouped_%s_256x256x64_pair", weights ? "weights" : d.layout_b == NK_TRANSPOSED ? "rows_t" : "rows");
+    p->split_slot = take_split_slot(d.device, p->pairs, &p->counters);
+    snprintf(p->name, sizeof(p->name), "grouped_%s_256x256x64_pair%s", weights ? "weights" : d.layout_b == NK_TRANSPOSED ? "rows_t" : "rows",
+             p->split_slot < 0 ? "_uncut" : "");
     *out = p;
     return NK_OK;
 }

@@ -81,10 +81,11 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     const int64_t short_rows = p->few || d.rows < LORA_ROWS * d.requests ? d.rows : LORA_ROWS * d.requests;
     p->side_bytes = p->h_bytes + align256(static_cast<size_t>(short_rows) * d.N * sizeof(float));
     for (int i = p->few ? 1 : 0; i < 2; ++i) {
-        p->split_slot[i] = take_split_slot(d.device, &p->counters[i]);
+        p->split_slot[i] = take_split_slot(d.device, p->pairs, &p->counters[i]);
         p->part_bytes[i] = p->split_slot[i] < 0 ? 0 : grouped_partial_bytes(p->pairs, grouped_slab_cols(d.rows));
     }
-    snprintf(p->name, sizeof(p->name), "lora_%s_%s", p->few ? "few" : "many", row ? "rows" : "rows_t");
+    snprintf(p->name, sizeof(p->name), "lora_%s_%s%s", p->few ? "few" : "many", row ? "rows" : "rows_t",
+             p->split_slot[1] < 0 || (!p->few && p->split_slot[0] < 0) ? "_uncut" : "");
     *out = p;
     return NK_OK;
 }

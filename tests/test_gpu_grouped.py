@@ -230,6 +230,19 @@ def test_more_plans_than_counters():
 
 
 @pytest.mark.gpu
+def test_plan_without_counters_says_so():
+    plans = [nk.GroupedPlan(1, 40, 512, 8192, out_dtype=nk.F32) for _ in range(1025)]
+    late = nk.LoraPlan(40, 64, 64, 8, 1, 1), nk.LoraPlan(4000, 64, 64, 8, 1, 1)
+    for plan in (plans[-1],) + late:
+        assert plan.kernel_name.endswith("_uncut")
+    assert not plans[0].kernel_name.endswith("_uncut")
+    for plan in (*plans, *late):
+        plan.destroy()
+    again = nk.LoraPlan(4000, 64, 64, 8, 1, 1), nk.GroupedPlan(1, 40, 512, 8192)
+    assert not any(plan.kernel_name.endswith("_uncut") for plan in again)
+
+
+@pytest.mark.gpu
 def test_plan_destroyed_with_runs_queued():
     """The next plan of cut tiles, on another stream, does not count in the words of the runs that are left."""
     gen = torch.Generator().manual_seed(20)
