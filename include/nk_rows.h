@@ -149,9 +149,11 @@ nk_status_t nk_route_destroy(nk_route_t plan);
  *   layout NK_TRANSPOSED   W [N][K],  A [adapters][rank][K],  B [adapters][N][rank]   (linear layers' [out][in])
  *
  * Adapters of a lower rank are padded with zeros.  16-bit operands of one type, FP32 accumulation, Y in FP32 or rounded
- * once to the operands' type.  X . A_a is held in FP32, or where the tensor cores multiply it by B_a as the sum of two 16-bit
- * numbers (good to 2^-16 of it with NK_BF16, 2^-21 with NK_F16) or, for an FP32 Y of NK_BF16 operands, three (2^-24); with
- * NK_F16 |scale * X . A_a| has to stay within the type's range.
+ * once to the operands' type.  X . A_a is held in FP32, or where the tensor cores multiply it by B_a (requests of more than eight
+ * rows) as the sum of 16-bit numbers.  NK_BF16: two, good to 2^-16 of each element, or for an FP32 Y three (2^-24).  NK_F16: two, good
+ * to 2^-22 of each element and never worse than 2^-20 of its row's largest, or for an FP32 Y three (2^-33, 2^-40), whatever the
+ * row's size: rows that FP16 has no range for are scaled by a power of two.  (An infinite element of B_a times such a sum is an
+ * infinity or NaN.)
  * Offsets that break the rule are clamped and reported by nk_lora_check, as for nk_grouped.
  */
 typedef struct nk_lora_s* nk_lora_t;

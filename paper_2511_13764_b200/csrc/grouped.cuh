@@ -79,6 +79,7 @@ __global__ void __launch_bounds__(MODE == GRP_ROWS && OUT != GRP_OUT_F32 ? 512 :
 grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, LoraMaps, GroupedMaps> maps, const __grid_constant__ GroupedParams p) {
     constexpr bool WEIGHTS = MODE == GRP_WEIGHTS, LORA = MODE == GRP_LORA;
     constexpr bool OUT16 = OUT == GRP_OUT_BF16 || OUT == GRP_OUT_F16, F16 = OUT == GRP_OUT_F16;
+    constexpr bool SCALED = LORA && OUT != GRP_OUT_BF16;   // operands may be FP16: rows of h16 may have a factor (p.unscale)
     constexpr int STAGING = OUT == GRP_OUT_H ? 0 : GRP_STAGING;
     static_assert(!WEIGHTS || A_MN, "rows are contiguous in their features");
     extern __shared__ uint8_t smem_raw[];
@@ -181,9 +182,10 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
     auto rows_of = [&](const GroupedUnit& u, int kb) { return min(GRP_BK, u.rows - kb * GRP_BK); };
 
     // LORA: the requests' blocks follow the last k-block of a tile.  A request that has all of the tile's rows goes into
-    // the tile's own accumulator.  Of the others each gets an accumulator of its own, of which the epilogue adds the
-    // request's columns to the tile's sum: an adapter of infinities or NaN cannot reach another request's rows.  Requests
-    // of p.min_rows rows or fewer are not worth an accumulator: theirs comes in FP32 from the kernel before (`add`).
+    // the tile's own accumulator, unless rows of it have a factor (p.unscale).  Of the others each gets an accumulator of its own, of
+    // which the epilogue adds the request's columns to the tile's sum: an adapter of infinities or NaN cannot reach another
+    // request's rows.  Requests of p.min_rows rows or fewer are not worth an accumulator: theirs comes in FP32 from the
+    // kernel before (`add`).
     auto has_part = [&](int q) { return s_alt[q] >= 0 && s_row[q + 1] - s_row[q] > p.min_rows; };
     auto is_short = [&](int q) { return s_alt[q] >= 0 && s_row[q + 1] > s_row[q] && s_row[q + 1] - s_row[q] <= p.min_rows; };
 
@@ -310,6 +312,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                 tail_len = (tiles - from) * padded;
             }
         }
+        bool waited = false;
         int next_tile = pair_id, x = pair_id * share;     // this pair's next whole tile, its place in the tail
         const int tail_hi = min(x + share, tail_len);
         GroupedUnit u = {};
@@ -385,7 +388,16 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                     parts_of = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(parts_of)));
                     u.shorts = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(shorts)));
                     if (u.kb1 == kbs && parts_of) {
-                        if (s_row[u.req] <= u.c0 && s_row[u.req + 1] >= u.c0 + u.cols) u.req_whole = p.rank_blocks;
+                        bool whole = s_row[u.req] <= u.c0 && s_row[u.req + 1] >= u.c0 + u.cols;
+                        if (SCALED && whole && p.unscale) {
+                            // (the kernel before this one writes the factors)
+                            if (!waited) launch_wait();
+                            waited = true;
+                            bool plain = true;
+                            for (int r = lane; r < u.cols; r += 32) plain &= __ldcg(p.unscale + u.c0 + r) == 1.0f;
+                            whole = __all_sync(~0u, plain);
+                        }
+                        if (whole) u.req_whole = p.rank_blocks;
                         else u.req_parts = parts_of;
                     }
                 }
@@ -653,7 +665,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
             const int n = min(32, u.cols - c), i0 = u.i0 + static_cast<int>(rank) * 128 + quarter * 32;
             const size_t row0 = static_cast<size_t>(u.c0 + c);
             if (OUT == GRP_OUT_H || (MODE == GRP_ROWS && OUT == GRP_OUT_F32 && p.h16)) {
-                // X . A_a for the adapters: the scaled product as a leading 16-bit part and one or two remainders (none behind an
+                // X . A_a for the adapters: the scaled product as a leading BF16 part and one or two remainders (none behind an
                 // infinite leading part); ranks beyond the last are zeros
                 const float scale = __ldg(p.scale + u.w);
                 const int pitch = p.rank_blocks * 64, per = p.planes == 3 ? 16 : 32, i = i0 + lane;
@@ -666,8 +678,8 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
 #pragma unroll
                             for (int z = 0; z < 3; ++z) {
                                 if (z == p.planes) break;
-                                const uint32_t bits = pack_half2(x, 0.0f, p.f16) & 0xFFFFu;
-                                const float lead = half_bits_to_f32(bits, p.f16);
+                                const uint32_t bits = pack_half2(x, 0.0f, 0) & 0xFFFFu;
+                                const float lead = half_bits_to_f32(bits, 0);
                                 h[z * per] = static_cast<uint16_t>(bits);
                                 x = fabsf(lead) <= 3.4028235e38f ? x - lead : 0.0f;
                             }
@@ -678,6 +690,11 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                 return;
             }
             const bool live = i0 + lane < p.I;
+            if (MODE == GRP_ROWS && OUT == GRP_OUT_F32 && p.scale) {
+                const float scale = __ldg(p.scale + u.w);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] *= scale;
+            }
             if (MODE == GRP_ROWS && p.add) {
                 if (!waited) launch_wait();
                 waited = true;
@@ -788,6 +805,11 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                         ++at;
                     }
                     const uint32_t taddr = tmem_base + (local & 1) * GRP_TILE + lane_addr;
+                    const bool unscale = SCALED && n >= chunks && p.unscale;
+                    if (unscale && !waited) {
+                        launch_wait();
+                        waited = true;
+                    }
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int c = set * 32 + q * 64;
@@ -795,7 +817,15 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                             uint32_t v[32];
                             tmem_ld_32x32(taddr + c, v);
                             tmem_ld_wait();
-                            if (!LORA || (c >= lo && c + 32 <= hi)) {
+                            if (unscale) {
+                                // lane l has the factor of the piece's row l
+                                const float factor = lane < u.cols - c ? __ldcg(p.unscale + u.c0 + c + lane) : 0.0f;
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) {
+                                    const float f = __shfl_sync(~0u, factor, j);
+                                    if (c + j >= lo && c + j < hi) sum[q][j] += __uint_as_float(v[j]) * f;
+                                }
+                            } else if (!LORA || (c >= lo && c + 32 <= hi)) {
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) sum[q][j] += __uint_as_float(v[j]);
                             } else {

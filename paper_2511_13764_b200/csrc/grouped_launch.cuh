@@ -47,11 +47,15 @@ struct GroupedParams {
     int slab_cols;         // columns of a slab
     unsigned int* counter; // arrivals, a byte per (cut tile, CTA of the pair, 32-column piece, warp); zero before and after
     unsigned int* status;
-    // adapters.  ROWS with h16 (out H, or F32: by chunks): instead of C the product times scale[weight] is stored as two or three
-    // 16-bit numbers (`planes`) that add up to it, each the rounding of what the ones before it leave: blocks of 64 to a row, of 32
-    // (two) or 16 (three) ranks, plane after plane.  LORA: each request's rows of h16 times its B_a are further k-blocks of a tile.
+    // adapters.  LORA: each request's rows of h16 times its B_a are further k-blocks of a tile.  A row of h16 is a row of X . A_a as two
+    // or three 16-bit numbers (`planes`) that add up to it, each the rounding of what the ones before it leave: blocks of 64
+    // to a row, of 32 (two) or 16 (three) ranks, plane after plane.
+    // BF16: ROWS with h16 (out H, or F32: by chunks) stores the product times scale[weight] that way instead of C.
+    // FP16: ROWS (out F32) stores the product times scale[weight] as C, from which lora_split_kernel makes h16, with rows that need it
+    // multiplied by a power of two; LORA's epilogue multiplies their part by the inverse, `unscale`.
     uint16_t* h16;
-    const float* scale;
+    const float* scale;    // ROWS; null: none
+    const float* unscale;  // FP32 [rows]; null: BF16
     int rank_blocks, rank, planes;
     int requests;
     const int* request_offsets;

@@ -9,7 +9,8 @@ struct nk_lora_s : nk::PlanBase {
     int pairs, rank_blocks, planes;
     int split_slot[2];            // of X . A and of the projection: the two overlap
     unsigned int* counters[2];
-    size_t part_bytes[2], h_bytes, side_bytes;   // partial sums of the two; X . A; it and the FP32 contributions
+    size_t part_bytes[2], side_bytes;   // partial sums of the two; what lies before them:
+    size_t h32_at, unscale_at, d_at;    // X . A in 16-bit numbers, then (FP16) in FP32 and the rows' factors, then the FP32 contributions
     nk::GroupedKernel projection, shrinking;
     nk::LoraMaps maps;            // of the projection
     nk::GroupedMaps shrink;       // of X . A
@@ -66,20 +67,24 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     const bool row = d.layout == NK_ROW_MAJOR;
     p->few = d.rows <= LORA_ROWS * d.requests || (!row && d.rank <= 64 && d.rows / LORA_ROWS + d.requests <= 32);
     p->projection = {p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
-    // (one accumulator for all of K is cut short by up to K 2^-28 of itself, far below what a 16-bit Y keeps, and its kernel leaves
-    // room for lora_delta_kernel's blocks; an FP32 Y has X . A_a summed by chunks)
-    p->shrinking = {GRP_ROWS, row, d.out_dtype == NK_F32 ? GRP_OUT_F32 : GRP_OUT_H};
+    // (BF16 with a 16-bit Y: one accumulator for all of K is cut short by up to K 2^-28 of itself, far below what Y keeps, and its
+    // kernel leaves room for lora_delta_kernel's blocks; an FP32 Y, and FP16 by way of FP32, has X . A_a summed by chunks)
+    const bool f16 = d.in_dtype == NK_F16;
+    p->shrinking = {GRP_ROWS, row, d.out_dtype == NK_F32 || f16 ? GRP_OUT_F32 : GRP_OUT_H};
     cudaError_t e = grouped_prepare(p->projection);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(d.in_dtype == NK_F16 ? lora_delta_kernel<true> : lora_delta_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, lora_smem(LORA_MAX_RANK, LORA_MAX_REQUESTS, false));
     if (e == cudaSuccess && !p->few) e = grouped_prepare(p->shrinking);
     if (e != cudaSuccess || !encode_tiled()) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
-    // two BF16 numbers hold X . A_a to 2^-16 of it: enough for a 16-bit Y, not for an FP32 one, which gets three (2^-24)
-    p->planes = d.out_dtype == NK_F32 && d.in_dtype == NK_BF16 ? 3 : 2;
+    // two 16-bit numbers hold X . A_a to 2^-16 (BF16) or 2^-22 (FP16) of it: enough for a 16-bit Y, not for an FP32 one, which gets
+    // three (2^-24 and better)
+    p->planes = d.out_dtype == NK_F32 ? 3 : 2;
     p->rank_blocks = static_cast<int>(div_up(d.rank, p->planes == 3 ? 16 : 32));
-    p->h_bytes = p->few ? 0 : align256(static_cast<size_t>(d.rows) * p->rank_blocks * 128);
     const int64_t short_rows = p->few || d.rows < LORA_ROWS * d.requests ? d.rows : LORA_ROWS * d.requests;
-    p->side_bytes = p->h_bytes + align256(static_cast<size_t>(short_rows) * d.N * sizeof(float));
+    p->h32_at = p->few ? 0 : align256(static_cast<size_t>(d.rows) * p->rank_blocks * 128);
+    p->unscale_at = p->h32_at + (p->few || !f16 ? 0 : align256(static_cast<size_t>(d.rows) * d.rank * sizeof(float)));
+    p->d_at = p->unscale_at + (p->few || !f16 ? 0 : align256(static_cast<size_t>(d.rows) * sizeof(float)));
+    p->side_bytes = p->d_at + align256(static_cast<size_t>(short_rows) * d.N * sizeof(float));
     for (int i = p->few ? 1 : 0; i < 2; ++i) {
         p->split_slot[i] = take_split_slot(d.device, p->pairs, &p->counters[i]);
         p->part_bytes[i] = p->split_slot[i] < 0 ? 0 : grouped_partial_bytes(p->pairs, grouped_slab_cols(d.rows));
@@ -121,6 +126,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
             ok = ok && encode_rows(m.h, workspace, f16, h, d.rows, h) &&
                  (row ? encode_map(&s.a, A, f16, r, d.K, d.adapters, r, r * d.K, 64) : encode_map(&s.a, A, f16, d.K, r, d.adapters, d.K, r * d.K, 128)) &&
                  (row ? encode_map(&m.c, B, f16, d.N, r, d.adapters, d.N, r * d.N, 32) : encode_map(&m.c, B, f16, r, d.N, d.adapters, r, r * d.N, 128));
+            if (f16) ok = ok && encode_out(&s.out, static_cast<char*>(workspace) + p->h32_at, NK_F32, r, d.rows, 1, r, 0);
             memcpy(s.b, m.b, sizeof(s.b));
         }
         if (!ok) {
@@ -149,7 +155,6 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     g.rank = static_cast<int>(d.rank);
     g.rank_blocks = p->rank_blocks;
     g.planes = p->planes;
-    g.scale = scale;
     LoraParams l = {};
     l.rows = g.rows;
     l.N = static_cast<int>(d.N);
@@ -166,7 +171,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     l.scale = scale;
     l.offsets = offsets;
     l.adapter = adapter;
-    l.D = reinterpret_cast<float*>(ws + p->h_bytes);
+    l.D = reinterpret_cast<float*>(ws + p->d_at);
     l.status = p->status_dev;
     // Clusters: no more than there can be chunks of rows.  Up to two rounds of them go to as many clusters as fit with one block
     // to an SM (two in each of eight GPCs), beside which the projection's or X . A's blocks find room; more of them are bound by
@@ -189,14 +194,25 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
         h.index = adapter;
         h.index_max = l.adapters;
         h.min_rows = LORA_ROWS;
+        h.scale = scale;
         h.I = g.rank;
         h.tiles_i = 1;
-        h.chunk = d.out_dtype == NK_F32 ? GRP_CHUNK : 0;
-        h.h16 = reinterpret_cast<uint16_t*>(ws);
+        h.chunk = p->shrinking.out == GRP_OUT_F32 ? GRP_CHUNK : 0;
+        LoraSplitParams split = {};
+        if (f16) {
+            h.C = ws + p->h32_at;
+            h.ldc = d.rank;
+            split = {h.rows, h.I, g.rank_blocks, g.planes, static_cast<const float*>(h.C), reinterpret_cast<uint16_t*>(ws), reinterpret_cast<float*>(ws + p->unscale_at)};
+            g.unscale = split.unscale;
+        } else {
+            h.h16 = reinterpret_cast<uint16_t*>(ws);
+        }
         h.partial = partial[0];
         h.counter = p->counters[0];
         e = grouped_launch(p->shrinking, p->pairs, st, p->shrink, h);
         if (e != cudaSuccess) return p->cuda("lora shrink launch", e);
+        if (f16 && (e = launch_beside(lora_split_kernel, static_cast<unsigned>(div_up(d.rows, LORA_SPLIT_ROWS)), 32 * LORA_SPLIT_ROWS, 0, st, split)) != cudaSuccess)
+            return p->cuda("lora split launch", e);
         g.requests = h.groups;
         g.request_offsets = offsets;
         g.index = adapter;

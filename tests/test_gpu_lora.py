@@ -212,6 +212,65 @@ def test_nan_stays_with_its_request(name, layout):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("out", ["f16", "f32"])
+@pytest.mark.parametrize("rank", [8, 40, 128])
+@pytest.mark.parametrize("size", [2.0 ** -30, 2.0 ** -17, 2.0 ** -10, 1.0, 2.0 ** 18])
+def test_fp16_adapters_of_any_size(layout, out, rank, size):
+    """The adapters' part alone (W = 0), scale X . A_a from far below FP16's smallest number to far above its largest, rows of
+    a request up to 2^11 apart: every row is as good as FP32 sums and two FP16 numbers of its own scale make it, in short requests and long.
+    Of a row: 1e-5 of its largest sum of |products| (what the other tests allow of the largest row's), 2^-21 of its largest
+    |scale X . A_a| times the sums of |B_a|, and half a unit in the last place of the result."""
+    sizes = [300, 9, 8, 1, 20, 256]
+    data = make(sizes, 264, 328, rank, 4, "f16", seed=14)
+    X, W, A, B, scale, off, which = data
+    W.zero_()
+    X.mul_(2.0 ** -(torch.arange(X.shape[0]) % 12).to(X.dtype)[:, None])
+    scale.mul_(size)
+    if out == "f16" and size > 1:
+        B.mul_(1.0 / 512)
+    got, plan = run(data, layout, out)
+    assert plan.kernel_name.startswith("lora_many")
+    for q, a in enumerate(which.tolist()):
+        lo, hi, s = int(off[q]), int(off[q + 1]), float(scale[a])
+        x, f, g = X[lo:hi].double(), A[a].double(), B[a].double()
+        h = s * x @ f
+        want, sums = h @ g, (s * (x.abs() @ f.abs()) @ g.abs()).amax(1, keepdim=True)
+        tol = TOL_REL_SMAX * sums + 2.0 ** -21 * h.abs().amax(1, keepdim=True) * g.abs().sum(0)
+        if out == "f16":
+            tol = tol + TOL_F16_REL * want.abs() + TOL_F16_ABS
+        bad = ~((got[lo:hi].double() - want).abs() <= tol)
+        assert not bad.any(), f"request {q}: {int(bad.sum())} of {bad.numel()} off, got {got[lo:hi][bad][0]} want {want[bad][0]}"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("out", ["f16", "f32"])
+def test_fp16_nan_stays_with_its_request(layout, out):
+    data = make(SHAPES["edges"], 264, 328, 40, 9, "f16", seed=15)
+    X, W, A, B, scale, off, which = data
+    which.copy_(torch.arange(8))
+    A[2] = float("nan")
+    B[3] = float("inf")
+    scale[6] = float("inf")
+    X[int(off[7]):int(off[8])] = float("nan")
+    X[3] = float("inf")                              # one row of the first request
+    got, _ = run(data, layout, out)
+    bad = torch.zeros(X.shape[0], dtype=torch.bool)
+    bad[3] = True
+    for q in (2, 3, 6, 7):
+        bad[int(off[q]):int(off[q + 1])] = True
+    assert got[~bad].isfinite().all() and not got[bad].isfinite().any()
+    data[2][2], data[3][3], data[4][6] = 0, 0, 0
+    keep = ~bad
+    clean = tuple(d.clone() for d in data)
+    clean[0][bad] = 0
+    want, size, h16 = want_of(clean)
+    tol = TOL_REL_SMAX * size + h16 + (TOL_F16_REL * want.abs() + TOL_F16_ABS if out == "f16" else 0)
+    assert ((got.double() - want).abs() <= tol)[keep].all()
+
+
+@pytest.mark.gpu
 def test_same_bits_every_time():
     data = make(SHAPES["mixed"], 264, 4096, 16, 4, "bf16", seed=6)
     first, _ = run(data)
