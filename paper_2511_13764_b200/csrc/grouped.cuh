@@ -25,10 +25,11 @@
 // 8192^3: 720-755 us, 1.46-1.53 PFLOP/s); little work, a launch's start, schedule and end (one tile 5.4 us after another
 // launch, 16 x 4096 x 4096 13.9 us).  The gradient of the weights of 8 groups, 8192 rows, 1024 x 4096: 54 us to BF16, 67 to FP32.
 //
-// FP32 results (p.chunk): the tensor core's accumulator is cut short, not rounded, at every step, an error
-// that grows with the number of steps; so after `chunk` k-blocks the accumulator is added to an FP32 sum in
-// the epilogue's registers while the other accumulator is being filled: 8192 rows in one accumulator were 9.1e-6 off
-// (relative 2-norm), by chunks of 8 k-blocks 4.1e-7, where FP32 FMAs are 2.4e-7.  16-bit results do not need it.
+// The tensor core's accumulator is cut short, not rounded, at every step, an error that goes one way and grows with the number of steps.
+// So after p.chunk k-blocks the accumulator is added to an FP32 sum in the epilogue's registers while the other accumulator is being
+// filled.  FP32 results, chunks of 8 k-blocks (512 of the contraction): 8192 rows in one accumulator were 9.1e-6 off (relative 2-norm),
+// so 4.1e-7, where FP32 FMAs are 2.4e-7 (chunks of 4: half of that, for 5 % of the gradient's time).  16-bit results, 64 (4096 of the
+// contraction; shorter ones need no sums): 2^18 products of one sign were 1.6e-3 too small, so 2.6e-5, a twentieth of what FP16's rounding may be.
 //
 // Warps: 0 TMA producer, 1 MMA issuer, 2-9 epilogue (warps 2-5 take the even 32-column chunks, 6-9 the odd
 // ones), 10 (WEIGHTS) clears the rows of a group's last k-block that belong to the next group, 11 scheduler: it alone
@@ -72,15 +73,16 @@ __device__ __forceinline__ int round32(int x) { return (x + 31) & ~31; }
 
 // MODE: GroupedMode.  A_MN: the features' operand is MN-major (row-major weights [K][I], or rows [t][I]), else
 // K-major (weights [I][K]).
-// OUT: type of C (GroupedOut).  (The bound of 512 threads keeps the 16-bit ROWS kernels at 128 registers, which leaves an
-// SM room for a block of the adapters' kernel beside them.)
-template <int MODE, bool A_MN, int OUT>
-__global__ void __launch_bounds__(MODE == GRP_ROWS && OUT != GRP_OUT_F32 ? 512 : GRP_THREADS, 1) __cluster_dims__(2, 1, 1)
+// OUT: type of C (GroupedOut).  SUMS: a tile may have several accumulators to add.  (The bound of 512 threads keeps the 16-bit ROWS
+// kernels without sums at 128 registers, which leaves an SM room for a block of the adapters' kernel beside them.)
+template <int MODE, bool A_MN, int OUT, bool SUMS>
+__global__ void __launch_bounds__(MODE == GRP_ROWS && !SUMS ? 512 : GRP_THREADS, 1) __cluster_dims__(2, 1, 1)
 grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, LoraMaps, GroupedMaps> maps, const __grid_constant__ GroupedParams p) {
     constexpr bool WEIGHTS = MODE == GRP_WEIGHTS, LORA = MODE == GRP_LORA;
     constexpr bool OUT16 = OUT == GRP_OUT_BF16 || OUT == GRP_OUT_F16, F16 = OUT == GRP_OUT_F16;
     constexpr bool SCALED = LORA && OUT != GRP_OUT_BF16;   // operands may be FP16: rows of h16 may have a factor (p.unscale)
     constexpr int STAGING = OUT == GRP_OUT_H ? 0 : GRP_STAGING;
+    static_assert(SUMS || (!LORA && OUT != GRP_OUT_F32), "FP32 results, and adapters, are sums");
     static_assert(!WEIGHTS || A_MN, "rows are contiguous in their features");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -543,7 +545,6 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                 ring();
                 const uint32_t idesc = p.idesc | (static_cast<uint32_t>(u.jn >> 3) << 17);
                 const int base = u.kb1 - u.kb0, own = base + u.req_whole, blocks = own + u.req_parts * p.rank_blocks;
-                const int chunk = p.chunk ? p.chunk : own;
                 int in_chunk = 0, rb = 0;
                 uint32_t d_tmem = 0;
                 if (blocks == 0) {                        // (an empty group's gradient: the epilogue stores zeros)
@@ -612,7 +613,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                     // (a request's accumulator has all of its ranks, however short the tile's own chunks are: one with K <= 64 and
                     // ranks above 32 closed before its last block would leave the epilogue an accumulator nobody waits for)
                     ++in_chunk;
-                    if (n < own ? in_chunk == chunk || n == own - 1 : rb == 0) {
+                    if (n < own ? in_chunk == p.chunk || n == own - 1 : rb == 0) {
                         umma_commit_pair_if(tfull_bar(acc), 3, elected);
                         in_chunk = 0;
                         ++local;
@@ -785,9 +786,9 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
             // the accumulators that make up the tile: chunks of its own k-blocks, then one for each request with some of its rows
             bool held = true;                             // the sum is in tensor memory, not stored yet
             const int blocks = u.kb1 - u.kb0 + u.req_whole;
-            const int chunks = p.chunk ? max(1, (blocks + p.chunk - 1) / p.chunk) : 1, all = chunks + u.req_parts;
+            const int chunks = max(1, (blocks + p.chunk - 1) / p.chunk), all = chunks + u.req_parts;
             if (!await()) break;
-            if ((OUT == GRP_OUT_F32 || LORA) && all > 1) {
+            if (SUMS && all > 1) {
                 // they are added in registers
                 float sum[4][32];
 #pragma unroll

@@ -20,7 +20,8 @@ constexpr int GRP_BLOCK = 600;                         // clocks of a k-block fo
 // (a kernel that only writes h16 has no staging: more room for other blocks beside it)
 __host__ __device__ constexpr int grp_smem(bool staging) { return GRP_RING + (staging ? GRP_STAGING : 0) + 1024 + 3 * GRP_TABLE + 1024; }
 
-constexpr int GRP_CHUNK = 8;                           // k-blocks between additions to the FP32 sums of FP32 results
+// k-blocks between additions to the FP32 sums (see grouped.cuh): of FP32 results, and of 16-bit ones
+constexpr int GRP_CHUNK = 8, GRP_CHUNK_16 = 64;
 
 enum GroupedMode { GRP_ROWS = 0, GRP_WEIGHTS = 1, GRP_LORA = 2 };
 enum GroupedOut { GRP_OUT_F32 = 0, GRP_OUT_BF16 = 1, GRP_OUT_F16 = 2, GRP_OUT_H = 3 };   // H: h16 only (see GroupedParams), from one accumulator
@@ -32,7 +33,7 @@ struct GroupedParams {
     int tiles_i;           // ceil(I / 256)
     int tiles_j;           // WEIGHTS: ceil(J / 256)
     int beta, f16;
-    int chunk;             // k-blocks summed in tensor memory before they are added to an FP32 sum in registers; 0: all
+    int chunk;             // k-blocks summed in tensor memory before they are added to an FP32 sum
     uint32_t idesc;        // without the N field
     int a_slabs, b_slabs;  // MN-major operands of whole 64-feature slabs: a CTA's 128 features in one box
     const int* offsets;    // [groups + 1]; null: one group of all rows
@@ -81,14 +82,20 @@ struct LoraMaps : GroupedMaps {    // (LORA alone: another KB of arguments costs
 // (grouped_rows.cu, grouped_weights.cu, grouped_lora.cu: the instantiations; nk_grouped.cu: the rest)
 typedef void (*GroupedFunction)(GroupedMaps, GroupedParams);
 typedef void (*LoraFunction)(LoraMaps, GroupedParams);
-GroupedFunction grouped_rows_kernel(bool a_mn, GroupedOut out);
-GroupedFunction grouped_weights_kernel(GroupedOut out);
+GroupedFunction grouped_rows_kernel(bool a_mn, GroupedOut out, bool sums);
+GroupedFunction grouped_weights_kernel(GroupedOut out, bool sums);
 LoraFunction grouped_lora_kernel(bool a_mn, GroupedOut out);
 struct GroupedKernel {     // one instantiation
     GroupedMode mode;
     bool a_mn;
     GroupedOut out;
+    bool sums;             // a contraction may be longer than a chunk
+    int chunk() const { return out == GRP_OUT_F32 ? GRP_CHUNK : GRP_CHUNK_16; }
 };
+// (`longest`: of the contractions)
+inline GroupedKernel grouped_choose(GroupedMode mode, bool a_mn, GroupedOut out, int64_t longest) {
+    return {mode, a_mn, out, mode == GRP_LORA || out == GRP_OUT_F32 || longest > GRP_CHUNK_16 * GRP_BK};
+}
 inline GroupedOut grouped_out(bool out16, bool f16) { return !out16 ? GRP_OUT_F32 : f16 ? GRP_OUT_F16 : GRP_OUT_BF16; }
 cudaError_t grouped_prepare(const GroupedKernel& k);     // once per kernel and device: its shared memory
 cudaError_t grouped_launch(const GroupedKernel& k, int pairs, cudaStream_t st, const GroupedMaps& maps, const GroupedParams& p);   // (LORA: LoraMaps)

@@ -5,10 +5,10 @@ namespace nk {
 
 LoraFunction grouped_lora_kernel(bool a_mn, GroupedOut out) {
     if (a_mn)
-        return out == GRP_OUT_F32 ? grouped_kernel<GRP_LORA, true, GRP_OUT_F32>
-               : out == GRP_OUT_BF16 ? grouped_kernel<GRP_LORA, true, GRP_OUT_BF16> : grouped_kernel<GRP_LORA, true, GRP_OUT_F16>;
-    return out == GRP_OUT_F32 ? grouped_kernel<GRP_LORA, false, GRP_OUT_F32>
-           : out == GRP_OUT_BF16 ? grouped_kernel<GRP_LORA, false, GRP_OUT_BF16> : grouped_kernel<GRP_LORA, false, GRP_OUT_F16>;
+        return out == GRP_OUT_F32 ? grouped_kernel<GRP_LORA, true, GRP_OUT_F32, true>
+               : out == GRP_OUT_BF16 ? grouped_kernel<GRP_LORA, true, GRP_OUT_BF16, true> : grouped_kernel<GRP_LORA, true, GRP_OUT_F16, true>;
+    return out == GRP_OUT_F32 ? grouped_kernel<GRP_LORA, false, GRP_OUT_F32, true>
+           : out == GRP_OUT_BF16 ? grouped_kernel<GRP_LORA, false, GRP_OUT_BF16, true> : grouped_kernel<GRP_LORA, false, GRP_OUT_F16, true>;
 }
 
 }  // namespace nk

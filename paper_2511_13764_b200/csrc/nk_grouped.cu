@@ -36,7 +36,7 @@ void give_split_slot(int device, int slot, bool in_flight, bool captured) {
 }
 
 static GroupedFunction function_of(const GroupedKernel& k) {
-    return k.mode == GRP_WEIGHTS ? grouped_weights_kernel(k.out) : grouped_rows_kernel(k.a_mn, k.out);
+    return k.mode == GRP_WEIGHTS ? grouped_weights_kernel(k.out, k.sums) : grouped_rows_kernel(k.a_mn, k.out, k.sums);
 }
 cudaError_t grouped_prepare(const GroupedKernel& k) {
     const int smem = grp_smem(k.out != GRP_OUT_H);
@@ -107,7 +107,8 @@ nk_status_t nk_grouped_create(const nk_grouped_desc_t* desc, nk_grouped_t* out) 
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     DeviceGuard guard(d.device);
     if (!encode_tiled()) { delete p; return NK_ERR_CUDA; }
-    p->kernel = {weights ? GRP_WEIGHTS : GRP_ROWS, weights || d.layout_b == NK_ROW_MAJOR, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
+    p->kernel = grouped_choose(weights ? GRP_WEIGHTS : GRP_ROWS, weights || d.layout_b == NK_ROW_MAJOR,
+                               grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16), weights ? d.rows : d.K);
     if (grouped_prepare(p->kernel) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
     p->slab_cols = grouped_slab_cols(weights ? d.K : d.rows);
@@ -183,7 +184,7 @@ nk_status_t nk_grouped_run(nk_grouped_t p, const void* A, const void* B, void* C
     g.slab_cols = p->slab_cols;
     g.a_slabs = d.N % 64 == 0;
     g.b_slabs = d.K % 64 == 0;
-    g.chunk = d.out_dtype == NK_F32 ? GRP_CHUNK : 0;
+    g.chunk = p->kernel.chunk();
     base_runs(p, static_cast<cudaStream_t>(cuda_stream));
     const cudaError_t e = grouped_launch(p->kernel, p->pairs, static_cast<cudaStream_t>(cuda_stream), p->maps, g);
     return e == cudaSuccess ? NK_OK : p->cuda("grouped launch", e);

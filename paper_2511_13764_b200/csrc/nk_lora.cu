@@ -66,11 +66,11 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     DeviceGuard guard(d.device);
     const bool row = d.layout == NK_ROW_MAJOR;
     p->few = d.rows <= LORA_ROWS * d.requests || (!row && d.rank <= 64 && d.rows / LORA_ROWS + d.requests <= 32);
-    p->projection = {p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16)};
-    // (BF16 with a 16-bit Y: one accumulator for all of K is cut short by up to K 2^-28 of itself, far below what Y keeps, and its
-    // kernel leaves room for lora_delta_kernel's blocks; an FP32 Y, and FP16 by way of FP32, has X . A_a summed by chunks)
+    p->projection = grouped_choose(p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16), d.K);
+    // (BF16, a 16-bit Y and a K of one chunk: from one accumulator, in a kernel that leaves room for lora_delta_kernel's blocks; else
+    // X . A_a is summed by the chunks of FP32 results)
     const bool f16 = d.in_dtype == NK_F16;
-    p->shrinking = {GRP_ROWS, row, d.out_dtype == NK_F32 || f16 ? GRP_OUT_F32 : GRP_OUT_H};
+    p->shrinking = grouped_choose(GRP_ROWS, row, d.out_dtype == NK_F32 || f16 || d.K > GRP_CHUNK_16 * GRP_BK ? GRP_OUT_F32 : GRP_OUT_H, d.K);
     cudaError_t e = grouped_prepare(p->projection);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(d.in_dtype == NK_F16 ? lora_delta_kernel<true> : lora_delta_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, lora_smem(LORA_MAX_RANK, LORA_MAX_REQUESTS, false));
     if (e == cudaSuccess && !p->few) e = grouped_prepare(p->shrinking);
@@ -197,7 +197,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
         h.scale = scale;
         h.I = g.rank;
         h.tiles_i = 1;
-        h.chunk = p->shrinking.out == GRP_OUT_F32 ? GRP_CHUNK : 0;
+        h.chunk = p->shrinking.chunk();
         LoraSplitParams split = {};
         if (f16) {
             h.C = ws + p->h32_at;
@@ -223,7 +223,7 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
     g.I = static_cast<int>(d.N);
     g.tiles_i = static_cast<int>(div_up(d.N, GRP_TILE));
     g.a_slabs = d.N % 64 == 0;
-    g.chunk = d.out_dtype == NK_F32 ? GRP_CHUNK : 0;
+    g.chunk = p->projection.chunk();
     g.C = Y;
     g.ldc = d.ldy;
     g.partial = partial[1];

@@ -363,6 +363,63 @@ def test_fp32_sums_do_not_drift(rows):
     assert float((C[0].double() - want).norm() / want.norm()) <= 32 / 3 * 2.0 ** -23
 
 
+def positive(shape, kind, seed, scale):
+    """Values of one sign, half to three halves of `scale` (the truncated bits of their sums all go one way)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return ((torch.rand(shape, generator=g, device="cuda") + 0.5) * scale).to(TYPES[kind][1])
+
+
+def drift(got, want):
+    """Mean relative error; what rounding the results to FP16 leaves of it: 2^-11 / sqrt(12) at most for one, so six times that
+    over the root of their number."""
+    return float(((got.double() - want) / want).mean().abs()), 6 * 2.0 ** -11 / np.sqrt(12 * want.numel())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["rows", "rows_t", "weights"])
+def test_long_sums_of_16_bit_results_do_not_drift(form):
+    """2^18 products of one sign to an FP16 result, 2^14 truncated additions where one accumulator takes them all: the mean error
+    stays within 2^-15, an eighth of what the rounding of one result to FP16 may be off on average of its spacing (2^-12)."""
+    long_, st = 1 << 18, torch.cuda.current_stream().cuda_stream
+    # about a wave of whole tiles: those of one group
+    if form == "weights":
+        N, K = 2304, 2304
+        A, B = positive((long_, K), "f16", 1, 2.0 ** -6), positive((long_, N), "f16", 2, 2.0 ** -2)
+        A *= torch.linspace(0.5, 1, K, device="cuda").half()
+        plan = nk.GroupedPlan(1, long_, N, K, kind=nk.GROUPED_WEIGHTS, in_dtype=nk.F16, out_dtype=nk.F16)
+        C, off = torch.empty(K, N, dtype=torch.float16, device="cuda"), torch.tensor([0, long_], dtype=torch.int32).cuda()
+        want = A[:, :64].double().t() @ B[:, :256].double()
+    else:
+        rows, N = 1024, 2560
+        A = positive((rows, long_), "f16", 3, 2.0 ** -6)
+        A *= torch.linspace(0.5, 1, rows, device="cuda").half()[:, None]
+        B = positive((long_, N) if form == "rows" else (N, long_), "f16", 4, 2.0 ** -2)
+        plan = nk.GroupedPlan(1, rows, N, long_, in_dtype=nk.F16, out_dtype=nk.F16, layout_b=nk.ROW_MAJOR if form == "rows" else nk.TRANSPOSED)
+        C, off = torch.empty(rows, N, dtype=torch.float16, device="cuda"), torch.tensor([0, rows], dtype=torch.int32).cuda()
+        want = A[:64].double() @ (B[:, :256].double() if form == "rows" else B[:256].double().t())
+    plan.run(A, B, C, off, workspace=scratch(plan), stream=st)
+    plan.check()
+    off_by, rounding = drift(C[:64, :256], want)
+    assert off_by <= 2.0 ** -15 + rounding, (off_by, rounding)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+def test_rows_of_several_chunks(kind, layout):
+    """Contractions around a whole number of chunks (64 k-blocks of 64), whole tiles and cut ones."""
+    for K in (4096, 4104, 8192, 8200, 16384, 20488):
+        run_rows([300, 0, 1, 70], 520, K, kind=kind, out=kind, layout=layout, beta=1, seed=22)
+    run_rows([5000, 3900], 1032, 4168, kind=kind, out=kind, layout=layout, seed=23)
+    run_rows([5000, 3900], 1032, 8264, kind=kind, out=kind, layout=layout, seed=23)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_weights_of_several_chunks(kind):
+    run_weights([4096, 4097, 8192, 8193, 0, 20000, 16384], 1032, 1288, kind=kind, out=kind, beta=1, seed=24)
+
+
 @pytest.mark.gpu
 def test_rows_neighbours_of_nan():
     """Infinities and NaN of a row or a weight stay in the rows they belong to."""

@@ -271,6 +271,38 @@ def test_fp16_nan_stays_with_its_request(layout, out):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("K", [4096, 4104, 8192, 8264, 20488])
+def test_contractions_of_several_chunks(layout, kind, K):
+    data = make([1, 300, 7, 40, 256, 9], 520, K, 40, 3, kind, seed=16)
+    got, _ = run(data, layout, kind)
+    close(got, data, kind)
+
+
+@pytest.mark.gpu
+def test_long_sums_of_16_bit_results_do_not_drift():
+    """2^17 products of one sign to an FP16 result, the adapter's among them: a mean error within 2^-15 (an eighth of half of FP16's spacing),
+    and what is left of the rounding of the results."""
+    rows, N, K, g = 1024, 2560, 1 << 17, torch.Generator(device="cuda").manual_seed(17)
+
+    def positive(*shape, scale):
+        return ((torch.rand(shape, generator=g, device="cuda") + 0.5) * scale).half()
+
+    X, W, A, B = positive(rows, K, scale=2.0 ** -6), positive(K, N, scale=2.0 ** -2), positive(1, K, 8, scale=2.0 ** -8), positive(1, 8, N, scale=2.0 ** -3)
+    X *= torch.linspace(0.5, 1, rows, device="cuda").half()[:, None]
+    scale, off, which = torch.ones(1, device="cuda"), torch.tensor([0, rows], dtype=torch.int32).cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    plan = nk.LoraPlan(rows, N, K, 8, 1, 1, in_dtype=nk.F16, out_dtype=nk.F16)
+    Y, ws = torch.empty(rows, N, dtype=torch.float16, device="cuda"), torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    plan.run(X, W, A, B, scale, off, which, Y, workspace=ws, stream=torch.cuda.current_stream().cuda_stream)
+    plan.check()
+    x = X[:64].double()
+    want = x @ W[:, :256].double() + x @ A[0].double() @ B[0, :, :256].double()
+    off_by = float(((Y[:64, :256].double() - want) / want).mean().abs())
+    assert off_by <= 2.0 ** -15 + 6 * 2.0 ** -11 / np.sqrt(12 * want.numel())
+
+
+@pytest.mark.gpu
 def test_same_bits_every_time():
     data = make(SHAPES["mixed"], 264, 4096, 16, 4, "bf16", seed=6)
     first, _ = run(data)
