@@ -303,7 +303,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                 const int most_parts = best_parts(longest, w, min(2 * n, num_pairs + n));
                 share = max(max(4, (tail_len + num_pairs - 1) / num_pairs), (longest + most_parts - 1) / most_parts);
                 const int tile_parts = (longest + share - 1) / share + 1, all_parts = min(n * tile_parts, num_pairs + n);
-                if (static_cast<float>((longest - share) * GRP_BLOCK) > 4000.0f + share_of(w, all_parts) * tile_parts) tail_from = from;
+                if (static_cast<float>(longest - share) * GRP_BLOCK > 4000.0f + share_of(w, all_parts) * tile_parts) tail_from = from;
             }
         } else {
             estimate(tiles, width, parts);
