@@ -26,10 +26,20 @@ static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Which way the adapters' part goes.  Requests of up to LORA_ROWS rows are lora_delta_kernel's: their weights are all that
 // counts, and its clusters read them at the speed of memory; more rows want the tensor cores: X . A_a as a grouped
-// product, (X . A_a) . B_a as further k-blocks of the projection.  Where a plan's requests have so few rows on average
-// lora_delta_kernel takes all of them, and the launch of the grouped product is saved.  So it does with longer requests where
-// its chunks of rows are a round or two of clusters and it reads A as rows of K, 16 bytes to a lane (59 rows of 2 requests, K =
-// 1240, N = 976, rank 8: 17 us against 27; but 465 rows of one, row-major, rank 104: 31 against 20, 12 rows, rank 112: 24 against 18).
+// product, (X . A_a) . B_a as further k-blocks of the projection ("many").  A plan knows its rows and requests, not how the ones
+// are spread over the others, so it leaves all of them to lora_delta_kernel ("few", one or two launches less), long ones too, where
+// that costs little in the worst spread, one long request beside requests of one row.  Times in us, few against many, BF16, K = N = 4096
+// unless said:
+//   up to two rows to a request: 1000 of one row, rank 16: 237 / 300, rank 128: 888 / 954; 999 and one of 1001 rows: 335 / 389, 1175 / 1028
+//   up to eight, rows x rank <= 48K: 64 requests of 8 rows, rank 16: 48 / 75, rank 64: 80 / 110; 63 and one of 400: 54 / 67, 84 / 74.
+//     (Beyond: 256 of 8 rows, rank 128: 377 / 480, but 240 and 16 of 100 rows: 500 / 251; 1023 and one of 7000: 2189 / 919)
+//   more, A as rows of K (16 bytes to a lane), few chunks of eight rows and a low rank: one of 240 rows, rank 16: 32 / 39, rank 32:
+//     40 / 39, rank 64: 60 / 39; four of 12, rank 48: 29 / 33, rank 64: 34 / 33; N = K = 1024: 20 / 23, 22 / 23
+static bool lora_few(int64_t rows, int64_t requests, int64_t rank, bool row) {
+    const int64_t chunks = rows / LORA_ROWS + requests;
+    return rows <= 2 * requests || (rows <= LORA_ROWS * requests && rows * rank <= 48 * 1024) ||
+           (!row && rank <= 48 && chunks <= 32 && rank * chunks <= 640);
+}
 
 }  // namespace nk
 
@@ -65,7 +75,7 @@ nk_status_t nk_lora_create(const nk_lora_desc_t* desc, nk_lora_t* out) {
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     DeviceGuard guard(d.device);
     const bool row = d.layout == NK_ROW_MAJOR;
-    p->few = d.rows <= LORA_ROWS * d.requests || (!row && d.rank <= 64 && d.rows / LORA_ROWS + d.requests <= 32);
+    p->few = lora_few(d.rows, d.requests, d.rank, row);
     p->projection = grouped_choose(p->few ? GRP_ROWS : GRP_LORA, row, grouped_out(d.out_dtype != NK_F32, d.in_dtype == NK_F16), d.K);
     // (BF16, a 16-bit Y and a K of one chunk: from one accumulator, in a kernel that leaves room for lora_delta_kernel's blocks; else
     // X . A_a is summed by the chunks of FP32 results)

@@ -165,6 +165,21 @@ def test_many_tiles_and_a_cut_last_wave(layout, out):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("layout", ["row", "transposed"])
+def test_a_long_prompt_among_many_short_requests(layout):
+    """Whatever the plan's average, a long request beside many of one row is right, and where it may be long it has the tensor cores."""
+    for sizes, rank, name in (([1] * 200 + [1400], 16, "lora_few"), ([1] * 200 + [1400], 64, "lora_many"),
+                              ([0] * 500 + [700] + [0] * 99, 32, "lora_few"), ([1] * 500 + [3000] + [1] * 523, 40, "lora_many")):
+        data = make(sizes, 264, 200, rank, 5, "bf16", seed=18)
+        got, plan = run(data, layout, "bf16")
+        assert plan.kernel_name.startswith(name)
+        close(got, data, "bf16")
+    # (nothing runs: 8 rows to a request on average, 7000 to one if it comes so)
+    assert nk.LoraPlan(8023, 4096, 4096, 128, 32, 1024, layout=nk.TRANSPOSED).kernel_name.startswith("lora_many")
+    assert nk.LoraPlan(240, 4096, 4096, 64, 1, 1, layout=nk.TRANSPOSED).kernel_name.startswith("lora_many")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["row", "transposed"])
 def test_most_requests(layout):
     gen = np.random.default_rng(10)
     data = make(gen.integers(0, 3, 1024).tolist(), 72, 136, 8, 60, "bf16", seed=10)
