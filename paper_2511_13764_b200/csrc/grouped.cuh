@@ -941,6 +941,11 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
         }
     }
 
+    if (*abort_flag) {
+        // a wait ran out: what is still on its way into shared memory, or at work on it, needs some microseconds
+        const long long t0 = clock64();
+        while (clock64() - t0 < (1ll << 20)) __nanosleep(1000);
+    }
     if (warp == 0) launch_wait();        // this launch ends after the one before it, whatever it read
     tc_fence_before_sync();
     __syncthreads();
