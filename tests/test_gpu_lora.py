@@ -318,6 +318,36 @@ def test_long_sums_of_16_bit_results_do_not_drift():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["row", "transposed"])
+@pytest.mark.parametrize("name", ["step", "mixed", "edges"])
+def test_gradient_of_the_rows(layout, name):
+    """dX of sum(dY * Y) by the same call with N and K exchanged, the other layout and A and B in each other's place; the loss is
+    linear in X, so the difference quotient of the 64-bit formula is exact up to its rounding."""
+    K, N, r, L = 328, 264, 24, 4
+    X, W, A, B, scale, off, which = make(SHAPES[name], N, K, r, L, "bf16", seed=19)
+    which[0] = -1
+    dY = rand((X.shape[0], N), "bf16", torch.Generator().manual_seed(20))
+    Ws, As, Bs = (m if layout == "row" else m.transpose(-1, -2).contiguous() for m in (W, A, B))     # as the forward pass keeps them
+    plan = nk.LoraPlan(X.shape[0], K, N, r, L, len(which), layout=nk.TRANSPOSED if layout == "row" else nk.ROW_MAJOR)
+    dX = torch.full((X.shape[0], K), float("nan"), device="cuda")
+    ws = torch.full((plan.workspace_bytes,), 255, dtype=torch.uint8, device="cuda")
+    plan.run(dY.cuda(), Ws.cuda(), Bs.cuda(), As.cuda(), scale.cuda(), off.cuda(), which.cuda(), dX, workspace=ws,
+             stream=torch.cuda.current_stream().cuda_stream)
+    plan.check()
+    back = (dY, W.t().contiguous(), B.transpose(1, 2).contiguous(), A.transpose(1, 2).contiguous(), scale, off, which)
+    close(dX.cpu(), back, "f32")
+    loss = lambda x: float((want_of((x, W, A, B, scale, off, which))[0] * dY.double()).sum())   # noqa: E731
+    for seed in range(3):
+        e = torch.randn(X.shape, generator=torch.Generator().manual_seed(seed)).double()
+        terms = dX.cpu().double() * e
+        # every element of dX within 1e-5 of its largest sum of |products| (and 2^-16 of the adapter's part of it): the errors of many elements
+        # add up at most like their sizes
+        size = want_of(back)[1]
+        num = (loss(X.double() + e) - loss(X.double() - e)) / 2
+        assert abs(num - float(terms.sum())) <= (TOL_REL_SMAX + 2.0 ** -16) * size * float(e.abs().sum())
+
+
+@pytest.mark.gpu
 def test_same_bits_every_time():
     data = make(SHAPES["mixed"], 264, 4096, 16, 4, "bf16", seed=6)
     first, _ = run(data)
