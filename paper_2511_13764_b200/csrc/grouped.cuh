@@ -117,6 +117,13 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
         if (p.status) atomicCAS(p.status, 0u, code);
     };
 
+    // after a wait that ran out: what is still on its way into shared memory, or at work on it, needs some microseconds, and the pair
+    // ends together
+    auto settle = [&]() {
+        const long long t0 = clock64();
+        while (clock64() - t0 < (1ll << 20)) __nanosleep(1000);
+    };
+
     // offsets -> shared memory (LORA: the requests'; its one group is all the rows)
     const int* offsets = LORA ? p.request_offsets : p.offsets;
     const int entries = LORA ? p.requests : p.groups;
@@ -314,7 +321,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                 tail_len = (tiles - from) * padded;
             }
         }
-        bool waited = false;
+        bool waited = false, handed = false;              // `handed`: a unit, to the other warps
         int next_tile = pair_id, x = pair_id * share;     // this pair's next whole tile, its place in the tail
         const int tail_hi = min(x + share, tail_len);
         GroupedUnit u = {};
@@ -392,12 +399,16 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                     if (u.kb1 == kbs && parts_of) {
                         bool whole = s_row[u.req] <= u.c0 && s_row[u.req + 1] >= u.c0 + u.cols;
                         if (SCALED && whole && p.unscale) {
-                            // (the kernel before this one writes the factors)
-                            if (!waited) launch_wait();
-                            waited = true;
-                            bool plain = true;
-                            for (int r = lane; r < u.cols; r += 32) plain &= __ldcg(p.unscale + u.c0 + r) == 1.0f;
-                            whole = __all_sync(~0u, plain);
+                            // Which rows have a factor says the kernel before this one; the pair's first tile does not wait to know.
+                            if (!handed) {
+                                whole = false;
+                            } else {
+                                if (!waited) launch_wait();
+                                waited = true;
+                                bool plain = true;
+                                for (int r = lane; r < u.cols; r += 32) plain &= __ldcg(p.unscale + u.c0 + r) == 1.0f;
+                                whole = __all_sync(~0u, plain);
+                            }
                         }
                         if (whole) u.req_whole = p.rank_blocks;
                         else u.req_parts = parts_of;
@@ -413,6 +424,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                 mbar_arrive(ufull_bar(unit_at));
             }
             __syncwarp();
+            handed = true;
             if (++unit_at == GRP_UNITS) { unit_at = 0; unit_phase ^= 1u; }
         }
     } else if (warp == 0) {
@@ -517,12 +529,11 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                 }
             }
         }
-        if (ok) {   // drain: every stage this CTA filled has been consumed
-            for (int s = 0; s < S; ++s) {
-                if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) break;
-                if (++stage == S) { stage = 0; phase ^= 1u; }
-            }
+        for (int s = 0; ok && s < S; ++s) {   // drain: every stage this CTA filled has been consumed
+            ok = mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag);
+            if (++stage == S) { stage = 0; phase ^= 1u; }
         }
+        if (!ok) settle();
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issuer (leader only)
         if (rank == 0) {
@@ -613,7 +624,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                     // (a request's accumulator has all of its ranks, however short the tile's own chunks are: one with K <= 64 and
                     // ranks above 32 closed before its last block would leave the epilogue an accumulator nobody waits for)
                     ++in_chunk;
-                    if (n < own ? in_chunk == p.chunk || n == own - 1 : rb == 0) {
+                    if (!LORA || n < own ? (SUMS && in_chunk == p.chunk) || n == own - 1 : rb == 0) {
                         umma_commit_pair_if(tfull_bar(acc), 3, elected);
                         in_chunk = 0;
                         ++local;
@@ -622,6 +633,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                     if (++stage == S) { stage = 0; phase ^= 1u; }
                 }
             }
+            if (*abort_flag) settle();
         }
     } else if (warp < 10) {
         // ------------------------------------------------ epilogue (both CTAs, own 128 features)
@@ -786,7 +798,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
             // the accumulators that make up the tile: chunks of its own k-blocks, then one for each request with some of its rows
             bool held = true;                             // the sum is in tensor memory, not stored yet
             const int blocks = u.kb1 - u.kb0 + u.req_whole;
-            const int chunks = max(1, (blocks + p.chunk - 1) / p.chunk), all = chunks + u.req_parts;
+            const int chunks = !SUMS || blocks <= p.chunk ? 1 : (blocks + p.chunk - 1) / p.chunk, all = chunks + u.req_parts;
             if (!await()) break;
             if (SUMS && all > 1) {
                 // they are added in registers
@@ -941,11 +953,6 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
         }
     }
 
-    if (*abort_flag) {
-        // a wait ran out: what is still on its way into shared memory, or at work on it, needs some microseconds
-        const long long t0 = clock64();
-        while (clock64() - t0 < (1ll << 20)) __nanosleep(1000);
-    }
     if (warp == 0) launch_wait();        // this launch ends after the one before it, whatever it read
     tc_fence_before_sync();
     __syncthreads();

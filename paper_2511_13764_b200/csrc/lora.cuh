@@ -442,40 +442,49 @@ struct LoraSplitParams {
     uint16_t* h16;              // [rows][rank_blocks * 64]
     float* unscale;             // [rows]
 };
-constexpr int LORA_SPLIT_ROWS = 8;               // of a block of 256 threads
+constexpr int LORA_SPLIT_ROWS = 8;               // of a block of 256 threads at a time
 __global__ void __launch_bounds__(32 * LORA_SPLIT_ROWS) lora_split_kernel(const LoraSplitParams p) {
-    const int lane = threadIdx.x & 31, row = blockIdx.x * LORA_SPLIT_ROWS + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    constexpr int V = LORA_MAX_RANK / 32;
     launch_wait();
     launch_next();
-    if (row >= p.rows) return;
-    const float* x = p.x + static_cast<size_t>(row) * p.rank;
-    float v[LORA_MAX_RANK / 32];
-    uint32_t top = 0u;
+    int row = blockIdx.x * LORA_SPLIT_ROWS + (threadIdx.x >> 5);
+    float next[V];
+    auto fetch = [&](int r) {
 #pragma unroll
-    for (int n = 0; n < LORA_MAX_RANK / 32; ++n) {
-        v[n] = lane + 32 * n < p.rank ? __ldcg(x + lane + 32 * n) : 0.0f;
-        const uint32_t bits = __float_as_uint(v[n]) & 0x7FFFFFFFu;
-        if (bits < 0x7F800000u) top = max(top, bits);
-    }
-    top = __reduce_max_sync(~0u, top);
-    // (subnormal rows: 2^126 is as far as a factor and its inverse are both ordinary numbers)
-    const int ex = static_cast<int>(top >> 23) - 127;
-    const bool plain = p.planes == 2 && (top == 0u || (ex >= -5 && ex < 15));
-    const int e = plain ? 0 : min(126, 14 - ex);
-    const float up = __int_as_float((127 + e) << 23);
-    if (lane == 0) p.unscale[row] = __int_as_float((127 - e) << 23);
-    const int per = p.planes == 3 ? 16 : 32;
-    uint16_t* h = p.h16 + static_cast<size_t>(row) * p.rank_blocks * 64;
+        for (int n = 0; n < V; ++n) next[n] = r < p.rows && lane + 32 * n < p.rank ? __ldcg(p.x + static_cast<size_t>(r) * p.rank + lane + 32 * n) : 0.0f;
+    };
+    fetch(row);
+    for (; row < p.rows; row += gridDim.x * LORA_SPLIT_ROWS) {
+        float v[V];
+        uint32_t top = 0u;
 #pragma unroll
-    for (int n = 0; n < LORA_MAX_RANK / 32; ++n) {
-        const int i = lane + 32 * n;
-        if (i >= p.rank_blocks * per) break;       // (ranks beyond the last are zeros)
-        float left = v[n] * up;
-        for (int z = 0; z < p.planes; ++z) {
-            const uint32_t bits = pack_half2(left, 0.0f, 1) & 0xFFFFu;
-            const float lead = half_bits_to_f32(bits, 1);
-            h[i / per * 64 + z * per + i % per] = static_cast<uint16_t>(bits);
-            left = fabsf(lead) <= 65504.0f ? left - lead : 0.0f;     // (nothing behind an infinity or NaN)
+        for (int n = 0; n < V; ++n) {
+            v[n] = next[n];
+            const uint32_t bits = __float_as_uint(v[n]) & 0x7FFFFFFFu;
+            if (bits < 0x7F800000u) top = max(top, bits);
+        }
+        fetch(row + gridDim.x * LORA_SPLIT_ROWS);      // the next row is on the way
+        top = __reduce_max_sync(~0u, top);
+        // (subnormal rows: 2^126 is as far as a factor and its inverse are both ordinary numbers)
+        const int ex = static_cast<int>(top >> 23) - 127;
+        const bool plain = p.planes == 2 && (top == 0u || (ex >= -5 && ex < 15));
+        const int e = plain ? 0 : min(126, 14 - ex);
+        const float up = __int_as_float((127 + e) << 23);
+        if (lane == 0) p.unscale[row] = __int_as_float((127 - e) << 23);
+        const int per = p.planes == 3 ? 16 : 32;
+        uint16_t* h = p.h16 + static_cast<size_t>(row) * p.rank_blocks * 64;
+#pragma unroll
+        for (int n = 0; n < V; ++n) {
+            const int i = lane + 32 * n;
+            if (i >= p.rank_blocks * per) break;       // (ranks beyond the last are zeros)
+            float left = v[n] * up;
+            for (int z = 0; z < p.planes; ++z) {
+                const uint32_t bits = pack_half2(left, 0.0f, 1) & 0xFFFFu;
+                const float lead = half_bits_to_f32(bits, 1);
+                h[i / per * 64 + z * per + i % per] = static_cast<uint16_t>(bits);
+                left = fabsf(lead) <= 65504.0f ? left - lead : 0.0f;     // (nothing behind an infinity or NaN)
+            }
         }
     }
 }

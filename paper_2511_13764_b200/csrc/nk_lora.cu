@@ -221,7 +221,9 @@ nk_status_t nk_lora_run(nk_lora_t p, const void* X, const void* W, const void* A
         h.counter = p->counters[0];
         e = grouped_launch(p->shrinking, p->pairs, st, p->shrink, h);
         if (e != cudaSuccess) return p->cuda("lora shrink launch", e);
-        if (f16 && (e = launch_beside(lora_split_kernel, static_cast<unsigned>(div_up(d.rows, LORA_SPLIT_ROWS)), 32 * LORA_SPLIT_ROWS, 0, st, split)) != cudaSuccess)
+        // (few blocks: the projection's start when all of them have, which they do where X . A_a is done first)
+        const int64_t blocks = div_up(d.rows, LORA_SPLIT_ROWS), most_blocks = 2 * p->sm_count;
+        if (f16 && (e = launch_beside(lora_split_kernel, static_cast<unsigned>(blocks < most_blocks ? blocks : most_blocks), 32 * LORA_SPLIT_ROWS, 0, st, split)) != cudaSuccess)
             return p->cuda("lora split launch", e);
         g.requests = h.groups;
         g.request_offsets = offsets;
