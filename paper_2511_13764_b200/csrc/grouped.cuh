@@ -827,24 +827,27 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                     for (int q = 0; q < 4; ++q) {
                         const int c = set * 32 + q * 64;
                         if (c < hi && c + 32 > lo) {
-                            uint32_t v[32];
-                            tmem_ld_32x32(taddr + c, v);
-                            tmem_ld_wait();
-                            if (unscale) {
-                                // lane l has the factor of the piece's row l
-                                const float factor = lane < u.cols - c ? __ldcg(p.unscale + u.c0 + c + lane) : 0.0f;
+                            // lane l has the factor of the piece's row l
+                            const float factor = unscale && lane < u.cols - c ? __ldcg(p.unscale + u.c0 + c + lane) : 0.0f;
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) {
-                                    const float f = __shfl_sync(~0u, factor, j);
-                                    if (c + j >= lo && c + j < hi) sum[q][j] += __uint_as_float(v[j]) * f;
+                            for (int b = 0; b < 32; b += 16) {                   // (halves of a piece: fewer registers beside the sums)
+                                uint32_t v[16];
+                                tmem_ld_32x16(taddr + c + b, v);
+                                tmem_ld_wait();
+                                if (unscale) {
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) {
+                                        const float f = __shfl_sync(~0u, factor, b + j);
+                                        if (c + b + j >= lo && c + b + j < hi) sum[q][b + j] += __uint_as_float(v[j]) * f;
+                                    }
+                                } else if (!LORA || (c >= lo && c + 32 <= hi)) {
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) sum[q][b + j] += __uint_as_float(v[j]);
+                                } else {
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j)
+                                        if (c + b + j >= lo && c + b + j < hi) sum[q][b + j] += __uint_as_float(v[j]);
                                 }
-                            } else if (!LORA || (c >= lo && c + 32 <= hi)) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) sum[q][j] += __uint_as_float(v[j]);
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j)
-                                    if (c + j >= lo && c + j < hi) sum[q][j] += __uint_as_float(v[j]);
                             }
                         }
                     }
