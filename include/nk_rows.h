@@ -154,7 +154,7 @@ nk_status_t nk_route_destroy(nk_route_t plan);
  * The gradient of the rows, dX[t] = dY[t] . W^T + scale[a] (dY[t] . B_a^T) . A_a^T, is the same call: a plan with N and K exchanged
  * and the other layout, and dY, W, B, A in the places of X, W, A, B (no copy of the weights is made).
  * Adapters of a lower rank are padded with zeros.  16-bit operands of one type, FP32 accumulation, Y in FP32 or rounded
- * once to the operands' type.  X . A_a is held in FP32, or where the tensor cores multiply it by B_a (requests of more than eight
+ * once to the operands' type, sums as in nk_grouped.  X . A_a is held in FP32, or where the tensor cores multiply it by B_a (requests of more than eight
  * rows) as the sum of 16-bit numbers.  NK_BF16: two, good to 2^-16 of each element, or for an FP32 Y three (2^-24).  NK_F16: two, good
  * to 2^-22 of each element and never worse than 2^-20 of its row's largest, or for an FP32 Y three (2^-33, 2^-40), whatever the
  * row's size: rows that FP16 has no range for are scaled by a power of two.  (An infinite element of B_a times such a sum is an

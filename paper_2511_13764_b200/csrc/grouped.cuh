@@ -23,7 +23,7 @@
 // What bounds it, and measured: few rows a group, HBM (64 groups of one row, 4096 x 4096: 305 us, 7.0 TB/s); many rows, the
 // operand feed from L2, 0.33-0.385 us a k-block of 256 x 256 (8 groups, 8192 x 4096 x 1024: 55 us, 1.25 PFLOP/s; one group,
 // 8192^3: 720-755 us, 1.46-1.53 PFLOP/s); little work, a launch's start, schedule and end (one tile 5.4 us after another
-// launch, 16 x 4096 x 4096 13.9 us).  The gradient of the weights of 8 groups, 8192 rows, 1024 x 4096: 54 us to BF16, 67 to FP32.
+// launch, 16 x 4096 x 4096 13.9 us).  The gradient of the weights of 8 groups, 8192 rows, 1024 x 4096: 54 us to BF16, 64 to FP32.
 //
 // The tensor core's accumulator is cut short, not rounded, at every step, an error that goes one way and grows with the number of steps.
 // So after p.chunk k-blocks the accumulator is added to an FP32 sum in the epilogue's registers while the other accumulator is being
@@ -224,7 +224,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
         // Estimated time, in clocks, of n tiles of w rows, and into how many parts (1: none) the tiles of the last, partial wave are cut:
         // equal parts, so that no pair has parts of two tiles, where they fill at most half a wave.  A k-block of a tile costs about
         // 260 + 1.5 w (operand feed; the tensor core alone would need 2 w for w = 256), for which GRP_BLOCK stands where the width is
-        // settled.  (600 + w / 8 held for a slower producer; with it 4099 rows in 8 groups took 43.2 us instead of 38.9, 5000
+        // settled.  (600 + w / 8 held for a slower producer; with it 4099 rows in 8 groups took 43.2 us instead of 38.9 (a card below its power cap), 5000
         // rows 43.1 instead of 37.1, 4096 x 1024 both, and 29 groups of 35 rows, 2048 x 32, 13.2 instead of 14.0; with 400 at
         // least 32 groups of 64 rows, 2048 x 768, 28.6 instead of 27.0, those of 35 rows 13.2.)  Parts are written to memory
         // at the end and the last to arrive reads them all: about 4000 clocks, and for every part and row (64 at least: a warp's
