@@ -99,6 +99,18 @@ nk_status_t nk_grouped_destroy(nk_grouped_t plan);
  * nk_route_backward: dlogits[t][e] (FP32) from dgates[t][j] = dL / dgates[t][j], logits and experts of the run:
  *   dz_e = p_e (d_e - sum_j d_j gates_j), d_e = dgates[t][j] where e = experts[t][j], else 0; p the softmax above.
  *   A row whose logits are all minus infinity gets zeros.
+ * nk_route_balance: how evenly the experts are loaded.  Over the n tokens that count (mask[t] is not 0; mask NULL: all), p_te the
+ *   softmax of z[t] over all experts and c_e how often their choices experts[t][j] are e:
+ *     counts[e] = c_e, counts[experts] = n          INT32, experts + 1 of them
+ *     share[e]  = 1/n sum_t p_te                    FP32
+ *     losses[0] = experts / (n topk) sum_e c_e share[e]      1 where loads or shares are even
+ *     losses[1] = 1/n sum_t (log sum_e exp z_te)^2           the size of the logits
+ *   A choice outside [0, experts) is not counted (a dropped pair).  A row whose logits are all minus infinity counts as a token and adds
+ *   nothing; one with a NaN makes share and losses NaN.  n = 0: all zeros.
+ * nk_route_balance_backward: dlogits[t][e] (FP32) from dlosses[i] = dL / dlosses[i] (two FP32 numbers on the device) and the run's counts:
+ *     p_te (dlosses[0] experts / (n^2 topk) (c_e - sum_j c_j p_tj) + dlosses[1] 2/n log sum_j exp z_tj)
+ *   accumulate = 1 adds it to dlogits (which nk_route_backward has written); with 0 tokens that do not count get zeros.  Of loads over
+ *   several ranks: counts may be their sum (n included); dlosses is then the gradient of the losses of all tokens.
  * nk_route_dispatch: Xs[slots[t][j]] = X[t].
  * nk_route_combine:  Y[t] = sum_j gates[t][j] * Ys[slots[t][j]], summed in j's order in FP32, rounded once; gates NULL:
  *   all ones, which is the gradient of nk_route_dispatch.
@@ -130,6 +142,11 @@ nk_status_t nk_route_run(nk_route_t plan, const void* logits, float* gates, int3
                          void* workspace, size_t workspace_bytes, void* cuda_stream);
 nk_status_t nk_route_backward(nk_route_t plan, const void* logits, const int32_t* experts, const float* dgates, float* dlogits,
                               void* cuda_stream);
+size_t nk_route_balance_workspace_bytes(nk_route_t plan); /* of nk_route_balance; contents need no initialisation */
+nk_status_t nk_route_balance(nk_route_t plan, const void* logits, const int32_t* experts, const uint8_t* mask, int32_t* counts,
+                             float* share, float* losses, void* workspace, size_t workspace_bytes, void* cuda_stream);
+nk_status_t nk_route_balance_backward(nk_route_t plan, const void* logits, const uint8_t* mask, const int32_t* counts, const float* dlosses,
+                                      float* dlogits, int32_t accumulate, void* cuda_stream);
 nk_status_t nk_route_dispatch(nk_route_t plan, const void* X, const int32_t* slots, void* Xs, void* cuda_stream);
 nk_status_t nk_route_combine(nk_route_t plan, const void* Ys, const int32_t* slots, const float* gates, void* Y, void* cuda_stream);
 nk_status_t nk_route_combine_backward(nk_route_t plan, const void* dY, const void* Ys, const int32_t* slots, const float* gates,

@@ -1,0 +1,243 @@
+// The balance of a router's loads: how many rows each expert got, its mean probability, the two losses made of them and
+// their gradient.  Over the n tokens that count (mask), with c_e the choices of expert e and p_te the softmax of a row:
+//   P_e = 1/n sum_t p_te,  balance = E / (n k) sum_e c_e P_e,  size = 1/n sum_t lse_t^2,  lse_t = log sum_e exp z_te
+//   dz_te = p_te (g0 E / (n^2 k) (c_e - sum_j c_j p_tj) + g1 2/n lse_t)
+// A warp has a token, a lane the experts l, l + 32, ..., and adds up the probabilities of its tokens in registers: one pass
+// over the logits each way.  Sums of at most 64 tokens and then of a block's warps are FP32, those over blocks 64 bits; every
+// sum has one order (counts are integers, added in any).
+// Bound by instruction issue and a launch's start and end: see the figures in the design notes' table of the cases.
+#pragma once
+#include "route.cuh"
+
+namespace nk {
+
+struct BalanceParams {
+    const uint8_t* mask;        // [tokens], 0: the token does not count; null: all do
+    int* counts;                // [experts + 1]; the last: tokens that count
+    float* share;               // [experts]
+    float* losses;              // [2]
+    float* partial;             // [blocks][2 experts + 2]: sums of probabilities, counts, sum of lse^2, tokens
+    int blocks, per_block;
+};
+constexpr int BALANCE_RUN = 64;                    // tokens of a warp at most
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+    return x;
+}
+
+// A row's softmax in place: z becomes the probabilities; returns the row's log-sum-exp.  A row whose logits are all minus
+// infinity has neither: zeros.
+template <int V>
+__device__ __forceinline__ float row_softmax(float (&z)[V]) {
+    uint32_t top = 0u;
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        nan |= z[i] != z[i];
+        top = max(top, route_key(z[i]));
+    }
+    nan = __any_sync(~0u, nan);
+    const float m = route_unkey(__reduce_max_sync(~0u, top));
+    if (nan || m == -INFINITY) {
+        const float x = nan ? __int_as_float(0x7FC00000) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) z[i] = x;
+        return x;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        z[i] = expf(z[i] - m);
+        sum += z[i];
+    }
+    sum = warp_sum(sum);
+    const float inv = 1.0f / sum;
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] *= inv;
+    return m + logf(sum);
+}
+
+// The losses from sums and counts in shared memory (experts of them), by the whole block; `part`: 32 doubles.
+__device__ __forceinline__ void balance_finish(const RouteParams& p, const BalanceParams& b, const double* sum, const int* count, double size,
+                                               int tokens, double* part) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const double n = tokens;
+    double loss = 0.0;
+    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
+        const double s = tokens ? sum[e] / n : 0.0;
+        b.share[e] = static_cast<float>(s);
+        b.counts[e] = count[e];
+        loss += s * count[e];
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) loss += __shfl_xor_sync(~0u, loss, d);
+    if (lane == 0) part[warp] = loss;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < warps; ++w) loss += part[w];
+        b.losses[0] = tokens ? static_cast<float>(loss * p.experts / (n * p.topk)) : 0.0f;
+        b.losses[1] = tokens ? static_cast<float>(size / n) : 0.0f;
+        b.counts[p.experts] = tokens;
+    }
+}
+
+// shared memory of balance_kernel: a row of probabilities for each warp, then sums, counts, the warps' two numbers
+__host__ __device__ constexpr int balance_smem(int v) { return route_threads(v) / 32 * (32 * v * 4 + 8) + 32 * v * (8 + 4) + 32 * 8 + 16; }
+
+template <int V, bool ONE>
+__global__ void __launch_bounds__(route_threads(V)) balance_kernel(const RouteParams p, const BalanceParams b) {
+    constexpr int THREADS = route_threads(V), WARPS = THREADS / 32;
+    extern __shared__ double balance_sm[];
+    double* total = balance_sm;                                  // [32 V]
+    double* part = total + 32 * V;                               // [32]
+    float* rows = reinterpret_cast<float*>(part + 32);           // [WARPS][32 V]
+    int* hist = reinterpret_cast<int*>(rows + WARPS * 32 * V);   // [32 V]
+    float* sizes = reinterpret_cast<float*>(hist + 32 * V);      // [WARPS]
+    int* alive = reinterpret_cast<int*>(sizes + WARPS);          // [WARPS]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = p.experts;
+    const int t0 = blockIdx.x * b.per_block, t1 = min(p.tokens, t0 + b.per_block);
+    for (int e = threadIdx.x; e < E; e += THREADS) hist[e] = 0;
+    launch_wait();
+    launch_next();
+    __syncthreads();
+    float acc[V], size = 0.0f;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    for (int t = t0 + warp; t < t1; t += WARPS) {
+        if (b.mask && !b.mask[t]) continue;
+        float z[V];
+        route_fetch<V>(p, t, lane, -INFINITY, z);
+        const int e = lane < p.topk ? p.chosen[static_cast<size_t>(t) * p.topk + lane] : -1;
+        const float lse = row_softmax<V>(z);
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] += z[i];
+        size += lse * lse;
+        ++n;
+        if (e >= 0 && e < E) atomicAdd(hist + e, 1);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) rows[warp * 32 * V + lane + 32 * i] = acc[i];
+    if (lane == 0) { sizes[warp] = size; alive[warp] = n; }
+    __syncthreads();
+    if (ONE) {
+        for (int e = threadIdx.x; e < E; e += THREADS) {
+            double s = 0.0;
+            for (int w = 0; w < WARPS; ++w) s += rows[w * 32 * V + e];
+            total[e] = s;
+        }
+        double s = 0.0;
+        int m = 0;
+        if (threadIdx.x == 0)
+            for (int w = 0; w < WARPS; ++w) { s += sizes[w]; m += alive[w]; }
+        if (threadIdx.x == 0) alive[0] = m;
+        __syncthreads();
+        balance_finish(p, b, total, hist, s, alive[0], part);
+    } else {
+        float* out = b.partial + static_cast<size_t>(blockIdx.x) * (2 * E + 2);
+        for (int e = threadIdx.x; e < E; e += THREADS) {
+            float s = 0.0f;
+            for (int w = 0; w < WARPS; ++w) s += rows[w * 32 * V + e];
+            out[e] = s;
+            out[E + e] = __int_as_float(hist[e]);
+        }
+        if (threadIdx.x == 0) {
+            float s = 0.0f;
+            int m = 0;
+            for (int w = 0; w < WARPS; ++w) { s += sizes[w]; m += alive[w]; }
+            out[2 * E] = s;
+            out[2 * E + 1] = __int_as_float(m);
+        }
+    }
+}
+
+// One block: the blocks' sums into the results.
+__global__ void __launch_bounds__(1024) balance_total_kernel(const RouteParams p, const BalanceParams b) {
+    __shared__ double part[1024], total[NK_ROUTE_MAX_EXPERTS], line[32], size;
+    __shared__ int count[NK_ROUTE_MAX_EXPERTS], tokens;
+    const int E = p.experts, lanes = min(E, 1024), sets = 1024 / lanes, set = threadIdx.x / lanes, e = threadIdx.x - set * lanes;
+    const size_t pitch = 2 * E + 2;
+    for (int i = threadIdx.x; i < E; i += 1024) count[i] = 0;
+    if (threadIdx.x == 0) tokens = 0;
+    launch_wait();
+    launch_next();
+    __syncthreads();
+    if (set < sets) {
+        double s = 0.0;
+        int c = 0;
+#pragma unroll 4
+        for (int i = set; i < b.blocks; i += sets) {
+            s += b.partial[i * pitch + e];
+            c += __float_as_int(b.partial[i * pitch + E + e]);
+        }
+        part[threadIdx.x] = s;
+        atomicAdd(count + e, c);
+    }
+    // the last warp: the sums over rows
+    if (threadIdx.x >= 992) {
+        double s = 0.0;
+        int m = 0;
+        for (int i = threadIdx.x - 992; i < b.blocks; i += 32) {
+            s += b.partial[i * pitch + 2 * E];
+            m += __float_as_int(b.partial[i * pitch + 2 * E + 1]);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            s += __shfl_xor_sync(~0u, s, d);
+            m += __shfl_xor_sync(~0u, m, d);
+        }
+        if (threadIdx.x == 992) { size = s; tokens = m; }
+    }
+    __syncthreads();
+    if (threadIdx.x < E) {
+        double s = 0.0;
+        for (int i = 0; i < sets; ++i) s += part[i * lanes + threadIdx.x];
+        total[threadIdx.x] = s;
+    }
+    __syncthreads();
+    balance_finish(p, b, total, count, size, tokens, line);
+}
+
+// One warp per token.  The counts are taken from their mean, which changes nothing (the probabilities of a row add up to 1)
+// but leaves the differences of even loads their digits.
+template <int V>
+__global__ void __launch_bounds__(256) balance_backward_kernel(const RouteParams p, const BalanceParams b, const float* dlosses, float* dlogits, int accumulate) {
+    const int lane = threadIdx.x & 31;
+    const int t = blockIdx.x * 8 + (threadIdx.x >> 5);
+    launch_wait();
+    launch_next();
+    if (t >= p.tokens) return;
+    float* out = dlogits + static_cast<size_t>(t) * p.experts;
+    if (b.mask && !b.mask[t]) {
+        if (!accumulate)
+            for (int e = lane; e < p.experts; e += 32) out[e] = 0.0f;
+        return;
+    }
+    float z[V];
+    route_fetch<V>(p, t, lane, -INFINITY, z);
+    const int n = b.counts[p.experts];
+    const int mean = static_cast<int>(static_cast<long long>(n) * p.topk / p.experts);
+    const float lse = row_softmax<V>(z);
+    float c[V], inner = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = lane + 32 * i;
+        c[i] = e < p.experts ? static_cast<float>(b.counts[e] - mean) : 0.0f;
+        inner += c[i] * z[i];
+    }
+    inner = warp_sum(inner);
+    const float per = 1.0f / static_cast<float>(n);
+    const float up = dlosses[0] * (static_cast<float>(p.experts) / static_cast<float>(p.topk)) * per * per, size = dlosses[1] * 2.0f * per * lse;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = lane + 32 * i;
+        if (e < p.experts) {
+            const float x = z[i] * (up * (c[i] - inner) + size);
+            out[e] = accumulate ? out[e] + x : x;
+        }
+    }
+}
+
+}  // namespace nk

@@ -1,10 +1,12 @@
 // Host side of nk_route: descriptor validation and the launches.
 #include "rows_host.cuh"
+#include "balance.cuh"
 #include "route.cuh"
 
 struct nk_route_s : nk::PlanBase {
     nk_route_desc_t d;            // strides filled in
     int blocks, per_block;        // of nk_route_run; one block: a single launch
+    int balance_blocks, balance_per_block;   // of nk_route_balance, likewise
 };
 
 using namespace nk;
@@ -38,6 +40,28 @@ static void (*backward_kernel(int v))(RouteParams, const float*, float*) {
         case 16: return route_backward_kernel<16>;
     }
     return route_backward_kernel<32>;
+}
+
+template <bool ONE>
+static void (*balance_forward(int v))(RouteParams, BalanceParams) {
+    switch (v) {
+        case 1: return balance_kernel<1, ONE>;
+        case 2: return balance_kernel<2, ONE>;
+        case 4: return balance_kernel<4, ONE>;
+        case 8: return balance_kernel<8, ONE>;
+        case 16: return balance_kernel<16, ONE>;
+    }
+    return balance_kernel<32, ONE>;
+}
+static void (*balance_backward(int v))(RouteParams, BalanceParams, const float*, float*, int) {
+    switch (v) {
+        case 1: return balance_backward_kernel<1>;
+        case 2: return balance_backward_kernel<2>;
+        case 4: return balance_backward_kernel<4>;
+        case 8: return balance_backward_kernel<8>;
+        case 16: return balance_backward_kernel<16>;
+    }
+    return balance_backward_kernel<32>;
 }
 
 static RouteParams route_params(const nk_route_s* p) {
@@ -98,8 +122,18 @@ nk_status_t nk_route_create(const nk_route_desc_t* desc, nk_route_t* out) {
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     p->per_block = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? ROUTE_ONE_BLOCK : div_up(d.tokens, sms) < 32 ? 32 : div_up(d.tokens, sms));
     p->blocks = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? 1 : div_up(d.tokens, p->per_block));
+    // a block for each SM, but two tokens to a warp at least and BALANCE_RUN at most
+    const int warps = route_threads(route_width(d.experts)) / 32;
+    const int64_t even = div_up(d.tokens, sms);
+    p->balance_per_block = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? ROUTE_ONE_BLOCK : even < 2 * warps ? 2 * warps : even > BALANCE_RUN * warps ? BALANCE_RUN * warps : even);
+    p->balance_blocks = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? 1 : div_up(d.tokens, p->balance_per_block));
     DeviceGuard guard(d.device);
     const int v = route_width(d.experts);
+    if (cudaFuncSetAttribute(p->balance_blocks == 1 ? balance_forward<true>(v) : balance_forward<false>(v), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             balance_smem(v)) != cudaSuccess) {
+        delete p;
+        return NK_ERR_CUDA;
+    }
     if (cudaFuncSetAttribute(backward_kernel(v), cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * 32 * 32 * sizeof(float2)) != cudaSuccess) {
         delete p;
         return NK_ERR_CUDA;
@@ -163,6 +197,54 @@ nk_status_t nk_route_backward(nk_route_t p, const void* logits, const int32_t* e
     const cudaError_t e = launch_beside(backward_kernel(route_width(p->d.experts)), static_cast<unsigned>(div_up(r.tokens, 8)), 256, 8 * 32 * route_width(p->d.experts) * sizeof(float2),
                                         static_cast<cudaStream_t>(cuda_stream), r, dgates, dlogits);
     return e == cudaSuccess ? NK_OK : p->cuda("route backward launch", e);
+}
+
+size_t nk_route_balance_workspace_bytes(nk_route_t p) {
+    if (!p || p->balance_blocks == 1) return 0;
+    return static_cast<size_t>(p->balance_blocks) * (2 * p->d.experts + 2) * sizeof(float);
+}
+
+nk_status_t nk_route_balance(nk_route_t p, const void* logits, const int32_t* experts, const uint8_t* mask, int32_t* counts, float* share,
+                             float* losses, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!p || !counts || !share || !losses) return NK_ERR_INVALID_ARG;
+    if (p->d.tokens > 0 && (!logits || !experts)) return NK_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(logits) & (p->d.logits_dtype == NK_F32 ? 3u : 1u)) || misaligned4(experts) || misaligned4(counts) ||
+        misaligned4(share) || misaligned4(losses) || misaligned4(workspace))
+        return NK_ERR_MISALIGNED;
+    const size_t need = nk_route_balance_workspace_bytes(p);
+    if (need && (!workspace || workspace_bytes < need)) return NK_ERR_WORKSPACE;
+    DeviceGuard guard(p->device);
+    if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
+    RouteParams r = route_params(p);
+    r.logits = logits;
+    r.chosen = const_cast<int32_t*>(experts);
+    const BalanceParams b = {mask, counts, share, losses, static_cast<float*>(workspace), p->balance_blocks, p->balance_per_block};
+    const int v = route_width(p->d.experts);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = launch_beside(b.blocks == 1 ? balance_forward<true>(v) : balance_forward<false>(v), b.blocks, route_threads(v), balance_smem(v), st, r, b);
+    if (e != cudaSuccess) return p->cuda("balance launch", e);
+    if (b.blocks > 1 && (e = launch_beside(balance_total_kernel, 1, 1024, 0, st, r, b)) != cudaSuccess) return p->cuda("balance total launch", e);
+    return NK_OK;
+}
+
+nk_status_t nk_route_balance_backward(nk_route_t p, const void* logits, const uint8_t* mask, const int32_t* counts, const float* dlosses,
+                                      float* dlogits, int32_t accumulate, void* cuda_stream) {
+    if (!p || (accumulate != 0 && accumulate != 1)) return NK_ERR_INVALID_ARG;
+    if (p->d.tokens == 0) return NK_OK;
+    if (!logits || !counts || !dlosses || !dlogits) return NK_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(logits) & (p->d.logits_dtype == NK_F32 ? 3u : 1u)) || misaligned4(counts) || misaligned4(dlosses) ||
+        misaligned4(dlogits))
+        return NK_ERR_MISALIGNED;
+    DeviceGuard guard(p->device);
+    if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
+    RouteParams r = route_params(p);
+    r.logits = logits;
+    BalanceParams b = {};
+    b.mask = mask;
+    b.counts = const_cast<int32_t*>(counts);
+    const cudaError_t e = launch_beside(balance_backward(route_width(p->d.experts)), static_cast<unsigned>(div_up(r.tokens, 8)), 256, 0,
+                                        static_cast<cudaStream_t>(cuda_stream), r, b, dlosses, dlogits, accumulate);
+    return e == cudaSuccess ? NK_OK : p->cuda("balance backward launch", e);
 }
 
 nk_status_t nk_route_dispatch(nk_route_t p, const void* X, const int32_t* slots, void* Xs, void* cuda_stream) {

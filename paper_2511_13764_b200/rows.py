@@ -12,6 +12,7 @@ GROUPED_ROWS, GROUPED_WEIGHTS = 0, 1
 EXPORTS = ["nk_grouped_create", "nk_grouped_workspace_bytes", "nk_grouped_run", "nk_grouped_check",
            "nk_grouped_kernel_name", "nk_grouped_last_cuda_error", "nk_grouped_destroy",
            "nk_route_create", "nk_route_workspace_bytes", "nk_route_run", "nk_route_backward", "nk_route_dispatch",
+           "nk_route_balance_workspace_bytes", "nk_route_balance", "nk_route_balance_backward",
            "nk_route_combine", "nk_route_combine_backward", "nk_route_check", "nk_route_kernel_name",
            "nk_route_last_cuda_error", "nk_route_destroy",
            "nk_lora_create", "nk_lora_workspace_bytes", "nk_lora_run", "nk_lora_check", "nk_lora_kernel_name",
@@ -59,6 +60,10 @@ def lib():
         for name, pointers in (("backward", 4), ("dispatch", 3), ("combine", 4), ("combine_backward", 6)):
             f = getattr(L, f"nk_route_{name}")
             f.restype, f.argtypes = ctypes.c_int, [vp] * (pointers + 2)
+        L.nk_route_balance_workspace_bytes.restype, L.nk_route_balance_workspace_bytes.argtypes = sz, [vp]
+        L.nk_route_balance.restype = L.nk_route_balance_backward.restype = ctypes.c_int
+        L.nk_route_balance.argtypes = [vp] * 8 + [sz, vp]
+        L.nk_route_balance_backward.argtypes = [vp] * 6 + [ctypes.c_int32, vp]
         _lib = L
     return _lib
 
@@ -152,6 +157,25 @@ class RoutePlan(_Handle):
 
     def backward(self, logits, experts, dgates, dlogits, stream=None):
         status = _lib.nk_route_backward(self._raw, _ptr(logits), _ptr(experts), _ptr(dgates), _ptr(dlogits), stream)
+        if status:
+            self._check(status)
+
+    @property
+    def balance_workspace_bytes(self) -> int:
+        return _lib.nk_route_balance_workspace_bytes(self._raw)
+
+    def balance(self, logits, experts, counts, share, losses, mask=None, workspace=None, workspace_bytes=None, stream=None):
+        """counts (INT32 [experts + 1]), mean probabilities (FP32 [experts]) and the two losses (FP32 [2]) of the tokens whose
+        mask (UINT8 [tokens]; None: all) is not 0."""
+        status = _lib.nk_route_balance(self._raw, _ptr(logits), _ptr(experts), _ptr(mask), _ptr(counts), _ptr(share), _ptr(losses),
+                                        _ptr(workspace), _bytes(workspace, workspace_bytes), stream)
+        if status:
+            self._check(status)
+
+    def balance_backward(self, logits, counts, dlosses, dlogits, mask=None, accumulate=False, stream=None):
+        """accumulate: add to dlogits (of backward) instead of writing it."""
+        status = _lib.nk_route_balance_backward(self._raw, _ptr(logits), _ptr(mask), _ptr(counts), _ptr(dlosses), _ptr(dlogits),
+                                                 int(accumulate), stream)
         if status:
             self._check(status)
 
