@@ -8,3 +8,4 @@ from .binding import (  # noqa: F401
     flag_splitk, flag_tile_n, flag_tail_split, flag_raster, plan_for, quantize_s8, STATIC_SCRATCH_BYTES,
 )
 from .rows import GroupedPlan, LoraPlan, RoutePlan, GROUPED_ROWS, GROUPED_WEIGHTS  # noqa: F401
+from .mx import MxPlan, PackPlan, MXF4, NVF4  # noqa: F401

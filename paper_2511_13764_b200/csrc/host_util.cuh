@@ -32,9 +32,9 @@ struct DeviceGuard {
 // Launch that may begin while the kernel before it in the stream ends.  Every kernel launched this way waits for that
 // one (griddepcontrol.wait) before it touches global memory, unless it says otherwise, and again before it ends.
 template <typename... P, typename... A>
-static cudaError_t launch_beside(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, const A&... args) {
+static cudaError_t launch_beside(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, const A&... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

@@ -1,0 +1,61 @@
+// The 4-bit formats: geometry of packed arrays (host and device) and conversions of scales and elements.
+#pragma once
+#include "half.cuh"
+
+namespace nk {
+
+constexpr int MX_TILE_ROWS = 128, MX_TILE_BYTES = 512;          // a tile of scales: 128 rows x 4 blocks
+__host__ __device__ constexpr int mx_block(int nv) { return nv ? 16 : 32; }
+__host__ __device__ constexpr long long mx_padded(long long length) { return (length + 63) / 64 * 64; }
+// tiles of scales along the contraction
+__host__ __device__ constexpr long long mx_tiles(long long length, int nv) {
+    return (mx_padded(length) + 4 * mx_block(nv) - 1) / (4 * mx_block(nv));
+}
+// first tile of scales of a group whose rows begin at row0: groups' tiles never meet, since ceil(n / 128) <= (row0 + n) / 128 - row0 / 128 + 1
+__host__ __device__ constexpr int mx_group_tile(int row0, int g) { return row0 / MX_TILE_ROWS + g; }
+
+#ifdef __CUDACC__
+// E8M0 byte to its number (2^-127 is a subnormal)
+__device__ __forceinline__ float e8m0_to_f32(uint32_t b) { return __uint_as_float(b == 0u ? 0x00400000u : b == 255u ? 0x7FC00000u : b << 23); }
+__device__ __forceinline__ uint32_t f32_to_e4m3(float x) {       // round to nearest even, at most 448; NaN: 0x7F
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(x));
+    return r & 0xFFu;
+}
+__device__ __forceinline__ float e4m3_to_f32(uint32_t b) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(b)));
+    return half_bits_to_f32(r & 0xFFFFu, 1);
+}
+// eight numbers to E2M1 (nearest even, at most 6 in size), the first in the lowest four bits
+__device__ __forceinline__ uint32_t f32_to_e2m1x8(const float (&x)[8]) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r)
+        : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+    return r;
+}
+__device__ __forceinline__ void e2m1x8_to_f32(uint32_t w, float (&x)[8]) {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = half_bits_to_f32(h[i] & 0xFFFFu, 1);
+        x[2 * i + 1] = half_bits_to_f32(h[i] >> 16, 1);
+    }
+}
+#endif
+
+}  // namespace nk

@@ -322,20 +322,6 @@ struct ExchangeParams {
     const float* gates;
 };
 
-template <bool F16>
-__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = half_bits_to_f32(w[i] & 0xFFFFu, F16);
-        x[2 * i + 1] = half_bits_to_f32(w[i] >> 16, F16);
-    }
-}
-template <bool F16>
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-    return make_uint4(pack_half2(x[0], x[1], F16), pack_half2(x[2], x[3], F16), pack_half2(x[4], x[5], F16), pack_half2(x[6], x[7], F16));
-}
-
 // A block of 256 threads has the rows of 256 >> p.lanes_log2 tokens, 1 << p.lanes_log2 threads to a row.  (One index over all
 // pieces of all rows and a division by a row's pieces cost as many instructions as the sum itself.)
 __device__ __forceinline__ int exchange_token(const ExchangeParams& p) {
