@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libnk_gemm.so")
 SOURCES = ["nk_gemm.cu", "nk_grouped.cu", "grouped_rows.cu", "grouped_weights.cu", "grouped_lora.cu",
-           "nk_route.cu", "nk_lora.cu", "nk_pack.cu"]
+           "nk_route.cu", "nk_lora.cu", "nk_pack.cu", "nk_mx.cu",
+           "mx_nv.cu", "mx_mx.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 

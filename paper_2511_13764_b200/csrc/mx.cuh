@@ -1,0 +1,598 @@
+// Products of 4-bit operands with block scales, of all rows with one weight or grouped by expert:
+//   C[t][i] = ta tb sum_k X[t][k] W_g[i][k]      for the rows t of group g
+// The shape of the kernel is that of the grouped products (grouped.cuh): the features are the MMA's M dimension and the ragged rows
+// its N, a CTA pair computes 256 features x up to 256 rows, the groups' offsets are read on the device by a scheduler warp, and
+// tiles of the last, partial wave are cut along k.  What is different:
+//
+// A k-block is 256 elements (128 bytes of a row), four MMAs of 64.  Its scales arrive by TMA as the tiles of 128 rows x 4 blocks that
+// tensor memory wants and go there by tcgen05.cp, issued before the MMAs that use them, into one of two places in turn.  Each CTA has
+// the scales of its own 128 features and of all the tile's rows.
+//
+// Tensor memory: two accumulators of 256 columns would leave no room for the scales (2 x 48 columns).  So for tiles of more than 128 rows the
+// second begins at column 160: they share 96 columns.  The epilogue takes the shared columns of an accumulator first, into
+// registers, and gives them back; the next tile may begin then, while the rest is taken and stored.
+//
+// Tiles begin at multiples of 64 rows of a group (or at its first row): scales of 64 rows are two columns, by which the place of the
+// rows' scales moves where a tile begins in the middle of 128.
+//
+// Warps: 0 TMA producer, 1 MMA issuer, 2-9 epilogue (warps 2-5 take the even 32-column pieces, 6-9 the odd ones), 10 scheduler.
+// All waits are bounded (see mbar_wait).
+#pragma once
+#include "grouped.cuh"
+#include "mx_format.cuh"
+#include "mx_launch.cuh"
+
+namespace nk {
+
+// One piece of work: k-blocks kb0 .. kb1-1 of a tile.
+struct __align__(16) MxUnit {
+    int some;              // 0: no more work
+    int g, i0;             // group (and its weight), first feature
+    int c0, cols, jn;      // first row of C, rows of the tile, the MMA's N (rows rounded up to 32)
+    int tile, shift;       // first tile of the rows' scales, columns before the first row's
+    int kb0, kb1;
+    int cut, parts, part, first_pair;   // a cut tile: its number among the tail's tiles, its parts, this one, the pair of part 0
+};
+constexpr int MX_UNITS = 4;             // of them on the way
+constexpr int MX_SHARED = 160;          // first of the columns that both accumulators have
+constexpr int MX_SCALES = 416;          // columns of the scales: two places of 48, the features' 16 and the rows' 32
+
+template <bool NV, int OUT, bool SUMS>
+__global__ void __launch_bounds__(MX_THREADS, 1) __cluster_dims__(2, 1, 1)
+mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams p) {
+    constexpr bool OUT16 = OUT != MX_OUT_F32, F16 = OUT == MX_OUT_F16;
+    constexpr int S_BOX = NV ? 2048 : 1024;               // scales of 128 rows and a k-block
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
+    int* s_row = reinterpret_cast<int*>(gen_base + MX_RING + MX_STAGING);   // first row of each group, clamped and monotone
+    int* s_pre = s_row + MX_MAX_GROUPS + 1;                                  // tiles before each group
+    const uint32_t bar_base = smem_base + MX_RING + MX_STAGING + 2 * MX_TABLE;
+    static_assert(2 * MX_TABLE % 8 == 0, "barriers are 8-byte aligned");
+    constexpr int MS = MX_MAX_STAGES;
+    auto full_bar = [&](int s) { return bar_base + 8u * s; };
+    auto empty_bar = [&](int s) { return bar_base + 8u * (MS + s); };
+    auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * MS + a); };
+    auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * MS + 2 + a); };
+    auto ufull_bar = [&](int n) { return bar_base + 8u * (2 * MS + 4 + n); };    // a unit is there
+    auto uempty_bar = [&](int n) { return bar_base + 8u * (2 * MS + 4 + MX_UNITS + n); };   // every role has read it
+    constexpr int NB = 2 * MS + 4 + 2 * MX_UNITS;
+    const uint32_t peer_ready_bar = bar_base + 8u * NB;
+    uint8_t* after = gen_base + (bar_base - smem_base) + 8 * (NB + 1);
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(after);
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+    volatile int* s_width = reinterpret_cast<volatile int*>(after + 8);      // rows of a tile at most
+    MxUnit* s_unit = reinterpret_cast<MxUnit*>(gen_base + ((MX_RING + MX_STAGING + 2 * MX_TABLE + 8 * (NB + 1) + 12 + 15) & ~15));
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair_id = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+    auto give_up = [&](unsigned int code) {
+        *abort_flag = 1;
+        if (p.status) atomicCAS(p.status, 0u, code);
+    };
+    // after a wait that ran out: what is still on its way into shared memory, or at work on it, needs some microseconds, and the pair
+    // ends together
+    auto settle = [&]() {
+        const long long t0 = clock64();
+        while (clock64() - t0 < (1ll << 20)) __nanosleep(1000);
+    };
+
+    if (warp == 0) {
+        for (int n = lane; n < NB; n += 32) {
+            // tempty: one arrival per epilogue warp of both CTAs; uempty: producer, epilogue warps, the leader's MMA issuer
+            const uint32_t count = n >= 2 * MS + 2 && n < 2 * MS + 4 ? 16 : n >= 2 * MS + 4 + MX_UNITS ? 9 + (rank == 0) : 1;
+            mbar_init(bar_base + 8u * n, count);
+        }
+        if (lane == 31) mbar_init(peer_ready_bar, 1);
+        if (lane == 0) *abort_flag = 0;
+        fence_mbar_init();
+        __syncwarp();
+    } else if (warp == 2) {
+        if (lane < 8) tma_prefetch_desc(&maps.b[lane]);
+        if (lane == 8) tma_prefetch_desc(&maps.a);
+        if (lane == 9) tma_prefetch_desc(&maps.sa);
+        if (lane == 10) tma_prefetch_desc(&maps.sb);
+    } else if (warp == 1) {
+        tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before_sync();
+    cluster_arrive();
+    // up to here the launch may have run beside the end of the one before it in the stream
+    launch_wait();
+    launch_next();
+    for (int g = threadIdx.x; g <= p.groups; g += MX_THREADS) s_row[g] = p.offsets ? p.offsets[g] : g == 0 ? 0 : p.rows;
+    __syncthreads();
+    cluster_wait();          // the barriers of both CTAs are initialised
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+    if (warp == 1 && rank == 1 && lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(peer_ready_bar, 0));
+
+    // the roles' view of the schedule: wait for the next unit, read it, give its place back
+    int unit_at = 0;
+    uint32_t unit_phase = 0;
+    auto next = [&](MxUnit& u) -> bool {
+        if (!mbar_wait(ufull_bar(unit_at), unit_phase, abort_flag)) {
+            if (lane == 0) give_up(0x800u + warp);
+            return false;
+        }
+        u = s_unit[unit_at];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(uempty_bar(unit_at));
+        if (++unit_at == MX_UNITS) { unit_at = 0; unit_phase ^= 1u; }
+        return u.some != 0;
+    };
+    // settled once the first unit is there: stages of the ring, and whether the accumulators share columns
+    int stage_bytes = 0, S = 1, apart = 128;
+    bool sharing = false;
+    auto ring = [&]() {
+        const int width = *s_width;
+        stage_bytes = mx_stage_bytes(width);
+        S = min(MS, MX_RING / stage_bytes);
+        sharing = width > 128;
+        apart = sharing ? MX_SHARED : 128;
+    };
+
+    if (warp == MX_THREADS / 32 - 1) {
+        // ------------------------------------------------ scheduler (both CTAs of a pair come to the same schedule)
+        // offsets that break their rule are clamped to the running maximum
+        bool bad = false;
+        for (int g = lane; g <= p.groups; g += 32) bad |= s_row[g] < (g ? s_row[g - 1] : 0) || s_row[g] > p.rows;
+        if (__any_sync(~0u, bad)) {
+            if (lane == 0) {
+                if (blockIdx.x == 0 && p.status) atomicCAS(p.status, 0u, 0x10000u);
+                int top = 0;
+                for (int g = 0; g <= p.groups; ++g) s_row[g] = top = max(top, min(s_row[g], p.rows));
+            }
+            __syncwarp();
+        }
+        auto rows_in = [&](int g) { return s_row[g + 1] - s_row[g]; };
+        int most = 0;
+        for (int g = lane; g < p.groups; g += 32) most = max(most, rows_in(g));
+        most = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(most)));
+        // Estimated time, in clocks, of n tiles of w rows, and into how many parts (1: none) the tiles of the last, partial wave are cut: see
+        // grouped.cuh, whose costs of parts these are; a k-block costs MX_KB + 1.5 w.
+        auto share_of = [&](int w, int t) { return static_cast<float>(max(64, w)) * (10.0f + static_cast<float>(t) * t * (1.0f / 450)); };
+        auto block_of = [&](int w) { return 400.0f + w * 1.5f; };
+        auto best_parts = [&](int kbs, int w, int t) {
+            return max(1, min(__float2int_rn(sqrtf(__fdividef(static_cast<float>(kbs) * block_of(w), share_of(w, t)))), kbs / 2));
+        };
+        auto estimate = [&](int n, int w, int& parts) {
+            const int waves = n / num_pairs, rest = n - waves * num_pairs, most_parts = rest ? num_pairs / rest : 1;
+            const float kb = block_of(w), k = static_cast<float>(p.kb_total), whole = (waves + (rest ? 1 : 0)) * (k * kb + 500.0f);
+            parts = p.partial && most_parts > 1 ? min(most_parts, best_parts(p.kb_total, w, rest * most_parts)) : 1;
+            const float cut = waves * (k * kb + 500.0f) + (p.kb_total + parts - 1) / parts * kb + 4000.0f + share_of(w, rest * parts) * parts;
+            if (parts > 1 && cut < whole) return cut;
+            parts = 1;
+            return whole;
+        };
+        // rows of the tiles of a group: its rows cut evenly, in steps of 64
+        auto tile_rows = [&](int rows, int w) {
+            const int nt = (rows + w - 1) / w;
+            return nt <= 1 ? w : ((rows + nt - 1) / nt + 63) & ~63;
+        };
+        int width = most <= 32 ? 32 : 64, parts = 1;
+        if (most > 64) {
+            // the width of least estimated time: lane l looks at 64 (l + 1)
+            const int limit = min(MX_TILE, (most + 63) & ~63), w = min(64 * ((lane & 3) + 1), limit);
+            int n = 0;
+            for (int g = lane >> 2; g < p.groups; g += 8) n += (rows_in(g) + w - 1) / w;
+            n += __shfl_xor_sync(~0u, n, 4);
+            n += __shfl_xor_sync(~0u, n, 8);
+            n += __shfl_xor_sync(~0u, n, 16);
+            const float t = estimate(n * p.tiles_i, w, parts);
+            // the smallest; of equals the widest: a time's upper bits, then the width
+            const unsigned won = __reduce_min_sync(~0u, (__float_as_uint(t) & ~7u) | (4u - static_cast<unsigned>(w >> 6)));
+            width = static_cast<int>(4u - (won & 7u)) << 6;
+        }
+        if (lane == 0) *s_width = width;
+        // tiles before each group
+        int tiles = 0;
+        for (int base = 0; base <= p.groups; base += 32) {
+            const int g = base + lane;
+            const int n = g >= p.groups ? 0 : (rows_in(g) + width - 1) / width * p.tiles_i;
+            int v = n;
+#pragma unroll 1
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(~0u, v, d);
+                if (lane >= d) v += o;
+            }
+            if (g <= p.groups) s_pre[g] = tiles + v - n;
+            tiles += __shfl_sync(~0u, v, 31);
+        }
+        __syncwarp();
+        // Whole tiles in turn, then the tail [tail_from, tiles), the last, partial wave: `tail_len` k-blocks, `share` of them to each pair; a
+        // tile counts `padded` k-blocks there, a whole number of shares.
+        const int from = tiles / num_pairs * num_pairs;
+        int tail_from = tiles, tail_len = 0, share = 1, padded = p.kb_total;
+        estimate(tiles, width, parts);
+        if (parts > 1) {
+            tail_from = from;
+            share = (p.kb_total + parts - 1) / parts;
+            padded = (p.kb_total + share - 1) / share * share;
+            tail_len = (tiles - from) * padded;
+        }
+        int next_tile = pair_id, x = pair_id * share;     // this pair's next whole tile, its place in the tail
+        const int tail_hi = min(x + share, tail_len);
+        MxUnit u = {};
+        for (u.some = 1; u.some;) {
+            int tile = 0, at = 0;                         // `at`: the tile's k-block to begin with
+            if (next_tile < tail_from) {
+                tile = next_tile;
+                next_tile += num_pairs;
+            } else if (tail_from < tiles && x < tail_hi) {
+                const int rel = x / padded;
+                tile = tail_from + rel;
+                at = x - rel * padded;
+            } else {
+                u.some = 0;
+            }
+            if (u.some) {
+                u.g = find_last(s_pre, p.groups, tile);
+                const int rel = tile - s_pre[u.g], row0 = s_row[u.g], rows = rows_in(u.g);
+                const int jt = tile_rows(rows, width), nt = (rows + width - 1) / width;
+                // eight tiles of a group's rows sweep the features together
+                const int block = div_small(rel, 8 * p.tiles_i);
+                const int within = rel - block * 8 * p.tiles_i;
+                const int wide = min(8, nt - block * 8);
+                const int ti = div_small(within, wide), first = (block * 8 + within - ti * wide) * jt;
+                u.c0 = row0 + first;
+                u.cols = min(jt, rows - first);           // (at least 1: rows > width (nt - 1) >= jt (nt - 1))
+                u.tile = mx_group_tile(row0, u.g) + (first >> 7);
+                u.shift = (first & 127) >> 5;
+                u.i0 = ti * MX_TILE;
+                u.jn = round32(u.cols);
+                u.kb0 = 0;
+                u.kb1 = p.kb_total;
+                u.parts = 1;
+                u.part = 0;
+                if (tile >= tail_from) {
+                    const int start = x - at;             // the tile's place in the tail
+                    u.kb0 = min(at, p.kb_total);
+                    u.kb1 = min(p.kb_total, at + tail_hi - x);
+                    x += min(padded - at, tail_hi - x);
+                    u.first_pair = start / share;
+                    u.parts = (start + p.kb_total - 1) / share - u.first_pair + 1;
+                    u.part = pair_id - u.first_pair;
+                    u.cut = tile - tail_from;
+                }
+            }
+            if (!mbar_wait(uempty_bar(unit_at), unit_phase ^ 1u, abort_flag)) {
+                if (lane == 0) give_up(0x900u);
+                break;
+            }
+            if (lane == 0) {
+                s_unit[unit_at] = u;
+                mbar_arrive(ufull_bar(unit_at));
+            }
+            __syncwarp();
+            if (++unit_at == MX_UNITS) { unit_at = 0; unit_phase ^= 1u; }
+        }
+    } else if (warp == 0) {
+        // ------------------------------------------------ TMA producer (both CTAs)
+        const uint32_t lead_full0 = map_to_cta(full_bar(0), 0);
+        const uint32_t elected = elect_one();
+        const uint32_t lead_elected = rank == 0 ? elected : 0u;
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        MxUnit u = {};
+        while (ok && next(u)) {
+            ring();
+            const int half = u.jn >> 1, high = (half >> 4) - 1;       // rows of this CTA, and the map whose boxes have them
+            const int i = u.i0 + static_cast<int>(rank) * 128, c = u.c0 + static_cast<int>(rank) * half;
+            const int s_tile = u.g * p.scale_tiles + (i >> 7);
+            const bool two = u.shift * 32 + u.jn > 128;               // tiles of the rows' scales
+            const uint32_t bytes = 2u * (MX_A_BYTES + half * 128u + (two ? 3u : 2u) * S_BOX);
+            const int s_off = MX_A_BYTES + *s_width * 64;
+            for (int kb = u.kb0; kb < u.kb1; ++kb) {
+                if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) {
+                    if (lane == 0) give_up(0x100u + stage);
+                    ok = false;
+                    break;
+                }
+                const uint32_t sa = smem_base + stage * stage_bytes, lfb = lead_full0 + 8u * stage, ss = sa + s_off;
+                const int kx = kb * (MX_BK / 2), ks = kb * (S_BOX / MX_TILE_BYTES);
+                mbar_arrive_expect_tx_if(full_bar(stage), bytes, lead_elected);
+                tma_load_3d_pair_if(sa, &maps.a, lfb, kx, i, u.g, elected);
+                tma_load_3d_pair_if(sa + MX_A_BYTES, &maps.b[high], lfb, kx, c, 0, elected);
+                tma_load_3d_pair_if(ss, &maps.sa, lfb, 0, ks, s_tile, elected);
+                tma_load_3d_pair_if(ss + MX_S_BYTES, &maps.sb, lfb, 0, ks, u.tile, elected);
+                if (two) tma_load_3d_pair_if(ss + 2 * MX_S_BYTES, &maps.sb, lfb, 0, ks, u.tile + 1, elected);
+                __syncwarp();
+                if (++stage == S) { stage = 0; phase ^= 1u; }
+            }
+        }
+        for (int s = 0; ok && s < S; ++s) {   // drain: every stage this CTA filled has been consumed
+            ok = mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag);
+            if (++stage == S) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) settle();
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issuer (leader only)
+        if (rank == 0) {
+            const uint64_t da = make_smem_desc(smem_base, 16, 1024, 2), ds = make_smem_desc(smem_base, 16, 128, 0);
+            const uint32_t hi = static_cast<uint32_t>(da >> 32), s_hi = static_cast<uint32_t>(ds >> 32);
+            const uint32_t a_lo0 = static_cast<uint32_t>(da), s_lo0 = static_cast<uint32_t>(ds);
+            const uint32_t elected = elect_one();
+            int stage = 0, local = 0;                     // local: accumulators filled so far
+            uint32_t phase = 0, place = 0;                // place: of the scales
+            // The tensor core's order holds for a copy and the MMAs behind it, not for MMAs and a copy behind them: what a place held before
+            // is two k-blocks back, whose MMAs are waited for (while those of the block before are at work)
+            uint32_t done[2] = {0u, 0u}, done_phase[2] = {0u, 0u};
+            bool ok = true;
+            if (!mbar_wait(peer_ready_bar, 0u, abort_flag)) {
+                if (lane == 0) give_up(0x700u);
+                ok = false;
+            }
+            MxUnit u;
+            while (ok && next(u)) {
+                ring();
+                const uint32_t idesc = p.idesc | (static_cast<uint32_t>(u.jn >> 3) << 17);
+                const uint32_t s_off = (MX_A_BYTES + *s_width * 64) >> 4;
+                const bool two = u.shift * 32 + u.jn > 128;
+                int in_chunk = 0;
+                uint32_t d_tmem = 0;
+                for (int kb = u.kb0; kb < u.kb1; ++kb) {
+                    const int acc = local & 1;
+                    if (in_chunk == 0) {
+                        // sharing: the accumulator before this one has given the shared columns back (and so its predecessor all of its own);
+                        // else: the one before that is free
+                        const bool free = !sharing ? mbar_wait(tempty_bar(acc), ((local >> 1) & 1u) ^ 1u, abort_flag)
+                                                   : local == 0 || mbar_wait(tempty_bar(acc ^ 1), ((local - 1) >> 1) & 1u, abort_flag);
+                        if (!free) {
+                            if (lane == 0) give_up(0x200u + acc);
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after_sync();
+                        d_tmem = tmem_base + acc * apart;
+                    }
+                    if (!mbar_wait(full_bar(stage), phase, abort_flag)) {
+                        if (lane == 0) give_up(0x300u + stage);
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after_sync();
+                    const int steps = min(4, p.steps - 4 * kb);
+                    const uint32_t a_lo = a_lo0 + stage * (stage_bytes >> 4), b_lo = a_lo + (MX_A_BYTES >> 4);
+                    const uint32_t s_lo = s_lo0 + stage * (stage_bytes >> 4) + s_off;
+                    const uint32_t sa_t = tmem_base + MX_SCALES + place * 48, sb_t = sa_t + 16;
+                    if (done[place] && !mbar_wait(done[place], done_phase[place], abort_flag)) {
+                        if (lane == 0) give_up(0x500u + stage);
+                        ok = false;
+                        break;
+                    }
+                    done[place] = empty_bar(stage);
+                    done_phase[place] = phase;
+                    place ^= 1u;
+                    // tiles of scales: four columns of the features' and four or eight of the rows', of one step (NV) or two
+#pragma unroll
+                    for (int s = 0; s < (NV ? 4 : 2); ++s) {
+                        if (s > 0 && (NV ? s : 2 * s) >= steps) break;
+                        tmem_copy_scales_pair_if(sa_t + 4 * s, s_lo + 32 * s, s_hi, elected);
+                        tmem_copy_scales_pair_if(sb_t + 8 * s, s_lo + (MX_S_BYTES >> 4) + 32 * s, s_hi, elected);
+                        if (two) tmem_copy_scales_pair_if(sb_t + 8 * s + 4, s_lo + (2 * MX_S_BYTES >> 4) + 32 * s, s_hi, elected);
+                    }
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        if (s > 0 && s >= steps) break;
+                        // (two steps' scales in a column's word: the second's in its upper half)
+                        const uint32_t id = NV ? 0u : (s & 1u) << 1, col = NV ? s : s >> 1;
+                        umma_mx_pair_if<NV>(d_tmem, a_lo + 2 * s, hi, b_lo + 2 * s, hi, idesc | id << 4 | id << 29, sa_t + 4 * col,
+                                            sb_t + 8 * col + u.shift, in_chunk > 0 || s > 0 ? 1u : 0u, elected);
+                    }
+                    umma_commit_pair_if(empty_bar(stage), 3, elected);
+                    ++in_chunk;
+                    if ((SUMS && in_chunk == p.chunk) || kb == u.kb1 - 1) {
+                        umma_commit_pair_if(tfull_bar(acc), 3, elected);
+                        in_chunk = 0;
+                        ++local;
+                    }
+                    __syncwarp();
+                    if (++stage == S) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (*abort_flag) settle();
+        }
+    } else {
+        // ------------------------------------------------ epilogue (both CTAs, own 128 features)
+        const int set = warp >= 6 ? 1 : 0;
+        const int quarter = warp & 3;
+        const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
+        const uint32_t staging = smem_base + MX_RING + (warp - 2) * 4096;
+        uint32_t parity = 0;
+        int local = 0;
+        bool ok = true;
+        float alpha = 1.0f;
+        MxUnit u = {};
+        auto await = [&]() {
+            const int acc = local & 1;
+            if (!mbar_wait(tfull_bar(acc), (local >> 1) & 1u, abort_flag)) {
+                if (lane == 0) give_up(0x400u + acc);
+                return false;
+            }
+            tc_fence_after_sync();
+            return true;
+        };
+        auto release = [&]() {
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(tempty_bar(local & 1), 0));
+        };
+        // Cut tiles.  The slab of a pair: 0 for the tile its share begins in, 1 for the one it ends in.  A piece is 4 KB of it,
+        // lane after lane.
+        auto slab_of = [&](int part, int c) {
+            return reinterpret_cast<float4*>(p.partial) + (2 * (u.first_pair + part) + (part > 0 ? 0 : 1)) * (static_cast<size_t>(MX_TILE / 4) * p.slab_cols) +
+                   ((rank * p.slab_cols + c) / 32 * 4 + quarter) * 256 + lane;
+        };
+        auto to_slab = [&](const float (&v)[32], int c) {
+            float4* dst = slab_of(u.part, c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) __stcg(dst + j * 32, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+        };
+        // One 32 x 32 piece of C (columns c .. c + 31 of the tile, this warp's 32 features): lane l has feature l, v[j] is row j.
+        // It goes through two 2 KB buffers of shared memory, from where a TMA store writes it (and clips what lies beyond C's
+        // edges); of a piece that ends inside the box, because the next row is another group's, lanes write 16 bytes each.
+        auto deliver = [&](float (&v)[32], int c) {
+            const int n = min(32, u.cols - c), i0 = u.i0 + static_cast<int>(rank) * 128 + quarter * 32;
+            const size_t row0 = static_cast<size_t>(u.c0 + c);
+            const bool live = i0 + lane < p.I;
+            const float bias = p.bias && live ? __ldg(p.bias + static_cast<size_t>(u.g) * p.I + i0 + lane) : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], alpha, bias);
+            const size_t base = row0 * p.ldc + i0;
+            if (p.beta) {
+                const uint16_t* c16 = static_cast<const uint16_t*>(p.C) + base + lane;
+                const float* c32 = static_cast<const float*>(p.C) + base + lane;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    if (live && j < n) v[j] += OUT16 ? half_bits_to_f32(*c16, F16) : *c32;
+                    c16 += p.ldc;
+                    c32 += p.ldc;
+                }
+            }
+            if (p.relu) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = v[j] < 0.0f ? 0.0f : v[j];          // (a NaN stays)
+            }
+            constexpr int ROWS = OUT16 ? 32 : 16, PITCH = 2048 / ROWS;    // of a buffer; 64 or 128 bytes
+#pragma unroll
+            for (int half = 0; half < 32; half += ROWS) {
+                if (half > 0 && half >= n) break;
+                const uint32_t box = staging + parity * 2048;
+                parity ^= 1u;
+                if (lane == 0) bulk_wait_read<1>();       // the store before the last has read this buffer
+                __syncwarp();
+                if (OUT16) {
+                    // a lane packs its feature of rows j and j + 1 and exchanges words with its neighbour: even lanes then hold row j of
+                    // features (l, l + 1), odd lanes row j + 1 of (l - 1, l): two rows of 64 bytes per store, no bank twice
+                    const uint32_t odd = lane & 1, pick = odd ? 0x3276u : 0x5410u, dst = box + odd * 64 + (lane >> 1) * 4;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const uint32_t w = pack_half2(v[2 * j], v[2 * j + 1], F16);
+                        const uint32_t got = __shfl_xor_sync(~0u, w, 1);
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + j * 128), "r"(__byte_perm(w, got, pick)) : "memory");
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < ROWS; ++j)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(box + lane * 4 + j * PITCH), "f"(v[half + j]) : "memory");
+                }
+                if (n >= half + ROWS) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) tma_store_3d(&maps.out, box, i0, static_cast<int>(row0) + half, 0);
+                } else {
+                    __syncwarp();
+                    constexpr int LANES = PITCH / 16, WIDE = OUT16 ? 8 : 4;       // lanes of a row, elements of a lane
+                    const int f = (lane % LANES) * WIDE;
+                    if (i0 + f < p.I) {                   // (the number of features is a multiple of 8)
+#pragma unroll 1
+                        for (int r = lane / LANES; r < n - half; r += 32 / LANES) {
+                            uint32_t x[4];
+                            ld_shared_v4(box + r * PITCH + (lane % LANES) * 16, x);
+                            const size_t o = base + (half + r) * p.ldc + f;
+                            uint4* dst = OUT16 ? reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.C) + o) : reinterpret_cast<uint4*>(static_cast<float*>(p.C) + o);
+                            *dst = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (lane == 0) bulk_commit();             // (an empty group where nothing was stored: the buffers take turns)
+            }
+        };
+        while (ok && next(u)) {
+            ring();
+            alpha = (p.scale_a ? __ldg(p.scale_a) : 1.0f) * (p.scale_b ? __ldg(p.scale_b + u.g) : 1.0f);
+            // the accumulators that make up the unit
+            const int blocks = u.kb1 - u.kb0, all = SUMS ? (blocks + p.chunk - 1) / p.chunk : 1;
+            float sum[4][32];                             // pieces set * 32 + 64 q
+#pragma unroll 1
+            for (int n = 0; n < all; ++n) {
+                if (!await()) { ok = false; break; }
+                const uint32_t taddr = tmem_base + (local & 1) * apart + lane_addr + set * 32;
+                auto take = [&](int q) {
+                    if (set * 32 + q * 64 >= u.cols) return;
+#pragma unroll
+                    for (int b = 0; b < 32; b += 16) {
+                        uint32_t v[16];
+                        tmem_ld_32x16(taddr + q * 64 + b, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[q][b + j] = SUMS && n > 0 ? sum[q][b + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+                    }
+                };
+                if (sharing && (local & 1) == 0) {        // the shared columns first: 160 .. 255 of the first accumulator,
+                    take(3);
+                    take(2);
+                    release();
+                    take(1);
+                    take(0);
+                } else {                                  // 0 .. 95 of the second
+                    take(0);
+                    take(1);
+                    if (sharing) release();
+                    take(2);
+                    take(3);
+                    if (!sharing) release();
+                }
+                ++local;
+            }
+            if (!ok) break;
+            const int mine = (u.cols - set * 32 + 63) >> 6;
+            unsigned int last = (1u << max(0, mine)) - 1u;    // the pieces this warp stores
+            if (u.parts > 1) {
+                // this part's pieces go to its slab; then one count for each of them says which have all their parts
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (q < mine) to_slab(sum[q], set * 32 + q * 64);
+                __syncwarp();
+                bool done = false;
+                if (lane < mine) {
+                    unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + set + 2 * lane;
+                    const unsigned int old = (atomic_add_acq_rel(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
+                    done = old == static_cast<unsigned>(u.parts) - 1u;
+                    if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
+                }
+                last = __ballot_sync(~0u, done);
+#pragma unroll 1
+                for (int q = 0; q < mine; ++q) {
+                    if (!((last >> q) & 1u)) continue;
+                    const int c = set * 32 + q * 64;
+                    float f[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[j] = 0.0f;
+#pragma unroll 2
+                    for (int s = 0; s < u.parts; ++s) {
+                        const float4* src = slab_of(s, c);
+                        float4 y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = __ldcg(src + j * 32);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[4 * j] += y[j].x, f[4 * j + 1] += y[j].y, f[4 * j + 2] += y[j].z, f[4 * j + 3] += y[j].w;
+                    }
+                    deliver(f, c);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (q < mine) deliver(sum[q], set * 32 + q * 64);
+            }
+        }
+        if (lane == 0) bulk_wait_read<0>();               // the stores are done with this CTA's shared memory
+        __syncwarp();
+    }
+
+    if (warp == 0) launch_wait();        // this launch ends after the one before it, whatever it read
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
+}  // namespace nk

@@ -1,0 +1,61 @@
+// What the host code and the kernel of the 4-bit products share: parameters and shared memory.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <cstddef>
+#include <cstdint>
+
+namespace nk {
+
+constexpr int MX_THREADS = 352;
+constexpr int MX_MAX_GROUPS = 1024;
+constexpr int MX_BK = 256;                              // of the contraction to a k-block: 128 bytes of a row
+constexpr int MX_A_BYTES = 128 * 128;                   // a stage: 16 KB of features, up to 16 KB of rows, then 2 KB of the features' scales
+constexpr int MX_S_BYTES = 2048;                        // and 2 KB for each 128 rows, per CTA
+constexpr int MX_TILE = 256;                            // features of a tile, and the most rows of one
+constexpr int MX_RING = 180 * 1024;                     // four stages of 256 rows, more where the tiles are narrower
+constexpr int MX_MAX_STAGES = 8;
+constexpr int MX_TABLE = 4 * (MX_MAX_GROUPS + 1);
+constexpr int MX_STAGING = 8 * 4096;                    // of the stores: two buffers of 2 KB for each epilogue warp
+constexpr int MX_SMEM = MX_RING + MX_STAGING + 1024 + 2 * MX_TABLE + 1024;
+static_assert(MX_SMEM <= 227 * 1024, "shared memory of an SM");
+__host__ __device__ constexpr int mx_stage_bytes(int width) { return MX_A_BYTES + 64 * width + MX_S_BYTES * (1 + (width + 127) / 128); }
+
+struct MxParams {
+    int groups, rows;      // rows: extent of the row arrays; offsets are clamped to it
+    int I;                 // features (contiguous in C)
+    int kb_total;          // k-blocks of the contraction
+    int steps;             // of 64, of the whole contraction
+    int tiles_i;           // ceil(I / 256)
+    int scale_tiles;       // of a weight along its features: ceil(I / 128)
+    int beta, relu;
+    int chunk;             // k-blocks summed in tensor memory before they are added to an FP32 sum
+    uint32_t idesc;        // without the N field
+    const int* offsets;    // [groups + 1]; null: one group of all rows
+    const float *scale_a, *scale_b, *bias;   // [1], [groups], [groups][I]; null: 1, 1, 0
+    void* C;
+    long long ldc;
+    float* partial;        // slabs of tiles cut along k, two per CTA pair; null: no tile is cut
+    int slab_cols;         // columns of a slab
+    unsigned int* counter; // arrivals, a byte per (cut tile, CTA of the pair, 32-column piece, warp); zero before and after
+    unsigned int* status;
+};
+
+struct MxMaps {
+    CUtensorMap a;         // the features' operand (bytes): boxes of 128 features x 256 of k
+    CUtensorMap b[8];      // the rows' operand in boxes of 16, 32, .. 128 rows
+    CUtensorMap sa, sb;    // scales: boxes of the tiles of one k-block
+    CUtensorMap out;       // C in boxes of 2 KB: 32 features x 32 (16-bit) or 16 (FP32) rows
+};
+
+enum MxOut { MX_OUT_F32 = 0, MX_OUT_BF16 = 1, MX_OUT_F16 = 2 };
+constexpr int MX_CHUNK = 8, MX_CHUNK_16 = 64;           // k-blocks between additions to the FP32 sums: of FP32 results, of 16-bit ones
+
+// tcgen05 instruction descriptor without N: block-scaled E2M1 operands, M = 256 over the pair, scales E8M0 or (nv) E4M3
+inline uint32_t mx_idesc(bool nv) { return 1u << 7 | 1u << 10 | (nv ? 0u : 1u << 23) | (256u >> 7) << 27; }
+
+typedef void (*MxFunction)(MxMaps, MxParams);
+MxFunction mx_kernel_nv(MxOut out, bool sums);         // (mx_nv.cu, mx_mx.cu)
+MxFunction mx_kernel_mx(MxOut out, bool sums);
+
+}  // namespace nk

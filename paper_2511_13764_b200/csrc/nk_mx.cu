@@ -1,0 +1,172 @@
+// Host side of nk_mx: descriptor validation, TMA maps, the launch.
+#include "rows_host.cuh"
+#include "../../include/nk_mx.h"
+#include "grouped_launch.cuh"
+#include "mx_format.cuh"
+#include "mx_launch.cuh"
+
+namespace nk {
+
+// bytes [outer][mid][inner] as boxes of `box_mid` rows of 128 bytes, swizzled; what lies outside arrives as zeros
+static bool encode_packed(CUtensorMap* m, const void* base, int64_t inner, int64_t mid, int64_t outer, int box_mid) {
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(mid), static_cast<cuuint64_t>(outer)};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(inner * mid)};
+    cuuint32_t box[3] = {128, static_cast<cuuint32_t>(box_mid), 1};
+    cuuint32_t es[3] = {1, 1, 1};
+    return encode_tiled()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// tiles of scales [rows][tiles][512 bytes] as boxes of `box` tiles of a row
+static bool encode_scales(CUtensorMap* m, const void* base, int64_t tiles, int64_t rows, int box_tiles) {
+    cuuint64_t dims[3] = {MX_TILE_BYTES / 4, static_cast<cuuint64_t>(tiles), static_cast<cuuint64_t>(rows)};
+    cuuint64_t strides[2] = {MX_TILE_BYTES, static_cast<cuuint64_t>(MX_TILE_BYTES * tiles)};
+    cuuint32_t box[3] = {MX_TILE_BYTES / 4, static_cast<cuuint32_t>(box_tiles), 1};
+    cuuint32_t es[3] = {1, 1, 1};
+    return encode_tiled()(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace nk
+
+struct nk_mx_s : nk::PlanBase {
+    nk_mx_desc_t d;               // strides filled in
+    int pairs;                    // CTA pairs that fit the device
+    nk::MxFunction kernel;
+    int chunk;
+    int split_slot;
+    unsigned int* counters;
+    nk::MxMaps maps;
+    int slab_cols;                // columns of a slab of partial sums
+    const void* cached[5];        // what the maps are of: A, its scales, B, its scales, C
+    char name[64];
+};
+
+using namespace nk;
+
+extern "C" {
+
+nk_status_t nk_mx_create(const nk_mx_desc_t* desc, nk_mx_t* out) {
+    if (out) *out = nullptr;
+    if (!desc || !out) return NK_ERR_INVALID_ARG;
+    nk_mx_desc_t d = *desc;
+    if (d.groups < 0 || d.rows < 0 || d.N <= 0 || d.K <= 0) return NK_ERR_INVALID_ARG;
+    if ((d.format != NK_MXF4 && d.format != NK_NVF4) || d.out_dtype < NK_F32 || d.out_dtype > NK_E5M2) return NK_ERR_INVALID_ARG;
+    if (d.out_dtype != NK_F32 && !is_half_type(d.out_dtype)) return NK_ERR_UNSUPPORTED;
+    if ((d.epilogue != NK_EPI_NONE && d.epilogue != NK_EPI_BIAS_RELU) || (d.beta != 0 && d.beta != 1)) return NK_ERR_INVALID_ARG;
+    if (d.groups > NK_GROUPED_MAX_GROUPS || d.N > (1 << 24) || d.K >= (1ll << 31) - 4096 || d.rows >= (1ll << 31) - 4096) return NK_ERR_UNSUPPORTED;
+    if (d.N % 8 || d.ldc % 8) return NK_ERR_MISALIGNED;
+    if (d.ldc == 0) d.ldc = d.N;
+    if (d.ldc < d.N) return NK_ERR_INVALID_ARG;
+    const int64_t groups = d.groups ? d.groups : 1;
+    // TMA strides are below 2^40 bytes; unit numbers stay below 2^24
+    if (d.ldc >= (1ll << 37) || d.N * mx_padded(d.K) >= (1ll << 40)) return NK_ERR_UNSUPPORTED;
+    if ((d.rows / 64 + groups) * div_up(d.N, MX_TILE) >= (1 << 24)) return NK_ERR_UNSUPPORTED;
+    int sms = 0;
+    nk_status_t s = usable_device(d.device, &sms);
+    if (s != NK_OK) return s;
+    nk_mx_s* p = new (std::nothrow) nk_mx_s();
+    if (!p) return NK_ERR_INVALID_ARG;
+    p->d = d;
+    p->split_slot = -1;
+    if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
+    DeviceGuard guard(d.device);
+    if (!encode_tiled()) { delete p; return NK_ERR_CUDA; }
+    const MxOut type = d.out_dtype == NK_F32 ? MX_OUT_F32 : d.out_dtype == NK_BF16 ? MX_OUT_BF16 : MX_OUT_F16;
+    p->chunk = type == MX_OUT_F32 ? MX_CHUNK : MX_CHUNK_16;
+    const bool sums = div_up(d.K, MX_BK) > p->chunk;
+    p->kernel = d.format == NK_NVF4 ? mx_kernel_nv(type, sums) : mx_kernel_mx(type, sums);
+    if (cudaFuncSetAttribute(p->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MX_SMEM) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
+    p->pairs = sms / 2;
+    p->slab_cols = static_cast<int>(d.rows >= MX_TILE ? MX_TILE : div_up(d.rows, 32) * 32);
+    p->split_slot = take_split_slot(d.device, p->pairs, &p->counters);
+    snprintf(p->name, sizeof(p->name), "mx_%s%s_256x256x256_pair%s", d.format == NK_NVF4 ? "nvf4" : "mxf4", d.groups ? "_grouped" : "", p->split_slot < 0 ? "_uncut" : "");
+    *out = p;
+    return NK_OK;
+}
+
+// partial sums of cut tiles: two FP32 slabs for each pair
+size_t nk_mx_workspace_bytes(nk_mx_t p) {
+    if (!p || p->split_slot < 0) return 0;
+    return grouped_partial_bytes(p->pairs, p->slab_cols);
+}
+
+nk_status_t nk_mx_run(nk_mx_t p, const void* A, const void* A_scales, const void* B, const void* B_scales, const float* scale_a,
+                      const float* scale_b, const float* bias, const int32_t* offsets, void* C, void* workspace, size_t workspace_bytes,
+                      void* cuda_stream) {
+    if (!p || (p->d.groups > 0) != (offsets != nullptr)) return NK_ERR_INVALID_ARG;
+    const nk_mx_desc_t& d = p->d;
+    if ((d.format != NK_NVF4 && (scale_a || scale_b)) || (d.epilogue == NK_EPI_NONE && bias)) return NK_ERR_INVALID_ARG;
+    if (d.rows == 0) return NK_OK;
+    if (!A || !A_scales || !B || !B_scales || !C) return NK_ERR_INVALID_ARG;
+    auto misaligned4 = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 3u) != 0; };
+    if (misaligned16(A) || misaligned16(A_scales) || misaligned16(B) || misaligned16(B_scales) || misaligned16(C) || misaligned16(workspace) ||
+        misaligned4(scale_a) || misaligned4(scale_b) || misaligned4(bias) || misaligned4(offsets))
+        return NK_ERR_MISALIGNED;
+    const size_t need = nk_mx_workspace_bytes(p);
+    if (need && (!workspace || workspace_bytes < need)) return NK_ERR_WORKSPACE;
+    DeviceGuard guard(d.device);
+    if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
+    const int64_t groups = d.groups ? d.groups : 1;
+    const bool nv = d.format == NK_NVF4;
+    const void* now[5] = {A, A_scales, B, B_scales, C};
+    if (memcmp(now, p->cached, sizeof(now)) != 0) {
+        const int64_t pitch = mx_padded(d.K) / 2, tiles = mx_tiles(d.K, nv), box = nv ? 4 : 2;
+        MxMaps& m = p->maps;
+        bool ok = encode_packed(&m.a, B, pitch, d.N, groups, 128) && encode_scales(&m.sa, B_scales, tiles, groups * div_up(d.N, MX_TILE_ROWS), box) &&
+                  encode_scales(&m.sb, A_scales, tiles, d.groups ? d.rows / MX_TILE_ROWS + groups : div_up(d.rows, MX_TILE_ROWS), box) &&
+                  encode_out(&m.out, C, d.out_dtype, d.N, d.rows, 1, d.ldc, 0);
+        for (int z = 0; ok && z < 8; ++z) ok = encode_packed(&m.b[z], A, pitch, d.rows, 1, 16 * (z + 1));
+        if (!ok) {
+            memset(p->cached, 0, sizeof(p->cached));
+            snprintf(p->cuda_err, sizeof(p->cuda_err), "cuTensorMapEncodeTiled failed");
+            return NK_ERR_CUDA;
+        }
+        memcpy(p->cached, now, sizeof(now));     // (none is null: the maps are valid)
+    }
+    MxParams g = {};
+    g.groups = static_cast<int>(groups);
+    g.rows = static_cast<int>(d.rows);
+    g.I = static_cast<int>(d.N);
+    g.kb_total = static_cast<int>(div_up(d.K, MX_BK));
+    g.steps = static_cast<int>(mx_padded(d.K) / 64);
+    g.tiles_i = static_cast<int>(div_up(d.N, MX_TILE));
+    g.scale_tiles = static_cast<int>(div_up(d.N, MX_TILE_ROWS));
+    g.beta = d.beta;
+    g.relu = d.epilogue == NK_EPI_BIAS_RELU;
+    g.chunk = p->chunk;
+    g.idesc = mx_idesc(nv);
+    g.offsets = offsets;
+    g.scale_a = scale_a;
+    g.scale_b = scale_b;
+    g.bias = bias;
+    g.C = C;
+    g.ldc = d.ldc;
+    g.partial = need ? static_cast<float*>(workspace) : nullptr;
+    g.slab_cols = p->slab_cols;
+    g.counter = p->counters;
+    g.status = p->status_dev;
+    base_runs(p, static_cast<cudaStream_t>(cuda_stream));
+    const cudaError_t e = launch_beside(p->kernel, 2 * p->pairs, MX_THREADS, MX_SMEM, static_cast<cudaStream_t>(cuda_stream), p->maps, g);
+    return e == cudaSuccess ? NK_OK : p->cuda("mx launch", e);
+}
+
+nk_status_t nk_mx_check(nk_mx_t p) {
+    if (!p) return NK_ERR_INVALID_ARG;
+    const nk_status_t s = base_check(p);
+    if (s == NK_ERR_TIMEOUT && p->counters) {
+        DeviceGuard guard(p->device);
+        cudaMemset(p->counters, 0, SPLIT_COUNTERS * sizeof(unsigned int));   // an abandoned tile may have left a count
+    }
+    return s;
+}
+
+const char* nk_mx_kernel_name(nk_mx_t p) { return p ? p->name : ""; }
+const char* nk_mx_last_cuda_error(nk_mx_t p) { return p ? p->cuda_err : ""; }
+
+nk_status_t nk_mx_destroy(nk_mx_t p) {
+    if (p) give_split_slot(p->device, p->split_slot, p->in_flight, p->captured);
+    delete p;
+    return NK_OK;
+}
+
+}  // extern "C"

@@ -554,6 +554,41 @@ __device__ __forceinline__ void umma_commit_if(uint32_t bar, uint32_t elected) {
                  "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(elected)
                  : "memory");
 }
+// 4-bit operands with block scales over both CTAs of a pair: 64 of k.  NV: scales E4M3 of blocks of 16 (four to a row), else E8M0 of
+// blocks of 32 (two).  The scales lie in tensor memory: lane r % 32, column r / 32 has those of row r, a byte each, the same in all
+// four quarters of the lanes; each CTA has those of its own 128 rows of A and of all columns of B.
+template <bool NV>
+__device__ __forceinline__ void umma_mx_pair_if(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                                uint32_t sa_tmem, uint32_t sb_tmem, uint32_t accumulate, uint32_t elected) {
+    if (NV) {
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "setp.ne.b32 q, %7, 0;\n\t"
+            "mov.b64 da, {%1, %2};\n\t"
+            "mov.b64 db, {%3, %4};\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], da, db, %5, [%8], [%9], p;\n\t}" ::"r"(d_tmem),
+            "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(elected), "r"(sa_tmem), "r"(sb_tmem)
+            : "memory");
+    } else {
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "setp.ne.b32 q, %7, 0;\n\t"
+            "mov.b64 da, {%1, %2};\n\t"
+            "mov.b64 db, {%3, %4};\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %5, [%8], [%9], p;\n\t}" ::"r"(d_tmem),
+            "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(elected), "r"(sa_tmem), "r"(sb_tmem)
+            : "memory");
+    }
+}
+// 512 bytes of shared memory of each CTA of the pair (32 rows of 16) into four columns of its tensor memory, into all quarters of the
+// lanes; done before an MMA issued later reads them.
+__device__ __forceinline__ void tmem_copy_scales_pair_if(uint32_t d_tmem, uint32_t lo, uint32_t hi, uint32_t elected) {
+    asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 d;\n\tsetp.ne.b32 q, %3, 0;\n\tmov.b64 d, {%1, %2};\n\t"
+                 "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], d;\n\t}" ::"r"(d_tmem), "r"(lo), "r"(hi), "r"(elected)
+                 : "memory");
+}
 // (An mbarrier signal to the CTAs of `cta_mask`, not a data load.)
 __device__ __forceinline__ void umma_commit_pair_if(uint32_t bar, uint16_t cta_mask, uint32_t elected) {
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"

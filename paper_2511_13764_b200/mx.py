@@ -34,7 +34,7 @@ def lib():
     if _lib is None:
         L = binding.lib()
         vp, sz = ctypes.c_void_p, ctypes.c_size_t
-        for family, desc, sizes in (("pack", PackDesc, ("data_bytes", "scales_bytes", "workspace_bytes")), ) + ((("mx", MxDesc, ("workspace_bytes",)),) if hasattr(L, "nk_mx_run") else ()):
+        for family, desc, sizes in (("pack", PackDesc, ("data_bytes", "scales_bytes", "workspace_bytes")), ("mx", MxDesc, ("workspace_bytes",))):
             create = getattr(L, f"nk_{family}_create")
             create.restype, create.argtypes = ctypes.c_int, [ctypes.POINTER(desc), ctypes.POINTER(vp)]
             for name, result in [(n, sz) for n in sizes] + [("check", ctypes.c_int), ("destroy", ctypes.c_int),
@@ -42,7 +42,7 @@ def lib():
                 f = getattr(L, f"nk_{family}_{name}")
                 f.restype, f.argtypes = result, [vp]
         for name, arguments in (("pack_scale", [vp] * 4 + [sz, vp]), ("pack_run", [vp] * 7), ("pack_values", [vp] * 7),
-                                ) + ((("mx_run", [vp] * 11 + [sz, vp]),) if hasattr(L,"nk_mx_run") else ()):
+                                ("mx_run", [vp] * 11 + [sz, vp])):
             f = getattr(L, f"nk_{name}")
             f.restype, f.argtypes = ctypes.c_int, arguments
         _lib = L
