@@ -5,17 +5,19 @@
 // tiles of the last, partial wave are cut along k.  What is different:
 //
 // A k-block is 256 elements (128 bytes of a row), four MMAs of 64.  Its scales arrive by TMA as the tiles of 128 rows x 4 blocks that
-// tensor memory wants and go there by tcgen05.cp, issued before the MMAs that use them, into one of two places in turn.  Each CTA has
-// the scales of its own 128 features and of all the tile's rows.
+// tensor memory wants and go there by tcgen05.cp, from a warp of its own that is some k-blocks ahead of the MMAs.  (Issued by the MMAs' warp the
+// copies, twelve to a k-block of NVF4, took a third of its time: 8192^3 264 us, from their own warp 230.)  Each CTA has the scales of
+// its own 128 features and of all the tile's rows.
 //
-// Tensor memory: two accumulators of 256 columns would leave no room for the scales (2 x 48 columns).  So for tiles of more than 128 rows the
-// second begins at column 160: they share 96 columns.  The epilogue takes the shared columns of an accumulator first, into
+// Tensor memory: two accumulators of 256 columns would leave no room for the scales.  So for tiles of more than 128 rows they share
+// columns (NVF4 144, MXF4 96).  The epilogue takes the shared columns of an accumulator first, into
 // registers, and gives them back; the next tile may begin then, while the rest is taken and stored.
 //
 // Tiles begin at multiples of 64 rows of a group (or at its first row): scales of 64 rows are two columns, by which the place of the
 // rows' scales moves where a tile begins in the middle of 128.
 //
-// Warps: 0 TMA producer, 1 MMA issuer, 2-9 epilogue (warps 2-5 take the even 32-column pieces, 6-9 the odd ones), 10 scheduler.
+// Warps: 0-7 epilogue (warps 0-3 take the even 32-column pieces, 4-7 the odd ones), 8 TMA producer, 9 MMA issuer, 10 copies the
+// scales, 11 scheduler.
 // All waits are bounded (see mbar_wait).
 #pragma once
 #include "grouped.cuh"
@@ -34,20 +36,28 @@ struct __align__(16) MxUnit {
     int cut, parts, part, first_pair;   // a cut tile: its number among the tail's tiles, its parts, this one, the pair of part 0
 };
 constexpr int MX_UNITS = 4;             // of them on the way
-constexpr int MX_SHARED = 160;          // first of the columns that both accumulators have
-constexpr int MX_SCALES = 416;          // columns of the scales: two places of 48, the features' 16 and the rows' 32
+// Tensor memory's columns.  A k-block's scales take a third of a place for the features and the rest for the rows; three places (NVF4) or four, so
+// that copies are as far ahead of the MMAs as the ring of stages.  (With two, 8192^3 NVF4 took 230 us.)
+__host__ __device__ constexpr int mx_places(bool nv) { return nv ? 3 : 4; }
+__host__ __device__ constexpr int mx_place(bool nv) { return nv ? 48 : 24; }
+__host__ __device__ constexpr int mx_scales(bool nv) { return 512 - mx_places(nv) * mx_place(nv); }    // first column of the scales
+__host__ __device__ constexpr int mx_shared(bool nv) { return mx_scales(nv) - MX_TILE; }               // first of the columns that both accumulators have
+
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
 
 template <bool NV, int OUT, bool SUMS>
 __global__ void __launch_bounds__(MX_THREADS, 1) __cluster_dims__(2, 1, 1)
 mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams p) {
     constexpr bool OUT16 = OUT != MX_OUT_F32, F16 = OUT == MX_OUT_F16;
     constexpr int S_BOX = NV ? 2048 : 1024;               // scales of 128 rows and a k-block
+    constexpr int PLACES = mx_places(NV), PLACE = mx_place(NV), SCALES = mx_scales(NV), SHARED = mx_shared(NV);
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
-    int* s_row = reinterpret_cast<int*>(gen_base + MX_RING + MX_STAGING);   // first row of each group, clamped and monotone
+    int* s_row = reinterpret_cast<int*>(gen_base + MX_RING);   // first row of each group, clamped and monotone
     int* s_pre = s_row + MX_MAX_GROUPS + 1;                                  // tiles before each group
-    const uint32_t bar_base = smem_base + MX_RING + MX_STAGING + 2 * MX_TABLE;
+    const uint32_t bar_base = smem_base + MX_RING + 2 * MX_TABLE;
     static_assert(2 * MX_TABLE % 8 == 0, "barriers are 8-byte aligned");
     constexpr int MS = MX_MAX_STAGES;
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
@@ -56,13 +66,14 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
     auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * MS + 2 + a); };
     auto ufull_bar = [&](int n) { return bar_base + 8u * (2 * MS + 4 + n); };    // a unit is there
     auto uempty_bar = [&](int n) { return bar_base + 8u * (2 * MS + 4 + MX_UNITS + n); };   // every role has read it
-    constexpr int NB = 2 * MS + 4 + 2 * MX_UNITS;
+    auto sready_bar = [&](int n) { return bar_base + 8u * (2 * MS + 4 + 2 * MX_UNITS + n); };   // scales are in place n
+    constexpr int NB = 2 * MS + 4 + 2 * MX_UNITS + PLACES;
     const uint32_t peer_ready_bar = bar_base + 8u * NB;
     uint8_t* after = gen_base + (bar_base - smem_base) + 8 * (NB + 1);
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(after);
     volatile uint32_t* abort_flag = tmem_slot + 1;
     volatile int* s_width = reinterpret_cast<volatile int*>(after + 8);      // rows of a tile at most
-    MxUnit* s_unit = reinterpret_cast<MxUnit*>(gen_base + ((MX_RING + MX_STAGING + 2 * MX_TABLE + 8 * (NB + 1) + 12 + 15) & ~15));
+    MxUnit* s_unit = reinterpret_cast<MxUnit*>(gen_base + ((MX_RING + 2 * MX_TABLE + 8 * (NB + 1) + 12 + 15) & ~15));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -78,22 +89,24 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         while (clock64() - t0 < (1ll << 20)) __nanosleep(1000);
     };
 
-    if (warp == 0) {
+    if (warp == 8) {
         for (int n = lane; n < NB; n += 32) {
-            // tempty: one arrival per epilogue warp of both CTAs; uempty: producer, epilogue warps, the leader's MMA issuer
-            const uint32_t count = n >= 2 * MS + 2 && n < 2 * MS + 4 ? 16 : n >= 2 * MS + 4 + MX_UNITS ? 9 + (rank == 0) : 1;
+            // tempty: one arrival per epilogue warp of both CTAs; uempty: producer, epilogue warps, the leader's warps 9 and 10
+            const uint32_t count = n >= 2 * MS + 2 && n < 2 * MS + 4                                      ? 16
+                                   : n >= 2 * MS + 4 + MX_UNITS && n < 2 * MS + 4 + 2 * MX_UNITS ? 9 + 2 * (rank == 0)
+                                                                                                         : 1;
             mbar_init(bar_base + 8u * n, count);
         }
         if (lane == 31) mbar_init(peer_ready_bar, 1);
         if (lane == 0) *abort_flag = 0;
         fence_mbar_init();
         __syncwarp();
-    } else if (warp == 2) {
+    } else if (warp == 0) {
         if (lane < 8) tma_prefetch_desc(&maps.b[lane]);
         if (lane == 8) tma_prefetch_desc(&maps.a);
         if (lane == 9) tma_prefetch_desc(&maps.sa);
         if (lane == 10) tma_prefetch_desc(&maps.sb);
-    } else if (warp == 1) {
+    } else if (warp == 9) {
         tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
         tmem_relinquish_pair();
     }
@@ -107,7 +120,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
     cluster_wait();          // the barriers of both CTAs are initialised
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
-    if (warp == 1 && rank == 1 && lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(peer_ready_bar, 0));
+    if (warp == 9 && rank == 1 && lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(peer_ready_bar, 0));
 
     // the roles' view of the schedule: wait for the next unit, read it, give its place back
     int unit_at = 0;
@@ -131,10 +144,57 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         stage_bytes = mx_stage_bytes(width);
         S = min(MS, MX_RING / stage_bytes);
         sharing = width > 128;
-        apart = sharing ? MX_SHARED : 128;
+        apart = sharing ? SHARED : 128;
     };
 
-    if (warp == MX_THREADS / 32 - 1) {
+    // Sums of accumulators take 128 registers of a thread: the warps without any leave theirs (208 x 256 + 80 x 128 <= 168 x 384).
+    if (SUMS && warp >= 8) fewer_registers();
+    if (warp == 10) {
+        // ------------------------------------------------ scales into tensor memory (leader only)
+        if (rank == 0) {
+            const uint64_t ds = make_smem_desc(smem_base, 16, 128, 0);
+            const uint32_t s_hi = static_cast<uint32_t>(ds >> 32), s_lo0 = static_cast<uint32_t>(ds);
+            const uint32_t elected = elect_one();
+            int stage = 0;
+            uint32_t phase = 0, place = 0;
+            int count = 0;
+            bool ok = mbar_wait(peer_ready_bar, 0u, abort_flag);
+            MxUnit u;
+            while (ok && next(u)) {
+                ring();
+                const uint32_t s_off = (MX_A_BYTES + *s_width * 64) >> 4;
+                const bool two = u.shift * 32 + u.jn > 128;
+                for (int kb = u.kb0; kb < u.kb1; ++kb) {
+                    // what the place held before was used PLACES k-blocks ago: those MMAs have to be done (a stage given back says so)
+                    const int old = stage >= PLACES ? stage - PLACES : stage - PLACES + S;
+                    const bool free = count < PLACES || mbar_wait(empty_bar(old), stage >= PLACES ? phase : phase ^ 1u, abort_flag);
+                    if (!free || !mbar_wait(full_bar(stage), phase, abort_flag)) {
+                        if (lane == 0) give_up(0x500u + stage);
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after_sync();
+                    count = min(count + 1, PLACES);
+                    const int steps = min(4, p.steps - 4 * kb);
+                    const uint32_t s_lo = s_lo0 + stage * (stage_bytes >> 4) + s_off;
+                    const uint32_t sa_t = tmem_base + SCALES + place * PLACE, sb_t = sa_t + PLACE / 3;
+                    // tiles of scales: four columns of the features' and four or eight of the rows', of one step (NV) or two
+#pragma unroll
+                    for (int s = 0; s < (NV ? 4 : 2); ++s) {
+                        if (s > 0 && (NV ? s : 2 * s) >= steps) break;
+                        tmem_copy_scales_pair_if(sa_t + 4 * s, s_lo + 32 * s, s_hi, elected);
+                        tmem_copy_scales_pair_if(sb_t + 8 * s, s_lo + (MX_S_BYTES >> 4) + 32 * s, s_hi, elected);
+                        if (two) tmem_copy_scales_pair_if(sb_t + 8 * s + 4, s_lo + (2 * MX_S_BYTES >> 4) + 32 * s, s_hi, elected);
+                    }
+                    umma_commit_pair_if(sready_bar(place), 1, elected);
+                    if (++place == PLACES) place = 0;
+                    __syncwarp();
+                    if (++stage == S) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (*abort_flag) settle();
+        }
+    } else if (warp == MX_THREADS / 32 - 1) {
         // ------------------------------------------------ scheduler (both CTAs of a pair come to the same schedule)
         // offsets that break their rule are clamped to the running maximum
         bool bad = false;
@@ -269,7 +329,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             __syncwarp();
             if (++unit_at == MX_UNITS) { unit_at = 0; unit_phase ^= 1u; }
         }
-    } else if (warp == 0) {
+    } else if (warp == 8) {
         // ------------------------------------------------ TMA producer (both CTAs)
         const uint32_t lead_full0 = map_to_cta(full_bar(0), 0);
         const uint32_t elected = elect_one();
@@ -309,18 +369,14 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             if (++stage == S) { stage = 0; phase ^= 1u; }
         }
         if (!ok) settle();
-    } else if (warp == 1) {
+    } else if (warp == 9) {
         // ------------------------------------------------ MMA issuer (leader only)
         if (rank == 0) {
-            const uint64_t da = make_smem_desc(smem_base, 16, 1024, 2), ds = make_smem_desc(smem_base, 16, 128, 0);
-            const uint32_t hi = static_cast<uint32_t>(da >> 32), s_hi = static_cast<uint32_t>(ds >> 32);
-            const uint32_t a_lo0 = static_cast<uint32_t>(da), s_lo0 = static_cast<uint32_t>(ds);
+            const uint64_t da = make_smem_desc(smem_base, 16, 1024, 2);
+            const uint32_t hi = static_cast<uint32_t>(da >> 32), a_lo0 = static_cast<uint32_t>(da);
             const uint32_t elected = elect_one();
             int stage = 0, local = 0;                     // local: accumulators filled so far
-            uint32_t phase = 0, place = 0;                // place: of the scales
-            // The tensor core's order holds for a copy and the MMAs behind it, not for MMAs and a copy behind them: what a place held before
-            // is two k-blocks back, whose MMAs are waited for (while those of the block before are at work)
-            uint32_t done[2] = {0u, 0u}, done_phase[2] = {0u, 0u};
+            uint32_t phase = 0, place = 0, place_phase = 0;   // place: of the scales
             bool ok = true;
             if (!mbar_wait(peer_ready_bar, 0u, abort_flag)) {
                 if (lane == 0) give_up(0x700u);
@@ -330,8 +386,6 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             while (ok && next(u)) {
                 ring();
                 const uint32_t idesc = p.idesc | (static_cast<uint32_t>(u.jn >> 3) << 17);
-                const uint32_t s_off = (MX_A_BYTES + *s_width * 64) >> 4;
-                const bool two = u.shift * 32 + u.jn > 128;
                 int in_chunk = 0;
                 uint32_t d_tmem = 0;
                 for (int kb = u.kb0; kb < u.kb1; ++kb) {
@@ -357,24 +411,14 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                     tc_fence_after_sync();
                     const int steps = min(4, p.steps - 4 * kb);
                     const uint32_t a_lo = a_lo0 + stage * (stage_bytes >> 4), b_lo = a_lo + (MX_A_BYTES >> 4);
-                    const uint32_t s_lo = s_lo0 + stage * (stage_bytes >> 4) + s_off;
-                    const uint32_t sa_t = tmem_base + MX_SCALES + place * 48, sb_t = sa_t + 16;
-                    if (done[place] && !mbar_wait(done[place], done_phase[place], abort_flag)) {
-                        if (lane == 0) give_up(0x500u + stage);
+                    const uint32_t sa_t = tmem_base + SCALES + place * PLACE, sb_t = sa_t + PLACE / 3;
+                    if (!mbar_wait(sready_bar(place), place_phase, abort_flag)) {
+                        if (lane == 0) give_up(0x600u + place);
                         ok = false;
                         break;
                     }
-                    done[place] = empty_bar(stage);
-                    done_phase[place] = phase;
-                    place ^= 1u;
-                    // tiles of scales: four columns of the features' and four or eight of the rows', of one step (NV) or two
-#pragma unroll
-                    for (int s = 0; s < (NV ? 4 : 2); ++s) {
-                        if (s > 0 && (NV ? s : 2 * s) >= steps) break;
-                        tmem_copy_scales_pair_if(sa_t + 4 * s, s_lo + 32 * s, s_hi, elected);
-                        tmem_copy_scales_pair_if(sb_t + 8 * s, s_lo + (MX_S_BYTES >> 4) + 32 * s, s_hi, elected);
-                        if (two) tmem_copy_scales_pair_if(sb_t + 8 * s + 4, s_lo + (2 * MX_S_BYTES >> 4) + 32 * s, s_hi, elected);
-                    }
+                    if (++place == PLACES) { place = 0; place_phase ^= 1u; }
+                    tc_fence_after_sync();
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
                         if (s > 0 && s >= steps) break;
@@ -398,11 +442,10 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         }
     } else {
         // ------------------------------------------------ epilogue (both CTAs, own 128 features)
-        const int set = warp >= 6 ? 1 : 0;
+        if (SUMS) more_registers();
+        const int set = warp >> 2;
         const int quarter = warp & 3;
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
-        const uint32_t staging = smem_base + MX_RING + (warp - 2) * 4096;
-        uint32_t parity = 0;
         int local = 0;
         bool ok = true;
         float alpha = 1.0f;
@@ -432,9 +475,9 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
 #pragma unroll
             for (int j = 0; j < 8; ++j) __stcg(dst + j * 32, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
         };
-        // One 32 x 32 piece of C (columns c .. c + 31 of the tile, this warp's 32 features): lane l has feature l, v[j] is row j.
-        // It goes through two 2 KB buffers of shared memory, from where a TMA store writes it (and clips what lies beyond C's
-        // edges); of a piece that ends inside the box, because the next row is another group's, lanes write 16 bytes each.
+        // One 32 x 32 piece of C (columns c .. c + 31 of the tile, this warp's 32 features): lane l has feature l, v[j] is row j.  A store
+        // writes 64 bytes of two rows, or 128 of one.  (By way of shared memory and TMA stores, which wait behind the loads of the ring,
+        // 8192 x 4096 x 1024 took 42 us.)
         auto deliver = [&](float (&v)[32], int c) {
             const int n = min(32, u.cols - c), i0 = u.i0 + static_cast<int>(rank) * 128 + quarter * 32;
             const size_t row0 = static_cast<size_t>(u.c0 + c);
@@ -457,50 +500,26 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = v[j] < 0.0f ? 0.0f : v[j];          // (a NaN stays)
             }
-            constexpr int ROWS = OUT16 ? 32 : 16, PITCH = 2048 / ROWS;    // of a buffer; 64 or 128 bytes
+            if (OUT16) {
+                // a lane packs its feature of rows j and j + 1 and exchanges words with its neighbour: even lanes then hold row j of
+                // features (l, l + 1), odd lanes row j + 1 of (l - 1, l)
+                const int odd = lane & 1;
+                const uint32_t pick = odd ? 0x3276u : 0x5410u;
+                uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.C) + base + odd * p.ldc + (lane & 30));
 #pragma unroll
-            for (int half = 0; half < 32; half += ROWS) {
-                if (half > 0 && half >= n) break;
-                const uint32_t box = staging + parity * 2048;
-                parity ^= 1u;
-                if (lane == 0) bulk_wait_read<1>();       // the store before the last has read this buffer
-                __syncwarp();
-                if (OUT16) {
-                    // a lane packs its feature of rows j and j + 1 and exchanges words with its neighbour: even lanes then hold row j of
-                    // features (l, l + 1), odd lanes row j + 1 of (l - 1, l): two rows of 64 bytes per store, no bank twice
-                    const uint32_t odd = lane & 1, pick = odd ? 0x3276u : 0x5410u, dst = box + odd * 64 + (lane >> 1) * 4;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const uint32_t w = pack_half2(v[2 * j], v[2 * j + 1], F16);
-                        const uint32_t got = __shfl_xor_sync(~0u, w, 1);
-                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + j * 128), "r"(__byte_perm(w, got, pick)) : "memory");
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < ROWS; ++j)
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(box + lane * 4 + j * PITCH), "f"(v[half + j]) : "memory");
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t w = pack_half2(v[2 * j], v[2 * j + 1], F16);
+                    const uint32_t got = __shfl_xor_sync(~0u, w, 1);
+                    if (live && 2 * j + odd < n) *dst = __byte_perm(w, got, pick);
+                    dst += p.ldc;                         // (two rows, in words)
                 }
-                if (n >= half + ROWS) {
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) tma_store_3d(&maps.out, box, i0, static_cast<int>(row0) + half, 0);
-                } else {
-                    __syncwarp();
-                    constexpr int LANES = PITCH / 16, WIDE = OUT16 ? 8 : 4;       // lanes of a row, elements of a lane
-                    const int f = (lane % LANES) * WIDE;
-                    if (i0 + f < p.I) {                   // (the number of features is a multiple of 8)
-#pragma unroll 1
-                        for (int r = lane / LANES; r < n - half; r += 32 / LANES) {
-                            uint32_t x[4];
-                            ld_shared_v4(box + r * PITCH + (lane % LANES) * 16, x);
-                            const size_t o = base + (half + r) * p.ldc + f;
-                            uint4* dst = OUT16 ? reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.C) + o) : reinterpret_cast<uint4*>(static_cast<float*>(p.C) + o);
-                            *dst = make_uint4(x[0], x[1], x[2], x[3]);
-                        }
-                    }
-                    __syncwarp();
+            } else {
+                float* dst = static_cast<float*>(p.C) + base + lane;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    if (live && j < n) *dst = v[j];
+                    dst += p.ldc;
                 }
-                if (lane == 0) bulk_commit();             // (an empty group where nothing was stored: the buffers take turns)
             }
         };
         while (ok && next(u)) {
@@ -508,88 +527,105 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             alpha = (p.scale_a ? __ldg(p.scale_a) : 1.0f) * (p.scale_b ? __ldg(p.scale_b + u.g) : 1.0f);
             // the accumulators that make up the unit
             const int blocks = u.kb1 - u.kb0, all = SUMS ? (blocks + p.chunk - 1) / p.chunk : 1;
-            float sum[4][32];                             // pieces set * 32 + 64 q
+            const int mine = (u.cols - set * 32 + 63) >> 6;   // pieces of this warp: columns set * 32 + 64 q
+            if (SUMS && all > 1) {
+                // Accumulators are added in registers; the last one's place takes the sum, so that there is one way from here to C.  (Code that
+                // runs once a launch costs its fetch: with a copy of that way for each piece of a sum this was 7 us slower.)
+                float sum[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[q][j] = 0.0f;
 #pragma unroll 1
-            for (int n = 0; n < all; ++n) {
-                if (!await()) { ok = false; break; }
-                const uint32_t taddr = tmem_base + (local & 1) * apart + lane_addr + set * 32;
-                auto take = [&](int q) {
-                    if (set * 32 + q * 64 >= u.cols) return;
+                for (int n = 0; n < all; ++n) {
+                    if (!await()) { ok = false; break; }
+                    const uint32_t taddr = tmem_base + (local & 1) * apart + lane_addr + set * 32;
 #pragma unroll
-                    for (int b = 0; b < 32; b += 16) {
-                        uint32_t v[16];
-                        tmem_ld_32x16(taddr + q * 64 + b, v);
-                        tmem_ld_wait();
+                    for (int q = 0; q < 4; ++q) {
+                        if (q >= mine) continue;
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[q][b + j] = SUMS && n > 0 ? sum[q][b + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+                        for (int b = 0; b < 32; b += 16) {
+                            uint32_t v[16];
+                            tmem_ld_32x16(taddr + q * 64 + b, v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) sum[q][b + j] += __uint_as_float(v[j]);
+                            if (n == all - 1) tmem_st_32x16(taddr + q * 64 + b, sum[q] + b);
+                        }
                     }
-                };
-                if (sharing && (local & 1) == 0) {        // the shared columns first: 160 .. 255 of the first accumulator,
-                    take(3);
-                    take(2);
-                    release();
-                    take(1);
-                    take(0);
-                } else {                                  // 0 .. 95 of the second
-                    take(0);
-                    take(1);
-                    if (sharing) release();
-                    take(2);
-                    take(3);
-                    if (!sharing) release();
+                    if (n < all - 1) {
+                        release();
+                        ++local;
+                    }
                 }
-                ++local;
+                if (!ok) break;
+                tmem_st_wait();
+            } else if (!await()) {
+                break;
             }
-            if (!ok) break;
-            const int mine = (u.cols - set * 32 + 63) >> 6;
-            unsigned int last = (1u << max(0, mine)) - 1u;    // the pieces this warp stores
-            if (u.parts > 1) {
-                // this part's pieces go to its slab; then one count for each of them says which have all their parts
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (q < mine) to_slab(sum[q], set * 32 + q * 64);
-                __syncwarp();
-                bool done = false;
-                if (lane < mine) {
-                    unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + set + 2 * lane;
-                    const unsigned int old = (atomic_add_acq_rel(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
-                    done = old == static_cast<unsigned>(u.parts) - 1u;
-                    if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
-                }
-                last = __ballot_sync(~0u, done);
+            // Pieces from tensor memory to C, the shared columns' first.  Of a cut tile they go to this part's slab; then one count for each of
+            // them says which have all their parts, and those are added up.
+            const uint32_t taddr = tmem_base + (local & 1) * apart + lane_addr + set * 32;
+            const bool down = sharing && (local & 1) == 0;
+            const int given = !sharing ? 3 : SHARED >= 128 ? 1 : 2;
+            unsigned int last = ~0u;
 #pragma unroll 1
-                for (int q = 0; q < mine; ++q) {
-                    if (!((last >> q) & 1u)) continue;
-                    const int c = set * 32 + q * 64;
+            for (int pass = u.parts > 1 ? 0 : 1; pass < 2; ++pass) {
+                const bool gather = pass == 1 && u.parts > 1;
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    const int q = down ? 3 - i : i, c = set * 32 + q * 64;
+                    const bool there = q < mine && ((last >> q) & 1u);
                     float f[32];
+                    if (!gather) {
+                        if (there) {
+                            uint32_t v[32];
+                            tmem_ld_32x32(taddr + q * 64, v);
+                            tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = 0.0f;
+                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                        }
+                        if (i == given) {
+                            release();
+                            ++local;
+                        }
+                    } else if (there) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[j] = 0.0f;
 #pragma unroll 2
-                    for (int s = 0; s < u.parts; ++s) {
-                        const float4* src = slab_of(s, c);
-                        float4 y[8];
+                        for (int s = 0; s < u.parts; ++s) {
+                            const float4* src = slab_of(s, c);
+                            float4 y[8];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) y[j] = __ldcg(src + j * 32);
+                            for (int j = 0; j < 8; ++j) y[j] = __ldcg(src + j * 32);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) f[4 * j] += y[j].x, f[4 * j + 1] += y[j].y, f[4 * j + 2] += y[j].z, f[4 * j + 3] += y[j].w;
+                            for (int j = 0; j < 8; ++j) f[4 * j] += y[j].x, f[4 * j + 1] += y[j].y, f[4 * j + 2] += y[j].z, f[4 * j + 3] += y[j].w;
+                        }
                     }
-                    deliver(f, c);
+                    if (!there) continue;
+                    if (pass == 0) to_slab(f, c);
+                    else deliver(f, c);
                 }
-            } else {
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (q < mine) deliver(sum[q], set * 32 + q * 64);
+                if (pass == 0) {
+                    __syncwarp();
+                    bool done = false;
+                    if (lane < mine) {
+                        unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + set + 2 * lane;
+                        const unsigned int old = (atomic_add_acq_rel(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
+                        done = old == static_cast<unsigned>(u.parts) - 1u;
+                        if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
+                    }
+                    last = __ballot_sync(~0u, done);
+                }
             }
         }
-        if (lane == 0) bulk_wait_read<0>();               // the stores are done with this CTA's shared memory
-        __syncwarp();
     }
 
-    if (warp == 0) launch_wait();        // this launch ends after the one before it, whatever it read
+    if (warp == 8) launch_wait();        // this launch ends after the one before it, whatever it read
     tc_fence_before_sync();
     __syncthreads();
     cluster_sync_all();
-    if (warp == 1) {
+    if (warp == 9) {
         tc_fence_after_sync();
         tmem_dealloc_pair(tmem_base, 512);
     }

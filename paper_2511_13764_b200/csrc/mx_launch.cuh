@@ -7,17 +7,16 @@
 
 namespace nk {
 
-constexpr int MX_THREADS = 352;
+constexpr int MX_THREADS = 384;
 constexpr int MX_MAX_GROUPS = 1024;
 constexpr int MX_BK = 256;                              // of the contraction to a k-block: 128 bytes of a row
 constexpr int MX_A_BYTES = 128 * 128;                   // a stage: 16 KB of features, up to 16 KB of rows, then 2 KB of the features' scales
 constexpr int MX_S_BYTES = 2048;                        // and 2 KB for each 128 rows, per CTA
 constexpr int MX_TILE = 256;                            // features of a tile, and the most rows of one
-constexpr int MX_RING = 180 * 1024;                     // four stages of 256 rows, more where the tiles are narrower
+constexpr int MX_RING = 190 * 1024;                     // five stages of 256 rows, more where the tiles are narrower
 constexpr int MX_MAX_STAGES = 8;
 constexpr int MX_TABLE = 4 * (MX_MAX_GROUPS + 1);
-constexpr int MX_STAGING = 8 * 4096;                    // of the stores: two buffers of 2 KB for each epilogue warp
-constexpr int MX_SMEM = MX_RING + MX_STAGING + 1024 + 2 * MX_TABLE + 1024;
+constexpr int MX_SMEM = MX_RING + 1024 + 2 * MX_TABLE + 1024;
 static_assert(MX_SMEM <= 227 * 1024, "shared memory of an SM");
 __host__ __device__ constexpr int mx_stage_bytes(int width) { return MX_A_BYTES + 64 * width + MX_S_BYTES * (1 + (width + 127) / 128); }
 
@@ -45,7 +44,6 @@ struct MxMaps {
     CUtensorMap a;         // the features' operand (bytes): boxes of 128 features x 256 of k
     CUtensorMap b[8];      // the rows' operand in boxes of 16, 32, .. 128 rows
     CUtensorMap sa, sb;    // scales: boxes of the tiles of one k-block
-    CUtensorMap out;       // C in boxes of 2 KB: 32 features x 32 (16-bit) or 16 (FP32) rows
 };
 
 enum MxOut { MX_OUT_F32 = 0, MX_OUT_BF16 = 1, MX_OUT_F16 = 2 };

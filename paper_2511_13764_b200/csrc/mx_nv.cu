@@ -4,7 +4,7 @@
 namespace nk {
 
 MxFunction mx_kernel_nv(MxOut out, bool sums) {
-    if (out == MX_OUT_F32) return mx_kernel<true, MX_OUT_F32, true>;
+    if (out == MX_OUT_F32) return sums ? mx_kernel<true, MX_OUT_F32, true> : mx_kernel<true, MX_OUT_F32, false>;
     if (out == MX_OUT_BF16) return sums ? mx_kernel<true, MX_OUT_BF16, true> : mx_kernel<true, MX_OUT_BF16, false>;
     return sums ? mx_kernel<true, MX_OUT_F16, true> : mx_kernel<true, MX_OUT_F16, false>;
 }

@@ -37,7 +37,7 @@ struct nk_mx_s : nk::PlanBase {
     unsigned int* counters;
     nk::MxMaps maps;
     int slab_cols;                // columns of a slab of partial sums
-    const void* cached[5];        // what the maps are of: A, its scales, B, its scales, C
+    const void* cached[4];        // what the maps are of: A, its scales, B, its scales
     char name[64];
 };
 
@@ -108,13 +108,12 @@ nk_status_t nk_mx_run(nk_mx_t p, const void* A, const void* A_scales, const void
     if (guard.err != cudaSuccess) return NK_ERR_DEVICE;
     const int64_t groups = d.groups ? d.groups : 1;
     const bool nv = d.format == NK_NVF4;
-    const void* now[5] = {A, A_scales, B, B_scales, C};
+    const void* now[4] = {A, A_scales, B, B_scales};
     if (memcmp(now, p->cached, sizeof(now)) != 0) {
         const int64_t pitch = mx_padded(d.K) / 2, tiles = mx_tiles(d.K, nv), box = nv ? 4 : 2;
         MxMaps& m = p->maps;
         bool ok = encode_packed(&m.a, B, pitch, d.N, groups, 128) && encode_scales(&m.sa, B_scales, tiles, groups * div_up(d.N, MX_TILE_ROWS), box) &&
-                  encode_scales(&m.sb, A_scales, tiles, d.groups ? d.rows / MX_TILE_ROWS + groups : div_up(d.rows, MX_TILE_ROWS), box) &&
-                  encode_out(&m.out, C, d.out_dtype, d.N, d.rows, 1, d.ldc, 0);
+                  encode_scales(&m.sb, A_scales, tiles, d.groups ? d.rows / MX_TILE_ROWS + groups : div_up(d.rows, MX_TILE_ROWS), box);
         for (int z = 0; ok && z < 8; ++z) ok = encode_packed(&m.b[z], A, pitch, d.rows, 1, 16 * (z + 1));
         if (!ok) {
             memset(p->cached, 0, sizeof(p->cached));
