@@ -227,11 +227,6 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             parts = 1;
             return whole;
         };
-        // rows of the tiles of a group: its rows cut evenly, in steps of 64
-        auto tile_rows = [&](int rows, int w) {
-            const int nt = (rows + w - 1) / w;
-            return nt <= 1 ? w : ((rows + nt - 1) / nt + 63) & ~63;
-        };
         int width = most <= 32 ? 32 : 64, parts = 1;
         if (most > 64) {
             // the width of least estimated time: lane l looks at 64 (l + 1)
@@ -278,6 +273,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         MxUnit u = {};
         for (u.some = 1; u.some;) {
             int tile = 0, at = 0;                         // `at`: the tile's k-block to begin with
+            // (tiles come in order: the group is found from the one before, 32 at a time)
             if (next_tile < tail_from) {
                 tile = next_tile;
                 next_tile += num_pairs;
@@ -289,16 +285,26 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                 u.some = 0;
             }
             if (u.some) {
-                u.g = find_last(s_pre, p.groups, tile);
+                for (;;) {
+                    const int g = u.g + lane;
+                    const unsigned before = __ballot_sync(~0u, g < p.groups && s_pre[g + 1] <= tile);
+                    u.g += __popc(before);
+                    if (before != ~0u) break;
+                }
                 const int rel = tile - s_pre[u.g], row0 = s_row[u.g], rows = rows_in(u.g);
-                const int jt = tile_rows(rows, width), nt = (rows + width - 1) / width;
-                // eight tiles of a group's rows sweep the features together
-                const int block = div_small(rel, 8 * p.tiles_i);
-                const int within = rel - block * 8 * p.tiles_i;
-                const int wide = min(8, nt - block * 8);
-                const int ti = div_small(within, wide), first = (block * 8 + within - ti * wide) * jt;
+                int ti = rel, first = 0;
+                u.cols = rows;
+                if (rows > width) {
+                    // eight tiles of a group's rows sweep the features together
+                    const int nt = (rows + width - 1) / width, jt = ((rows + nt - 1) / nt + 63) & ~63;    // cut evenly, in steps of 64
+                    const int block = div_small(rel, 8 * p.tiles_i);
+                    const int within = rel - block * 8 * p.tiles_i;
+                    const int wide = min(8, nt - block * 8);
+                    ti = div_small(within, wide);
+                    first = (block * 8 + within - ti * wide) * jt;
+                    u.cols = min(jt, rows - first);       // (at least 1: rows > width (nt - 1) >= jt (nt - 1))
+                }
                 u.c0 = row0 + first;
-                u.cols = min(jt, rows - first);           // (at least 1: rows > width (nt - 1) >= jt (nt - 1))
                 u.tile = mx_group_tile(row0, u.g) + (first >> 7);
                 u.shift = (first & 127) >> 5;
                 u.i0 = ti * MX_TILE;
@@ -508,6 +514,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                 uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.C) + base + odd * p.ldc + (lane & 30));
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
+                    if (j % 4 == 0 && 2 * j >= n) break;
                     const uint32_t w = pack_half2(v[2 * j], v[2 * j + 1], F16);
                     const uint32_t got = __shfl_xor_sync(~0u, w, 1);
                     if (live && 2 * j + odd < n) *dst = __byte_perm(w, got, pick);
@@ -517,6 +524,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                 float* dst = static_cast<float*>(p.C) + base + lane;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
+                    if (j % 8 == 0 && j >= n) break;
                     if (live && j < n) *dst = v[j];
                     dst += p.ldc;
                 }
