@@ -20,7 +20,7 @@
  * An element is the E2M1 number nearest to x / scale, ties to the one with an even last bit; beyond 6 it is 6.  Every such decision is
  * that of exact arithmetic where t has at most 8 significant bits (nk_pack_scale's has); with another t a quotient within 2^-16 of a
  * border may go either way (a block's scale never does).  A block with an infinity or a NaN has the scale NaN (0xFF, 0x7F), and so have all blocks
- * if t is not a positive finite number.
+ * if t is not between 2^-100 and 2^120.
  *
  * Packed arrays of a matrix of `outer` rows along the contraction of length L:
  *   data     [outer][Lp / 2] bytes, Lp = L rounded up to a multiple of 64; byte i holds element 2i in its low four bits, 2i + 1 above.

@@ -3,8 +3,7 @@
 //   P_e = 1/n sum_t p_te,  balance = E / (n k) sum_e c_e P_e,  size = 1/n sum_t lse_t^2,  lse_t = log sum_e exp z_te
 //   dz_te = p_te (g0 E / (n^2 k) (c_e - sum_j c_j p_tj) + g1 2/n lse_t)
 // A warp has a token, a lane the experts l, l + 32, ..., and adds up the probabilities of its tokens in registers: one pass
-// over the logits each way.  Sums of at most 64 tokens and then of a block's warps are FP32, those over blocks 64 bits; every
-// sum has one order (counts are integers, added in any).
+// over the logits each way.  Sums of at most 64 tokens, of a block's warps and of the experts are FP32, those over blocks 64 bits; every sum has one order (counts are integers, added in any).
 // Bound by instruction issue and a launch's start and end: see the figures in the design notes' table of the cases.
 #pragma once
 #include "route.cuh"
@@ -153,51 +152,85 @@ __global__ void __launch_bounds__(route_threads(V)) balance_kernel(const RoutePa
     }
 }
 
-// One block: the blocks' sums into the results.
-__global__ void __launch_bounds__(1024) balance_total_kernel(const RouteParams p, const BalanceParams b) {
-    __shared__ double part[1024], total[NK_ROUTE_MAX_EXPERTS], line[32], size;
-    __shared__ int count[NK_ROUTE_MAX_EXPERTS], tokens;
-    const int E = p.experts, lanes = min(E, 1024), sets = 1024 / lanes, set = threadIdx.x / lanes, e = threadIdx.x - set * lanes;
+// The blocks' sums into the results: a cluster of eight, each an eighth of the experts, 2^narrow of them to a row of a warp's lanes.  (Short code: it
+// runs once, and what it costs is mostly its fetch.  By one block, or with 64-bit divisions, 5 to 7 us.)
+constexpr int BALANCE_CLUSTER = 8, BALANCE_TOTAL = 512;
+__global__ void __launch_bounds__(BALANCE_TOTAL) __cluster_dims__(BALANCE_CLUSTER, 1, 1)
+balance_total_kernel(const RouteParams p, const BalanceParams b, int narrow) {
+    constexpr int WARPS = BALANCE_TOTAL / 32;
+    __shared__ double part[WARPS][32];
+    __shared__ int count[WARPS][32];
+    __shared__ __align__(16) float4 losses[BALANCE_CLUSTER];               // of the first block: everyone's part
+    const int E = p.experts, rank = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int each = (E + BALANCE_CLUSTER - 1) / BALANCE_CLUSTER, first = rank * each, last = min(E, first + each);
+    const int at = lane & ((1 << narrow) - 1), row = (warp << (5 - narrow)) + (lane >> narrow), rows = WARPS << (5 - narrow);
     const size_t pitch = 2 * E + 2;
-    for (int i = threadIdx.x; i < E; i += 1024) count[i] = 0;
-    if (threadIdx.x == 0) tokens = 0;
     launch_wait();
     launch_next();
-    __syncthreads();
-    if (set < sets) {
+    // tokens and the sum over them, in every warp 0
+    double size = 0.0;
+    int n = 0;
+    if (warp == 0) {
+#pragma unroll 4
+        for (int i = lane; i < b.blocks; i += 32) {
+            const float* x = b.partial + i * pitch + 2 * E;
+            size += x[0];
+            n += __float_as_int(x[1]);
+        }
+        n = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(n)));
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) size += __shfl_xor_sync(~0u, size, d);
+    }
+    const float tokens = static_cast<float>(n);
+    float loss = 0.0f;
+    for (int e0 = first; e0 < last; e0 += 1 << narrow) {
+        const int e = e0 + at;
         double s = 0.0;
         int c = 0;
+        if (e < last) {
 #pragma unroll 4
-        for (int i = set; i < b.blocks; i += sets) {
-            s += b.partial[i * pitch + e];
-            c += __float_as_int(b.partial[i * pitch + E + e]);
+            for (int i = row; i < b.blocks; i += rows) {
+                const float* x = b.partial + i * pitch + e;
+                s += x[0];
+                c += __float_as_int(x[E]);
+            }
         }
-        part[threadIdx.x] = s;
-        atomicAdd(count + e, c);
-    }
-    // the last warp: the sums over rows
-    if (threadIdx.x >= 992) {
-        double s = 0.0;
-        int m = 0;
-        for (int i = threadIdx.x - 992; i < b.blocks; i += 32) {
-            s += b.partial[i * pitch + 2 * E];
-            m += __float_as_int(b.partial[i * pitch + 2 * E + 1]);
-        }
+        __syncthreads();
+        part[warp][lane] = s;
+        count[warp][lane] = c;
+        __syncthreads();
+        if (warp == 0) {
+            s = 0.0;
+            c = 0;
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            s += __shfl_xor_sync(~0u, s, d);
-            m += __shfl_xor_sync(~0u, m, d);
+            for (int w = 0; w < WARPS; ++w) {
+                s += part[w][lane];
+                c += count[w][lane];
+            }
+            for (int d = 16; d >= 1 << narrow; d >>= 1) {
+                s += __shfl_xor_sync(~0u, s, d);
+                c += __shfl_xor_sync(~0u, c, d);
+            }
+            if (e < last && lane >> narrow == 0) {
+                const float mean = n ? static_cast<float>(s) / tokens : 0.0f;
+                b.share[e] = mean;
+                b.counts[e] = c;
+                loss += mean * static_cast<float>(c);
+            }
         }
-        if (threadIdx.x == 992) { size = s; tokens = m; }
     }
-    __syncthreads();
-    if (threadIdx.x < E) {
-        double s = 0.0;
-        for (int i = 0; i < sets; ++i) s += part[i * lanes + threadIdx.x];
-        total[threadIdx.x] = s;
+    if (warp == 0) {
+        loss = warp_sum(loss);
+        if (lane == 0) st_cluster_v4(map_to_cta(smem_u32(losses + rank), 0), __float_as_uint(loss), 0u, 0u, 0u);
     }
-    __syncthreads();
-    balance_finish(p, b, total, count, size, tokens, line);
+    cluster_sync_all();
+    if (rank == 0 && threadIdx.x == 0) {
+        loss = 0.0f;
+        for (int r = 0; r < BALANCE_CLUSTER; ++r) loss += losses[r].x;
+        b.losses[0] = n ? loss / tokens * (static_cast<float>(E) / static_cast<float>(p.topk)) : 0.0f;
+        b.losses[1] = n ? static_cast<float>(size) / tokens : 0.0f;
+        b.counts[E] = n;
+    }
 }
 
 // One warp per token.  The counts are taken from their mean, which changes nothing (the probabilities of a row add up to 1)

@@ -27,8 +27,40 @@ __device__ __forceinline__ float e4m3_to_f32(uint32_t b) {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(b)));
     return half_bits_to_f32(r & 0xFFFFu, 1);
 }
+// two FP32 operations in one instruction
+__device__ __forceinline__ unsigned long long pair_bits(float2 x) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x.x), "f"(x.y));
+    return r;
+}
+__device__ __forceinline__ float2 pair_of(unsigned long long r) {
+    float2 x;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x.x), "=f"(x.y) : "l"(r));
+    return x;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(r);
+}
+// 1 / x to within one of its last places (x neither subnormal nor beyond 2^126)
+__device__ __forceinline__ float rcp_approx(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 // eight numbers to E2M1 (nearest even, at most 6 in size), the first in the lowest four bits
-__device__ __forceinline__ uint32_t f32_to_e2m1x8(const float (&x)[8]) {
+__device__ __forceinline__ uint32_t f32_to_e2m1x8(const float2 (&x)[4]) {
     uint32_t r;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
@@ -37,7 +69,7 @@ __device__ __forceinline__ uint32_t f32_to_e2m1x8(const float (&x)[8]) {
         "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
         "mov.b32 %0, {a, b, c, d};\n\t}"
         : "=r"(r)
-        : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+        : "f"(x[0].x), "f"(x[0].y), "f"(x[1].x), "f"(x[1].y), "f"(x[2].x), "f"(x[2].y), "f"(x[3].x), "f"(x[3].y));
     return r;
 }
 __device__ __forceinline__ void e2m1x8_to_f32(uint32_t w, float (&x)[8]) {

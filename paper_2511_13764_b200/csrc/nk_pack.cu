@@ -38,6 +38,7 @@ static PackParams pack_params(const nk_pack_s* p) {
     r.groups = static_cast<int>(p->d.groups);
     r.length = p->length;
     r.row_tiles = p->row_tiles;
+    r.chunks = static_cast<int>(div_up(mx_padded(p->length), PACK_CHUNK));
     r.tiles = p->tiles;
     r.ldx = p->d.ldx;
     r.stride_x = p->d.stride_x;
@@ -69,7 +70,9 @@ nk_status_t nk_pack_create(const nk_pack_desc_t* desc, nk_pack_t* out) {
     if (d.stride_x == 0) d.stride_x = d.rows * d.ldx;
     if (d.batch > 1 && d.stride_x < (d.rows ? (d.rows - 1) * d.ldx + d.K : 0)) return NK_ERR_INVALID_ARG;   // matrices overlap
     const int64_t outer = d.transposed ? d.K : d.rows, length = d.transposed ? d.rows : d.K;
-    if (div_up(mx_padded(length), d.transposed ? PACK_TURN : PACK_CHUNK) > 65535) return NK_ERR_UNSUPPORTED;
+    // grids: along the rows (and reading back) tiles x pieces, below 2^31; along the columns pieces in y
+    if (d.transposed && div_up(mx_padded(length), PACK_TURN) > 65535) return NK_ERR_UNSUPPORTED;
+    if ((outer / MX_TILE_ROWS + (d.groups ? d.groups : 1)) * div_up(mx_padded(length), PACK_CHUNK) >= (1ll << 31)) return NK_ERR_UNSUPPORTED;
     int sms = 0;
     nk_status_t s = usable_device(d.device, &sms);
     if (s != NK_OK) return s;
@@ -81,9 +84,10 @@ nk_status_t nk_pack_create(const nk_pack_desc_t* desc, nk_pack_t* out) {
     p->length = static_cast<int>(length);
     p->row_tiles = static_cast<int>(d.groups ? outer / MX_TILE_ROWS + d.groups : div_up(outer, MX_TILE_ROWS));
     p->tiles = static_cast<int>(mx_tiles(length, d.format == NK_NVF4));
-    // the tensor's scale: a turn of a block is 32 elements to a thread; blocks for all SMs over the whole batch
-    const int64_t turns = div_up(d.rows * d.K, PACK_THREADS * 32), most = div_up(4 * static_cast<int64_t>(sms), d.batch);
-    p->max_blocks = static_cast<int>(turns <= 2 ? 1 : turns < most ? turns : most);
+    // the tensor's scale: up to half a million elements are one cluster's (a second launch costs more: 16 x 4096 2.9 us instead of 3.7); else
+    // blocks of 256, a turn of 64 elements to a thread (FP32: 32) each at least, four to an SM over the whole batch
+    const int64_t turns = div_up(d.rows * d.K, PACK_THREADS * (d.in_dtype == NK_F32 ? 32 : 64)), most = div_up(4 * static_cast<int64_t>(sms), d.batch);
+    p->max_blocks = static_cast<int>(d.rows * d.K <= (1 << 19) ? 1 : turns < most ? turns : most);
     DeviceGuard guard(d.device);
     if (d.transposed && cudaFuncSetAttribute(pack_kernel_of(d), cudaFuncAttributeMaxDynamicSharedMemorySize, pack_columns_smem(d.in_dtype == NK_F32 ? 0 : 1)) != cudaSuccess) {
         delete p;
@@ -117,8 +121,14 @@ nk_status_t nk_pack_scale(nk_pack_t p, const void* X, float* scale, void* worksp
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const dim3 grid(p->max_blocks, static_cast<unsigned>(p->d.batch));
     uint32_t* partial = static_cast<uint32_t*>(workspace);
-    cudaError_t e = launch_beside(p->d.in_dtype == NK_F32 ? tensor_max_kernel<0> : p->d.in_dtype == NK_BF16 ? tensor_max_kernel<1> : tensor_max_kernel<2>, grid,
-                                  PACK_THREADS, 0, st, r, static_cast<int>(p->d.rows), static_cast<int>(p->d.K), partial, scale);
+    const int rows = static_cast<int>(p->d.rows), width = static_cast<int>(p->d.K);
+    cudaError_t e;
+    if (p->max_blocks == 1)
+        e = launch_beside(p->d.in_dtype == NK_F32 ? tensor_cluster_kernel<0> : p->d.in_dtype == NK_BF16 ? tensor_cluster_kernel<1> : tensor_cluster_kernel<2>,
+                          dim3(SCALE_CLUSTER, static_cast<unsigned>(p->d.batch)), SCALE_THREADS, 0, st, r, rows, width, scale);
+    else
+        e = launch_beside(p->d.in_dtype == NK_F32 ? tensor_max_kernel<0> : p->d.in_dtype == NK_BF16 ? tensor_max_kernel<1> : tensor_max_kernel<2>, grid,
+                          PACK_THREADS, 0, st, r, rows, width, partial);
     if (e != cudaSuccess) return p->cuda("tensor max launch", e);
     if (p->max_blocks > 1 && (e = launch_beside(tensor_scale_kernel, static_cast<unsigned>(p->d.batch), PACK_THREADS, 0, st, partial, p->max_blocks, scale)) != cudaSuccess)
         return p->cuda("tensor scale launch", e);
@@ -140,7 +150,8 @@ nk_status_t nk_pack_run(nk_pack_t p, const void* X, const float* scale, const in
     r.offsets = offsets;
     r.data = static_cast<uint8_t*>(data);
     r.scales = static_cast<uint8_t*>(scales);
-    const dim3 grid(p->row_tiles, static_cast<unsigned>(div_up(mx_padded(p->length), p->d.transposed ? PACK_TURN : PACK_CHUNK)), static_cast<unsigned>(p->d.batch));
+    const dim3 grid = p->d.transposed ? dim3(p->row_tiles, static_cast<unsigned>(div_up(mx_padded(p->length), PACK_TURN)), static_cast<unsigned>(p->d.batch))
+                                      : dim3(static_cast<unsigned>(p->row_tiles) * r.chunks, 1, static_cast<unsigned>(p->d.batch));
     const cudaError_t e = launch_beside(pack_kernel_of(p->d), grid, PACK_THREADS, p->d.transposed ? pack_columns_smem(p->d.in_dtype == NK_F32 ? 0 : 1) : 0,
                                         static_cast<cudaStream_t>(cuda_stream), r);
     return e == cudaSuccess ? NK_OK : p->cuda("pack launch", e);
@@ -161,7 +172,7 @@ nk_status_t nk_pack_values(nk_pack_t p, const void* data, const void* scales, co
     r.data = static_cast<uint8_t*>(const_cast<void*>(data));
     r.scales = static_cast<uint8_t*>(const_cast<void*>(scales));
     r.values = Y;
-    const dim3 grid(p->row_tiles, static_cast<unsigned>(div_up(p->length, PACK_CHUNK)), static_cast<unsigned>(p->d.batch));
+    const dim3 grid(static_cast<unsigned>(p->row_tiles) * r.chunks, 1, static_cast<unsigned>(p->d.batch));
     const cudaError_t e = launch_beside(values_kernel_of(p->d), grid, PACK_THREADS, 0, static_cast<cudaStream_t>(cuda_stream), r);
     return e == cudaSuccess ? NK_OK : p->cuda("values launch", e);
 }

@@ -122,10 +122,11 @@ nk_status_t nk_route_create(const nk_route_desc_t* desc, nk_route_t* out) {
     if ((s = base_init(p, d.device, sms)) != NK_OK) { delete p; return s; }
     p->per_block = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? ROUTE_ONE_BLOCK : div_up(d.tokens, sms) < 32 ? 32 : div_up(d.tokens, sms));
     p->blocks = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? 1 : div_up(d.tokens, p->per_block));
-    // a block for each SM, but two tokens to a warp at least and BALANCE_RUN at most
-    const int warps = route_threads(route_width(d.experts)) / 32;
-    const int64_t even = div_up(d.tokens, sms);
-    p->balance_per_block = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? ROUTE_ONE_BLOCK : even < 2 * warps ? 2 * warps : even > BALANCE_RUN * warps ? BALANCE_RUN * warps : even);
+    // as many blocks as fit the device at once (of 1024 threads two to an SM; a lane of 8 experts or more has the registers of one), but a token to
+    // a warp at least and BALANCE_RUN at most
+    const int v_lane = route_width(d.experts), warps = route_threads(v_lane) / 32;
+    const int64_t even = div_up(d.tokens, (v_lane <= 4 ? 2 : 1) * static_cast<int64_t>(sms));
+    p->balance_per_block = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? ROUTE_ONE_BLOCK : even < warps ? warps : even > BALANCE_RUN * warps ? BALANCE_RUN * warps : even);
     p->balance_blocks = static_cast<int>(d.tokens <= ROUTE_ONE_BLOCK ? 1 : div_up(d.tokens, p->balance_per_block));
     DeviceGuard guard(d.device);
     const int v = route_width(d.experts);
@@ -223,7 +224,9 @@ nk_status_t nk_route_balance(nk_route_t p, const void* logits, const int32_t* ex
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = launch_beside(b.blocks == 1 ? balance_forward<true>(v) : balance_forward<false>(v), b.blocks, route_threads(v), balance_smem(v), st, r, b);
     if (e != cudaSuccess) return p->cuda("balance launch", e);
-    if (b.blocks > 1 && (e = launch_beside(balance_total_kernel, 1, 1024, 0, st, r, b)) != cudaSuccess) return p->cuda("balance total launch", e);
+    int narrow = 0;
+    while (narrow < 5 && (BALANCE_CLUSTER << narrow) < r.experts) ++narrow;
+    if (b.blocks > 1 && (e = launch_beside(balance_total_kernel, BALANCE_CLUSTER, BALANCE_TOTAL, 0, st, r, b, narrow)) != cudaSuccess) return p->cuda("balance total launch", e);
     return NK_OK;
 }
 

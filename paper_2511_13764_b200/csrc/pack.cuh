@@ -2,13 +2,13 @@
 //   MXF4   scale 2^(floor(log2 m) - 2): bits of m's exponent; x / scale is exact
 //   NVF4   scale s = RN_e4m3(m / (6 t)), element RN_e2m1(x / (s t))
 // The element's decision has to be that of exact arithmetic.  With t of 8 significant bits d = s t has 12 and is exact, a border b of
-// the elements (0.25 .. 5) times d has 15, so for x of a 16-bit type x / d is either b or at least 2^-14 away from it.  x times the
-// FP32 reciprocal of d is within 2^-20 of the quotient; rounded to a multiple of 2^-16 (one FMA onto 192 and a subtraction) it is b
+// the elements (0.25 .. 5) times d has 15, so for x of a 16-bit type x / d is either b or at least 2^-14 away from it.  x times a
+// reciprocal of d that is off by 3 of its last places is within 2^-18 of the quotient (which is below 9 where it matters); rounded to a multiple of 2^-16 (one FMA onto 192 and a subtraction) it is b
 // exactly where the quotient is, and on the quotient's side of b elsewhere.  So there is no division for an element.  FP32 x take one: a
 // correctly rounded x / d is b only where the quotient is (24 bits against 15: the next quotient is more than half a step away).
 //
-// A block of threads has a tile of scales' 128 rows, so that the scales of 256 of the contraction leave as 2 KB in one piece; a warp reads
-// 256 consecutive elements of a row (8 to a lane), and a block's maximum is one or two shuffles.  Along the columns a tile of 128 x
+// A block of threads has a tile of scales' 128 rows, so that the scales of 256 of the contraction leave as 2 KB in one piece; a thread has
+// a block of the format.  Along the columns a tile of 128 x
 // 128 goes through shared memory, where a thread has a word of adjacent features.  Bound by memory.
 #pragma once
 #include "mx_format.cuh"
@@ -25,6 +25,7 @@ struct PackParams {
     int outer;                 // rows of the packed matrix (of one of the batch)
     int groups;                // 0: none
     int length;                // of the contraction
+    int chunks;                // of PACK_CHUNK along the contraction (not along the columns)
     int row_tiles, tiles;      // tiles of scales: along the rows of a matrix (groups: of all), along the contraction
     long long ldx, stride_x;   // in elements
     const void* x;
@@ -42,35 +43,37 @@ template <int T> __device__ __forceinline__ constexpr uint32_t pack_not_finite()
 template <int T> __device__ __forceinline__ float pack_widen(uint32_t bits) { return T == 0 ? __uint_as_float(bits) : half_bits_to_f32(bits, T == 2); }
 
 struct PackScale {
-    float t, six_t;            // NVF4
+    float t, per_t, per_six_t; // NVF4: the tensor's scale, 1 / t, 1 / (6 t)
     bool bad;
 };
 __device__ __forceinline__ PackScale pack_scale(const PackParams& p, int item) {
-    PackScale s = {1.0f, 6.0f, false};
+    PackScale s = {1.0f, 1.0f, 1.0f / 6.0f, false};
     if (p.nv && p.scale) {
         s.t = p.scale[item];
-        s.six_t = 6.0f * s.t;
-        s.bad = !(s.t > 0.0f && s.t < INFINITY);
+        s.bad = !(s.t >= 0x1p-100f && s.t <= 0x1p120f);
+        s.per_t = __frcp_rn(s.t);
+        s.per_six_t = __frcp_rn(6.0f * s.t);
     }
     return s;
 }
 
-// m / (6 t) to E4M3.  The FP32 quotient is off by 2 of its last places (6 t is rounded, too), so one that close to the border of two
-// scales is decided by the border itself: border x 6 t is exact in 64 bits (5 + 2 + 24).
-__device__ __forceinline__ uint32_t pack_e4m3(float m, const PackScale& s) {
-    float q = __fdiv_rn(m, s.six_t);
-    const uint32_t bits = __float_as_uint(q) + 4u;
+// m / (6 t) to E4M3.  m times the reciprocal is off by 2 of its last places, so one that close to the border of two scales is decided by the
+// border itself: border x 6 t is exact in 64 bits (5 + 2 + 24).
+__device__ __noinline__ float pack_at_border(float q, float m, float t) {
     float border = 0.0f;
     if (q >= 0x1p-6f) {
-        if (((bits - 0x80000u) & 0xFFFFFu) <= 8u) border = __uint_as_float(bits & ~0x7FFFFu);     // halfway between steps of 1/8
+        border = __uint_as_float((__float_as_uint(q) + 8u) & ~0x7FFFFu);        // halfway between steps of 1/8
     } else {
-        const float n = rintf(q * 1024.0f);                                // subnormals: odd multiples of 2^-10
-        if ((static_cast<int>(n) & 1) && fabsf(q * 1024.0f - n) <= n * 0x1p-21f) border = n * 0x1p-10f;
+        const float n = rintf(q * 1024.0f);                                   // subnormals: odd multiples of 2^-10
+        if ((static_cast<int>(n) & 1) && fabsf(q * 1024.0f - n) <= n * 0x1p-20f) border = n * 0x1p-10f;
     }
-    if (border > 0.0f) {
-        const double at = static_cast<double>(border) * 6.0 * static_cast<double>(s.t), x = m;
-        q = x > at ? __uint_as_float(__float_as_uint(border) + 1u) : x < at ? __uint_as_float(__float_as_uint(border) - 1u) : border;
-    }
+    if (border == 0.0f) return q;
+    const double at = static_cast<double>(border) * 6.0 * static_cast<double>(t), x = m;
+    return x > at ? __uint_as_float(__float_as_uint(border) + 1u) : x < at ? __uint_as_float(__float_as_uint(border) - 1u) : border;
+}
+__device__ __forceinline__ uint32_t pack_e4m3(float m, const PackScale& s) {
+    float q = m * s.per_six_t;
+    if (((__float_as_uint(q) + 8u - 0x80000u) & 0xFFFFFu) <= 16u || q < 0x1p-6f) q = pack_at_border(q, m, s.t);
     return f32_to_e4m3(q);
 }
 
@@ -86,15 +89,22 @@ __device__ __forceinline__ uint32_t pack_block(uint32_t most, const PackScale& s
         return byte;
     }
     const uint32_t byte = pack_e4m3(m, s);
-    const float d = e4m3_to_f32(byte) * s.t;
-    factor = T == 0 ? d : d > 0.0f ? __frcp_rn(d) : 0.0f;
+    const float b = e4m3_to_f32(byte);
+    factor = T == 0 ? b * s.t : b > 0.0f ? rcp_approx(b) * s.per_t : 0.0f;
     return byte;
 }
+// Quotients of two elements, each by its own factor: FP32 ...
+template <bool NV>
+__device__ __forceinline__ float2 pack_quotients(float2 x, float2 factor) {
+    if (!NV) return mul2(x, factor);
+    return make_float2(factor.x > 0.0f ? __fdiv_rn(x.x, factor.x) : 0.0f, factor.y > 0.0f ? __fdiv_rn(x.y, factor.y) : 0.0f);
+}
+// ... and of a word of 16-bit elements
 template <int T, bool NV>
-__device__ __forceinline__ float pack_quotient(float x, float factor) {
-    if (!NV) return x * factor;
-    if (T == 0) return factor > 0.0f ? __fdiv_rn(x, factor) : 0.0f;
-    return fmaf(x, factor, 192.0f) - 192.0f;
+__device__ __forceinline__ float2 pack_quotients(uint32_t word, float2 factor) {
+    const float2 x = make_float2(half_bits_to_f32(word & 0xFFFFu, T == 2), T == 2 ? half_bits_to_f32(word >> 16, 1) : __uint_as_float(word & 0xFFFF0000u));
+    if (!NV) return mul2(x, factor);
+    return add2(fma2(x, factor, make_float2(192.0f, 192.0f)), make_float2(-192.0f, -192.0f));
 }
 
 // the rows of a tile of scales
@@ -145,81 +155,93 @@ template <int T>
 __device__ __forceinline__ void pack_load(const void* x, size_t at, uint32_t (&w)[T == 0 ? 8 : 4]) {
     if (T == 0) {
         const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(x) + at);
-        const uint4 a = __ldcs(p), b = __ldcs(p + 1);
+        const uint4 a = __ldg(p), b = __ldg(p + 1);
         w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
         w[T == 0 ? 4 : 0] = b.x, w[T == 0 ? 5 : 0] = b.y, w[T == 0 ? 6 : 0] = b.z, w[T == 0 ? 7 : 0] = b.w;
     } else {
-        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + at));
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + at));
         w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
     }
 }
+// The largest magnitudes of words, one (FP32) or two (by halves) to a word; joined; and the one of a word.
+template <int T>
+__device__ __forceinline__ uint32_t pack_join(uint32_t a, uint32_t b) { return T == 0 ? max(a, b) : __vmaxu2(a, b); }
 template <int T, int N>
 __device__ __forceinline__ uint32_t pack_most(const uint32_t (&w)[N]) {
-    if (T == 0) {
-        uint32_t m = 0u;
-#pragma unroll
-        for (int i = 0; i < N; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
-        return m;
-    }
     uint32_t m = 0u;
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
-    return max(m & 0xFFFFu, m >> 16);
+    for (int i = 0; i < N; ++i) m = pack_join<T>(m, w[i] & (T == 0 ? 0x7FFFFFFFu : 0x7FFF7FFFu));
+    return m;
 }
 template <int T>
-__device__ __forceinline__ float pack_element(const uint32_t (&w)[T == 0 ? 8 : 4], int i) {
-    return T == 0 ? __uint_as_float(w[T == 0 ? i : 0]) : pack_widen<T>(i & 1 ? w[T == 0 ? 0 : i >> 1] >> 16 : w[T == 0 ? 0 : i >> 1] & 0xFFFFu);
-}
-
-// Along the rows: blockIdx.x a tile's rows, y 256 of the contraction, z the matrix.
+__device__ __forceinline__ uint32_t pack_one(uint32_t m) { return T == 0 ? m : max(m & 0xFFFFu, m >> 16); }
+// Along the rows: blockIdx.x 256 of the contraction of a tile's rows (pieces of the same rows side by side, so that blocks at work
+// together read whole rows), z the matrix.  A thread has a block: no exchange, one division.
 template <int T, bool NV>
 __global__ void __launch_bounds__(PACK_THREADS) pack_rows_kernel(const PackParams p) {
-    constexpr int LANES = NV ? 2 : 4;                    // of a block
-    constexpr int TILES = PACK_CHUNK / (4 * mx_block(NV));
+    constexpr int BLOCK = mx_block(NV), EIGHTS = BLOCK / 8, WORDS = T == 0 ? 8 : 4;
+    constexpr int LANES = PACK_CHUNK / BLOCK;            // threads of a row: 16 or 8
+    constexpr int STEP = PACK_THREADS / LANES;           // rows at a time: 16 or 32
+    constexpr int AHEAD = NV && T != 0 ? 4 : 2;          // of them on the way
+    constexpr int TILES = PACK_CHUNK / (4 * BLOCK);
     __shared__ int s_off[PACK_MAX_GROUPS + 1], s_found[2];
     __shared__ __align__(16) uint8_t s_scale[TILES * MX_TILE_BYTES];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, item = blockIdx.z;
+    const int item = blockIdx.z;
+    const int tile = blockIdx.x / p.chunks, chunk = blockIdx.x - tile * p.chunks;
     launch_wait();
     launch_next();
-    const PackRows rows = pack_rows(p, blockIdx.x, s_off, s_found);
+    const PackRows rows = pack_rows(p, tile, s_off, s_found);
     if (rows.count <= 0) return;
     const PackScale s = pack_scale(p, item);
     for (int i = threadIdx.x; i < TILES * MX_TILE_BYTES / 4; i += PACK_THREADS) reinterpret_cast<uint32_t*>(s_scale)[i] = 0u;
     __syncthreads();
-    const int k = blockIdx.y * PACK_CHUNK + lane * 8, pitch = static_cast<int>(mx_padded(p.length) / 2);
-    const bool there = k < p.length, kept = k < 2 * pitch;
+    const int c = threadIdx.x % LANES, k = chunk * PACK_CHUNK + c * BLOCK, pitch = static_cast<int>(mx_padded(p.length) / 2);
+    const int eights = min(EIGHTS, (p.length - k) / 8);  // (the length is a multiple of 8; 0 or less: none)
+    const bool kept = k < 2 * pitch;
     const size_t x0 = item * static_cast<size_t>(p.stride_x) + rows.first * static_cast<size_t>(p.ldx) + k;
     uint8_t* data = p.data + (static_cast<size_t>(item) * p.outer + rows.first) * pitch + k / 2;
-    const int c = lane / LANES;                          // the block's place in the chunk
-    constexpr int AHEAD = 4;                             // rows on the way
-    for (int r0 = warp; r0 < rows.count; r0 += AHEAD * 8) {
-        uint32_t w[AHEAD][T == 0 ? 8 : 4];
+    for (int r0 = threadIdx.x / LANES; r0 < rows.count; r0 += AHEAD * STEP) {
+        uint32_t w[AHEAD][EIGHTS][WORDS];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n)
+#pragma unroll
+            for (int q = 0; q < EIGHTS; ++q) {
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) w[n][q][i] = 0u;
+                if (q < eights && r0 + n * STEP < rows.count) pack_load<T>(p.x, x0 + (r0 + n * STEP) * static_cast<size_t>(p.ldx) + 8 * q, w[n][q]);
+            }
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
+            const int r = r0 + n * STEP;
+            if (r >= rows.count || !kept) break;
+            uint32_t most = 0u;
 #pragma unroll
-            for (int i = 0; i < (T == 0 ? 8 : 4); ++i) w[n][i] = 0u;
-            if (there && r0 + 8 * n < rows.count) pack_load<T>(p.x, x0 + (r0 + 8 * n) * static_cast<size_t>(p.ldx), w[n]);
-        }
-#pragma unroll
-        for (int n = 0; n < AHEAD; ++n) {
-            const int r = r0 + 8 * n;
-            if (r >= rows.count) break;
-            uint32_t most = pack_most<T>(w[n]);
-            most = max(most, __shfl_xor_sync(~0u, most, 1));
-            if (!NV) most = max(most, __shfl_xor_sync(~0u, most, 2));
-            float factor, y[8];
+            for (int q = 0; q < EIGHTS; ++q) most = pack_join<T>(most, pack_most<T>(w[n][q]));
+            most = pack_one<T>(most);
+            float factor;
             const uint32_t byte = pack_block<T, NV>(most, s, factor);
+            uint32_t e[EIGHTS];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = pack_quotient<T, NV>(pack_element<T>(w[n], i), factor);
-            // (a block that is not finite has factor 0 and may have products that are NaN)
-            const uint32_t e = most >= pack_not_finite<T>() ? 0u : f32_to_e2m1x8(y);
-            if (kept) *reinterpret_cast<uint32_t*>(data + static_cast<size_t>(r) * pitch) = e;
-            if (there && lane % LANES == 0) s_scale[c / 4 * MX_TILE_BYTES + (r & 31) * 16 + (r >> 5) * 4 + (c & 3)] = static_cast<uint8_t>(byte);
+            for (int q = 0; q < EIGHTS; ++q) {
+                float2 y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = make_float2(factor, factor);
+                    if constexpr (T == 0) y[i] = pack_quotients<NV>(make_float2(__uint_as_float(w[n][q][2 * i]), __uint_as_float(w[n][q][2 * i + 1])), f);
+                    else y[i] = pack_quotients<T, NV>(w[n][q][i], f);
+                }
+                // (a block that is not finite has factor 0 and may have products that are NaN)
+                e[q] = most >= pack_not_finite<T>() ? 0u : f32_to_e2m1x8(y);
+            }
+            uint8_t* out = data + static_cast<size_t>(r) * pitch;
+            if (NV) *reinterpret_cast<uint2*>(out) = make_uint2(e[0], e[1]);
+            else *reinterpret_cast<uint4*>(out) = make_uint4(e[0], e[1], e[EIGHTS - 2], e[EIGHTS - 1]);
+            if (eights > 0) s_scale[c / 4 * MX_TILE_BYTES + (r & 31) * 16 + (r >> 5) * 4 + (c & 3)] = static_cast<uint8_t>(byte);
         }
     }
     __syncthreads();
-    const int first = blockIdx.y * TILES, n = min(TILES, p.tiles - first) * (MX_TILE_BYTES / 16);
-    uint4* out = reinterpret_cast<uint4*>(p.scales + ((static_cast<size_t>(item) * p.row_tiles + blockIdx.x) * p.tiles + first) * MX_TILE_BYTES);
+    const int first = chunk * TILES, n = min(TILES, p.tiles - first) * (MX_TILE_BYTES / 16);
+    uint4* out = reinterpret_cast<uint4*>(p.scales + ((static_cast<size_t>(item) * p.row_tiles + tile) * p.tiles + first) * MX_TILE_BYTES);
     for (int i = threadIdx.x; i < n; i += PACK_THREADS) out[i] = reinterpret_cast<const uint4*>(s_scale)[i];
 }
 
@@ -250,7 +272,7 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_columns_kernel(const PackPa
         const int t = row + n * (PACK_THREADS / PIECES);
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
         if (there && t0 + t < p.length)
-            v = __ldcs(reinterpret_cast<const uint4*>(x + static_cast<size_t>(t0 + t) * p.ldx * (T == 0 ? 4 : 2) + piece * 16));
+            v = __ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(t0 + t) * p.ldx * (T == 0 ? 4 : 2) + piece * 16));
         reinterpret_cast<uint4*>(tile)[t * PIECES + piece] = v;
     }
     __syncthreads();
@@ -264,25 +286,44 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_columns_kernel(const PackPa
             v[i] = at[i * WORDS];
             m = T == 0 ? max(m, v[i] & 0x7FFFFFFFu) : __vmaxu2(m, v[i] & 0x7FFF7FFFu);
         }
+        uint32_t most[EACH], byte[EACH];
+        float factor[EACH];
 #pragma unroll
         for (int h = 0; h < EACH; ++h) {
-            const uint32_t most = T == 0 ? m : h ? m >> 16 : m & 0xFFFFu;
-            const int f = w * EACH + h;
-            float factor;
-            uint32_t byte = pack_block<T, NV>(most, s, factor);
+            most[h] = T == 0 ? m : h ? m >> 16 : m & 0xFFFFu;
+            byte[h] = pack_block<T, NV>(most[h], s, factor[h]);
+        }
 #pragma unroll
-            for (int q = 0; q < BLOCK / 8; ++q) {
-                float y[8];
+        for (int q = 0; q < BLOCK / 8; ++q) {
+            uint32_t e[EACH];
+            if constexpr (T == 0) {
+                float2 y[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t bits = v[q * 8 + i];
-                    y[i] = pack_quotient<T, NV>(pack_widen<T>(T == 0 ? bits : h ? bits >> 16 : bits & 0xFFFFu), factor);
+                for (int i = 0; i < 4; ++i)
+                    y[i] = pack_quotients<NV>(make_float2(__uint_as_float(v[q * 8 + 2 * i]), __uint_as_float(v[q * 8 + 2 * i + 1])), make_float2(factor[0], factor[0]));
+                e[0] = f32_to_e2m1x8(y);
+            } else {
+                // both features of a word at once
+                float2 a[4], z[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = make_float2(factor[0], factor[EACH - 1]);
+                    const float2 y0 = pack_quotients<T, NV>(v[q * 8 + 2 * i], f), y1 = pack_quotients<T, NV>(v[q * 8 + 2 * i + 1], f);
+                    a[i] = make_float2(y0.x, y1.x);
+                    z[i] = make_float2(y0.y, y1.y);
                 }
-                const uint32_t e = most >= pack_not_finite<T>() ? 0u : f32_to_e2m1x8(y);
-                *reinterpret_cast<uint32_t*>(out + f * OUT + b * (BLOCK / 2) + q * 4) = e;
+                e[0] = f32_to_e2m1x8(a);
+                e[EACH - 1] = f32_to_e2m1x8(z);
             }
-            if (f >= features || t0 + b * BLOCK >= p.length) byte = 0u;
-            s_scale[b / 4 * MX_TILE_BYTES + (f & 31) * 16 + (f >> 5) * 4 + (b & 3)] = static_cast<uint8_t>(byte);
+#pragma unroll
+            for (int h = 0; h < EACH; ++h)
+                *reinterpret_cast<uint32_t*>(out + (w * EACH + h) * OUT + b * (BLOCK / 2) + q * 4) = most[h] >= pack_not_finite<T>() ? 0u : e[h];
+        }
+#pragma unroll
+        for (int h = 0; h < EACH; ++h) {
+            const int f = w * EACH + h;
+            if (f >= features || t0 + b * BLOCK >= p.length) byte[h] = 0u;
+            s_scale[b / 4 * MX_TILE_BYTES + (f & 31) * 16 + (f >> 5) * 4 + (b & 3)] = static_cast<uint8_t>(byte[h]);
         }
     }
     __syncthreads();
@@ -299,51 +340,65 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_columns_kernel(const PackPa
 }
 __host__ __device__ constexpr int pack_columns_smem(int type) { return PACK_TURN * PACK_TURN * (type == 0 ? 4 : 2) + PACK_TURN * (PACK_TURN / 2 + 8) + 2 * MX_TILE_BYTES; }
 
-// Reading back: blocks as in pack_rows_kernel.  A lane has eight elements.
+// Reading back: a thread has eight elements of a row, a warp 256.  Where the rows of Y are not whole pieces of eight, a warp's
+// elements go by way of shared memory, from where consecutive lanes store consecutive ones.
 template <int T, bool NV>
 __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackParams p) {
-    constexpr int LANES = NV ? 2 : 4, TILES = PACK_CHUNK / (4 * mx_block(NV));
+    constexpr int LANES = NV ? 2 : 4, TILES = PACK_CHUNK / (4 * mx_block(NV)), AHEAD = 4;
     __shared__ int s_off[PACK_MAX_GROUPS + 1], s_found[2];
+    __shared__ __align__(16) float s_line[PACK_THREADS / 32][PACK_CHUNK];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, item = blockIdx.z;
+    const int tile = blockIdx.x / p.chunks, chunk = blockIdx.x - tile * p.chunks;
     launch_wait();
     launch_next();
-    const PackRows rows = pack_rows(p, blockIdx.x, s_off, s_found);
+    const PackRows rows = pack_rows(p, tile, s_off, s_found);
     if (rows.count <= 0) return;
     const float t = NV && p.scale ? p.scale[item] : 1.0f;
-    const int k = blockIdx.y * PACK_CHUNK + lane * 8, pitch = static_cast<int>(mx_padded(p.length) / 2), c = lane / LANES;
-    if (k >= p.length) return;
+    const int k0 = chunk * PACK_CHUNK, k = k0 + lane * 8, pitch = static_cast<int>(mx_padded(p.length) / 2), c = lane / LANES;
+    const bool whole = p.length % 8 == 0, there = k < p.length;
     const uint8_t* data = p.data + (static_cast<size_t>(item) * p.outer + rows.first) * pitch + k / 2;
-    const uint8_t* scales = p.scales + ((static_cast<size_t>(item) * p.row_tiles + blockIdx.x) * p.tiles + blockIdx.y * TILES + c / 4) * MX_TILE_BYTES + (c & 3);
-    const size_t y0 = (static_cast<size_t>(item) * p.outer + rows.first) * p.length + k;
-    const bool whole = p.length % 8 == 0;                // rows of Y are pieces of eight, 16-byte aligned
-#pragma unroll 4
-    for (int r = warp; r < rows.count; r += 8) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(data + static_cast<size_t>(r) * pitch);
-        const uint32_t b = scales[(r & 31) * 16 + (r >> 5) * 4];
-        const float s = NV ? e4m3_to_f32(b) : e8m0_to_f32(b);
-        float x[8];
-        e2m1x8_to_f32(w, x);
+    const uint8_t* scales = p.scales + ((static_cast<size_t>(item) * p.row_tiles + tile) * p.tiles + chunk * TILES + c / 4) * MX_TILE_BYTES + (c & 3);
+    const size_t y0 = (static_cast<size_t>(item) * p.outer + rows.first) * p.length + k0;
+    for (int r0 = warp; r0 < rows.count; r0 += 8 * AHEAD) {
+        uint32_t w[AHEAD], b[AHEAD];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = NV ? x[i] * s * t : x[i] * s;
-        const size_t y = y0 + static_cast<size_t>(r) * p.length;
-        if (T == 0) {
-            float* out = static_cast<float*>(p.values) + y;
+        for (int n = 0; n < AHEAD; ++n) {
+            const int r = r0 + 8 * n;
+            const bool load = there && r < rows.count;
+            w[n] = load ? __ldg(reinterpret_cast<const uint32_t*>(data + static_cast<size_t>(r) * pitch)) : 0u;
+            b[n] = load ? __ldg(scales + (r & 31) * 16 + (r >> 5) * 4) : 0u;
+        }
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) {
+            const int r = r0 + 8 * n;
+            if (r >= rows.count) break;
+            const float s = NV ? e4m3_to_f32(b[n]) : e8m0_to_f32(b[n]);
+            float x[8];
+            e2m1x8_to_f32(w[n], x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = NV ? x[i] * s * t : x[i] * s;
+            const size_t y = y0 + static_cast<size_t>(r) * p.length;
             if (whole) {
-                __stcs(reinterpret_cast<float4*>(out), make_float4(x[0], x[1], x[2], x[3]));
-                __stcs(reinterpret_cast<float4*>(out) + 1, make_float4(x[4], x[5], x[6], x[7]));
+                if (there && T == 0) {
+                    float4* out = reinterpret_cast<float4*>(static_cast<float*>(p.values) + y + lane * 8);
+                    __stcs(out, make_float4(x[0], x[1], x[2], x[3]));
+                    __stcs(out + 1, make_float4(x[4], x[5], x[6], x[7]));
+                } else if (there) {
+                    __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.values) + y + lane * 8), pack8<T == 2>(x));
+                }
             } else {
+                float4* line = reinterpret_cast<float4*>(s_line[warp]) + lane * 2;
+                line[0] = make_float4(x[0], x[1], x[2], x[3]);
+                line[1] = make_float4(x[4], x[5], x[6], x[7]);
+                __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (k + i < p.length) out[i] = x[i];
-            }
-        } else {
-            uint16_t* out = static_cast<uint16_t*>(p.values) + y;
-            if (whole) {
-                __stcs(reinterpret_cast<uint4*>(out), pack8<T == 2>(x));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (k + i < p.length) out[i] = static_cast<uint16_t>(pack_half2(x[i], 0.0f, T == 2) & 0xFFFFu);
+                for (int i = 0; i < 8; ++i) {
+                    const float v = s_line[warp][i * 32 + lane];
+                    if (k0 + i * 32 + lane >= p.length) continue;
+                    if (T == 0) static_cast<float*>(p.values)[y + i * 32 + lane] = v;
+                    else static_cast<uint16_t*>(p.values)[y + i * 32 + lane] = static_cast<uint16_t>(pack_half2(v, 0.0f, T == 2) & 0xFFFFu);
+                }
+                __syncwarp();
             }
         }
     }
@@ -365,38 +420,64 @@ __device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* line) {
     return m;                                            // (of the first warp)
 }
 
-// blockIdx.x of gridDim.x takes every gridDim.x-th piece of 8 elements x 256 threads x 4; y the matrix.  ONE block writes the scale.
-template <int T>
-__global__ void __launch_bounds__(PACK_THREADS) tensor_max_kernel(const PackParams p, int rows, int width, uint32_t* partial, float* scale) {
+// blockIdx.x of gridDim.x takes its share of the pieces of 8 elements, 4 to a thread at a time; y the matrix.  CLUSTER: the blocks are one
+// cluster, whose first writes the scale; else tensor_scale_kernel does.
+constexpr int SCALE_CLUSTER = 8, SCALE_THREADS = 512;
+template <int T, bool CLUSTER, bool DENSE>
+__device__ __forceinline__ void tensor_max(const PackParams& p, int rows, int width, uint32_t* partial, float* scale) {
+    constexpr int AHEAD = CLUSTER ? 2 : T == 0 ? 4 : 8, WORDS = T == 0 ? 8 : 4;
     __shared__ uint32_t line[32];
+    __shared__ __align__(16) uint4 maxima[SCALE_CLUSTER];
     const size_t x0 = blockIdx.y * static_cast<size_t>(p.stride_x);
     const int per_row = width / 8;
-    const long long pieces = static_cast<long long>(rows) * per_row, step = static_cast<long long>(gridDim.x) * PACK_THREADS;
+    const long long pieces = static_cast<long long>(rows) * per_row;
+    const int turn = AHEAD * static_cast<int>(blockDim.x);
     launch_wait();
     launch_next();
     uint32_t m = 0u;
-    const bool dense = p.ldx == width;
-    for (long long i = blockIdx.x * static_cast<long long>(PACK_THREADS) + threadIdx.x; i < pieces; i += 4 * step) {
-        uint32_t w[4][T == 0 ? 8 : 4];
+    for (long long i = blockIdx.x * static_cast<long long>(turn) + threadIdx.x; i < pieces; i += static_cast<long long>(gridDim.x) * turn) {
+        uint32_t w[AHEAD][WORDS];
+        const int left = static_cast<int>(min(pieces - i, static_cast<long long>(turn)));
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const long long j = i + n * step;
+        for (int n = 0; n < AHEAD; ++n) {
+            const int j = n * static_cast<int>(blockDim.x);
 #pragma unroll
-            for (int q = 0; q < (T == 0 ? 8 : 4); ++q) w[n][q] = 0u;
-            if (j < pieces) {
-                const long long r = dense ? 0 : j / per_row;
-                pack_load<T>(p.x, x0 + (dense ? j * 8 : r * p.ldx + (j - r * per_row) * 8), w[n]);
+            for (int q = 0; q < WORDS; ++q) w[n][q] = 0u;
+            if (j < left) {
+                if (DENSE) {
+                    pack_load<T>(p.x, x0 + (i + j) * 8, w[n]);
+                } else {
+                    const long long r = (i + j) / per_row;
+                    pack_load<T>(p.x, x0 + r * p.ldx + (i + j - r * per_row) * 8, w[n]);
+                }
             }
         }
 #pragma unroll
-        for (int n = 0; n < 4; ++n) m = max(m, pack_most<T>(w[n]));
+        for (int n = 0; n < AHEAD; ++n) m = pack_join<T>(m, pack_most<T>(w[n]));
     }
-    m = __float_as_uint(pack_widen<T>(m));               // (order of FP32 bits from here on)
+    m = __float_as_uint(pack_widen<T>(pack_one<T>(m)));  // (order of FP32 bits from here on)
     m = block_max(m, line);
-    if (threadIdx.x == 0) {
-        if (gridDim.x == 1) scale[blockIdx.y] = tensor_scale_of(__uint_as_float(m));
-        else partial[blockIdx.y * gridDim.x + blockIdx.x] = m;
+    if (CLUSTER) {
+        if (threadIdx.x == 0) st_cluster_v4(map_to_cta(smem_u32(maxima + cluster_ctarank()), 0), m, 0u, 0u, 0u);
+        cluster_sync_all();
+        if (blockIdx.x == 0 && threadIdx.x < SCALE_CLUSTER) {
+            m = __reduce_max_sync((1u << SCALE_CLUSTER) - 1u, maxima[threadIdx.x].x);
+            if (threadIdx.x == 0) scale[blockIdx.y] = tensor_scale_of(__uint_as_float(m));
+        }
+    } else if (threadIdx.x == 0) {
+        partial[blockIdx.y * gridDim.x + blockIdx.x] = m;
     }
+}
+template <int T>
+__global__ void __launch_bounds__(PACK_THREADS) tensor_max_kernel(const PackParams p, int rows, int width, uint32_t* partial) {
+    if (p.ldx == width) tensor_max<T, false, true>(p, rows, width, partial, nullptr);
+    else tensor_max<T, false, false>(p, rows, width, partial, nullptr);
+}
+template <int T>
+__global__ void __launch_bounds__(SCALE_THREADS) __cluster_dims__(SCALE_CLUSTER, 1, 1)
+tensor_cluster_kernel(const PackParams p, int rows, int width, float* scale) {
+    if (p.ldx == width) tensor_max<T, true, true>(p, rows, width, nullptr, scale);
+    else tensor_max<T, true, false>(p, rows, width, nullptr, scale);
 }
 __global__ void __launch_bounds__(PACK_THREADS) tensor_scale_kernel(const uint32_t* partial, int blocks, float* scale) {
     __shared__ uint32_t line[32];
