@@ -2,7 +2,7 @@
 //   C[t][i] = ta tb sum_k X[t][k] W_g[i][k]      for the rows t of group g
 // The shape of the kernel is that of the grouped products (grouped.cuh): the features are the MMA's M dimension and the ragged rows
 // its N, a CTA pair computes 256 features x up to 256 rows, the groups' offsets are read on the device by a scheduler warp, and
-// tiles of the last, partial wave are cut along k.  What is different:
+// of one group the plan may have the tiles of the last, partial wave cut along k.  What is different:
 //
 // A k-block is 256 elements (128 bytes of a row), four MMAs of 64.  Its scales arrive by TMA as the tiles of 128 rows x 4 blocks that
 // tensor memory wants and go there by tcgen05.cp, from a warp of its own that is some k-blocks ahead of the MMAs.  (Issued by the MMAs' warp the
@@ -208,38 +208,26 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             __syncwarp();
         }
         auto rows_in = [&](int g) { return s_row[g + 1] - s_row[g]; };
-        int most = 0;
-        for (int g = lane; g < p.groups; g += 32) most = max(most, rows_in(g));
-        most = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(most)));
-        // Estimated time, in clocks, of n tiles of w rows, and into how many parts (1: none) the tiles of the last, partial wave are cut: see
-        // grouped.cuh, whose costs of parts these are; a k-block costs MX_KB + 1.5 w.
-        auto share_of = [&](int w, int t) { return static_cast<float>(max(64, w)) * (10.0f + static_cast<float>(t) * t * (1.0f / 450)); };
-        auto block_of = [&](int w) { return 400.0f + w * 1.5f; };
-        auto best_parts = [&](int kbs, int w, int t) {
-            return max(1, min(__float2int_rn(sqrtf(__fdividef(static_cast<float>(kbs) * block_of(w), share_of(w, t)))), kbs / 2));
-        };
-        auto estimate = [&](int n, int w, int& parts) {
-            const int waves = n / num_pairs, rest = n - waves * num_pairs, most_parts = rest ? num_pairs / rest : 1;
-            const float kb = block_of(w), k = static_cast<float>(p.kb_total), whole = (waves + (rest ? 1 : 0)) * (k * kb + 500.0f);
-            parts = p.partial && most_parts > 1 ? min(most_parts, best_parts(p.kb_total, w, rest * most_parts)) : 1;
-            const float cut = waves * (k * kb + 500.0f) + (p.kb_total + parts - 1) / parts * kb + 4000.0f + share_of(w, rest * parts) * parts;
-            if (parts > 1 && cut < whole) return cut;
-            parts = 1;
-            return whole;
-        };
-        int width = most <= 32 ? 32 : 64, parts = 1;
-        if (most > 64) {
-            // the width of least estimated time: lane l looks at 64 (l + 1)
-            const int limit = min(MX_TILE, (most + 63) & ~63), w = min(64 * ((lane & 3) + 1), limit);
-            int n = 0;
-            for (int g = lane >> 2; g < p.groups; g += 8) n += (rows_in(g) + w - 1) / w;
-            n += __shfl_xor_sync(~0u, n, 4);
-            n += __shfl_xor_sync(~0u, n, 8);
-            n += __shfl_xor_sync(~0u, n, 16);
-            const float t = estimate(n * p.tiles_i, w, parts);
-            // the smallest; of equals the widest: a time's upper bits, then the width
-            const unsigned won = __reduce_min_sync(~0u, (__float_as_uint(t) & ~7u) | (4u - static_cast<unsigned>(w >> 6)));
-            width = static_cast<int>(4u - (won & 7u)) << 6;
+        // The width of the tiles: the plan's (one group), or that of the least estimated time of whole waves (lane l looks at 64 (l + 1) rows)
+        int width = p.width;
+        if (!width) {
+            int most = 0;
+            for (int g = lane; g < p.groups; g += 32) most = max(most, rows_in(g));
+            most = static_cast<int>(__reduce_max_sync(~0u, static_cast<unsigned>(most)));
+            width = most <= 32 ? 32 : 64;
+            if (most > 64) {
+                const int limit = min(MX_TILE, (most + 63) & ~63), w = min(64 * ((lane & 3) + 1), limit);
+                int n = 0;
+                for (int g = lane >> 2; g < p.groups; g += 8) n += (rows_in(g) + w - 1) / w;
+                n += __shfl_xor_sync(~0u, n, 4);
+                n += __shfl_xor_sync(~0u, n, 8);
+                n += __shfl_xor_sync(~0u, n, 16);
+                const unsigned waves = (n * p.tiles_i + num_pairs - 1) / num_pairs;
+                const unsigned t = waves * (p.kb_total * mx_block_clocks(w) + MX_TILE_CLOCKS) + MX_ROW_CLOCKS * w;
+                // the smallest; of equals the widest
+                const unsigned won = __reduce_min_sync(~0u, (min(t, 0x1FFFFFFFu) << 3) | (4u - static_cast<unsigned>(w >> 6)));
+                width = static_cast<int>(4u - (won & 7u)) << 6;
+            }
         }
         if (lane == 0) *s_width = width;
         // tiles before each group
@@ -261,10 +249,9 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         // tile counts `padded` k-blocks there, a whole number of shares.
         const int from = tiles / num_pairs * num_pairs;
         int tail_from = tiles, tail_len = 0, share = 1, padded = p.kb_total;
-        estimate(tiles, width, parts);
-        if (parts > 1) {
+        if (p.parts > 1) {
             tail_from = from;
-            share = (p.kb_total + parts - 1) / parts;
+            share = (p.kb_total + p.parts - 1) / p.parts;
             padded = (p.kb_total + share - 1) / share * share;
             tail_len = (tiles - from) * padded;
         }

@@ -20,7 +20,13 @@ constexpr int MX_SMEM = MX_RING + 1024 + 2 * MX_TABLE + 1024;
 static_assert(MX_SMEM <= 227 * 1024, "shared memory of an SM");
 __host__ __device__ constexpr int mx_stage_bytes(int width) { return MX_A_BYTES + 64 * width + MX_S_BYTES * (1 + (width + 127) / 128); }
 
+// Clocks, for the choice of tiles.  A k-block of tiles of w rows when all pairs are at work (the operand feed; 8192^3: 64 rows 0.30 us, 128 0.33,
+// 192 0.39, 256 0.455), and by a pair alone; the rest of a tile, and of the last one for each of its rows.
+constexpr int MX_ALONE_CLOCKS = 460, MX_TILE_CLOCKS = 300, MX_ROW_CLOCKS = 8;
+__host__ __device__ constexpr int mx_block_clocks(int w) { return 450 + w + w / 2; }
+
 struct MxParams {
+    int width, parts;      // one group: rows of a tile, and into how many parts the tiles of the last wave are cut (1: none); 0, 1: the kernel's choice
     int groups, rows;      // rows: extent of the row arrays; offsets are clamped to it
     int I;                 // features (contiguous in C)
     int kb_total;          // k-blocks of the contraction

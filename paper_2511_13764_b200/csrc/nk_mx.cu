@@ -26,6 +26,31 @@ static bool encode_scales(CUtensorMap* m, const void* base, int64_t tiles, int64
                           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles of one group of rows: their width, and into how many parts those of the last, partial wave are cut, by the least estimated time.
+// Joining parts costs 2900 clocks and 700 a part, and what is written and read again of them at 3500 bytes a clock.  (16 rows, 4096
+// features: K 4096 10.0 us uncut, 9.7 in four parts, K 8192 14.8 and 11.5; 128 rows, K 4096 10.8 uncut, 12.1 in four.  Cuts of
+// groups' tiles gain nothing below K = 8192, so only one group's are cut, and the kernel has no code for that choice, which costs 1.5 us.)
+static void mx_tiles_of(int64_t rows, int tiles_i, int kbs, int pairs, bool cut, int* width, int* parts) {
+    double best = 1e300;
+    for (int w = rows <= 32 ? 32 : 64; w <= MX_TILE; w += w < 64 ? 32 : 64) {
+        const int64_t n = div_up(rows, w) * tiles_i, waves = n / pairs, rest = n % pairs;
+        auto block = [&](int64_t active) {
+            return MX_ALONE_CLOCKS + (mx_block_clocks(w) - MX_ALONE_CLOCKS) * (active < pairs ? static_cast<double>(active) / pairs : 1.0);
+        };
+        const double full = static_cast<double>(waves) * (kbs * block(pairs) + MX_TILE_CLOCKS), end = MX_TILE_CLOCKS + MX_ROW_CLOCKS * w;
+        for (int c = 1; c == 1 || (cut && rest && c <= 8 && c <= kbs && c * rest <= pairs); ++c) {
+            const double join = c > 1 ? 2900.0 + 700.0 * c + static_cast<double>(rest * c) * w * (2048.0 / 3500.0) : 0.0;
+            const double t = full + (rest ? div_up(kbs, c) * block(rest * c) : 0.0) + end + join;
+            if (t < best * 0.999 || (t <= best * 1.001 && c == 1 && *parts == 1)) {      // (of equals the widest)
+                best = t < best ? t : best;
+                *width = w;
+                *parts = c;
+            }
+        }
+        if (w >= rows) break;
+    }
+}
+
 }  // namespace nk
 
 struct nk_mx_s : nk::PlanBase {
@@ -33,6 +58,7 @@ struct nk_mx_s : nk::PlanBase {
     int pairs;                    // CTA pairs that fit the device
     nk::MxFunction kernel;
     int chunk;
+    int width, parts;             // of one group's tiles; groups: 0, 1
     int split_slot;
     unsigned int* counters;
     nk::MxMaps maps;
@@ -74,12 +100,22 @@ nk_status_t nk_mx_create(const nk_mx_desc_t* desc, nk_mx_t* out) {
     const MxOut type = d.out_dtype == NK_F32 ? MX_OUT_F32 : d.out_dtype == NK_BF16 ? MX_OUT_BF16 : MX_OUT_F16;
     p->chunk = type == MX_OUT_F32 ? MX_CHUNK : MX_CHUNK_16;
     const bool sums = div_up(d.K, MX_BK) > p->chunk;
+    bool uncut = false;
     p->kernel = d.format == NK_NVF4 ? mx_kernel_nv(type, sums) : mx_kernel_mx(type, sums);
     if (cudaFuncSetAttribute(p->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MX_SMEM) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
     p->slab_cols = static_cast<int>(d.rows >= MX_TILE ? MX_TILE : div_up(d.rows, 32) * 32);
-    p->split_slot = take_split_slot(d.device, p->pairs, &p->counters);
-    snprintf(p->name, sizeof(p->name), "mx_%s%s_256x256x256_pair%s", d.format == NK_NVF4 ? "nvf4" : "mxf4", d.groups ? "_grouped" : "", p->split_slot < 0 ? "_uncut" : "");
+    p->parts = 1;
+    if (!d.groups) {
+        const int tiles_i = static_cast<int>(div_up(d.N, MX_TILE)), kbs = static_cast<int>(div_up(d.K, MX_BK));
+        mx_tiles_of(d.rows, tiles_i, kbs, p->pairs, true, &p->width, &p->parts);
+        if (p->parts > 1) p->split_slot = take_split_slot(d.device, p->pairs, &p->counters);
+        if (p->parts > 1 && p->split_slot < 0) {         // no counters: uncut
+            uncut = true;
+            mx_tiles_of(d.rows, tiles_i, kbs, p->pairs, false, &p->width, &p->parts);
+        }
+    }
+    snprintf(p->name, sizeof(p->name), "mx_%s%s_256x256x256_pair%s", d.format == NK_NVF4 ? "nvf4" : "mxf4", d.groups ? "_grouped" : "", uncut ? "_uncut" : "");
     *out = p;
     return NK_OK;
 }
@@ -123,6 +159,8 @@ nk_status_t nk_mx_run(nk_mx_t p, const void* A, const void* A_scales, const void
         memcpy(p->cached, now, sizeof(now));     // (none is null: the maps are valid)
     }
     MxParams g = {};
+    g.width = p->width;
+    g.parts = p->parts;
     g.groups = static_cast<int>(groups);
     g.rows = static_cast<int>(d.rows);
     g.I = static_cast<int>(d.N);
