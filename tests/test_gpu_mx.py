@@ -99,3 +99,250 @@ def test_sizes(fmt, rows, N, K):
 @pytest.mark.parametrize("rows,N,K", [(5, 264, 640), (300, 264, 4360), (2000, 2056, 512), (4099, 1024, 2056)])
 def test_results(fmt, out, rows, N, K):
     check(rows, N, K, fmt, out)
+
+
+GROUPS = [[0, 5], [0, 0, 130, 130, 131, 300, 300], [7, 20, 20, 290], [0, 0], [128, 256, 300], [0, 64, 129, 193, 300], list(range(0, 301, 4)) + [300]]
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("offsets", GROUPS)
+@pytest.mark.parametrize("N,K,out", [(264, 136, "f32"), (136, 520, "bf16"), (8, 72, "f16"), (520, 64, "bf16")])
+def test_grouped(fmt, offsets, N, K, out):
+    rows, groups = 300, len(offsets) - 1
+    A = Packed(normal(rows, K, seed=K), fmt, offsets=offsets)
+    B = Packed(normal(groups, N, K, seed=N, scale=0.1), fmt)
+    got = run(A, B, N, K, fmt, out, groups=groups, offsets=A.offsets)
+    seen = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    for g, (lo, hi) in enumerate(zip(offsets, offsets[1:])):
+        y = A.values[lo:hi] @ B.values[g].t()
+        assert ((got[lo:hi] - y).abs() <= bound(A.values[lo:hi], B.values[g], K, out, y)).all(), g
+        seen[lo:hi] = True
+    assert (got[~seen] == 7.0).all(), "rows outside all groups are not touched"
+
+
+@pytest.mark.parametrize("sizes", [[1000, 3, 0, 400, 65, 130], [2000, 1], [1, 1, 1, 700]])
+def test_grouped_tiles_of_every_width(sizes):
+    """Groups of several tiles: cut evenly in steps of 64, scales that begin inside 128 rows."""
+    offsets = [0]
+    for n in sizes:
+        offsets.append(offsets[-1] + n)
+    rows, N, K = offsets[-1], 776, 264
+    A, B = Packed(normal(rows, K, seed=1), "nvf4", offsets=offsets), Packed(normal(len(sizes), N, K, seed=2), "nvf4")
+    got = run(A, B, N, K, "nvf4", "f32", groups=len(sizes), offsets=A.offsets)
+    for g, (lo, hi) in enumerate(zip(offsets, offsets[1:])):
+        y = A.values[lo:hi] @ B.values[g].t()
+        assert ((got[lo:hi] - y).abs() <= bound(A.values[lo:hi], B.values[g], K, "f32", y)).all(), g
+
+
+@pytest.mark.parametrize("offsets", [[0, 200, 100, 300], [-5, 100, 200, 300], [0, 100, 400, 500]])
+def test_bad_offsets_are_clamped_and_reported(offsets):
+    top, clamped = 0, []
+    for o in offsets:
+        top = max(top, min(o, 300))
+        clamped.append(top)
+    A, B = Packed(normal(300, 64, seed=1), "mxf4", offsets=clamped), Packed(normal(3, 64, 64, seed=2), "mxf4")
+    plan = nk.MxPlan(300, 64, 64, groups=3, format=nk.MXF4)
+    C = torch.full((300, 64), 7.0, device="cuda")
+    plan.run(A.data, A.scales, B.data, B.scales, C, offsets=torch.tensor(offsets, dtype=torch.int32, device="cuda"), stream=stream())
+    with pytest.raises(nk.NkError) as e:
+        plan.check()
+    assert e.value.status == 1
+    plan.check()
+    for g, (lo, hi) in enumerate(zip(clamped, clamped[1:])):
+        y = A.values[lo:hi] @ B.values[g].t()
+        assert ((C[lo:hi].double() - y).abs() <= bound(A.values[lo:hi], B.values[g], 64, "f32", y)).all()
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,N,K,groups", [(50, 136, 200, 0), (300, 264, 1032, 0), (300, 264, 136, 3)])
+@pytest.mark.parametrize("relu,bias,beta", [(True, True, 0), (True, False, 0), (False, False, 1), (True, True, 1)])
+def test_epilogues(out, rows, N, K, groups, relu, bias, beta):
+    offsets = [0, 100, 100, 300] if groups else None
+    A = Packed(normal(rows, K, seed=3), "nvf4", offsets=offsets)
+    B = Packed(normal(*((groups, N, K) if groups else (N, K)), seed=4, scale=0.1), "nvf4")
+    b = normal(*((groups, N) if groups else (N,)), seed=5, kind="f32").cuda() if bias else None
+    old = normal(rows, N, seed=6, kind=out).cuda() if beta else None
+    got = run(A, B, N, K, "nvf4", out, groups=groups, bias=b, relu=relu, beta=beta, c=old, ldc=N + 16, offsets=A.offsets)
+    for g, (lo, hi) in enumerate(zip(offsets, offsets[1:]) if groups else [(0, rows)]):
+        v = B.values[g] if groups else B.values
+        y = A.values[lo:hi] @ v.t()
+        tol = bound(A.values[lo:hi], v, K, out, torch.zeros_like(y))
+        if bias:
+            y = y + (b[g] if groups else b).double()
+        if beta:
+            y = y + old[lo:hi].double()
+        # (the additions round to nearest: 2^-23 of what is added)
+        more = 2.0 ** -23 * (2.0 * y.abs() + (b.abs().max() if bias else 0.0) + (old[lo:hi].double().abs() if beta else 0.0))
+        y = torch.relu(y) if relu else y
+        rel = {"f32": 0.0, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[out]
+        assert ((got[lo:hi] - y).abs() <= tol + more + rel * y.abs()).all()
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("rows,N,K", [(33, 264, 136), (333, 520, 776), (1000, 64, 264)])
+def test_gradients_of_a_layer(fmt, rows, N, K):
+    """dX = dY . W and dW = dY^T . X from operands packed along their columns; the length of dW's contraction is any number."""
+    x, w, dy = normal(rows, K, seed=1), normal(N, K, seed=2, scale=0.1), normal(rows, N, seed=3)
+    a, b = Packed(dy, fmt), Packed(w, fmt, transposed=1)
+    got = run(a, b, K, N, fmt, "f32")
+    y = a.values @ b.values.t()
+    assert ((got - y).abs() <= bound(a.values, b.values, N, "f32", y)).all()
+    a, b = Packed(dy, fmt, transposed=1), Packed(x, fmt, transposed=1)
+    got = run(a, b, K, rows, fmt, "f32")
+    y = a.values @ b.values.t()
+    assert ((got - y).abs() <= bound(a.values, b.values, rows, "f32", y)).all()
+    # against differences: <dY, X . W^T> changes along W by <dW, V>, as the products of the packed operands themselves do (they are linear)
+    xt, dyt = b.values.t(), a.values.t()
+    v = normal(N, K, seed=9).double().cuda()
+    h = 0.5
+
+    def loss(m):
+        return (dyt * (xt @ m.t())).sum()
+    slope = (loss(w.double().cuda() + h * v) - loss(w.double().cuda() - h * v)) / (2 * h)
+    assert abs((got * v).sum() - slope) <= (bound(a.values, b.values, rows, "f32", y) * v.abs()).sum() + 1e-9 * slope.abs()
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("out,K", [("f32", 65536), ("f32", 2304), ("bf16", 40000), ("f16", 20000)])
+@pytest.mark.parametrize("rows", [16, 300])
+def test_long_sums_of_one_sign(fmt, out, K, rows):
+    """The error of an accumulator goes one way: sums over it are taken in FP32."""
+    A, B = Packed(normal(rows, K, seed=1).abs(), fmt), Packed(normal(264, K, seed=2, scale=1.0 / K).abs(), fmt)
+    got = run(A, B, 264, K, fmt, out)
+    y = A.values @ B.values.t()
+    assert ((got - y).abs() <= bound(A.values, B.values, K, out, y)).all()
+    if out == "f32":
+        assert ((got - y) / y).abs().max() <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("rows,N,K", [(16, 256, 16384), (1, 8, 8192), (64, 1024, 16384), (40, 264, 10000), (300, 256, 33000)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_cut_tiles(rows, N, K, out):
+    """Few tiles and a long contraction: cut along it.  The same bits every time, and the counters are zero again."""
+    A, B = Packed(normal(rows, K, seed=1), "nvf4"), Packed(normal(N, K, seed=2, scale=0.1), "nvf4")
+    plan = nk.MxPlan(rows, N, K, out_dtype=TYPES[out][0])
+    assert plan.workspace_bytes > 0
+    ws = torch.full((plan.workspace_bytes,), 0xFF, dtype=torch.uint8, device="cuda")
+    results = []
+    for _ in range(20):
+        C = torch.empty(rows, N, dtype=TYPES[out][1], device="cuda")
+        plan.run(A.data, A.scales, B.data, B.scales, C, scale_a=A.scale, scale_b=B.scale, workspace=ws, stream=stream())
+        results.append(C)
+    plan.check()
+    assert all(torch.equal(results[0], r) for r in results)
+    y = A.values @ B.values.t()
+    assert ((results[0].double() - y).abs() <= bound(A.values, B.values, K, out, y)).all()
+    with pytest.raises(nk.NkError) as e:
+        plan.run(A.data, A.scales, B.data, B.scales, C, scale_a=A.scale, scale_b=B.scale, workspace=ws[:-16], stream=stream())
+    assert e.value.status == 4
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+def test_what_is_not_finite_stays_in_its_row_and_feature(fmt):
+    rows, N, K, offsets = 200, 264, 200, [0, 90, 200]
+    x, w = normal(rows, K, seed=1), normal(2, N, K, seed=2)
+    A0, B0 = Packed(x, fmt, offsets=offsets), Packed(w, fmt)
+    clean = run(A0, B0, N, K, fmt, "f32", groups=2, offsets=A0.offsets)
+    scale_a, scale_b = A0.scale, B0.scale
+    x[77, 13], w[1, 100, 7] = float("nan"), float("inf")
+    for P, m, s in ((A0, x, scale_a), (B0, w, scale_b)):    # the same tensor scales, so that all else stays as it is
+        P.plan.run(m.cuda(), P.data, P.scales, scale=s, offsets=P.offsets, stream=stream())
+    got = run(A0, B0, N, K, fmt, "f32", groups=2, offsets=A0.offsets)
+    hit = torch.zeros(rows, N, dtype=torch.bool, device="cuda")
+    hit[77] = True
+    hit[90:, 100] = True
+    assert got[hit].isnan().all() and torch.equal(got[~hit], clean[~hit])
+
+
+def test_rows_behind_the_last_and_scales_nobody_wrote():
+    """Scales and data of rows that are not there may hold anything, NaN patterns among them."""
+    A, B = Packed(normal(130, 72, seed=1), "nvf4"), Packed(normal(136, 72, seed=2), "nvf4")
+    y = A.values @ B.values.t()
+    # rows 130 .. 255 of A's tiles, 136 .. 255 of B's
+    for P, n in ((A, 130), (B, 136)):
+        t = P.scales.view(-1, 32, 4, 4)                      # 512-byte tiles: r % 32, r / 32, c
+        C = t.shape[0] // 2
+        r = torch.arange(n - 128, 128, device="cuda")
+        for c in range(C):
+            t[C + c, r % 32, r // 32, :] = 0x7F
+    got = run(A, B, 136, 72, "nvf4", "f32")
+    assert ((got - y).abs() <= bound(A.values, B.values, 72, "f32", y)).all()
+
+
+def test_tensor_scales_that_are_left_out():
+    x, w = normal(40, 128, seed=1), normal(64, 128, seed=2)
+    out = []
+    for s in (None, 0.25):
+        P = []
+        for m in (x, w):
+            p = Packed(m, "nvf4")
+            p.scale = None if s is None else torch.tensor([s], device="cuda")
+            p.plan.run(m.cuda(), p.data, p.scales, scale=p.scale, stream=stream())
+            codes, bytes_, _ = quantise(m.double().numpy(), "nvf4", 1.0 if s is None else s)
+            p.values = torch.from_numpy(values(codes, bytes_, "nvf4", 1.0 if s is None else s, 128)).cuda()
+            P.append(p)
+        got = run(*P, 64, 128, "nvf4", "f32")
+        y = P[0].values @ P[1].values.t()
+        assert ((got - y).abs() <= bound(P[0].values, P[1].values, 128, "f32", y)).all()
+        out.append(got)
+
+
+def test_streams_graphs_and_plans_destroyed_early():
+    A, B = Packed(normal(300, 512, seed=1), "nvf4"), Packed(normal(520, 512, seed=2), "nvf4")
+    want = run(A, B, 520, 512, "nvf4", "bf16")
+    # two plans at once on two streams, destroyed with work queued
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    results = []
+    torch.cuda.synchronize()
+    for s in (a, b) * 4:
+        plan = nk.MxPlan(300, 520, 512, out_dtype=nk.BF16)
+        C = torch.zeros(300, 520, dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(max(1, plan.workspace_bytes), dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(10):
+            plan.run(A.data, A.scales, B.data, B.scales, C, scale_a=A.scale, scale_b=B.scale, workspace=ws, stream=s.cuda_stream)
+        plan.destroy()
+        results.append((C, ws))
+    torch.cuda.synchronize()
+    assert all(torch.equal(C.double(), want) for C, _ in results)
+    # a cut plan in a graph, replayed on other inputs
+    A, B = Packed(normal(20, 16384, seed=1), "mxf4"), Packed(normal(264, 16384, seed=2), "mxf4")
+    plan = nk.MxPlan(20, 264, 16384, format=nk.MXF4)
+    C, ws = torch.empty(20, 264, device="cuda"), torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(3):
+            plan.run(A.data, A.scales, B.data, B.scales, C, workspace=ws, stream=stream())
+    plan.destroy()
+    for seed in (5, 6):
+        other = Packed(normal(20, 16384, seed=seed), "mxf4")
+        A.data.copy_(other.data)
+        A.scales.copy_(other.scales)
+        graph.replay()
+        torch.cuda.synchronize()
+        y = other.values @ B.values.t()
+        assert ((C.double() - y).abs() <= bound(other.values, B.values, 16384, "f32", y)).all()
+
+
+def test_no_rows_and_refusals():
+    plan = nk.MxPlan(0, 64, 64)
+    plan.run(None, None, None, None, None, stream=stream())
+    plan.check()
+    for status, args in ((1, dict(rows=-1)), (1, dict(N=0)), (1, dict(K=0)), (3, dict(N=12)), (3, dict(ldc=68)), (1, dict(ldc=56)), (1, dict(format=2)),
+                         (2, dict(out_dtype=nk.S32)), (1, dict(epilogue=2)), (1, dict(beta=2)), (1, dict(groups=-1)), (2, dict(groups=2000)),
+                         (5, dict(device=99)), (2, dict(rows=(1 << 31) - 10))):
+        with pytest.raises(nk.NkError) as e:
+            nk.MxPlan(**{**dict(rows=32, N=64, K=64), **args})
+        assert e.value.status == status, args
+    A, B = Packed(normal(32, 64, seed=1), "nvf4"), Packed(normal(64, 64, seed=2), "nvf4")
+    C, off, bias = torch.empty(32, 64, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(64, device="cuda")
+    plan, grouped, mx = nk.MxPlan(32, 64, 64), nk.MxPlan(32, 64, 64, groups=1), nk.MxPlan(32, 64, 64, format=nk.MXF4)
+    for status, call in ((1, lambda: plan.run(None, A.scales, B.data, B.scales, C)), (1, lambda: plan.run(A.data, A.scales, B.data, None, C)),
+                         (1, lambda: plan.run(A.data, A.scales, B.data, B.scales, None)), (1, lambda: plan.run(A.data, A.scales, B.data, B.scales, C, offsets=off)),
+                         (1, lambda: grouped.run(A.data, A.scales, B.data, B.scales, C)), (1, lambda: plan.run(A.data, A.scales, B.data, B.scales, C, bias=bias)),
+                         (1, lambda: mx.run(A.data, A.scales, B.data, B.scales, C, scale_a=A.scale)), (3, lambda: plan.run(A.data[8:], A.scales, B.data, B.scales, C)),
+                         (3, lambda: plan.run(A.data, A.scales, B.data, B.scales, C.data_ptr() + 4))):
+        with pytest.raises(nk.NkError) as e:
+            call()
+        assert e.value.status == status
