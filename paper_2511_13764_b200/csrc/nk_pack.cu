@@ -38,7 +38,7 @@ static PackParams pack_params(const nk_pack_s* p) {
     r.groups = static_cast<int>(p->d.groups);
     r.length = p->length;
     r.row_tiles = p->row_tiles;
-    r.chunks = static_cast<int>(div_up(mx_padded(p->length), PACK_CHUNK));
+    r.chunks = static_cast<int>(div_up(mx_padded(p->length), pack_chunk(r.nv)));
     r.tiles = p->tiles;
     r.ldx = p->d.ldx;
     r.stride_x = p->d.stride_x;
@@ -72,7 +72,7 @@ nk_status_t nk_pack_create(const nk_pack_desc_t* desc, nk_pack_t* out) {
     const int64_t outer = d.transposed ? d.K : d.rows, length = d.transposed ? d.rows : d.K;
     // grids: along the rows (and reading back) tiles x pieces, below 2^31; along the columns pieces in y
     if (d.transposed && div_up(mx_padded(length), PACK_TURN) > 65535) return NK_ERR_UNSUPPORTED;
-    if ((outer / MX_TILE_ROWS + (d.groups ? d.groups : 1)) * div_up(mx_padded(length), PACK_CHUNK) >= (1ll << 31)) return NK_ERR_UNSUPPORTED;
+    if ((outer / MX_TILE_ROWS + (d.groups ? d.groups : 1)) * div_up(mx_padded(length), 128) >= (1ll << 31)) return NK_ERR_UNSUPPORTED;
     int sms = 0;
     nk_status_t s = usable_device(d.device, &sms);
     if (s != NK_OK) return s;
@@ -172,6 +172,7 @@ nk_status_t nk_pack_values(nk_pack_t p, const void* data, const void* scales, co
     r.data = static_cast<uint8_t*>(const_cast<void*>(data));
     r.scales = static_cast<uint8_t*>(const_cast<void*>(scales));
     r.values = Y;
+    r.chunks = static_cast<int>(div_up(mx_padded(p->length), PACK_LINE));
     const dim3 grid(static_cast<unsigned>(p->row_tiles) * r.chunks, 1, static_cast<unsigned>(p->d.batch));
     const cudaError_t e = launch_beside(values_kernel_of(p->d), grid, PACK_THREADS, 0, static_cast<cudaStream_t>(cuda_stream), r);
     return e == cudaSuccess ? NK_OK : p->cuda("values launch", e);

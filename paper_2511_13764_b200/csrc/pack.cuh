@@ -7,7 +7,7 @@
 // exactly where the quotient is, and on the quotient's side of b elsewhere.  So there is no division for an element.  FP32 x take one: a
 // correctly rounded x / d is b only where the quotient is (24 bits against 15: the next quotient is more than half a step away).
 //
-// A block of threads has a tile of scales' 128 rows, so that the scales of 256 of the contraction leave as 2 KB in one piece; a thread has
+// A block of threads has a tile of scales' 128 rows, so that the scales of a chunk of the contraction leave in one piece; a thread has
 // a block of the format.  Along the columns a tile of 128 x
 // 128 goes through shared memory, where a thread has a word of adjacent features.  Bound by memory.
 #pragma once
@@ -16,7 +16,10 @@
 
 namespace nk {
 
-constexpr int PACK_THREADS = 256, PACK_CHUNK = 256;      // along rows: threads, elements of the contraction to a block
+constexpr int PACK_THREADS = 256;
+// along rows: elements of the contraction to a block of threads (8192 x 4096: NVF4 17.8 us by 256, 18.8 by 128; MXF4 16.1, 15.1)
+__host__ __device__ constexpr int pack_chunk(bool nv) { return nv ? 256 : 128; }
+constexpr int PACK_LINE = 256;                           // reading back, likewise
 constexpr int PACK_TURN = 128;                           // along columns: a tile's side
 constexpr int PACK_MAX_GROUPS = 1024;
 
@@ -25,7 +28,7 @@ struct PackParams {
     int outer;                 // rows of the packed matrix (of one of the batch)
     int groups;                // 0: none
     int length;                // of the contraction
-    int chunks;                // of PACK_CHUNK along the contraction (not along the columns)
+    int chunks;                // pack_chunk or PACK_LINE along the contraction (not along the columns)
     int row_tiles, tiles;      // tiles of scales: along the rows of a matrix (groups: of all), along the contraction
     long long ldx, stride_x;   // in elements
     const void* x;
@@ -175,15 +178,15 @@ __device__ __forceinline__ uint32_t pack_most(const uint32_t (&w)[N]) {
 }
 template <int T>
 __device__ __forceinline__ uint32_t pack_one(uint32_t m) { return T == 0 ? m : max(m & 0xFFFFu, m >> 16); }
-// Along the rows: blockIdx.x 256 of the contraction of a tile's rows (pieces of the same rows side by side, so that blocks at work
+// Along the rows: blockIdx.x a chunk of the contraction of a tile's rows (pieces of the same rows side by side, so that blocks at work
 // together read whole rows), z the matrix.  A thread has a block: no exchange, one division.
 template <int T, bool NV>
 __global__ void __launch_bounds__(PACK_THREADS) pack_rows_kernel(const PackParams p) {
     constexpr int BLOCK = mx_block(NV), EIGHTS = BLOCK / 8, WORDS = T == 0 ? 8 : 4;
-    constexpr int LANES = PACK_CHUNK / BLOCK;            // threads of a row: 16 or 8
-    constexpr int STEP = PACK_THREADS / LANES;           // rows at a time: 16 or 32
-    constexpr int AHEAD = NV && T != 0 ? 4 : 2;          // of them on the way
-    constexpr int TILES = PACK_CHUNK / (4 * BLOCK);
+    constexpr int CHUNK = pack_chunk(NV), LANES = CHUNK / BLOCK;   // threads of a row: 16 or 4
+    constexpr int STEP = PACK_THREADS / LANES;           // rows at a time: 16 or 64
+    constexpr int AHEAD = (NV ? 4 : 2) / (T == 0 ? 2 : 1);         // of them on the way
+    constexpr int TILES = CHUNK / (4 * BLOCK);
     __shared__ int s_off[PACK_MAX_GROUPS + 1], s_found[2];
     __shared__ __align__(16) uint8_t s_scale[TILES * MX_TILE_BYTES];
     const int item = blockIdx.z;
@@ -195,7 +198,7 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_rows_kernel(const PackParam
     const PackScale s = pack_scale(p, item);
     for (int i = threadIdx.x; i < TILES * MX_TILE_BYTES / 4; i += PACK_THREADS) reinterpret_cast<uint32_t*>(s_scale)[i] = 0u;
     __syncthreads();
-    const int c = threadIdx.x % LANES, k = chunk * PACK_CHUNK + c * BLOCK, pitch = static_cast<int>(mx_padded(p.length) / 2);
+    const int c = threadIdx.x % LANES, k = chunk * CHUNK + c * BLOCK, pitch = static_cast<int>(mx_padded(p.length) / 2);
     const int eights = min(EIGHTS, (p.length - k) / 8);  // (the length is a multiple of 8; 0 or less: none)
     const bool kept = k < 2 * pitch;
     const size_t x0 = item * static_cast<size_t>(p.stride_x) + rows.first * static_cast<size_t>(p.ldx) + k;
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_rows_kernel(const PackParam
 
 // Along the columns: blockIdx.x 128 features (a tile's rows), y 128 rows of X, z the matrix.
 template <int T, bool NV>
-__global__ void __launch_bounds__(PACK_THREADS) pack_columns_kernel(const PackParams p) {
+__global__ void __launch_bounds__(PACK_THREADS, 4) pack_columns_kernel(const PackParams p) {
     constexpr int BLOCK = mx_block(NV), BLOCKS = PACK_TURN / BLOCK;           // of the contraction
     constexpr int WORDS = T == 0 ? PACK_TURN : PACK_TURN / 2;                 // 32-bit words of a row of the tile
     constexpr int EACH = T == 0 ? 1 : 2;                                      // features of a word
@@ -344,9 +347,9 @@ __host__ __device__ constexpr int pack_columns_smem(int type) { return PACK_TURN
 // elements go by way of shared memory, from where consecutive lanes store consecutive ones.
 template <int T, bool NV>
 __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackParams p) {
-    constexpr int LANES = NV ? 2 : 4, TILES = PACK_CHUNK / (4 * mx_block(NV)), AHEAD = 4;
+    constexpr int LANES = NV ? 2 : 4, TILES = PACK_LINE / (4 * mx_block(NV)), AHEAD = 4;
     __shared__ int s_off[PACK_MAX_GROUPS + 1], s_found[2];
-    __shared__ __align__(16) float s_line[PACK_THREADS / 32][PACK_CHUNK];
+    __shared__ __align__(16) float s_line[PACK_THREADS / 32][PACK_LINE];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, item = blockIdx.z;
     const int tile = blockIdx.x / p.chunks, chunk = blockIdx.x - tile * p.chunks;
     launch_wait();
@@ -354,7 +357,7 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackPar
     const PackRows rows = pack_rows(p, tile, s_off, s_found);
     if (rows.count <= 0) return;
     const float t = NV && p.scale ? p.scale[item] : 1.0f;
-    const int k0 = chunk * PACK_CHUNK, k = k0 + lane * 8, pitch = static_cast<int>(mx_padded(p.length) / 2), c = lane / LANES;
+    const int k0 = chunk * PACK_LINE, k = k0 + lane * 8, pitch = static_cast<int>(mx_padded(p.length) / 2), c = lane / LANES;
     const bool whole = p.length % 8 == 0, there = k < p.length;
     const uint8_t* data = p.data + (static_cast<size_t>(item) * p.outer + rows.first) * pitch + k / 2;
     const uint8_t* scales = p.scales + ((static_cast<size_t>(item) * p.row_tiles + tile) * p.tiles + chunk * TILES + c / 4) * MX_TILE_BYTES + (c & 3);
