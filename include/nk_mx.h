@@ -98,8 +98,9 @@ nk_status_t nk_pack_destroy(nk_pack_t plan);
  * dY^T . X the same with both packed along their columns.  By expert: dX likewise; dW_g contracts over ragged rows, which have
  * no whole blocks, and is nk_grouped's (NK_GROUPED_WEIGHTS, 16-bit operands).
  *
- * The tensor core drops low bits of its FP32 accumulator at every step of 64 elements, so the accumulator is emptied into an FP32 sum every
- * 2048 elements of the contraction for an FP32 C, every 16384 for a 16-bit one.
+ * The tensor core drops low bits of its FP32 accumulator at every step of 64 elements, so longer contractions than 8192 (FP32 C) or 16384
+ * (16-bit C) are FP32 sums of accumulators of 4096 or 16384.  Measured against 64 bits (2-norm, FP32 C): normal operands 2.5e-8,
+ * products of one sign up to 1e-7 however many, operands whose blocks differ by ten powers of two and more up to 1.2e-6.
  */
 typedef struct nk_mx_s* nk_mx_t;
 

@@ -535,23 +535,38 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                 for (int n = 0; n < all; ++n) {
                     if (!await()) { ok = false; break; }
                     const uint32_t taddr = tmem_base + (local & 1) * apart + lane_addr + set * 32;
+                    const bool end = n == all - 1;
+                    auto take = [&](int q) {
+                        if (q >= mine) return;
+                        uint32_t v[32];
+                        tmem_ld_32x32(taddr + q * 64, v);
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (q >= mine) continue;
-#pragma unroll
-                        for (int b = 0; b < 32; b += 16) {
-                            uint32_t v[16];
-                            tmem_ld_32x16(taddr + q * 64 + b, v);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) sum[q][b + j] += __uint_as_float(v[j]);
-                            if (n == all - 1) tmem_st_32x16(taddr + q * 64 + b, sum[q] + b);
+                        for (int j = 0; j < 32; ++j) sum[q][j] += __uint_as_float(v[j]);
+                        if (end) {
+                            tmem_st_32x16(taddr + q * 64, sum[q]);
+                            tmem_st_32x16(taddr + q * 64 + 16, sum[q] + 16);
                         }
+                    };
+                    auto give = [&](bool now) { if (now && !end) release(); };
+                    // the shared columns first: the last ones of the first accumulator, the first ones of the second
+                    if (sharing && (local & 1) == 0) {
+                        take(3);
+                        take(2);
+                        give(SHARED >= 128);
+                        take(1);
+                        give(SHARED < 128);
+                        take(0);
+                    } else {
+                        take(0);
+                        take(1);
+                        give(sharing && SHARED >= 128);
+                        take(2);
+                        give(sharing && SHARED < 128);
+                        take(3);
+                        give(!sharing);
                     }
-                    if (n < all - 1) {
-                        release();
-                        ++local;
-                    }
+                    if (!end) ++local;
                 }
                 if (!ok) break;
                 tmem_st_wait();

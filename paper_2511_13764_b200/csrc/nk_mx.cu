@@ -98,8 +98,8 @@ nk_status_t nk_mx_create(const nk_mx_desc_t* desc, nk_mx_t* out) {
     DeviceGuard guard(d.device);
     if (!encode_tiled()) { delete p; return NK_ERR_CUDA; }
     const MxOut type = d.out_dtype == NK_F32 ? MX_OUT_F32 : d.out_dtype == NK_BF16 ? MX_OUT_BF16 : MX_OUT_F16;
-    p->chunk = type == MX_OUT_F32 ? MX_CHUNK : MX_CHUNK_16;
-    const bool sums = div_up(d.K, MX_BK) > p->chunk;
+    const bool sums = div_up(d.K, MX_BK) > (type == MX_OUT_F32 ? MX_WHOLE : MX_WHOLE_16);
+    p->chunk = type == MX_OUT_F32 ? MX_CHUNK : MX_WHOLE_16;
     bool uncut = false;
     p->kernel = d.format == NK_NVF4 ? mx_kernel_nv(type, sums) : mx_kernel_mx(type, sums);
     if (cudaFuncSetAttribute(p->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MX_SMEM) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
