@@ -43,13 +43,19 @@ __host__ __device__ constexpr int mx_place(bool nv) { return nv ? 48 : 24; }
 __host__ __device__ constexpr int mx_scales(bool nv) { return 512 - mx_places(nv) * mx_place(nv); }    // first column of the scales
 __host__ __device__ constexpr int mx_shared(bool nv) { return mx_scales(nv) - MX_TILE; }               // first of the columns that both accumulators have
 
+// MODE: whole tiles only; tiles may be cut; they may be cut and be sums of several accumulators.
+// A launch of 384 threads has 168 registers for each.  Sums take 128, so the epilogue's 256 threads get some of the others' (208 x 256 + 88 x 128 = 168 x
+// 384); the other kernels must do without, as the loops of the other warps are slower for it (4096 x 1024 x 4096 16.0 us instead of 14.0),
+// and without spilling: there is next to no L1 beside this much shared memory (20 spilled registers: 8192 x 4096 x 256 38 us instead of 25).
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
 
-template <bool NV, int OUT, bool SUMS>
+template <bool NV, int OUT, int MODE>
 __global__ void __launch_bounds__(MX_THREADS, 1) __cluster_dims__(2, 1, 1)
 mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams p) {
     constexpr bool OUT16 = OUT != MX_OUT_F32, F16 = OUT == MX_OUT_F16;
+    constexpr int SIZE = OUT16 ? 2 : 4;
+    constexpr bool SUMS = MODE == MX_SUMS, CUT = MODE != MX_WHOLE_TILES;
     constexpr int S_BOX = NV ? 2048 : 1024;               // scales of 128 rows and a k-block
     constexpr int PLACES = mx_places(NV), PLACE = mx_place(NV), SCALES = mx_scales(NV), SHARED = mx_shared(NV);
     extern __shared__ uint8_t smem_raw[];
@@ -147,7 +153,6 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         apart = sharing ? SHARED : 128;
     };
 
-    // Sums of accumulators take 128 registers of a thread: the warps without any leave theirs (208 x 256 + 80 x 128 <= 168 x 384).
     if (SUMS && warp >= 8) fewer_registers();
     if (warp == 10) {
         // ------------------------------------------------ scales into tensor memory (leader only)
@@ -249,7 +254,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         // tile counts `padded` k-blocks there, a whole number of shares.
         const int from = tiles / num_pairs * num_pairs;
         int tail_from = tiles, tail_len = 0, share = 1, padded = p.kb_total;
-        if (p.parts > 1) {
+        if (CUT && p.parts > 1) {
             tail_from = from;
             share = (p.kb_total + p.parts - 1) / p.parts;
             padded = (p.kb_total + share - 1) / share * share;
@@ -264,7 +269,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             if (next_tile < tail_from) {
                 tile = next_tile;
                 next_tile += num_pairs;
-            } else if (tail_from < tiles && x < tail_hi) {
+            } else if (CUT && tail_from < tiles && x < tail_hi) {
                 const int rel = x / padded;
                 tile = tail_from + rel;
                 at = x - rel * padded;
@@ -300,7 +305,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                 u.kb1 = p.kb_total;
                 u.parts = 1;
                 u.part = 0;
-                if (tile >= tail_from) {
+                if (CUT && tile >= tail_from) {
                     const int start = x - at;             // the tile's place in the tail
                     u.kb0 = min(at, p.kb_total);
                     u.kb1 = min(p.kb_total, at + tail_hi - x);
@@ -441,7 +446,9 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
         int local = 0;
         bool ok = true;
+        const float scale_a = p.scale_a ? __ldg(p.scale_a) : 1.0f;
         float alpha = 1.0f;
+        int group = -1;                                   // that alpha is of
         MxUnit u = {};
         auto await = [&]() {
             const int acc = local & 1;
@@ -468,58 +475,66 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
 #pragma unroll
             for (int j = 0; j < 8; ++j) __stcg(dst + j * 32, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
         };
-        // One 32 x 32 piece of C (columns c .. c + 31 of the tile, this warp's 32 features): lane l has feature l, v[j] is row j.  A store
-        // writes 64 bytes of two rows, or 128 of one.  (By way of shared memory and TMA stores, which wait behind the loads of the ring,
-        // 8192 x 4096 x 1024 took 42 us.)
+        // One 32 x 32 piece of C (columns c .. c + 31 of the tile, this warp's 32 features): lane l has feature l, v[j] is row j.  A store writes 32
+        // consecutive features of a row.  (8192 x 4096 x 256 with 16-bit results: 20 us; pairs of features exchanged by shuffles and stored as
+        // words, or transposed by way of shared memory into 16-byte stores, 25; by TMA stores, which wait behind the ring's loads, 38.)
+        auto load = [&](uint32_t taddr, uint32_t (&v)[32]) {
+            tmem_ld_32x32(taddr, v);
+            tmem_ld_wait();
+        };
         auto deliver = [&](float (&v)[32], int c) {
             const int n = min(32, u.cols - c), i0 = u.i0 + static_cast<int>(rank) * 128 + quarter * 32;
-            const size_t row0 = static_cast<size_t>(u.c0 + c);
-            const bool live = i0 + lane < p.I;
-            const float bias = p.bias && live ? __ldg(p.bias + static_cast<size_t>(u.g) * p.I + i0 + lane) : 0.0f;
+            const size_t base = static_cast<size_t>(u.c0 + c) * p.ldc + i0;
+            if (p.bias) {
+                const float bias = i0 + lane < p.I ? __ldg(p.bias + static_cast<size_t>(u.g) * p.I + i0 + lane) : 0.0f;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], alpha, bias);
-            const size_t base = row0 * p.ldc + i0;
+                for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], alpha, bias);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] *= alpha;
+            }
             if (p.beta) {
-                const uint16_t* c16 = static_cast<const uint16_t*>(p.C) + base + lane;
-                const float* c32 = static_cast<const float*>(p.C) + base + lane;
+                // C's old values, row after row (the pointer is kept from being computed for all of them at once, which spills)
+                const char* old = static_cast<const char*>(p.C) + (base + lane) * SIZE;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
-                    if (live && j < n) v[j] += OUT16 ? half_bits_to_f32(*c16, F16) : *c32;
-                    c16 += p.ldc;
-                    c32 += p.ldc;
+                    if (j % 8 == 0) asm volatile("" : "+l"(old)::"memory");
+                    if (j < n && i0 + lane < p.I) v[j] += OUT16 ? half_bits_to_f32(*reinterpret_cast<const uint16_t*>(old), F16) : *reinterpret_cast<const float*>(old);
+                    old += p.ldc * SIZE;
                 }
             }
             if (p.relu) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = v[j] < 0.0f ? 0.0f : v[j];          // (a NaN stays)
             }
-            if (OUT16) {
-                // a lane packs its feature of rows j and j + 1 and exchanges words with its neighbour: even lanes then hold row j of
-                // features (l, l + 1), odd lanes row j + 1 of (l - 1, l)
-                const int odd = lane & 1;
-                const uint32_t pick = odd ? 0x3276u : 0x5410u;
-                uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.C) + base + odd * p.ldc + (lane & 30));
+            const bool live = i0 + lane < p.I;
+            char* dst = static_cast<char*>(p.C) + (base + lane) * SIZE;
+            uint32_t w[16];                               // 16 bits: rows 2 j and 2 j + 1
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (j % 4 == 0 && 2 * j >= n) break;
-                    const uint32_t w = pack_half2(v[2 * j], v[2 * j + 1], F16);
-                    const uint32_t got = __shfl_xor_sync(~0u, w, 1);
-                    if (live && 2 * j + odd < n) *dst = __byte_perm(w, got, pick);
-                    dst += p.ldc;                         // (two rows, in words)
-                }
+            for (int j = 0; OUT16 && j < 16; ++j) w[j] = pack_half2(v[2 * j], v[2 * j + 1], F16);
+            auto put = [&](int j) {
+                if (OUT16) *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(j & 1 ? w[j >> 1] >> 16 : w[j >> 1]);
+                else *reinterpret_cast<float*>(dst) = v[j];
+                dst += p.ldc * SIZE;
+            };
+            if (n == 32 && i0 + 32 <= p.I) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) put(j);
             } else {
-                float* dst = static_cast<float*>(p.C) + base + lane;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
                     if (j % 8 == 0 && j >= n) break;
-                    if (live && j < n) *dst = v[j];
-                    dst += p.ldc;
+                    if (live && j < n) put(j);
+                    else dst += p.ldc * SIZE;
                 }
             }
         };
         while (ok && next(u)) {
             ring();
-            alpha = (p.scale_a ? __ldg(p.scale_a) : 1.0f) * (p.scale_b ? __ldg(p.scale_b + u.g) : 1.0f);
+            if (u.g != group) {                           // (a load's latency for each tile otherwise)
+                group = u.g;
+                alpha = scale_a * (p.scale_b ? __ldg(p.scale_b + group) : 1.0f);
+            }
             // the accumulators that make up the unit
             const int blocks = u.kb1 - u.kb0, all = SUMS ? (blocks + p.chunk - 1) / p.chunk : 1;
             const int mine = (u.cols - set * 32 + 63) >> 6;   // pieces of this warp: columns set * 32 + 64 q
@@ -573,25 +588,25 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             } else if (!await()) {
                 break;
             }
-            // Pieces from tensor memory to C, the shared columns' first.  Of a cut tile they go to this part's slab; then one count for each of
-            // them says which have all their parts, and those are added up.
+            // Pieces from tensor memory to C, the shared columns' first.
             const uint32_t taddr = tmem_base + (local & 1) * apart + lane_addr + set * 32;
             const bool down = sharing && (local & 1) == 0;
+            auto piece = [&](int i) { return down ? mine - 1 - i : i; };
             const int given = !sharing ? 3 : SHARED >= 128 ? 1 : 2;
             unsigned int last = ~0u;
+            // Of a cut tile they go to this part's slab; then one count for each of them says which have all their parts, and those are added up.
 #pragma unroll 1
-            for (int pass = u.parts > 1 ? 0 : 1; pass < 2; ++pass) {
-                const bool gather = pass == 1 && u.parts > 1;
+            for (int pass = CUT && u.parts > 1 ? 0 : 1; pass < 2; ++pass) {
+                const bool gather = CUT && pass == 1 && u.parts > 1;
 #pragma unroll 1
                 for (int i = 0; i < 4; ++i) {
-                    const int q = down ? 3 - i : i, c = set * 32 + q * 64;
-                    const bool there = q < mine && ((last >> q) & 1u);
+                    const bool there = i < mine && ((last >> piece(i)) & 1u);
+                    const int c = set * 32 + piece(i) * 64;
                     float f[32];
                     if (!gather) {
                         if (there) {
                             uint32_t v[32];
-                            tmem_ld_32x32(taddr + q * 64, v);
-                            tmem_ld_wait();
+                            load(taddr + piece(i) * 64, v);
 #pragma unroll
                             for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
                         }
@@ -602,7 +617,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                     } else if (there) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) f[j] = 0.0f;
-#pragma unroll 2
+#pragma unroll 1
                         for (int s = 0; s < u.parts; ++s) {
                             const float4* src = slab_of(s, c);
                             float4 y[8];
@@ -613,10 +628,13 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                         }
                     }
                     if (!there) continue;
-                    if (pass == 0) to_slab(f, c);
-                    else deliver(f, c);
+                    if (CUT && pass == 0) {
+                        to_slab(f, c);
+                    } else {
+                        deliver(f, c);
+                    }
                 }
-                if (pass == 0) {
+                if (CUT && pass == 0) {
                     __syncwarp();
                     bool done = false;
                     if (lane < mine) {

@@ -52,6 +52,7 @@ struct MxMaps {
     CUtensorMap sa, sb;    // scales: boxes of the tiles of one k-block
 };
 
+enum MxMode { MX_WHOLE_TILES = 0, MX_CUT = 1, MX_SUMS = 2 };   // (sums: may be cut, too)
 enum MxOut { MX_OUT_F32 = 0, MX_OUT_BF16 = 1, MX_OUT_F16 = 2 };
 // K-blocks to an accumulator: contractions of more are summed in FP32, FP32 results by MX_CHUNK.  (What the tensor core drops of a sum of 4-bit
 // products is little, as they have few bits: against 64 bits, relative 2-norm, 8192 products of one sign are 5.3e-8 off in one accumulator, 4.9e-8 in
@@ -64,7 +65,7 @@ constexpr int MX_WHOLE = 32, MX_WHOLE_16 = 64, MX_CHUNK = 16;
 inline uint32_t mx_idesc(bool nv) { return 1u << 7 | 1u << 10 | (nv ? 0u : 1u << 23) | (256u >> 7) << 27; }
 
 typedef void (*MxFunction)(MxMaps, MxParams);
-MxFunction mx_kernel_nv(MxOut out, bool sums);         // (mx_nv.cu, mx_mx.cu)
-MxFunction mx_kernel_mx(MxOut out, bool sums);
+MxFunction mx_kernel_nv(MxOut out, MxMode mode);       // (mx_nv.cu, mx_mx.cu)
+MxFunction mx_kernel_mx(MxOut out, MxMode mode);
 
 }  // namespace nk

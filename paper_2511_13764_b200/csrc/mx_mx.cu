@@ -3,10 +3,12 @@
 
 namespace nk {
 
-MxFunction mx_kernel_mx(MxOut out, bool sums) {
-    if (out == MX_OUT_F32) return sums ? mx_kernel<false, MX_OUT_F32, true> : mx_kernel<false, MX_OUT_F32, false>;
-    if (out == MX_OUT_BF16) return sums ? mx_kernel<false, MX_OUT_BF16, true> : mx_kernel<false, MX_OUT_BF16, false>;
-    return sums ? mx_kernel<false, MX_OUT_F16, true> : mx_kernel<false, MX_OUT_F16, false>;
+template <int OUT>
+static MxFunction of_mode(MxMode mode) {
+    return mode == MX_SUMS ? mx_kernel<false, OUT, MX_SUMS> : mode == MX_CUT ? mx_kernel<false, OUT, MX_CUT> : mx_kernel<false, OUT, MX_WHOLE_TILES>;
+}
+MxFunction mx_kernel_mx(MxOut out, MxMode mode) {
+    return out == MX_OUT_F32 ? of_mode<MX_OUT_F32>(mode) : out == MX_OUT_BF16 ? of_mode<MX_OUT_BF16>(mode) : of_mode<MX_OUT_F16>(mode);
 }
 
 }  // namespace nk

@@ -101,8 +101,6 @@ nk_status_t nk_mx_create(const nk_mx_desc_t* desc, nk_mx_t* out) {
     const bool sums = div_up(d.K, MX_BK) > (type == MX_OUT_F32 ? MX_WHOLE : MX_WHOLE_16);
     p->chunk = type == MX_OUT_F32 ? MX_CHUNK : MX_WHOLE_16;
     bool uncut = false;
-    p->kernel = d.format == NK_NVF4 ? mx_kernel_nv(type, sums) : mx_kernel_mx(type, sums);
-    if (cudaFuncSetAttribute(p->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MX_SMEM) != cudaSuccess) { delete p; return NK_ERR_CUDA; }
     p->pairs = sms / 2;
     p->slab_cols = static_cast<int>(d.rows >= MX_TILE ? MX_TILE : div_up(d.rows, 32) * 32);
     p->parts = 1;
@@ -114,6 +112,13 @@ nk_status_t nk_mx_create(const nk_mx_desc_t* desc, nk_mx_t* out) {
             uncut = true;
             mx_tiles_of(d.rows, tiles_i, kbs, p->pairs, false, &p->width, &p->parts);
         }
+    }
+    const MxMode mode = sums ? MX_SUMS : p->parts > 1 ? MX_CUT : MX_WHOLE_TILES;
+    p->kernel = d.format == NK_NVF4 ? mx_kernel_nv(type, mode) : mx_kernel_mx(type, mode);
+    if (cudaFuncSetAttribute(p->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MX_SMEM) != cudaSuccess) {
+        give_split_slot(d.device, p->split_slot, false, false);
+        delete p;
+        return NK_ERR_CUDA;
     }
     snprintf(p->name, sizeof(p->name), "mx_%s%s_256x256x256_pair%s", d.format == NK_NVF4 ? "nvf4" : "mxf4", d.groups ? "_grouped" : "", uncut ? "_uncut" : "");
     *out = p;
