@@ -227,10 +227,10 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                 n += __shfl_xor_sync(~0u, n, 4);
                 n += __shfl_xor_sync(~0u, n, 8);
                 n += __shfl_xor_sync(~0u, n, 16);
-                const unsigned waves = (n * p.tiles_i + num_pairs - 1) / num_pairs;
-                const unsigned t = waves * (p.kb_total * mx_block_clocks(w) + MX_TILE_CLOCKS) + MX_ROW_CLOCKS * w;
-                // the smallest; of equals the widest
-                const unsigned won = __reduce_min_sync(~0u, (min(t, 0x1FFFFFFFu) << 3) | (4u - static_cast<unsigned>(w >> 6)));
+                const float waves = static_cast<float>((n * p.tiles_i + num_pairs - 1) / num_pairs);
+                const float t = waves * (static_cast<float>(p.kb_total) * static_cast<float>(mx_block_clocks(w)) + MX_TILE_CLOCKS) + static_cast<float>(MX_ROW_CLOCKS * w);
+                // the smallest; of equals the widest: a time's upper bits, then the width
+                const unsigned won = __reduce_min_sync(~0u, (__float_as_uint(t) & ~7u) | (4u - static_cast<unsigned>(w >> 6)));
                 width = static_cast<int>(4u - (won & 7u)) << 6;
             }
         }

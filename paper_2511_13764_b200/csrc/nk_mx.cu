@@ -10,7 +10,8 @@ namespace nk {
 // bytes [outer][mid][inner] as boxes of `box_mid` rows of 128 bytes, swizzled; what lies outside arrives as zeros
 static bool encode_packed(CUtensorMap* m, const void* base, int64_t inner, int64_t mid, int64_t outer, int box_mid) {
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(mid), static_cast<cuuint64_t>(outer)};
-    cuuint64_t strides[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(inner * mid)};
+    // (the outer stride of a single matrix only has to be legal)
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer > 1 ? inner * mid : inner)};
     cuuint32_t box[3] = {128, static_cast<cuuint32_t>(box_mid), 1};
     cuuint32_t es[3] = {1, 1, 1};
     return encode_tiled()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
