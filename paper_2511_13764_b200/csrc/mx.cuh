@@ -44,11 +44,11 @@ __host__ __device__ constexpr int mx_scales(bool nv) { return 512 - mx_places(nv
 __host__ __device__ constexpr int mx_shared(bool nv) { return mx_scales(nv) - MX_TILE; }               // first of the columns that both accumulators have
 
 // MODE: whole tiles only; tiles may be cut; they may be cut and be sums of several accumulators.
-// A launch of 384 threads has 168 registers for each.  Sums take 128, so the epilogue's 256 threads get some of the others' (208 x 256 + 88 x 128 = 168 x
-// 384); the other kernels must do without, as the loops of the other warps are slower for it (4096 x 1024 x 4096 16.0 us instead of 14.0),
+// A launch of 384 threads has 168 registers for each.  Sums take 128, so the epilogue's 256 threads get some of the others' (216 x 256 + 72 x 128 = 168 x
+// 384; 4096 x 4096 x 16384 122 us, with 208 and 88 127, without 155, in 16 bits and one accumulator 104); the other kernels must do without, as the loops of the other warps are slower for it (4096 x 1024 x 4096 16.0 us instead of 14.0),
 // and without spilling: there is next to no L1 beside this much shared memory (20 spilled registers: 8192 x 4096 x 256 38 us instead of 25).
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
 
 template <bool NV, int OUT, int MODE>
 __global__ void __launch_bounds__(MX_THREADS, 1) __cluster_dims__(2, 1, 1)
