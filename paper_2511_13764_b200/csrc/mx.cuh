@@ -16,8 +16,8 @@
 // Tiles begin at multiples of 64 rows of a group (or at its first row): scales of 64 rows are two columns, by which the place of the
 // rows' scales moves where a tile begins in the middle of 128.
 //
-// Warps: 0-7 epilogue (warps 0-3 take the even 32-column pieces, 4-7 the odd ones), 8 TMA producer, 9 MMA issuer, 10 copies the
-// scales, 11 scheduler.
+// Warps: eight or sixteen of the epilogue (see mx_sets), in sets of four for the quarters of the lanes, which take the 32-column pieces in turn; then
+// the TMA producer, the MMA issuer, one that copies the scales, the scheduler.
 // All waits are bounded (see mbar_wait).
 #pragma once
 #include "grouped.cuh"
@@ -51,11 +51,13 @@ __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
 
 template <bool NV, int OUT, int MODE>
-__global__ void __launch_bounds__(MX_THREADS, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(mx_threads(MODE, NV), 1) __cluster_dims__(2, 1, 1)
 mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams p) {
     constexpr bool OUT16 = OUT != MX_OUT_F32, F16 = OUT == MX_OUT_F16;
     constexpr int SIZE = OUT16 ? 2 : 4;
     constexpr bool SUMS = MODE == MX_SUMS, CUT = MODE != MX_WHOLE_TILES;
+    constexpr int SETS = mx_sets(MODE, NV), EPILOGUE = 4 * SETS, SPAN = 32 * SETS;       // sets of epilogue warps, warps, columns between a warp's pieces
+    constexpr int PRODUCER = EPILOGUE, ISSUER = EPILOGUE + 1, COPIER = EPILOGUE + 2, SCHEDULER = EPILOGUE + 3;
     constexpr int S_BOX = NV ? 2048 : 1024;               // scales of 128 rows and a k-block
     constexpr int PLACES = mx_places(NV), PLACE = mx_place(NV), SCALES = mx_scales(NV), SHARED = mx_shared(NV);
     extern __shared__ uint8_t smem_raw[];
@@ -95,11 +97,11 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         while (clock64() - t0 < (1ll << 20)) __nanosleep(1000);
     };
 
-    if (warp == 8) {
+    if (warp == PRODUCER) {
         for (int n = lane; n < NB; n += 32) {
-            // tempty: one arrival per epilogue warp of both CTAs; uempty: producer, epilogue warps, the leader's warps 9 and 10
-            const uint32_t count = n >= 2 * MS + 2 && n < 2 * MS + 4                                      ? 16
-                                   : n >= 2 * MS + 4 + MX_UNITS && n < 2 * MS + 4 + 2 * MX_UNITS ? 9 + 2 * (rank == 0)
+            // tempty: one arrival per epilogue warp of both CTAs; uempty: producer, epilogue warps, the leader's issuer and copier
+            const uint32_t count = n >= 2 * MS + 2 && n < 2 * MS + 4                                      ? 2 * EPILOGUE
+                                   : n >= 2 * MS + 4 + MX_UNITS && n < 2 * MS + 4 + 2 * MX_UNITS ? EPILOGUE + 1 + 2 * (rank == 0)
                                                                                                          : 1;
             mbar_init(bar_base + 8u * n, count);
         }
@@ -112,7 +114,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         if (lane == 8) tma_prefetch_desc(&maps.a);
         if (lane == 9) tma_prefetch_desc(&maps.sa);
         if (lane == 10) tma_prefetch_desc(&maps.sb);
-    } else if (warp == 9) {
+    } else if (warp == ISSUER) {
         tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
         tmem_relinquish_pair();
     }
@@ -121,12 +123,12 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
     // up to here the launch may have run beside the end of the one before it in the stream
     launch_wait();
     launch_next();
-    for (int g = threadIdx.x; g <= p.groups; g += MX_THREADS) s_row[g] = p.offsets ? p.offsets[g] : g == 0 ? 0 : p.rows;
+    for (int g = threadIdx.x; g <= p.groups; g += mx_threads(MODE, NV)) s_row[g] = p.offsets ? p.offsets[g] : g == 0 ? 0 : p.rows;
     __syncthreads();
     cluster_wait();          // the barriers of both CTAs are initialised
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
-    if (warp == 9 && rank == 1 && lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(peer_ready_bar, 0));
+    if (warp == ISSUER && rank == 1 && lane == 0) mbar_arrive_cluster_cta_release(map_to_cta(peer_ready_bar, 0));
 
     // the roles' view of the schedule: wait for the next unit, read it, give its place back
     int unit_at = 0;
@@ -153,8 +155,8 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         apart = sharing ? SHARED : 128;
     };
 
-    if (SUMS && warp >= 8) fewer_registers();
-    if (warp == 10) {
+    if (SUMS && warp >= EPILOGUE) fewer_registers();
+    if (warp == COPIER) {
         // ------------------------------------------------ scales into tensor memory (leader only)
         if (rank == 0) {
             const uint64_t ds = make_smem_desc(smem_base, 16, 128, 0);
@@ -199,7 +201,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             }
             if (*abort_flag) settle();
         }
-    } else if (warp == MX_THREADS / 32 - 1) {
+    } else if (warp == SCHEDULER) {
         // ------------------------------------------------ scheduler (both CTAs of a pair come to the same schedule)
         // offsets that break their rule are clamped to the running maximum
         bool bad = false;
@@ -327,7 +329,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             __syncwarp();
             if (++unit_at == MX_UNITS) { unit_at = 0; unit_phase ^= 1u; }
         }
-    } else if (warp == 8) {
+    } else if (warp == PRODUCER) {
         // ------------------------------------------------ TMA producer (both CTAs)
         const uint32_t lead_full0 = map_to_cta(full_bar(0), 0);
         const uint32_t elected = elect_one();
@@ -367,7 +369,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             if (++stage == S) { stage = 0; phase ^= 1u; }
         }
         if (!ok) settle();
-    } else if (warp == 9) {
+    } else if (warp == ISSUER) {
         // ------------------------------------------------ MMA issuer (leader only)
         if (rank == 0) {
             const uint64_t da = make_smem_desc(smem_base, 16, 1024, 2);
@@ -478,10 +480,6 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         // One 32 x 32 piece of C (columns c .. c + 31 of the tile, this warp's 32 features): lane l has feature l, v[j] is row j.  A store writes 32
         // consecutive features of a row.  (8192 x 4096 x 256 with 16-bit results: 20 us; pairs of features exchanged by shuffles and stored as
         // words, or transposed by way of shared memory into 16-byte stores, 25; by TMA stores, which wait behind the ring's loads, 38.)
-        auto load = [&](uint32_t taddr, uint32_t (&v)[32]) {
-            tmem_ld_32x32(taddr, v);
-            tmem_ld_wait();
-        };
         auto deliver = [&](float (&v)[32], int c) {
             const int n = min(32, u.cols - c), i0 = u.i0 + static_cast<int>(rank) * 128 + quarter * 32;
             const size_t base = static_cast<size_t>(u.c0 + c) * p.ldc + i0;
@@ -537,7 +535,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             }
             // the accumulators that make up the unit
             const int blocks = u.kb1 - u.kb0, all = SUMS ? (blocks + p.chunk - 1) / p.chunk : 1;
-            const int mine = (u.cols - set * 32 + 63) >> 6;   // pieces of this warp: columns set * 32 + 64 q
+            const int mine = (u.cols - set * 32 + SPAN - 1) / SPAN;   // pieces of this warp: columns set * 32 + SPAN q
             if (SUMS && all > 1) {
                 // Accumulators are added in registers; the last one's place takes the sum, so that there is one way from here to C.  (Code that
                 // runs once a launch costs its fetch: with a copy of that way for each piece of a sum this was 7 us slower.)
@@ -592,68 +590,74 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
             const uint32_t taddr = tmem_base + (local & 1) * apart + lane_addr + set * 32;
             const bool down = sharing && (local & 1) == 0;
             auto piece = [&](int i) { return down ? mine - 1 - i : i; };
-            const int given = !sharing ? 3 : SHARED >= 128 ? 1 : 2;
-            unsigned int last = ~0u;
-            // Of a cut tile they go to this part's slab; then one count for each of them says which have all their parts, and those are added up.
-#pragma unroll 1
-            for (int pass = CUT && u.parts > 1 ? 0 : 1; pass < 2; ++pass) {
-                const bool gather = CUT && pass == 1 && u.parts > 1;
+            auto column = [&](int i) { return set * 32 + piece(i) * SPAN; };
+            auto take = [&](float (&v)[32], int i) { tmem_ld_32x32(taddr + piece(i) * SPAN, reinterpret_cast<uint32_t (&)[32]>(v)); };
+            auto emit = [&](float (&v)[32], int i) {
+                if (CUT && u.parts > 1) to_slab(v, column(i));
+                else deliver(v, column(i));
+            };
+            float f[32];
+            if constexpr (SETS == 2) {                    // four pieces at most
 #pragma unroll 1
                 for (int i = 0; i < 4; ++i) {
-                    const bool there = i < mine && ((last >> piece(i)) & 1u);
-                    const int c = set * 32 + piece(i) * 64;
-                    float f[32];
-                    if (!gather) {
-                        if (there) {
-                            uint32_t v[32];
-                            load(taddr + piece(i) * 64, v);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
-                        }
-                        if (i == given) {
-                            release();
-                            ++local;
-                        }
-                    } else if (there) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) f[j] = 0.0f;
-#pragma unroll 1
-                        for (int s = 0; s < u.parts; ++s) {
-                            const float4* src = slab_of(s, c);
-                            float4 y[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) y[j] = __ldcg(src + j * 32);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) f[4 * j] += y[j].x, f[4 * j + 1] += y[j].y, f[4 * j + 2] += y[j].z, f[4 * j + 3] += y[j].w;
-                        }
+                    if (i < mine) {
+                        take(f, i);
+                        tmem_ld_wait();
                     }
-                    if (!there) continue;
-                    if (CUT && pass == 0) {
-                        to_slab(f, c);
-                    } else {
-                        deliver(f, c);
-                    }
+                    if (i == (!sharing ? 3 : SHARED >= 128 ? 1 : 2)) release();
+                    if (i < mine) emit(f, i);
                 }
-                if (CUT && pass == 0) {
-                    __syncwarp();
-                    bool done = false;
-                    if (lane < mine) {
-                        unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + set + 2 * lane;
-                        const unsigned int old = (atomic_add_acq_rel(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
-                        done = old == static_cast<unsigned>(u.parts) - 1u;
-                        if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
+            } else {
+                // two pieces at most, and no more than one of them with shared columns
+                static_assert(SETS == 2 || SHARED >= 128, "a warp's second piece has no shared columns");
+#pragma unroll 1
+                for (int i = 0; i < max(1, mine); ++i) {
+                    if (i < mine) {
+                        take(f, i);
+                        tmem_ld_wait();
                     }
-                    last = __ballot_sync(~0u, done);
+                    if (i == 0) release();
+                    if (i < mine) emit(f, i);
+                }
+            }
+            ++local;
+            if (CUT && u.parts > 1) {
+                // of a cut tile they went to this part's slab; one count for each of them says which have all their parts, and those are added up
+                __syncwarp();
+                bool done = false;
+                if (lane < mine) {
+                    unsigned int* counter = p.counter + (u.cut * 2 + rank) * 8 + set + SETS * lane;
+                    const unsigned int old = (atomic_add_acq_rel(counter, 1u << (8 * quarter)) >> (8 * quarter)) & 255u;
+                    done = old == static_cast<unsigned>(u.parts) - 1u;
+                    if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
+                }
+                const unsigned int last = __ballot_sync(~0u, done);
+#pragma unroll 1
+                for (int q = 0; q < mine; ++q) {
+                    if (!((last >> q) & 1u)) continue;
+                    const int c = set * 32 + q * SPAN;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[j] = 0.0f;
+#pragma unroll 1
+                    for (int s = 0; s < u.parts; ++s) {
+                        const float4* src = slab_of(s, c);
+                        float4 y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = __ldcg(src + j * 32);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[4 * j] += y[j].x, f[4 * j + 1] += y[j].y, f[4 * j + 2] += y[j].z, f[4 * j + 3] += y[j].w;
+                    }
+                    deliver(f, c);
                 }
             }
         }
     }
 
-    if (warp == 8) launch_wait();        // this launch ends after the one before it, whatever it read
+    if (warp == PRODUCER) launch_wait();     // this launch ends after the one before it, whatever it read
     tc_fence_before_sync();
     __syncthreads();
     cluster_sync_all();
-    if (warp == 9) {
+    if (warp == ISSUER) {
         tc_fence_after_sync();
         tmem_dealloc_pair(tmem_base, 512);
     }

@@ -7,7 +7,12 @@
 
 namespace nk {
 
-constexpr int MX_THREADS = 384;
+enum MxMode { MX_WHOLE_TILES = 0, MX_CUT = 1, MX_SUMS = 2 };   // (sums: may be cut, too)
+// Sets of four epilogue warps, and all threads (with four more warps).  Four sets have two pieces of a tile each, and the accumulator goes back once the
+// first are taken: 8192 x 4096 x 1024 MXF4 25.2 us, by two sets 26.0.  With NVF4, whose accumulators share more columns, one set of four would
+// have to take both first: 28.3 and 27.9.
+__host__ __device__ constexpr int mx_sets(int mode, bool nv) { return mode == MX_WHOLE_TILES && !nv ? 4 : 2; }
+__host__ __device__ constexpr int mx_threads(int mode, bool nv) { return 32 * (4 * mx_sets(mode, nv) + 4); }
 constexpr int MX_MAX_GROUPS = 1024;
 constexpr int MX_BK = 256;                              // of the contraction to a k-block: 128 bytes of a row
 constexpr int MX_A_BYTES = 128 * 128;                   // a stage: 16 KB of features, up to 16 KB of rows, then 2 KB of the features' scales
@@ -52,7 +57,6 @@ struct MxMaps {
     CUtensorMap sa, sb;    // scales: boxes of the tiles of one k-block
 };
 
-enum MxMode { MX_WHOLE_TILES = 0, MX_CUT = 1, MX_SUMS = 2 };   // (sums: may be cut, too)
 enum MxOut { MX_OUT_F32 = 0, MX_OUT_BF16 = 1, MX_OUT_F16 = 2 };
 // K-blocks to an accumulator: contractions of more are summed in FP32, FP32 results by MX_CHUNK.  (What the tensor core drops of a sum of 4-bit
 // products is little, as they have few bits: against 64 bits, relative 2-norm, 8192 products of one sign are 5.3e-8 off in one accumulator, 4.9e-8 in

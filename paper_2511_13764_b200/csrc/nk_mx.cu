@@ -59,6 +59,7 @@ struct nk_mx_s : nk::PlanBase {
     int pairs;                    // CTA pairs that fit the device
     nk::MxFunction kernel;
     int chunk;
+    nk::MxMode mode;
     int width, parts;             // of one group's tiles; groups: 0, 1
     int split_slot;
     unsigned int* counters;
@@ -115,6 +116,7 @@ nk_status_t nk_mx_create(const nk_mx_desc_t* desc, nk_mx_t* out) {
         }
     }
     const MxMode mode = sums ? MX_SUMS : p->parts > 1 ? MX_CUT : MX_WHOLE_TILES;
+    p->mode = mode;
     p->kernel = d.format == NK_NVF4 ? mx_kernel_nv(type, mode) : mx_kernel_mx(type, mode);
     if (cudaFuncSetAttribute(p->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MX_SMEM) != cudaSuccess) {
         give_split_slot(d.device, p->split_slot, false, false);
@@ -189,7 +191,7 @@ nk_status_t nk_mx_run(nk_mx_t p, const void* A, const void* A_scales, const void
     g.counter = p->counters;
     g.status = p->status_dev;
     base_runs(p, static_cast<cudaStream_t>(cuda_stream));
-    const cudaError_t e = launch_beside(p->kernel, 2 * p->pairs, MX_THREADS, MX_SMEM, static_cast<cudaStream_t>(cuda_stream), p->maps, g);
+    const cudaError_t e = launch_beside(p->kernel, 2 * p->pairs, mx_threads(p->mode, nv), MX_SMEM, static_cast<cudaStream_t>(cuda_stream), p->maps, g);
     return e == cudaSuccess ? NK_OK : p->cuda("mx launch", e);
 }
 
