@@ -45,10 +45,10 @@ __host__ __device__ constexpr int mx_shared(bool nv) { return mx_scales(nv) - MX
 
 // MODE: whole tiles only; tiles may be cut; they may be cut and be sums of several accumulators.
 // A launch of 384 threads has 168 registers for each.  Sums take 128, so the epilogue's 256 threads get some of the others' (216 x 256 + 72 x 128 = 168 x
-// 384; 4096 x 4096 x 16384 122 us, with 208 and 88 127, without 155, in 16 bits and one accumulator 104); the other kernels must do without, as the loops of the other warps are slower for it (4096 x 1024 x 4096 16.0 us instead of 14.0),
-// and without spilling: there is next to no L1 beside this much shared memory (20 spilled registers: 8192 x 4096 x 256 38 us instead of 25).
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
+// 384; 4096 x 4096 x 16384 122 us, with 208 and 88 127, without 155, in 16 bits and one accumulator 104); the other kernels must do without, as the
+// loops of the other warps are slower for it (4096 x 1024 x 4096 16.0 us instead of 14.0), and without spilling: there is next to no L1 beside this much shared memory (20 spilled registers: 8192 x 4096 x 256 38 us instead of 25).
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MX_MORE_REGISTERS)); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MX_FEWER_REGISTERS)); }
 
 template <bool NV, int OUT, int MODE>
 __global__ void __launch_bounds__(mx_threads(MODE, NV), 1) __cluster_dims__(2, 1, 1)
@@ -110,7 +110,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         fence_mbar_init();
         __syncwarp();
     } else if (warp == 0) {
-        if (lane < 8) tma_prefetch_desc(&maps.b[lane]);
+        if (lane < MX_BOXES) tma_prefetch_desc(&maps.b[lane]);
         if (lane == 8) tma_prefetch_desc(&maps.a);
         if (lane == 9) tma_prefetch_desc(&maps.sa);
         if (lane == 10) tma_prefetch_desc(&maps.sb);
@@ -340,11 +340,11 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
         MxUnit u = {};
         while (ok && next(u)) {
             ring();
-            const int half = u.jn >> 1, high = (half >> 4) - 1;       // rows of this CTA, and the map whose boxes have them
+            const int half = u.jn >> 1, high = mx_box(half);          // rows of this CTA, and the map whose boxes have them
             const int i = u.i0 + static_cast<int>(rank) * 128, c = u.c0 + static_cast<int>(rank) * half;
             const int s_tile = u.g * p.scale_tiles + (i >> 7);
             const bool two = u.shift * 32 + u.jn > 128;               // tiles of the rows' scales
-            const uint32_t bytes = 2u * (MX_A_BYTES + half * 128u + (two ? 3u : 2u) * S_BOX);
+            const uint32_t bytes = 2u * (MX_A_BYTES + mx_box_rows(high) * 128u + (two ? 3u : 2u) * S_BOX);
             const int s_off = MX_A_BYTES + *s_width * 64;
             for (int kb = u.kb0; kb < u.kb1; ++kb) {
                 if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) {

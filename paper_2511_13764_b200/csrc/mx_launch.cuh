@@ -13,6 +13,7 @@ enum MxMode { MX_WHOLE_TILES = 0, MX_CUT = 1, MX_SUMS = 2 };   // (sums: may be 
 // have to take both first: 28.3 and 27.9.
 __host__ __device__ constexpr int mx_sets(int mode, bool nv) { return mode == MX_WHOLE_TILES && !nv ? 4 : 2; }
 __host__ __device__ constexpr int mx_threads(int mode, bool nv) { return 32 * (4 * mx_sets(mode, nv) + 4); }
+constexpr int MX_MORE_REGISTERS = 216, MX_FEWER_REGISTERS = 72;   // of a thread where accumulators are summed: the epilogue's 256, the other 128
 constexpr int MX_MAX_GROUPS = 1024;
 constexpr int MX_BK = 256;                              // of the contraction to a k-block: 128 bytes of a row
 constexpr int MX_A_BYTES = 128 * 128;                   // a stage: 16 KB of features, up to 16 KB of rows, then 2 KB of the features' scales
@@ -51,9 +52,15 @@ struct MxParams {
     unsigned int* status;
 };
 
+// Boxes of the rows' operand: a CTA's half of a tile's rows takes the smallest that has them, which is no more than half of the tiles' width.  (Rows that
+// are loaded beyond them are not multiplied; a box for every sixteen rows would be three more maps among a launch's arguments.)
+constexpr int MX_BOXES = 5;
+__host__ __device__ constexpr int mx_box_rows(int z) { return z < 3 ? 16 << z : 32 * z; }                     // 16, 32, 64, 96, 128
+__host__ __device__ constexpr int mx_box(int rows) { return rows <= 16 ? 0 : rows <= 32 ? 1 : (rows + 31) / 32; }
+
 struct MxMaps {
     CUtensorMap a;         // the features' operand (bytes): boxes of 128 features x 256 of k
-    CUtensorMap b[8];      // the rows' operand in boxes of 16, 32, .. 128 rows
+    CUtensorMap b[MX_BOXES];   // the rows' operand in boxes of mx_box_rows rows
     CUtensorMap sa, sb;    // scales: boxes of the tiles of one k-block
 };
 

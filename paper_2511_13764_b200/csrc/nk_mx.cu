@@ -123,6 +123,14 @@ nk_status_t nk_mx_create(const nk_mx_desc_t* desc, nk_mx_t* out) {
         delete p;
         return NK_ERR_CUDA;
     }
+    // the epilogue's registers come from the launch's own (see mx.cuh): a kernel built with fewer would wait for them without end
+    cudaFuncAttributes built = {};
+    if (mode == MX_SUMS && (cudaFuncGetAttributes(&built, p->kernel) != cudaSuccess ||
+                            built.numRegs * mx_threads(mode, d.format == NK_NVF4) < MX_MORE_REGISTERS * 256 + MX_FEWER_REGISTERS * 128)) {
+        give_split_slot(d.device, p->split_slot, false, false);
+        delete p;
+        return NK_ERR_CUDA;
+    }
     snprintf(p->name, sizeof(p->name), "mx_%s%s_256x256x256_pair%s", d.format == NK_NVF4 ? "nvf4" : "mxf4", d.groups ? "_grouped" : "", uncut ? "_uncut" : "");
     *out = p;
     return NK_OK;
@@ -158,7 +166,7 @@ nk_status_t nk_mx_run(nk_mx_t p, const void* A, const void* A_scales, const void
         MxMaps& m = p->maps;
         bool ok = encode_packed(&m.a, B, pitch, d.N, groups, 128) && encode_scales(&m.sa, B_scales, tiles, groups * div_up(d.N, MX_TILE_ROWS), box) &&
                   encode_scales(&m.sb, A_scales, tiles, d.groups ? d.rows / MX_TILE_ROWS + groups : div_up(d.rows, MX_TILE_ROWS), box);
-        for (int z = 0; ok && z < 8; ++z) ok = encode_packed(&m.b[z], A, pitch, d.rows, 1, 16 * (z + 1));
+        for (int z = 0; ok && z < MX_BOXES; ++z) ok = encode_packed(&m.b[z], A, pitch, d.rows, 1, mx_box_rows(z));
         if (!ok) {
             memset(p->cached, 0, sizeof(p->cached));
             snprintf(p->cuda_err, sizeof(p->cuda_err), "cuTensorMapEncodeTiled failed");
@@ -190,7 +198,7 @@ nk_status_t nk_mx_run(nk_mx_t p, const void* A, const void* A_scales, const void
     g.slab_cols = p->slab_cols;
     g.counter = p->counters;
     g.status = p->status_dev;
-    base_runs(p, static_cast<cudaStream_t>(cuda_stream));
+    if (p->split_slot >= 0) base_runs(p, static_cast<cudaStream_t>(cuda_stream));       // (what has no counters leaves nothing behind)
     const cudaError_t e = launch_beside(p->kernel, 2 * p->pairs, mx_threads(p->mode, nv), MX_SMEM, static_cast<cudaStream_t>(cuda_stream), p->maps, g);
     return e == cudaSuccess ? NK_OK : p->cuda("mx launch", e);
 }

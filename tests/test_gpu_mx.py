@@ -325,6 +325,46 @@ def test_streams_graphs_and_plans_destroyed_early():
         assert ((C.double() - y).abs() <= bound(other.values, B.values, 16384, "f32", y)).all()
 
 
+def test_cut_plans_at_once_and_without_counters():
+    """Cut plans on two streams beside each other; a plan that finds no counters left cuts nothing."""
+    A, B = Packed(normal(16, 16384, seed=1), "nvf4"), Packed(normal(256, 16384, seed=2), "nvf4")
+    y = A.values @ B.values.t()
+    tol = bound(A.values, B.values, 16384, "f32", y)
+    plans = [nk.MxPlan(16, 256, 16384) for _ in range(1040)]
+    names = [p.kernel_name for p in plans]
+    assert not names[0].endswith("_uncut") and names[-1].endswith("_uncut") and plans[-1].workspace_bytes == 0
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    work = []
+    torch.cuda.synchronize()
+    for i, p in enumerate((plans[0], plans[1], plans[-1])):
+        C, ws = torch.empty(16, 256, device="cuda"), torch.empty(max(1, p.workspace_bytes), dtype=torch.uint8, device="cuda")
+        work.append((C, ws))
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for i, p in enumerate((plans[0], plans[1], plans[-1])):
+            p.run(A.data, A.scales, B.data, B.scales, work[i][0], scale_a=A.scale, scale_b=B.scale, workspace=work[i][1], stream=side[i % 2].cuda_stream)
+    torch.cuda.synchronize()
+    for p in plans:
+        p.destroy()
+    assert torch.equal(work[0][0], work[1][0])
+    assert all(((C.double() - y).abs() <= tol).all() for C, _ in work)
+
+
+def test_results_beyond_32_bits():
+    """More than 2^31 elements of C, and a group whose rows begin there."""
+    rows, N, K, first = 70016, 32768, 64, 69950
+    A, B = Packed(normal(rows, K, seed=1), "mxf4", offsets=[0, first, rows]), Packed(normal(2, N, K, seed=2), "mxf4")
+    plan = nk.MxPlan(rows, N, K, groups=2, format=nk.MXF4, out_dtype=nk.BF16)
+    C = torch.empty(rows, N, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(max(1, plan.workspace_bytes), dtype=torch.uint8, device="cuda")
+    plan.run(A.data, A.scales, B.data, B.scales, C, offsets=A.offsets, workspace=ws, stream=stream())
+    plan.check()
+    for r in (0, 1, 65535, 65536, first - 1, first, rows - 1):
+        a, b = A.values[r:r + 1], B.values[int(r >= first)]
+        y = a @ b.t()
+        assert ((C[r:r + 1].double() - y).abs() <= bound(a, b, K, "bf16", y)).all(), r
+
+
 def test_no_rows_and_refusals():
     plan = nk.MxPlan(0, 64, 64)
     plan.run(None, None, None, None, None, stream=stream())

@@ -217,6 +217,41 @@ def test_values_in_16_bits(kind, transposed, rows, K):
     check_values(plan, data, scales, scale, None, values(codes, bytes_, "nvf4", t, rows if transposed else K), kind)
 
 
+@pytest.mark.parametrize("transposed", [0, 1])
+def test_matrices_beyond_32_bits(transposed):
+    """More than 2^31 elements; the last rows are looked at."""
+    rows, K = 270000, 8192
+    x = torch.zeros(rows, K, dtype=torch.bfloat16, device="cuda")
+    tail = rows_of(40, K, "bf16", seed=4)
+    x[rows - 40:] = tail.cuda()
+    plan = nk.PackPlan(rows, K, transposed=transposed)
+    data = torch.full((plan.data_bytes,), 0xAA, dtype=torch.uint8, device="cuda")
+    scales = torch.full((plan.scales_bytes,), 0xAA, dtype=torch.uint8, device="cuda")
+    scale, ws = torch.empty(1, device="cuda"), torch.empty(max(1, plan.workspace_bytes), dtype=torch.uint8, device="cuda")
+    plan.tensor_scale(x, scale, workspace=ws, stream=stream())
+    plan.run(x, data, scales, scale=scale, stream=stream())
+    plan.check()
+    z = tail.double().numpy()
+    t = tensor_scale(z)
+    assert scale.item() == t
+    if transposed:
+        # the last 64 of the contraction of every 1000th feature (270000 is a multiple of 16: 16 blocks end there)
+        f = torch.arange(0, K, 1000)
+        got = data.view(K, -1)[f.cuda()][:, -(padded(rows) // 2 - (rows - 48) // 2):].cpu().numpy()
+        full = np.zeros((len(f), 48))
+        full[:, 8:] = z[:, f.numpy()].T
+        codes, _, _ = quantise(full, "nvf4", t)
+        low, high = got[:, :24] & 15, got[:, :24] >> 4
+        assert np.array_equal(one_zero(np.stack([low, high], 2).reshape(len(f), 48)), one_zero(codes[:, :48]))
+        assert not got[:, 24:].any()
+    else:
+        codes, bytes_, _ = quantise(z, "nvf4", t)
+        assert np.array_equal(unpack_data(data.view(rows, -1)[rows - 40:].cpu().numpy(), 40, K), one_zero(codes))
+        tiles = scales.view(-1, tiles_of(K, "nvf4") * 512)[-2:].cpu().numpy()
+        at = np.arange(rows - 40, rows) - (len(scales) // (tiles_of(K, "nvf4") * 512) - 2) * 128
+        assert np.array_equal(unpack_scales(tiles, at, K, "nvf4"), bytes_)
+
+
 def test_no_rows_and_refusals():
     plan = nk.PackPlan(0, 64)
     assert plan.data_bytes == 0
