@@ -343,11 +343,13 @@ __global__ void __launch_bounds__(PACK_THREADS, 4) pack_columns_kernel(const Pac
 }
 __host__ __device__ constexpr int pack_columns_smem(int type) { return PACK_TURN * PACK_TURN * (type == 0 ? 4 : 2) + PACK_TURN * (PACK_TURN / 2 + 8) + 2 * MX_TILE_BYTES; }
 
-// Reading back: a thread has eight elements of a row, a warp 256.  Where the rows of Y are not whole pieces of eight, a warp's
-// elements go by way of shared memory, from where consecutive lanes store consecutive ones.
+// Reading back: a warp has 256 elements of a row, a lane eight side by side, or for FP32 results twice four, so that a store of a warp is whole sectors
+// (32 bytes to a lane in two stores: 8192 x 4096 41 us instead of 27).  Where the rows of Y are not whole pieces of eight, a warp's elements go by
+// way of shared memory, from where consecutive lanes store consecutive ones.
 template <int T, bool NV>
 __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackParams p) {
-    constexpr int LANES = NV ? 2 : 4, TILES = PACK_LINE / (4 * mx_block(NV)), AHEAD = 4;
+    constexpr int TILES = PACK_LINE / (4 * mx_block(NV)), AHEAD = 4;
+    constexpr int PARTS = T == 0 ? 2 : 1, WIDE = 8 / PARTS;                   // runs of a lane's elements, their length
     __shared__ int s_off[PACK_MAX_GROUPS + 1], s_found[2];
     __shared__ __align__(16) float s_line[PACK_THREADS / 32][PACK_LINE];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, item = blockIdx.z;
@@ -357,42 +359,53 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackPar
     const PackRows rows = pack_rows(p, tile, s_off, s_found);
     if (rows.count <= 0) return;
     const float t = NV && p.scale ? p.scale[item] : 1.0f;
-    const int k0 = chunk * PACK_LINE, k = k0 + lane * 8, pitch = static_cast<int>(mx_padded(p.length) / 2), c = lane / LANES;
-    const bool whole = p.length % 8 == 0, there = k < p.length;
-    const uint8_t* data = p.data + (static_cast<size_t>(item) * p.outer + rows.first) * pitch + k / 2;
-    const uint8_t* scales = p.scales + ((static_cast<size_t>(item) * p.row_tiles + tile) * p.tiles + chunk * TILES + c / 4) * MX_TILE_BYTES + (c & 3);
+    const int k0 = chunk * PACK_LINE, pitch = static_cast<int>(mx_padded(p.length) / 2);
+    const bool whole = p.length % 8 == 0;
+    auto at = [&](int part) { return part * (PACK_LINE / PARTS) + lane * WIDE; };       // a run's place in the line
+    const uint8_t* data = p.data + (static_cast<size_t>(item) * p.outer + rows.first) * pitch + k0 / 2;
+    const uint8_t* scales = p.scales + ((static_cast<size_t>(item) * p.row_tiles + tile) * p.tiles + chunk * TILES) * MX_TILE_BYTES;
     const size_t y0 = (static_cast<size_t>(item) * p.outer + rows.first) * p.length + k0;
     for (int r0 = warp; r0 < rows.count; r0 += 8 * AHEAD) {
-        uint32_t w[AHEAD], b[AHEAD];
+        uint32_t w[AHEAD], b[AHEAD][PARTS];
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
             const int r = r0 + 8 * n;
-            const bool load = there && r < rows.count;
-            w[n] = load ? __ldg(reinterpret_cast<const uint32_t*>(data + static_cast<size_t>(r) * pitch)) : 0u;
-            b[n] = load ? __ldg(scales + (r & 31) * 16 + (r >> 5) * 4) : 0u;
+            w[n] = 0u;
+#pragma unroll
+            for (int h = 0; h < PARTS; ++h) {
+                const bool load = k0 + at(h) < p.length && r < rows.count;
+                const int c = at(h) / mx_block(NV);
+                const uint8_t* d = data + static_cast<size_t>(r) * pitch + at(h) / 2;
+                if (load) w[n] |= T == 0 ? static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(d))) << (16 * h) : __ldg(reinterpret_cast<const uint32_t*>(d));
+                b[n][h] = load ? __ldg(scales + c / 4 * MX_TILE_BYTES + (r & 31) * 16 + (r >> 5) * 4 + (c & 3)) : 0u;
+            }
         }
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
             const int r = r0 + 8 * n;
             if (r >= rows.count) break;
-            const float s = NV ? e4m3_to_f32(b[n]) : e8m0_to_f32(b[n]);
             float x[8];
             e2m1x8_to_f32(w[n], x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = NV ? x[i] * s * t : x[i] * s;
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t byte = b[n][i / WIDE];
+                const float s = NV ? e4m3_to_f32(byte) : e8m0_to_f32(byte);
+                x[i] = NV ? x[i] * s * t : x[i] * s;
+            }
             const size_t y = y0 + static_cast<size_t>(r) * p.length;
             if (whole) {
-                if (there && T == 0) {
-                    float4* out = reinterpret_cast<float4*>(static_cast<float*>(p.values) + y + lane * 8);
-                    __stcs(out, make_float4(x[0], x[1], x[2], x[3]));
-                    __stcs(out + 1, make_float4(x[4], x[5], x[6], x[7]));
-                } else if (there) {
-                    __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.values) + y + lane * 8), pack8<T == 2>(x));
+                if (T == 0) {
+#pragma unroll
+                    for (int h = 0; h < PARTS; ++h)
+                        if (k0 + at(h) < p.length)
+                            __stcs(reinterpret_cast<float4*>(static_cast<float*>(p.values) + y + at(h)), make_float4(x[h * WIDE], x[h * WIDE + 1], x[h * WIDE + 2], x[h * WIDE + 3]));
+                } else if (k0 + at(0) < p.length) {
+                    __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.values) + y + at(0)), pack8<T == 2>(x));
                 }
             } else {
-                float4* line = reinterpret_cast<float4*>(s_line[warp]) + lane * 2;
-                line[0] = make_float4(x[0], x[1], x[2], x[3]);
-                line[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+                for (int i = 0; i < 8; i += 4)
+                    *reinterpret_cast<float4*>(s_line[warp] + at(i / WIDE) + i % WIDE) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
