@@ -16,7 +16,7 @@ __host__ __device__ constexpr int mx_group_tile(int row0, int g) { return row0 /
 
 #ifdef __CUDACC__
 // E8M0 byte to its number (2^-127 is a subnormal)
-__device__ __forceinline__ float e8m0_to_f32(uint32_t b) { return __uint_as_float(b == 0u ? 0x00400000u : b == 255u ? 0x7FC00000u : b << 23); }
+__device__ __forceinline__ float e8m0_to_f32(uint32_t b) { return __uint_as_float(b == 255u ? 0x7FC00000u : max(b << 23, 0x00400000u)); }
 __device__ __forceinline__ uint32_t f32_to_e4m3(float x) {       // round to nearest even, at most 448; NaN: 0x7F
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(x));

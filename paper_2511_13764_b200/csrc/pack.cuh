@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(PACK_THREADS, 4) pack_columns_kernel(const Pac
 __host__ __device__ constexpr int pack_columns_smem(int type) { return PACK_TURN * PACK_TURN * (type == 0 ? 4 : 2) + PACK_TURN * (PACK_TURN / 2 + 8) + 2 * MX_TILE_BYTES; }
 
 // Reading back: a warp has 256 elements of a row, a lane eight side by side, or for FP32 results twice four, so that a store of a warp is whole sectors
-// (32 bytes to a lane in two stores: 8192 x 4096 41 us instead of 27).  Where the rows of Y are not whole pieces of eight, a warp's elements go by
+// (32 bytes to a lane in two stores: 8192 x 4096 41 us instead of 29).  Where the rows of Y are not whole pieces of eight, a warp's elements go by
 // way of shared memory, from where consecutive lanes store consecutive ones.
 template <int T, bool NV>
 __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackParams p) {
@@ -386,12 +386,11 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackPar
             if (r >= rows.count) break;
             float x[8];
             e2m1x8_to_f32(w[n], x);
+            float s[PARTS];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t byte = b[n][i / WIDE];
-                const float s = NV ? e4m3_to_f32(byte) : e8m0_to_f32(byte);
-                x[i] = NV ? x[i] * s * t : x[i] * s;
-            }
+            for (int h = 0; h < PARTS; ++h) s[h] = NV ? e4m3_to_f32(b[n][h]) : e8m0_to_f32(b[n][h]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = NV ? x[i] * s[i / WIDE] * t : x[i] * s[i / WIDE];
             const size_t y = y0 + static_cast<size_t>(r) * p.length;
             if (whole) {
                 if (T == 0) {
