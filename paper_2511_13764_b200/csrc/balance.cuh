@@ -165,6 +165,7 @@ balance_total_kernel(const RouteParams p, const BalanceParams b, int narrow) {
     const int each = (E + BALANCE_CLUSTER - 1) / BALANCE_CLUSTER, first = rank * each, last = min(E, first + each);
     const int at = lane & ((1 << narrow) - 1), row = (warp << (5 - narrow)) + (lane >> narrow), rows = WARPS << (5 - narrow);
     const size_t pitch = 2 * E + 2;
+    cluster_arrive();                                                      // everyone has started, once this is waited for: the stores below need it
     launch_wait();
     launch_next();
     // tokens and the sum over them, in every warp 0
@@ -219,6 +220,7 @@ balance_total_kernel(const RouteParams p, const BalanceParams b, int narrow) {
             }
         }
     }
+    cluster_wait();
     if (warp == 0) {
         loss = warp_sum(loss);
         if (lane == 0) st_cluster_v4(map_to_cta(smem_u32(losses + rank), 0), __float_as_uint(loss), 0u, 0u, 0u);

@@ -447,6 +447,7 @@ __device__ __forceinline__ void tensor_max(const PackParams& p, int rows, int wi
     const int per_row = width / 8;
     const long long pieces = static_cast<long long>(rows) * per_row;
     const int turn = AHEAD * static_cast<int>(blockDim.x);
+    if (CLUSTER) cluster_arrive();                       // everyone has started, once this is waited for: the stores below need it
     launch_wait();
     launch_next();
     uint32_t m = 0u;
@@ -473,6 +474,7 @@ __device__ __forceinline__ void tensor_max(const PackParams& p, int rows, int wi
     m = __float_as_uint(pack_widen<T>(pack_one<T>(m)));  // (order of FP32 bits from here on)
     m = block_max(m, line);
     if (CLUSTER) {
+        cluster_wait();
         if (threadIdx.x == 0) st_cluster_v4(map_to_cta(smem_u32(maxima + cluster_ctarank()), 0), m, 0u, 0u, 0u);
         cluster_sync_all();
         if (blockIdx.x == 0 && threadIdx.x < SCALE_CLUSTER) {
