@@ -3,8 +3,10 @@
 //   P_e = 1/n sum_t p_te,  balance = E / (n k) sum_e c_e P_e,  size = 1/n sum_t lse_t^2,  lse_t = log sum_e exp z_te
 //   dz_te = p_te (g0 E / (n^2 k) (c_e - sum_j c_j p_tj) + g1 2/n lse_t)
 // A warp has a token, a lane the experts l, l + 32, ..., and adds up the probabilities of its tokens in registers: one pass
-// over the logits each way.  Sums of at most 64 tokens, of a block's warps and of the experts are FP32, those over blocks 64 bits; every sum has one order (counts are integers, added in any).
-// Bound by instruction issue and a launch's start and end: see the figures in the design notes' table of the cases.
+// over the logits each way.  Sums of at most 64 tokens, of a block's warps and of the experts are FP32, those over blocks 64
+// bits; every sum has one order (counts are integers, added in any).
+// Bound by instruction issue (70 % of the slots) and by each launch's start and end: 16384 x 128 FP32 logits, 8.4 MB or 1.3 us of
+// HBM, take 8.6 us (two launches), the way back (8.4 MB more) 5.8; 16 x 64 take 3.4 (one launch) and 2.2.
 #pragma once
 #include "route.cuh"
 
@@ -26,21 +28,23 @@ __device__ __forceinline__ float warp_sum(float x) {
     return x;
 }
 
+// the largest of a warp's numbers, NaN if there is one
+__device__ __forceinline__ float warp_max_nan(float x) {
+    float r;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // A row's softmax in place: z becomes the probabilities; returns the row's log-sum-exp.  A row whose logits are all minus
 // infinity has neither: zeros.
 template <int V>
 __device__ __forceinline__ float row_softmax(float (&z)[V]) {
-    uint32_t top = 0u;
-    bool nan = false;
+    float m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        nan |= z[i] != z[i];
-        top = max(top, route_key(z[i]));
-    }
-    nan = __any_sync(~0u, nan);
-    const float m = route_unkey(__reduce_max_sync(~0u, top));
-    if (nan || m == -INFINITY) {
-        const float x = nan ? __int_as_float(0x7FC00000) : 0.0f;
+    for (int i = 0; i < V; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(z[i]));
+    m = warp_max_nan(m);
+    if (!(m > -INFINITY)) {
+        const float x = m != m ? m : 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) z[i] = x;
         return x;
@@ -152,53 +156,64 @@ __global__ void __launch_bounds__(route_threads(V)) balance_kernel(const RoutePa
     }
 }
 
-// The blocks' sums into the results: a cluster of eight, each an eighth of the experts, 2^narrow of them to a row of a warp's lanes.  (Short code: it
-// runs once, and what it costs is mostly its fetch.  By one block, or with 64-bit divisions, 5 to 7 us.)
+// The blocks' sums into the results: a cluster of eight, each an eighth of the experts, 2^narrow of them to a row of a warp's lanes; a warp of its
+// own has the tokens.  (Short code: it runs once, and what it costs is mostly its fetch.  By one block, or with 64-bit divisions, 5 to 7 us; ten
+// loads ahead instead of five 0.5 us more, the tokens' sums in front of the experts' 1.4.)
 constexpr int BALANCE_CLUSTER = 8, BALANCE_TOTAL = 512;
 __global__ void __launch_bounds__(BALANCE_TOTAL) __cluster_dims__(BALANCE_CLUSTER, 1, 1)
 balance_total_kernel(const RouteParams p, const BalanceParams b, int narrow) {
-    constexpr int WARPS = BALANCE_TOTAL / 32;
+    constexpr int WARPS = BALANCE_TOTAL / 32 - 1, AHEAD = 5;               // warps of the experts; the last has the tokens
     __shared__ double part[WARPS][32];
-    __shared__ int count[WARPS][32];
+    __shared__ int count[WARPS][32], all;
     __shared__ __align__(16) float4 losses[BALANCE_CLUSTER];               // of the first block: everyone's part
     const int E = p.experts, rank = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int each = (E + BALANCE_CLUSTER - 1) / BALANCE_CLUSTER, first = rank * each, last = min(E, first + each);
     const int at = lane & ((1 << narrow) - 1), row = (warp << (5 - narrow)) + (lane >> narrow), rows = WARPS << (5 - narrow);
     const size_t pitch = 2 * E + 2;
+    double s, size = 0.0;
+    int c;
+    // a column's sums (in s and c) of the blocks `from`, from + by, ..: numbers and, `gap` further on, counts
+    auto add = [&](const float* x, int from, int by, int gap) {
+        for (int i = from; i < b.blocks; i += AHEAD * by) {
+            float v[AHEAD];
+            int n[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const float* y = x + (i + j * by) * pitch;
+                v[j] = i + j * by < b.blocks ? y[0] : 0.0f;
+                n[j] = i + j * by < b.blocks ? __float_as_int(y[gap]) : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                s += v[j];
+                c += n[j];
+            }
+        }
+    };
     cluster_arrive();                                                      // everyone has started, once this is waited for: the stores below need it
     launch_wait();
     launch_next();
-    // tokens and the sum over them, in every warp 0
-    double size = 0.0;
-    int n = 0;
-    if (warp == 0) {
-#pragma unroll 4
-        for (int i = lane; i < b.blocks; i += 32) {
-            const float* x = b.partial + i * pitch + 2 * E;
-            size += x[0];
-            n += __float_as_int(x[1]);
-        }
-        n = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(n)));
+    if (warp == WARPS) {
+        s = 0.0;
+        c = 0;
+        add(b.partial + 2 * E, lane, 32, 1);
+        c = static_cast<int>(__reduce_add_sync(~0u, static_cast<unsigned>(c)));
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) size += __shfl_xor_sync(~0u, size, d);
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+        size = s;
+        if (lane == 0) all = c;
     }
-    const float tokens = static_cast<float>(n);
     float loss = 0.0f;
     for (int e0 = first; e0 < last; e0 += 1 << narrow) {
         const int e = e0 + at;
-        double s = 0.0;
-        int c = 0;
-        if (e < last) {
-#pragma unroll 4
-            for (int i = row; i < b.blocks; i += rows) {
-                const float* x = b.partial + i * pitch + e;
-                s += x[0];
-                c += __float_as_int(x[E]);
-            }
+        s = 0.0;
+        c = 0;
+        if (warp < WARPS && e < last) add(b.partial + e, row, rows, E);
+        if (e0 > first) __syncthreads();
+        if (warp < WARPS) {
+            part[warp][lane] = s;
+            count[warp][lane] = c;
         }
-        __syncthreads();
-        part[warp][lane] = s;
-        count[warp][lane] = c;
         __syncthreads();
         if (warp == 0) {
             s = 0.0;
@@ -213,7 +228,7 @@ balance_total_kernel(const RouteParams p, const BalanceParams b, int narrow) {
                 c += __shfl_xor_sync(~0u, c, d);
             }
             if (e < last && lane >> narrow == 0) {
-                const float mean = n ? static_cast<float>(s) / tokens : 0.0f;
+                const float mean = all ? static_cast<float>(s) / static_cast<float>(all) : 0.0f;
                 b.share[e] = mean;
                 b.counts[e] = c;
                 loss += mean * static_cast<float>(c);
@@ -226,12 +241,13 @@ balance_total_kernel(const RouteParams p, const BalanceParams b, int narrow) {
         if (lane == 0) st_cluster_v4(map_to_cta(smem_u32(losses + rank), 0), __float_as_uint(loss), 0u, 0u, 0u);
     }
     cluster_sync_all();
-    if (rank == 0 && threadIdx.x == 0) {
+    if (rank == 0 && threadIdx.x == WARPS * 32) {
         loss = 0.0f;
         for (int r = 0; r < BALANCE_CLUSTER; ++r) loss += losses[r].x;
-        b.losses[0] = n ? loss / tokens * (static_cast<float>(E) / static_cast<float>(p.topk)) : 0.0f;
-        b.losses[1] = n ? static_cast<float>(size) / tokens : 0.0f;
-        b.counts[E] = n;
+        const float tokens = static_cast<float>(all);
+        b.losses[0] = all ? loss / tokens * (static_cast<float>(E) / static_cast<float>(p.topk)) : 0.0f;
+        b.losses[1] = all ? static_cast<float>(size) / tokens : 0.0f;
+        b.counts[E] = all;
     }
 }
 
