@@ -5,7 +5,7 @@
 // A warp has a token, a lane the experts l, l + 32, ..., and adds up the probabilities of its tokens in registers: one pass
 // over the logits each way.  Sums of at most 64 tokens, of a block's warps and of the experts are FP32, those over blocks 64
 // bits; every sum has one order (counts are integers, added in any).
-// Bound by instruction issue (70 % of the slots) and by each launch's start and end: 16384 x 128 FP32 logits, 8.4 MB or 1.3 us of
+// Bound by instruction issue (65 to 74 % of the slots) and by each launch's start and end: 16384 x 128 FP32 logits, 8.4 MB or 1.3 us of
 // HBM, take 8.6 us (two launches), the way back (8.4 MB more) 5.8; 16 x 64 take 3.4 (one launch) and 2.2.
 #pragma once
 #include "route.cuh"
