@@ -3,13 +3,16 @@
 //   NVF4   scale s = RN_e4m3(m / (6 t)), element RN_e2m1(x / (s t))
 // The element's decision has to be that of exact arithmetic.  With t of 8 significant bits d = s t has 12 and is exact, a border b of
 // the elements (0.25 .. 5) times d has 15, so for x of a 16-bit type x / d is either b or at least 2^-14 away from it.  x times a
-// reciprocal of d that is off by 3 of its last places is within 2^-18 of the quotient (which is below 9 where it matters); rounded to a multiple of 2^-16 (one FMA onto 192 and a subtraction) it is b
-// exactly where the quotient is, and on the quotient's side of b elsewhere.  So there is no division for an element.  FP32 x take one: a
-// correctly rounded x / d is b only where the quotient is (24 bits against 15: the next quotient is more than half a step away).
+// reciprocal of d that is off by 3 of its last places is within 2^-18 of the quotient (which is below 9 where it matters); rounded to a
+// multiple of 2^-16 (one FMA onto 192 and a subtraction) it is b exactly where the quotient is, and on the quotient's side of b
+// elsewhere.  So there is no division for an element.  FP32 x take one: a correctly rounded x / d is b only where the quotient is
+// (24 bits against 15: the next quotient is more than half a step away).
 //
 // A block of threads has a tile of scales' 128 rows, so that the scales of a chunk of the contraction leave in one piece; a thread has
-// a block of the format.  Along the columns a tile of 128 x
-// 128 goes through shared memory, where a thread has a word of adjacent features.  Bound by memory.
+// a block of the format.  Along the columns a tile of 128 x 128 goes through shared memory, where a thread has a word of adjacent
+// features.  BF16, 64 matrices of 4096 x 1024 to NVF4 106 us: 6.3 TB/s, the rate of a copy.  8192 x 4096 is two waves of blocks, whose
+// loads and arithmetic overlap less (issue slots 60 % busy): NVF4 17.8 us (4.8 TB/s), along the columns 19.5-20.5; MXF4 15.1 and 17.6;
+// its scale of a tensor 15.4 (4.4 TB/s), values in FP32 29 (5.3 TB/s).  16 x 4096 takes 2.1 to 2.4 us, a launch's start and end.
 #pragma once
 #include "mx_format.cuh"
 #include "ptx.cuh"
@@ -17,7 +20,7 @@
 namespace nk {
 
 constexpr int PACK_THREADS = 256;
-// along rows: elements of the contraction to a block of threads (8192 x 4096: NVF4 17.8 us by 256, 18.8 by 128; MXF4 16.1, 15.1)
+// along rows: elements of the contraction to a block of threads (8192 x 4096: NVF4 17.8 us by 256, 18.8 by 128; MXF4 16.1 and 15.1)
 __host__ __device__ constexpr int pack_chunk(bool nv) { return nv ? 256 : 128; }
 constexpr int PACK_LINE = 256;                           // reading back, likewise
 constexpr int PACK_TURN = 128;                           // along columns: a tile's side
@@ -343,9 +346,9 @@ __global__ void __launch_bounds__(PACK_THREADS, 4) pack_columns_kernel(const Pac
 }
 __host__ __device__ constexpr int pack_columns_smem(int type) { return PACK_TURN * PACK_TURN * (type == 0 ? 4 : 2) + PACK_TURN * (PACK_TURN / 2 + 8) + 2 * MX_TILE_BYTES; }
 
-// Reading back: a warp has 256 elements of a row, a lane eight side by side, or for FP32 results twice four, so that a store of a warp is whole sectors
-// (32 bytes to a lane in two stores: 8192 x 4096 41 us instead of 29).  Where the rows of Y are not whole pieces of eight, a warp's elements go by
-// way of shared memory, from where consecutive lanes store consecutive ones.
+// Reading back: a warp has 256 elements of a row, a lane eight side by side, or for FP32 results twice four, so that a store of a warp
+// is whole sectors (32 bytes to a lane in two stores: 8192 x 4096 41 us instead of 29).  Where the rows of Y are not whole pieces of
+// eight, a warp's elements go by way of shared memory, from where consecutive lanes store consecutive ones.
 template <int T, bool NV>
 __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackParams p) {
     constexpr int TILES = PACK_LINE / (4 * mx_block(NV)), AHEAD = 4;
@@ -376,7 +379,9 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackPar
                 const bool load = k0 + at(h) < p.length && r < rows.count;
                 const int c = at(h) / mx_block(NV);
                 const uint8_t* d = data + static_cast<size_t>(r) * pitch + at(h) / 2;
-                if (load) w[n] |= T == 0 ? static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(d))) << (16 * h) : __ldg(reinterpret_cast<const uint32_t*>(d));
+                if (load)
+                    w[n] |= T == 0 ? static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(d))) << (16 * h)
+                                   : __ldg(reinterpret_cast<const uint32_t*>(d));
                 b[n][h] = load ? __ldg(scales + c / 4 * MX_TILE_BYTES + (r & 31) * 16 + (r >> 5) * 4 + (c & 3)) : 0u;
             }
         }
@@ -397,7 +402,8 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_values_kernel(const PackPar
 #pragma unroll
                     for (int h = 0; h < PARTS; ++h)
                         if (k0 + at(h) < p.length)
-                            __stcs(reinterpret_cast<float4*>(static_cast<float*>(p.values) + y + at(h)), make_float4(x[h * WIDE], x[h * WIDE + 1], x[h * WIDE + 2], x[h * WIDE + 3]));
+                            __stcs(reinterpret_cast<float4*>(static_cast<float*>(p.values) + y + at(h)),
+                                   make_float4(x[h * WIDE], x[h * WIDE + 1], x[h * WIDE + 2], x[h * WIDE + 3]));
                 } else if (k0 + at(0) < p.length) {
                     __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.values) + y + at(0)), pack8<T == 2>(x));
                 }
