@@ -92,7 +92,8 @@ nk_status_t nk_pack_destroy(nk_pack_t plan);
  * A [rows][K] and B [N][K] are packed along the contraction, in one format; ta and tb are their tensor scales (FP32 on the device; NULL: 1).
  * groups = 0: one B.  groups > 0: B, tb and bias are those of the row's group, B [groups][N][K] packed as a batch, A packed with the same
  * offsets; rows of C outside all groups are not touched.  FP32 accumulation, C in FP32 or rounded once to 16 bits.
- * NK_EPI_BIAS_RELU: max(0, .. + bias[n]), bias FP32 [N] (groups: [groups][N]); NULL: no bias.
+ * NK_EPI_BIAS_RELU: max(0, .. + bias[n]), bias FP32 [N] (groups: [groups][N]); NULL: no bias.  The tensor scales of packed operands may be of any
+ * size: where their product leaves FP32's range they are applied one after the other, and results that fit come out.
  *
  * Backward of Y = X . W^T: dX = dY . W is the same product with dY packed along its rows and W along its columns (transposed = 1); dW =
  * dY^T . X the same with both packed along their columns.  By expert: dX likewise; dW_g contracts over ragged rows, which have

@@ -386,3 +386,120 @@ def test_no_rows_and_refusals():
         with pytest.raises(nk.NkError) as e:
             call()
         assert e.value.status == status
+
+
+LARGEST = torch.finfo(torch.float32).max
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("groups", [0, 3])
+@pytest.mark.parametrize("relu", [False, True])
+def test_tensor_scales_whose_product_is_beyond_the_range(out, groups, relu):
+    """Each operand's scale is in range, their product is not: rows of zeros stay zeros, results that fit come out.  (A step more for the second
+    scale's rounding, 2^-24, which the bound's four hold.)"""
+    rows, N, K = 300, 264, 136
+    offsets = [0, 100, 100, 300] if groups else None
+    x, w = normal(rows, K, seed=1, scale=2.0 ** 74), normal(*((groups, N, K) if groups else (N, K)), seed=2, scale=2.0 ** 74)
+    x[0::3] *= 2.0 ** -14
+    x[1::3] = 0.0
+    x[2] = 2.0 ** 40                                        # every block rounds to zero
+    w[..., 0::2, :] *= 2.0 ** -14
+    w[..., 5, :] = 0.0
+    if groups:
+        w[0] *= 2.0 ** -80                                  # one group's scale is ordinary beside the others'
+    A, B = Packed(x, "nvf4", offsets=offsets), Packed(w, "nvf4")
+    assert torch.isinf(A.scale * B.scale).any() and torch.isfinite(A.scale).all() and torch.isfinite(B.scale).all()
+    bias = normal(*((groups, N) if groups else (N,)), seed=5, kind="f32").cuda() * 2.0 ** 100 if relu else None
+    got = run(A, B, N, K, "nvf4", out, groups=groups, relu=relu, bias=bias, offsets=A.offsets)
+    small = 0
+    for g, (lo, hi) in enumerate(zip(offsets, offsets[1:]) if groups else [(0, rows)]):
+        a, b = A.values[lo:hi], B.values[g] if groups else B.values
+        plain = a @ b.t()
+        y = plain + (bias[g] if groups else bias).double() if relu else plain
+        tol = bound(a, b, K, out, y) + (2.0 ** -23 * (y.abs() + 2.0 ** 103) if relu else 0.0)
+        y = torch.relu(y) if relu else y
+        fits, over = y.abs() + tol <= LARGEST * (1 - 2.0 ** -8), y.abs() - tol > LARGEST * (1 + 2.0 ** -8)
+        assert ((got[lo:hi] - y).abs() <= tol)[fits].all(), g
+        assert torch.equal(got[lo:hi][over], torch.sign(y[over]) * torch.inf), g
+        if not relu:
+            assert (got[lo:hi][plain == 0] == 0).all(), g
+        small += int((fits & (plain != 0)).sum())
+    assert small > 1000
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("groups", [0, 2])
+@pytest.mark.parametrize("ea,eb", [(-75, -75), (-74, -73), (-47, -100), (-98, -49)])
+def test_tensor_scales_whose_product_is_below_the_range(out, groups, ea, eb):
+    """A caller's small scales: their product is zero or has lost bits, the results have not.  (2^-149 and 2^-134: the types' smallest steps.)"""
+    ta, tb = 169 * 2.0 ** (ea - 7), 203 * 2.0 ** (eb - 7)
+    rows, N, K = 200, 264, 4096
+    offsets = [0, 90, 200] if groups else None
+    A = Packed(normal(rows, K, seed=1), "nvf4", offsets=offsets)
+    B = Packed(normal(*((groups, N, K) if groups else (N, K)), seed=2), "nvf4")
+    for P, seed, t in ((A, 3, ta), (B, 4, tb)):
+        shape = (rows, K) if P is A else (groups, N, K) if groups else (N, K)
+        m = (normal(*shape, seed=seed).clamp(-3, 3).double() * 800 * t).to(torch.bfloat16)
+        P.scale = torch.full((groups if P is B and groups else 1,), t, dtype=torch.float32, device="cuda")
+        P.plan.run(m.cuda(), P.data, P.scales, scale=P.scale, offsets=P.offsets, stream=stream())
+        z = m.double().numpy().reshape(-1, K)
+        codes, bytes_, _ = quantise(z, "nvf4", t)
+        P.values = torch.from_numpy(values(codes, bytes_, "nvf4", t, K)).cuda().reshape(shape)
+    got = run(A, B, N, K, "nvf4", out, groups=groups, offsets=A.offsets)
+    least = 2.0 ** -149 if out == "f32" else 2.0 ** -134
+    for g, (lo, hi) in enumerate(zip(offsets, offsets[1:]) if groups else [(0, rows)]):
+        a, b = A.values[lo:hi], B.values[g] if groups else B.values
+        y = a @ b.t()
+        assert ((got[lo:hi] - y).abs() <= bound(a, b, K, out, y) + least).all(), g
+        assert (y.abs() > 2.0 ** -126).any()
+
+
+class OnDevice:
+    """A matrix (or a batch) made and packed on the GPU; its values are read back (both compared with the definitions in test_gpu_pack.py)."""
+
+    def __init__(self, *shape, fmt="nvf4", seed=0, offsets=None, change=None):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        x = torch.randn(*shape, generator=g, device="cuda")
+        x = (x if change is None else change(x)).to(torch.bfloat16)
+        batch, rows, K = shape if len(shape) == 3 else (1, *shape)
+        groups = 0 if offsets is None else len(offsets) - 1
+        plan = nk.PackPlan(rows, K, format=FORMATS[fmt], batch=batch, groups=groups)
+        self.data = torch.empty(plan.data_bytes, dtype=torch.uint8, device="cuda")
+        self.scales = torch.full((plan.scales_bytes,), 0xFF, dtype=torch.uint8, device="cuda")
+        self.offsets = None if offsets is None else torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        self.scale = None
+        if fmt == "nvf4":
+            self.scale, ws = torch.empty(batch, device="cuda"), torch.empty(max(1, plan.workspace_bytes), dtype=torch.uint8, device="cuda")
+            plan.tensor_scale(x, self.scale, workspace=ws, stream=stream())
+        plan.run(x, self.data, self.scales, scale=self.scale, offsets=self.offsets, stream=stream())
+        y = torch.zeros(*shape, device="cuda")
+        plan.values(self.data, self.scales, y, scale=self.scale, offsets=self.offsets, stream=stream())
+        plan.check()
+        self.values = y.double()
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,N,K", [(16, 256, 16384), (300, 256, 33000), (1300, 1096, 264), (2000, 2056, 8448), (5537, 1712, 9216)])
+def test_scales_of_any_size_in_tiles_of_every_kind(out, rows, N, K):
+    """Cut tiles, sums of accumulators, wide tiles: other scales of the same packed operands, powers of two apart, give the same numbers that power of two
+    apart, but for a second rounding of the scales' product and what the type's smallest step takes.  (Where `want` has been rounded to 16 bits, too:
+    2^-23 apart, two numbers on either side of the middle of a step go to its two ends, which are 2^-7 of the smaller apart, two half steps.)"""
+    A, B = OnDevice(rows, K, seed=1, change=lambda x: x * (torch.arange(rows, device="cuda") % 5 > 0)[:, None]), OnDevice(N, K, seed=2)
+    plain = run(A, B, N, K, "nvf4", "f32", rows=rows)
+    ta, tb = A.scale, B.scale
+    rel, least = {"f32": (2.0 ** -22, 2.0 ** -149), "bf16": (2.0 ** -8 + 2.0 ** -20, 2.0 ** -134)}[out]
+    for a, b in ((-64, -64), (-12, -88), (80, 80), (100, 40)):
+        A.scale, B.scale = ta * 2.0 ** a, tb * 2.0 ** b
+        if K < 8192 or out == "f32":
+            want = plain * 2.0 ** (a + b)
+        else:                                               # (16-bit sums have longer accumulators: another order)
+            A.scale, B.scale = ta, tb
+            want = run(A, B, N, K, "nvf4", "bf16", rows=rows) * 2.0 ** (a + b)
+            A.scale, B.scale = ta * 2.0 ** a, tb * 2.0 ** b
+            rel = 2 * 2.0 ** -8 + 2.0 ** -20
+        got = run(A, B, N, K, "nvf4", out, rows=rows)
+        over = want.abs() > LARGEST
+        assert torch.equal(got[over], torch.sign(want[over]) * torch.inf)
+        rest = ~over & (want.abs() < LARGEST * (1 - 2.0 ** -7))
+        assert ((got - want).abs() <= rel * want.abs() + least)[rest].all(), (a, b)
+        assert (got[::5] == 0).all()
