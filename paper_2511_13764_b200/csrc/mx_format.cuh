@@ -1,6 +1,8 @@
 // The 4-bit formats: geometry of packed arrays (host and device) and conversions of scales and elements.
 #pragma once
+#ifdef __CUDACC__
 #include "half.cuh"
+#endif
 
 namespace nk {
 
@@ -13,6 +15,12 @@ __host__ __device__ constexpr long long mx_tiles(long long length, int nv) {
 }
 // first tile of scales of a group whose rows begin at row0: groups' tiles never meet, since ceil(n / 128) <= (row0 + n) / 128 - row0 / 128 + 1
 __host__ __device__ constexpr int mx_group_tile(int row0, int g) { return row0 / MX_TILE_ROWS + g; }
+// rows that the tile `at` tiles behind the first of a group of `rows` rows has; 0: it is none of the group's.  (`at` counts tiles of all groups, of
+// which there are up to 2^24 + 1024: 128 times that may pass 2^31, so it is not formed before `at` is known to be the group's.)
+__host__ __device__ constexpr int mx_tile_rows(int at, int rows) {
+    if (at < 0 || at >= (rows + MX_TILE_ROWS - 1) / MX_TILE_ROWS) return 0;
+    return rows - at * MX_TILE_ROWS < MX_TILE_ROWS ? rows - at * MX_TILE_ROWS : MX_TILE_ROWS;
+}
 
 #ifdef __CUDACC__
 // E8M0 byte to its number (2^-127 is a subnormal)

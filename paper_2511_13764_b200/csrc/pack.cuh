@@ -144,10 +144,10 @@ __device__ __forceinline__ PackRows pack_rows(const PackParams& p, int tile, int
         __syncthreads();
     }
     for (int g = threadIdx.x; g < p.groups; g += PACK_THREADS) {
-        const int lo = s_off[g], hi = s_off[g + 1], from = mx_group_tile(lo, g), at = tile - from;
-        if (at >= 0 && at * MX_TILE_ROWS < hi - lo) {
+        const int lo = s_off[g], at = tile - mx_group_tile(lo, g), count = mx_tile_rows(at, s_off[g + 1] - lo);
+        if (count > 0) {
             s_found[0] = lo + at * MX_TILE_ROWS;
-            s_found[1] = min(MX_TILE_ROWS, hi - lo - at * MX_TILE_ROWS);
+            s_found[1] = count;
         }
     }
     __syncthreads();
