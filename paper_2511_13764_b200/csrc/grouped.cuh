@@ -892,6 +892,7 @@ grouped_kernel(const __grid_constant__ std::conditional_t<MODE == GRP_LORA, Lora
                     if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
                 }
                 last = __ballot_sync(~0u, done);
+                __syncwarp();                                 // (a ballot orders no memory: what a lane acquired holds for the others from here on)
             }
 #pragma unroll 1
             for (int q = 0; q < mine; ++q) {

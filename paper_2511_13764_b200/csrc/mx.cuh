@@ -661,6 +661,7 @@ mx_kernel(const __grid_constant__ MxMaps maps, const __grid_constant__ MxParams 
                     if (done) atomicSub(counter, static_cast<unsigned>(u.parts) << (8 * quarter));
                 }
                 const unsigned int last = __ballot_sync(~0u, done);
+                __syncwarp();                             // (a ballot orders no memory: what a lane acquired holds for the others from here on)
 #pragma unroll 1
                 for (int q = 0; q < mine; ++q) {
                     if (!((last >> q) & 1u)) continue;
