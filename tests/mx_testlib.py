@@ -106,3 +106,40 @@ def tensor_scale(x):
     t = max(m / 2688, 2.0 ** -60)
     step = 2.0 ** (np.frexp(t)[1] - 8)
     return float(np.ceil(t / step) * step)
+
+
+def one_groups_tiles(rows, N, K, pairs, cut=True):
+    """Which tiles a plan without groups takes on `pairs` pairs of SMs (csrc/nk_mx.cu): rows of a tile, parts of those of the last wave."""
+    best, width, parts = 1e300, 0, 1
+    tiles_i, kbs = -(-N // 256), -(-K // 256)
+    w = 32 if rows <= 32 else 64
+    while w <= 256:
+        n = -(-rows // w) * tiles_i
+        waves, rest = divmod(n, pairs)
+
+        def block(active):
+            return 460 + (450 + w + w // 2 - 460) * min(1.0, active / pairs)
+        c = 1
+        while c == 1 or (cut and rest and c <= 8 and c <= kbs and c * rest <= pairs):
+            t = waves * (kbs * block(pairs) + 300) + (-(-kbs // c) * block(rest * c) if rest else 0) + 300 + 8 * w
+            t += 2900 + 700 * c + rest * c * w * (2048 / 3500) if c > 1 else 0
+            if t < best * 0.999 or (t <= best * 1.001 and c == 1 and parts == 1):
+                best, width, parts = min(best, t), w, c
+            c += 1
+        if w >= rows:
+            break
+        w += 32 if w < 64 else 64
+    return width, parts
+
+
+def groups_width(sizes, N, K, pairs):
+    """Rows of a tile where the rows are grouped, as the kernel's scheduler chooses them (csrc/mx.cuh)."""
+    most = max(sizes)
+    if most <= 64:
+        return 32 if most <= 32 else 64
+    found = []
+    for w in (64, 128, 192, 256):
+        w = min(w, (most + 63) // 64 * 64)
+        waves = -(-sum(-(-n // w) for n in sizes) * -(-N // 256) // pairs)
+        found.append((waves * (-(-K // 256) * (450 + w + w // 2) + 300) + 8 * w, -w))
+    return -min(found)[1]

@@ -195,3 +195,37 @@ def test_no_tokens_and_refusals():
         with pytest.raises(nk.NkError) as e:
             call()
         assert e.value.status == status
+
+
+@pytest.mark.parametrize("tokens,cut,experts,topk", [(64, 20, 24, 3), (5000, 1234, 96, 4), (300, 299, 8, 2), (2000, 0, 40, 1)])
+def test_loads_over_several_ranks(tokens, cut, experts, topk):
+    """Each rank has its own tokens; with the sum of the ranks' counts the gradients are those of the losses of all tokens, and the losses come from
+    shares weighted by the ranks' numbers of tokens."""
+    z, chosen = inputs(tokens, experts, topk, seed=tokens)
+    mask = (torch.rand(tokens, generator=torch.Generator().manual_seed(1)) < 0.8).to(torch.uint8)
+    d = [0.3, 0.02]
+    counts, n, share, losses, grad, size = formulas(z, chosen, mask, torch.tensor(d).double().tolist(), topk)
+    parts = []
+    for lo, hi in ((0, cut), (cut, tokens)):
+        plan = nk.RoutePlan(hi - lo, experts, topk)
+        c = torch.empty(experts + 1, dtype=torch.int32, device="cuda")
+        s, l = torch.empty(experts, device="cuda"), torch.empty(2, device="cuda")
+        ws = torch.empty(max(1, plan.balance_workspace_bytes), dtype=torch.uint8, device="cuda")
+        zd, ch, m = z[lo:hi].cuda(), chosen[lo:hi].cuda(), mask[lo:hi].cuda()
+        plan.balance(zd, ch, c, s, l, mask=m, workspace=ws, stream=stream())
+        plan.check()
+        parts.append((plan, zd, m, c, s.double().cpu(), l.double().cpu()))
+    total = parts[0][3] + parts[1][3]                      # what an all-reduce gives
+    assert torch.equal(total[:-1].cpu().long(), counts) and int(total[-1]) == n
+    own = [int(p[3][-1]) for p in parts]
+    mean = sum(k * p[4] for k, p in zip(own, parts)) / n
+    assert ((mean - share).abs() <= REL * share).all()
+    assert abs(experts / (n * topk) * (total[:-1].cpu().double() * mean).sum() - losses[0]) <= REL * losses[0]
+    assert abs(sum(k * p[5][1] for k, p in zip(own, parts)) / n - losses[1]) <= REL * losses[1]
+    got = []
+    for plan, zd, m, _, _, _ in parts:
+        dz = torch.full(zd.shape, float("nan"), device="cuda")
+        plan.balance_backward(zd, total, torch.tensor(d, device="cuda"), dz, mask=m, stream=stream())
+        plan.check()
+        got.append(dz.double().cpu())
+    assert ((torch.cat(got) - grad).abs() <= REL * size).all()

@@ -10,7 +10,7 @@ import pytest
 import torch
 
 import paper_2511_13764_b200 as nk
-from mx_testlib import quantise, tensor_scale, values
+from mx_testlib import groups_width, one_groups_tiles, quantise, tensor_scale, values
 
 pytestmark = pytest.mark.gpu
 
@@ -503,3 +503,83 @@ def test_scales_of_any_size_in_tiles_of_every_kind(out, rows, N, K):
         rest = ~over & (want.abs() < LARGEST * (1 - 2.0 ** -7))
         assert ((got - want).abs() <= rel * want.abs() + least)[rest].all(), (a, b)
         assert (got[::5] == 0).all()
+
+
+def pairs_of_sms():
+    return torch.cuda.get_device_properties(0).multi_processor_count // 2
+
+
+def compare_whole(A, B, rows, N, K, fmt, out, more=False):
+    """The whole of C with the product in 64 bits; `more`: bias, ReLU and beta, rows further apart than they are long."""
+    bias = old = None
+    if more:
+        g = torch.Generator(device="cuda").manual_seed(7)
+        bias, old = torch.randn(N, generator=g, device="cuda"), torch.randn(rows, N, generator=g, device="cuda").to(TYPES[out][1])
+    got = run(A, B, N, K, fmt, out, rows=rows, bias=bias, relu=more, beta=int(more), c=old, ldc=N + 8 if more else 0)
+    y = A.values @ B.values.t()
+    tol = bound(A.values, B.values, K, out, torch.zeros_like(y))
+    if more:
+        # (two additions that round to nearest: 2^-23 of what is added)
+        tol += 2.0 ** -23 * (y.abs() + bias.double().abs() + old.double().abs())
+        y = torch.relu(y + bias.double() + old.double())
+    tol += {"f32": 0.0, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[out] * y.abs()
+    bad = ~((got - y).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}, first {bad.nonzero()[:4].tolist()}, got {got[bad][:4].tolist()}, want {y[bad][:4].tolist()}"
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("out,more", [("f32", False), ("bf16", False), ("f16", False), ("f32", True), ("bf16", True)])
+@pytest.mark.parametrize("rows,N,K,width", [(4096, 4096, 520, 256), (4096, 4096, 2056, 256), (3500, 4104, 264, 256), (2100, 2568, 776, 192), (2500, 2056, 520, 192),
+                                            (1300, 4104, 520, 192), (1300, 2488, 208, 192), (1600, 2568, 264, 128)])
+def test_wide_tiles(fmt, out, more, rows, N, K, width):
+    """Tiles of every width, several of them to most pairs: accumulators that share columns follow each other, rows' scales begin in the middle of 128."""
+    assert one_groups_tiles(rows, N, K, pairs_of_sms()) == (width, 1), "this size no longer takes the tiles that it is here for"
+    compare_whole(OnDevice(rows, K, fmt=fmt, seed=rows), OnDevice(N, K, fmt=fmt, seed=N), rows, N, K, fmt, out, more)
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("out,more,rows,N,K,width,parts", [
+    ("f32", False, 2000, 2056, 8448, 256, 1), ("f32", False, 2560, 4096, 8448, 256, 1), ("f32", True, 2500, 4096, 8704, 256, 1), ("bf16", False, 2560, 4096, 16640, 256, 3),
+    ("f16", False, 2000, 2056, 16640, 256, 1), ("f16", False, 2600, 2568, 16640, 256, 1), ("bf16", True, 2900, 2056, 16640, 192, 1), ("f32", False, 1000, 2056, 8448, 128, 1), ("f32", False, 3000, 1544, 8448, 192, 1), ("bf16", True, 3000, 1544, 16640, 256, 3),
+    # cut, too; 16-bit results of one accumulator or of two
+    ("f32", False, 3848, 1248, 15016, 256, 4), ("f32", False, 5537, 1712, 9216, 256, 3), ("bf16", False, 3848, 1248, 15016, 256, 4), ("f16", True, 5537, 1712, 9216, 256, 3)])
+def test_sums_and_cuts_of_wide_tiles(fmt, out, more, rows, N, K, width, parts):
+    assert one_groups_tiles(rows, N, K, pairs_of_sms()) == (width, parts), "this size no longer takes the tiles that it is here for"
+    compare_whole(OnDevice(rows, K, fmt=fmt, seed=rows), OnDevice(N, K, fmt=fmt, seed=N), rows, N, K, fmt, out, more)
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [264, 1032])
+@pytest.mark.parametrize("sizes,width", [([1300, 1300], 192), ([1500, 3, 700, 900], 256), ([2500, 2500, 3, 0, 1500], 256), ([200, 190, 180, 0, 170], 128), ([60, 64, 1], 64), ([20, 0, 32], 32)])
+def test_grouped_tiles_of_each_width(fmt, out, K, sizes, width):
+    N, offsets = 2056, [0]
+    for n in sizes:
+        offsets.append(offsets[-1] + n)
+    assert groups_width(sizes, N, K, pairs_of_sms()) == width, "these loads no longer take the tiles that they are here for"
+    rows, G = offsets[-1], len(sizes)
+    A, B = OnDevice(rows, K, fmt=fmt, seed=1, offsets=offsets), OnDevice(G, N, K, fmt=fmt, seed=2)
+    got = run(A, B, N, K, fmt, out, groups=G, offsets=A.offsets, rows=rows)
+    for g, (lo, hi) in enumerate(zip(offsets, offsets[1:])):
+        y = A.values[lo:hi] @ B.values[g].t()
+        assert ((got[lo:hi] - y).abs() <= bound(A.values[lo:hi], B.values[g], K, out, y)).all(), g
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("rows", [64, 512])
+@pytest.mark.parametrize("K", [4096, 8192, 65536])
+@pytest.mark.parametrize("kind", ["normal", "one sign", "spread"])
+def test_error_of_fp32_results(fmt, rows, K, kind):
+    """The errors that nk_mx.h states (2-norm: 2.5e-8, 1e-7, 1.2e-6), within twice.  Spread: blocks that differ by ten powers of two."""
+    def change(x):
+        if kind == "one sign":
+            return x.abs()
+        if kind == "spread":
+            e = torch.randint(-5, 6, (x.shape[0], K // 32), generator=torch.Generator().manual_seed(x.shape[0])).cuda()
+            return x * (2.0 ** e).repeat_interleave(32, 1)
+        return x
+    A, B = OnDevice(rows, K, fmt=fmt, seed=1, change=change), OnDevice(520, K, fmt=fmt, seed=2, change=change)
+    got = run(A, B, 520, K, fmt, "f32", rows=rows)
+    y = A.values @ B.values.t()
+    error = float((got - y).norm() / y.norm())
+    assert error <= 2 * {"normal": 2.5e-8, "one sign": 1e-7, "spread": 1.2e-6}[kind], error

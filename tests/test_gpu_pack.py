@@ -304,3 +304,74 @@ def test_in_a_graph_and_on_another_stream():
         assert np.array_equal(unpack_data(data.cpu().numpy(), 200, 512), one_zero(codes))
         assert np.array_equal(unpack_scales(scales.cpu().numpy(), np.arange(200), 512, "nvf4"), bytes_)
     assert padded(512) == 512 and BLOCK["nvf4"] == 16
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("transposed,rows,K", [(0, 1, 8), (0, 33, 104), (0, 300, 1032), (1, 33, 104), (1, 64, 24), (1, 1000, 264), (1, 4099, 24)])
+def test_values_of_both_formats(fmt, kind, transposed, rows, K):
+    """Reading back, whole pieces of eight and odd lengths, one chunk of a row and several."""
+    x = rows_of(rows, K, "bf16", seed=rows + K)
+    t = tensor_scale(x.double().numpy()) if fmt == "nvf4" else 1.0
+    plan, data, scales, scale, _ = pack(x, fmt, "bf16", t if fmt == "nvf4" else None, transposed=transposed, value_dtype=TYPES[kind][0])
+    z = x.double().numpy()
+    codes, bytes_, _ = quantise(z.T.copy() if transposed else z, fmt, t)
+    check_values(plan, data, scales, scale, None, values(codes, bytes_, fmt, t, rows if transposed else K), kind)
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("offsets", [[0, 0, 130, 130, 131, 300, 300], [7, 20, 20, 290]])
+def test_values_of_groups_in_16_bits(fmt, kind, offsets):
+    x = rows_of(300, 264, "bf16", seed=len(offsets))
+    t = 0.0078125 if fmt == "nvf4" else 1.0
+    plan, data, scales, scale, off = pack(x, fmt, "bf16", t if fmt == "nvf4" else None, offsets=offsets, groups=len(offsets) - 1, value_dtype=TYPES[kind][0])
+    codes, bytes_, _ = quantise(x.double().numpy(), fmt, t)
+    check_values(plan, data, scales, scale, off, values(codes, bytes_, fmt, t, 264), kind, rows=group_places(offsets)[0])
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("transposed,rows,K", [(0, 150, 200), (1, 150, 200), (1, 77, 40)])
+def test_values_of_a_batch(fmt, kind, transposed, rows, K):
+    """Every matrix with its own tensor scale."""
+    batch = 3
+    x = torch.stack([rows_of(rows, K, "bf16", seed=b, scale=10.0 ** (b - 1)) for b in range(batch)])
+    plan = nk.PackPlan(rows, K, format=FORMATS[fmt], batch=batch, transposed=transposed, value_dtype=TYPES[kind][0])
+    data = torch.empty(plan.data_bytes, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(plan.scales_bytes, dtype=torch.uint8, device="cuda")
+    ts = [tensor_scale(m.double().numpy()) if fmt == "nvf4" else 1.0 for m in x]
+    scale = torch.tensor(ts, dtype=torch.float32, device="cuda") if fmt == "nvf4" else None
+    plan.run(x.cuda(), data, scales, scale=scale, stream=stream())
+    want = []
+    for m, t in zip(x, ts):
+        z = m.double().numpy()
+        codes, bytes_, _ = quantise(z.T.copy() if transposed else z, fmt, t)
+        want.append(values(codes, bytes_, fmt, t, rows if transposed else K))
+    check_values(plan, data, scales, scale, None, np.stack(want), kind)
+
+
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("transposed", [0, 1])
+def test_values_that_are_not_ordinary_read_back(fmt, kind, transposed):
+    """Blocks whose scale is a NaN, the smallest or the largest; tensor scales that make every block a NaN."""
+    dt = TYPES[kind][1]
+    x = rows_of(64, 128, kind, seed=3)
+    x[0, 5], x[1, 40], x[2, 127] = float("inf"), float("-inf"), float("nan")
+    x[3] = torch.finfo(dt).max
+    x[4] = torch.finfo(dt).smallest_normal
+    x[5] = torch.finfo(dt).smallest_normal / 4               # subnormal
+    x[6], x[7] = 0.0, -0.0
+    x[8, ::32] = torch.finfo(dt).max
+    x[9] = -torch.finfo(dt).max
+    src = x.t().contiguous() if transposed else x
+    for t in ([None] if fmt == "mxf4" else [None, 2.0 ** -20, 2.0 ** 20, 2.0 ** -100, 2.0 ** 120, float("nan"), float("inf"), 0.0, -1.0, 2.0 ** -101, 2.0 ** 121]):
+        for out in ("f32", kind):
+            plan, data, scales, scale, _ = pack(src, fmt, kind, t, transposed=transposed, value_dtype=TYPES[out][0])
+            legal = t is None or 2.0 ** -100 <= t <= 2.0 ** 120
+            codes, bytes_, _ = quantise(x.double().numpy(), fmt, 1.0 if t is None else t if legal else float("nan"))
+            assert np.array_equal(unpack_scales(scales.cpu().numpy(), np.arange(64), 128, fmt), bytes_), t
+            with np.errstate(all="ignore"):
+                want = values(codes, bytes_, fmt, 1.0 if t is None else t, 128)
+            check_values(plan, data, scales, scale, None, want, out)
