@@ -1,4 +1,5 @@
-"""The expert layer with its experts in 4-bit floating point and the balance of their loads, with the calls of this library only.
+"""The expert layer with its experts in 4-bit floating point and the balance of their loads, with the calls of this library (and, backwards, one
+elementwise product of torch: where the ReLU was 0).
 
     z      = h . Wr                                    the router's logits                              (nk_gemm)
     choice = the topk largest of z                     gates, experts' order                            (nk_route)

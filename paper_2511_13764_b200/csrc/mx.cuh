@@ -22,7 +22,8 @@
 //
 // Bound by the SMs' feed from L2, 46 bytes a clock: a k-block of 256 x 256 takes 0.45 us, the MMAs 0.28.  8192^3 to BF16: NVF4
 // 198 to 206 us (5.4 PFLOP/s), MXF4 189 (5.8); without pauses 240, the power cap's.  8192 x 4096 x 1024 29 us.  Few rows wait for their
-// weights: 16 x 16384 x 16384 31 us (4.9 TB/s), 16 x 4096 x 4096 9.1 (4 us of start and end), 64 experts of 4096 x 1024 with 32 rows 15.7.
+// weights: 16 x 16384 x 16384 31 us (4.9 TB/s), 16 x 4096 x 4096 9.2 (5.0 with one k-block, 0.27 for each more), 64 experts of 4096 x 1024 with 32
+// rows 15.7.  Short contractions wait for the epilogue, whose stores are two bytes a lane: 8192 x 4096 x 1024 takes 3.5 us a tile, its feed 1.8.
 #pragma once
 #include "grouped.cuh"
 #include "mx_format.cuh"

@@ -29,8 +29,9 @@ static bool encode_scales(CUtensorMap* m, const void* base, int64_t tiles, int64
 
 // Tiles of one group of rows: their width, and into how many parts those of the last, partial wave are cut, by the least estimated time.
 // Joining parts costs 2900 clocks and 700 a part, and what is written and read again of them at 3500 bytes a clock.  (16 rows, 4096
-// features: K 4096 10.0 us uncut, 9.7 in four parts, K 8192 14.8 and 11.5; 128 rows, K 4096 10.8 uncut, 12.1 in four.  Cuts of
-// groups' tiles gain nothing below K = 8192, so only one group's are cut, and the kernel has no code for that choice, which costs 1.5 us.)
+// features: K 4096 10.0 us uncut, 9.7 in four parts, K 8192 14.8 and 11.5; 128 rows, K 4096 10.8 uncut, 12.1 in four.  Groups' tiles are never
+// cut: their number is known on the device alone, where the choice costs every launch 1.5 us.  Below K = 8192 cuts gained nothing there; what
+// longer contractions with few tiles would gain, as one group's do, was not measured.)
 static void mx_tiles_of(int64_t rows, int tiles_i, int kbs, int pairs, bool cut, int* width, int* parts) {
     double best = 1e300;
     for (int w = rows <= 32 ? 32 : 64; w <= MX_TILE; w += w < 64 ? 32 : 64) {

@@ -12,7 +12,8 @@
 // a block of the format.  Along the columns a tile of 128 x 128 goes through shared memory, where a thread has a word of adjacent
 // features.  BF16, 64 matrices of 4096 x 1024 to NVF4 106 us: 6.3 TB/s, the rate of a copy.  8192 x 4096 is two waves of blocks, whose
 // loads and arithmetic overlap less (issue slots 60 % busy): NVF4 17.8 us (4.8 TB/s), along the columns 19.5-20.5; MXF4 15.1 and 17.6;
-// its scale of a tensor 15.4 (4.4 TB/s), values in FP32 29 (5.3 TB/s).  16 x 4096 takes 2.1 to 2.4 us, a launch's start and end.
+// its scale of a tensor 15.4 (4.4 TB/s), values in FP32 29 (5.3 TB/s).  From FP32, whose bytes take 24 us: MXF4 35.5 along the rows, 35 along the
+// columns, NVF4, a division an element, 43 and 51, the scale 23 (5.8 TB/s).  16 x 4096 takes 2.1 to 2.4 us, a launch's start and end.
 #pragma once
 #include "mx_format.cuh"
 #include "ptx.cuh"
@@ -182,7 +183,7 @@ __device__ __forceinline__ uint32_t pack_most(const uint32_t (&w)[N]) {
 template <int T>
 __device__ __forceinline__ uint32_t pack_one(uint32_t m) { return T == 0 ? m : max(m & 0xFFFFu, m >> 16); }
 // Along the rows: blockIdx.x a chunk of the contraction of a tile's rows (pieces of the same rows side by side, so that blocks at work
-// together read whole rows), z the matrix.  A thread has a block: no exchange, one division.
+// together read whole rows), z the matrix.  A thread has a block: no exchange, and no division but FP32 elements' to NVF4, one for each.
 template <int T, bool NV>
 __global__ void __launch_bounds__(PACK_THREADS) pack_rows_kernel(const PackParams p) {
     constexpr int BLOCK = mx_block(NV), EIGHTS = BLOCK / 8, WORDS = T == 0 ? 8 : 4;
